@@ -351,6 +351,145 @@ int pvmvmd_code_encode_scratch(const pvmvmd_ctx *ctx, int which, int L, size_t *
 int pvmvmd_code_encode_lanes(const pvmvmd_ctx *ctx, int which, const uint32_t *X_dev, int L,
                              uint32_t *Y_dev, void *scratch_dev, void *stream);
 
+/* ---------------------------------------------------------------------
+ * The client's attention (Sec. 7.2: the client evaluates what lies between
+ * two delegated products).  decode_verify returns q, k and v of the new tokens
+ * as field elements; these calls take them (or floating tensors) through rotary
+ * positions into a paged cache, attend over it, and bound the cache's size.
+ *
+ * Conventions, besides those at the top of this file:
+ *  - Types are PVMVMD_BF16, PVMVMD_F16, PVMVMD_F32 and PVMVMD_FIELD (uint32
+ *    field elements, read as centred integers).  Every floating input is taken to
+ *    32 bits, and every result is rounded once to its type.
+ *  - A tensor of T tokens x H heads x D is given by its address and its strides
+ *    between tokens and between heads, in elements; the D values of a head are
+ *    contiguous.
+ *  - Strides and offsets are 64 bits wide; counts are int.
+ *  - The structs are read during the call and may be freed after it; the device
+ *    arrays that they name are read in stream order.
+ */
+enum { PVMVMD_BF16 = 1, PVMVMD_F16 = 2, PVMVMD_F32 = 3, PVMVMD_FIELD = 4 };
+
+/* Rotary frequencies theta_i = base^(-2i/rot), i < rot/2, scaled for contexts
+ * longer than the model's own by a factor s >= 1:
+ *   PVMVMD_ROPE_PLAIN   as they are;
+ *   PVMVMD_ROPE_LINEAR  theta_i / s;
+ *   PVMVMD_ROPE_BASE    base s^(rot/(rot-2)) in the place of base (rot > 2);
+ *   PVMVMD_ROPE_RAMP    theta_i (g_i + (1 - g_i) / s) with
+ *                       g_i = clamp((n_i - slow) / (fast - slow), 0, 1) and
+ *                       n_i = original theta_i / (2 pi), the turns that the pair
+ *                       makes in the model's own context (fast > slow). */
+enum { PVMVMD_ROPE_PLAIN = 0, PVMVMD_ROPE_LINEAR = 1, PVMVMD_ROPE_BASE = 2, PVMVMD_ROPE_RAMP = 3 };
+typedef struct {
+    int rot;         /* rotated values of a head, even, >= 2 */
+    int scaling;     /* PVMVMD_ROPE_*                        */
+    double base;     /* > 0                                  */
+    double factor;   /* s                                    */
+    double original; /* RAMP: the model's own context        */
+    double slow, fast;
+} pvmvmd_rope_params;
+
+/* turns[i] = theta_i / (2 pi) in units of 2^-64 of a turn, modulo whole turns, for
+ * i < rot/2 (host array).  position * turns[i] modulo 2^64 is then the angle at
+ * any position without a loss of precision.  Host only; needs no GPU.  Returns
+ * PVMVMD_E_PARAM for parameters outside the ranges above. */
+int pvmvmd_rope_turns(const pvmvmd_rope_params *params, uint64_t *turns);
+
+/* How a call rotates: turns_dev the rot/2 values of pvmvmd_rope_turns on the
+ * device.  A pair (a, b) at position p becomes
+ *     magnitude (a cos x - b sin x, a sin x + b cos x),  x = p theta_i;
+ * the pairs are values i and i + rot/2 of a head, or 2i and 2i + 1 where
+ * interleaved is not 0.  Values from rot on are copied. */
+typedef struct {
+    const uint64_t *turns_dev;
+    int rot, interleaved;
+    float magnitude;
+} pvmvmd_rope_view;
+
+/* out = rotated (scale x) for T tokens of H heads of D values at positions
+ * pos_dev[T] (any int32).  x of any type, out of any floating type.  out may be x
+ * itself (the same address, strides and type size) and must not overlap it
+ * otherwise.  T = 0 does nothing.  2 <= rot <= D.  Errors: PVMVMD_E_ARG (null
+ * pointer, unknown type), PVMVMD_E_SHAPE (T < 0, H or D < 1, rot odd or outside
+ * [2, D]). */
+int pvmvmd_rope(const pvmvmd_rope_view *rope, const int32_t *pos_dev, int T, int H, int D, const void *x_dev,
+                int x_type, int64_t x_token, int64_t x_head, float scale, void *out_dev, int out_type,
+                int64_t out_token, int64_t out_head, void *stream);
+
+/* A pool of pages of keys and values, owned by the caller: slot o of page p holds
+ * the `dim` values of head h at K_dev + p k_page + o k_slot + h k_head (elements),
+ * V alike.  Type PVMVMD_BF16 or PVMVMD_F16.  Addresses on 16-byte boundaries,
+ * strides multiples of 8, dim a multiple of 8 up to PVMVMD_MAX_HEAD; any page
+ * size.  mass_dev: null, or float [pages][heads][page_size], the attention weight
+ * that each cached key has gathered. */
+#define PVMVMD_MAX_HEAD 128
+typedef struct {
+    void *K_dev, *V_dev;
+    float *mass_dev;
+    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
+    int pages, page_size, heads, dim, type;
+} pvmvmd_kv_pool;
+
+/* B sequences and their new tokens.  Sequence b has lens_dev[b] cached tokens,
+ * the new ones last; cache index i lies in slot i % page_size of page
+ * table_dev[b table_stride + i / page_size].  Entries behind its last page are not
+ * read.  Its new tokens are rows cu_dev[b] .. cu_dev[b+1] - 1 of the T token
+ * tensors (cu_dev[0] = 0, cu_dev[B] = T, ascending; null: one each, T = B).
+ * max_new: at least as many as any sequence has new ones, 0 if not known (then T).
+ * Lengths beyond max_pages pages are taken as max_pages pages; keys on pages
+ * outside the pool are not seen, and nothing is written there. */
+typedef struct {
+    const int32_t *table_dev, *lens_dev, *cu_dev;
+    int64_t table_stride;
+    int B, T, max_pages, max_new;
+} pvmvmd_kv_batch;
+
+/* Append: k and v of the new tokens (T x pool->heads x dim) go into the cache, k
+ * rotated by `rope` at positions pos_dev[T] (null: the cache indexes; they differ
+ * from them once a cache has been evicted).  With q_dev, q (T x Hq x dim) is
+ * rotated likewise into q_out_dev (T x Hq x dim, the pool's type, not overlapping
+ * the inputs).  rope null: nothing is rotated.  All inputs have type in_type, and
+ * are multiplied by scale.  The new tokens' mass is set to 0.  Sequences must not
+ * share the pages that their new tokens fall into.  T = 0 does nothing. */
+int pvmvmd_kv_append(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, const pvmvmd_rope_view *rope,
+                     const int32_t *pos_dev, int in_type, float scale, const void *k_dev, int64_t k_token,
+                     int64_t k_head, const void *v_dev, int64_t v_token, int64_t v_head, int Hq, const void *q_dev,
+                     int64_t q_token, int64_t q_head, void *q_out_dev, int64_t q_out_token, int64_t q_out_head,
+                     void *stream);
+
+/* Attention of the new tokens over the cache.  Row (t, h), h < Hq, of a token at
+ * cache index i sees the keys j of its sequence and of head h / (Hq / heads) with
+ * j <= i if causal, and i - j < window if window > 0:
+ *     s_j = scale q . k_j;  lse = log sum_j exp s_j;  out = sum_j exp(s_j - lse) v_j.
+ * A row that sees nothing gives out = 0 and lse = -infinity (a sequence may be
+ * shorter than its new tokens: those in front of its start see nothing).  With
+ * accumulate, exp(s_j - lse) of all rows is added to the mass of the keys they see;
+ * the sums are formed in an order that does not change from call to call.
+ * Hq a multiple of pool->heads; q and out of the pool's type, on 16-byte boundaries,
+ * strides multiples of 8; lse_dev float [T][Hq] or null.  What lies behind a
+ * sequence's end and on pages of others is not used, whatever it holds.  A key that
+ * is not finite gives rows that see it NaN; a value that is not finite may reach
+ * rows of the same call that do not see it (0 times it), among the keys in reach of
+ * any of them.  Partial results of long sequences live in library scratch held per
+ * stream, as for pvmvmd_server_mvm.  T = 0 does nothing. */
+int pvmvmd_paged_attention(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, int Hq, const void *q_dev,
+                           int64_t q_token, int64_t q_head, float scale, int causal, int window, int accumulate,
+                           void *out_dev, int64_t out_token, int64_t out_head, float *lse_dev, void *stream);
+
+/* Eviction: of every sequence, and for every head by itself, min(len, budget)
+ * tokens stay: the last min(recent, budget) ones, and of the others those with the
+ * largest mass (of equal ones those in front; NaN below everything), in their old
+ * order.  Their keys, values and masses move to cache indexes 0, 1, ... under
+ * new_table_dev (B x new_max_pages, stride new_table_stride), which may be the
+ * batch's own table (eviction in place; no other sequence may use those pages) or
+ * name pages that no sequence of the batch uses; new_lens_dev[b] = min(len, budget)
+ * (may be lens_dev itself).  Keys keep the rotation of their old positions.
+ * budget >= 1, recent >= 0, new_max_pages * page_size >= budget or >= max_pages *
+ * page_size.  cu_dev, T and max_new are not used. */
+int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, int budget, int recent,
+                    const int32_t *new_table_dev, int64_t new_table_stride, int new_max_pages, int32_t *new_lens_dev,
+                    void *stream);
+
 /* The number of kernels the library has enqueued in this process since it
  * was loaded, on every device and stream: each launch counts once when it is
  * enqueued, also while a stream is being captured.  Replaying a captured CUDA

@@ -83,8 +83,38 @@ class pvmvmd_mvm_job(ctypes.Structure):
                 ("m", ctypes.c_int), ("K", ctypes.c_int)]
 
 
+PVMVMD_BF16, PVMVMD_F16, PVMVMD_F32, PVMVMD_FIELD = 1, 2, 3, 4
+PVMVMD_MAX_HEAD = 128
+PVMVMD_ROPE = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class pvmvmd_rope_params(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int), ("scaling", ctypes.c_int), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original", ctypes.c_double), ("slow", ctypes.c_double),
+                ("fast", ctypes.c_double)]
+
+
+class pvmvmd_rope_view(ctypes.Structure):
+    _fields_ = [("turns_dev", ctypes.c_void_p), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("magnitude", ctypes.c_float)]
+
+
+class pvmvmd_kv_pool(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("K_dev", "V_dev", "mass_dev")] + \
+               [(f, ctypes.c_int64) for f in ("k_page", "k_slot", "k_head", "v_page", "v_slot", "v_head")] + \
+               [(f, ctypes.c_int) for f in ("pages", "page_size", "heads", "dim", "type")]
+
+
+class pvmvmd_kv_batch(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("table_dev", "lens_dev", "cu_dev")] + \
+               [("table_stride", ctypes.c_int64)] + \
+               [(f, ctypes.c_int) for f in ("B", "T", "max_pages", "max_new")]
+
+
 # Exported symbols and their ctypes signatures (mirrors include/pvmvmd.h).
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_l, _f = ctypes.c_int64, ctypes.c_float
+_rows = [_vp, _l, _l]  # a tensor of tokens x heads: address, strides
 SIGNATURES = {
     "pvmvmd_params_resolve": (_i, [ctypes.POINTER(pvmvmd_params), _i, _i, ctypes.POINTER(pvmvmd_params)]),
     "pvmvmd_preprocess": (_i, [_vp, _i, _i, ctypes.POINTER(pvmvmd_params), ctypes.POINTER(pvmvmd_key), _vp,
@@ -113,6 +143,14 @@ SIGNATURES = {
                                    ctypes.POINTER(_vp)]),
     "pvmvmd_code_encode_scratch": (_i, [_vp, _i, _i, ctypes.POINTER(_sz)]),
     "pvmvmd_code_encode_lanes": (_i, [_vp, _i, _vp, _i, _vp, _vp, _vp]),
+    "pvmvmd_rope_turns": (_i, [ctypes.POINTER(pvmvmd_rope_params), ctypes.POINTER(ctypes.c_uint64)]),
+    "pvmvmd_rope": (_i, [ctypes.POINTER(pvmvmd_rope_view), _vp, _i, _i, _i, _vp, _i, _l, _l, _f, _vp, _i, _l, _l, _vp]),
+    "pvmvmd_kv_append": (_i, [ctypes.POINTER(pvmvmd_kv_pool), ctypes.POINTER(pvmvmd_kv_batch),
+                              ctypes.POINTER(pvmvmd_rope_view), _vp, _i, _f, *_rows, *_rows, _i, *_rows, *_rows, _vp]),
+    "pvmvmd_paged_attention": (_i, [ctypes.POINTER(pvmvmd_kv_pool), ctypes.POINTER(pvmvmd_kv_batch), _i, *_rows, _f, _i,
+                                    _i, _i, *_rows, _vp, _vp]),
+    "pvmvmd_kv_evict": (_i, [ctypes.POINTER(pvmvmd_kv_pool), ctypes.POINTER(pvmvmd_kv_batch), _i, _i, _vp, _l, _i, _vp,
+                             _vp]),
     "pvmvmd_device_status": (_i, [_vp]),
     "pvmvmd_kernel_launches": (ctypes.c_ulonglong, []),
     "pvmvmd_debug_expire_wait": (_i, [_i, ctypes.c_uint32, ctypes.c_uint64]),
@@ -635,6 +673,190 @@ def pvmvmd_bv_check(ctx: BvCtx, X, Y, chal, u, key2, accept=None, stream=None):
                                 _stream_ptr(stream)),
            "pvmvmd_bv_check")
     return accept
+
+
+# ---------------------------------------------------------------- the client's attention
+# (argument checks of the tensors here, those of values in the library)
+
+_float_codes = None
+
+
+def _type_code(t, name: str, field: bool = False) -> int:
+    """PVMVMD_BF16, _F16, _F32, or, where field elements are taken, _FIELD."""
+    global _float_codes
+    if _float_codes is None:
+        torch = _torch or _lazy_torch()
+        _float_codes = {torch.bfloat16: PVMVMD_BF16, torch.float16: PVMVMD_F16, torch.float32: PVMVMD_F32}
+    code = _float_codes.get(t.dtype)
+    if code is None and field and t.dtype in _u32_types():
+        code = PVMVMD_FIELD
+    if code is None:
+        raise TypeError(f"{name} must be a floating{' or field' if field else ''} tensor, got {t.dtype}")
+    return code
+
+
+def _token_rows(t, name: str, T: int, H: int, D: int, dtype=None):
+    """(address, token stride, head stride) of a T x H x D tensor, heads contiguous."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != (T, H, D):
+        raise ValueError(f"{name} must be {T} x {H} x {D}, got {tuple(t.shape)}")
+    st, sh, sd = t.stride()
+    if sd != 1 and D > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), st, sh
+
+
+class RopeTable:
+    """Rotary frequencies on the device: what pvmvmd_rope and pvmvmd_kv_append rotate by."""
+
+    def __init__(self, turns, rot: int, magnitude: float):
+        self.turns, self.rot, self.magnitude = turns, rot, magnitude
+        self.views = [pvmvmd_rope_view(turns.data_ptr(), rot, i, magnitude) for i in (0, 1)]
+        self.refs = [ctypes.byref(v) for v in self.views]
+
+
+def pvmvmd_rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                      original: float = 0.0, slow: float = 1.0, fast: float = 32.0) -> np.ndarray:
+    """The rot/2 frequencies as fractions of a turn in units of 2^-64 (numpy uint64)."""
+    if scaling not in PVMVMD_ROPE:
+        raise ValueError(f"scaling must be one of {sorted(PVMVMD_ROPE)}")
+    out = np.zeros(max(1, int(rot) // 2), np.uint64)
+    p = pvmvmd_rope_params(rot, PVMVMD_ROPE[scaling], base, factor, original, slow, fast)
+    _check(_lib.pvmvmd_rope_turns(ctypes.byref(p), out.ctypes.data_as(ctypes.POINTER(ctypes.c_uint64))),
+           "pvmvmd_rope_turns")
+    return out
+
+
+def pvmvmd_rope_table(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                      original: float = 0.0, slow: float = 1.0, fast: float = 32.0, magnitude: float = 1.0,
+                      device="cuda") -> RopeTable:
+    """The frequencies of pvmvmd_rope_turns on the device; made once, kept by the caller."""
+    import torch
+    turns = pvmvmd_rope_turns(rot, base, scaling, factor, original, slow, fast)
+    return RopeTable(torch.from_numpy(turns.view(np.int64)).to(device), rot, magnitude)
+
+
+def pvmvmd_rope(x, positions, rope: RopeTable, out=None, interleaved: bool = False, scale: float = 1.0, stream=None):
+    """x (T x H x D; floating, or field elements) times scale, rotated at int32 positions (T).
+    out: a floating tensor of that shape (may be x); default: x's type, bf16 for field elements."""
+    if x.dim() != 3:
+        raise ValueError("x must be T x H x D")
+    T, H, D = x.shape
+    xp, xt, xh = _token_rows(x, "x", T, H, D)
+    code = _type_code(x, "x", True)
+    if out is None:
+        import torch
+        out = torch.empty((T, H, D), dtype=torch.bfloat16 if code == PVMVMD_FIELD else x.dtype, device=x.device)
+    op, ot, oh = _token_rows(out, "out", T, H, D)
+    _check(_lib.pvmvmd_rope(rope.refs[bool(interleaved)], _dev_ptr(positions, "positions", _i32_types(), T), T, H, D,
+                            xp, code, xt, xh, scale, op, _type_code(out, "out"), ot, oh, _stream_ptr(stream)),
+           "pvmvmd_rope")
+    return out
+
+
+class KvPool:
+    """A paged cache of the caller's: K and V (pages x page_size x heads x dim, bf16 or fp16, any strides whose last
+    is 1) and, for eviction, mass (float32, pages x heads x page_size, contiguous).  Checked once, used by every call
+    while the tensors live."""
+
+    def __init__(self, K, V, mass=None):
+        if K.dim() != 4 or K.shape != V.shape:
+            raise ValueError("K and V must be pages x page_size x heads x dim")
+        if not K.is_cuda or not V.is_cuda or K.dtype != V.dtype:
+            raise TypeError("K and V must be CUDA tensors of one dtype")
+        if K.stride(3) != 1 or V.stride(3) != 1:
+            raise ValueError("the last dimension of K and V must be contiguous")
+        pages, page, heads, dim = K.shape
+        self.K, self.V, self.mass = K, V, mass
+        self.heads, self.dim, self.page_size, self.pages = heads, dim, page, pages
+        mp = None
+        if mass is not None:
+            mp = _dev_ptr(mass, "mass", ((_torch or _lazy_torch()).float32,), pages * heads * page)
+        self.view = pvmvmd_kv_pool(K.data_ptr(), V.data_ptr(), mp, *K.stride()[:3], *V.stride()[:3], pages, page, heads,
+                                   dim, _type_code(K, "K"))
+        self.ref = ctypes.byref(self.view)
+
+
+class KvBatch:
+    """Sequences over a KvPool: table (B x max_pages int32, page numbers), lens (B int32, cached tokens with the new
+    ones), cu (B + 1 int32, the rows of each one's new tokens; None: one each) and max_new (at least as many as any
+    has new ones, 0 if not known).  Checked once; the tensors' values may change between calls."""
+
+    def __init__(self, table, lens, cu=None, max_new: int = 0):
+        if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) or table.dtype not in _i32_types():
+            raise ValueError("table must be an int32 tensor B x max_pages with contiguous rows")
+        if not table.is_cuda:
+            raise TypeError("table must be a CUDA tensor")
+        B = table.shape[0]
+        lp = _dev_ptr(lens, "lens", _i32_types(), B)
+        cp = _dev_ptr(cu, "cu", _i32_types(), B + 1) if cu is not None else None
+        self.table, self.lens, self.cu, self.B = table, lens, cu, B
+        self.view = pvmvmd_kv_batch(table.data_ptr(), lp, cp, table.stride(0), B, B, table.shape[1], max_new)
+        self.ref = ctypes.byref(self.view)
+
+
+def pvmvmd_kv_append(pool: KvPool, batch: KvBatch, k, v, positions=None, rope: RopeTable | None = None, q=None,
+                     q_out=None, interleaved: bool = False, scale: float = 1.0, stream=None):
+    """k and v of the new tokens (T x heads x dim, one floating or field type) into the cache, k rotated at positions
+    (default: the cache indexes).  q (T x Hq x dim) is rotated into q_out (the pool's type), which is returned."""
+    T, H, D = k.shape[0], pool.heads, pool.dim
+    kr = _token_rows(k, "k", T, H, D)
+    vr = _token_rows(v, "v", T, H, D, k.dtype)
+    code = _type_code(k, "k", True)
+    Hq, qr, outr = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        Hq = q.shape[1]
+        qr = _token_rows(q, "q", T, Hq, D, k.dtype)
+        if q_out is None:
+            import torch
+            q_out = torch.empty((T, Hq, D), dtype=pool.K.dtype, device=q.device)
+        outr = _token_rows(q_out, "q_out", T, Hq, D, pool.K.dtype)
+    pp = None if positions is None else _dev_ptr(positions, "positions", _i32_types(), T)
+    batch.view.T = T
+    _check(_lib.pvmvmd_kv_append(pool.ref, batch.ref, rope.refs[bool(interleaved)] if rope is not None else None, pp,
+                                 code, scale, *kr, *vr, Hq, *qr, *outr, _stream_ptr(stream)), "pvmvmd_kv_append")
+    return q_out
+
+
+def pvmvmd_paged_attention(pool: KvPool, batch: KvBatch, q, out=None, lse=None, scale: float | None = None,
+                           causal: bool = True, window: int = 0, accumulate: bool = False, stream=None):
+    """Attention of the new tokens' q (T x Hq x dim, the pool's type) over the cache -> out (T x Hq x dim).  lse: a
+    float32 T x Hq tensor to fill; accumulate: add the attention weights to the pool's mass; scale: default
+    dim^-1/2."""
+    if q.dim() != 3:
+        raise ValueError("q must be T x Hq x dim")
+    T, Hq, D = q.shape[0], q.shape[1], pool.dim
+    qr = _token_rows(q, "q", T, Hq, D, pool.K.dtype)
+    if out is None:
+        import torch
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    outr = _token_rows(out, "out", T, Hq, D, pool.K.dtype)
+    lp = None if lse is None else _dev_ptr(lse, "lse", (_torch.float32,), T * Hq)
+    batch.view.T = T
+    _check(_lib.pvmvmd_paged_attention(pool.ref, batch.ref, Hq, *qr, D**-0.5 if scale is None else scale, causal,
+                                       window, accumulate, *outr, lp, _stream_ptr(stream)), "pvmvmd_paged_attention")
+    return out
+
+
+def pvmvmd_kv_evict(pool: KvPool, batch: KvBatch, budget: int, recent: int = 0, new_lens=None, new_table=None,
+                    stream=None):
+    """Keep min(len, budget) tokens of every sequence and head: the last `recent` and those of largest mass.  They
+    move to the front of the sequence's own pages, or to the pages of new_table.  Returns new_lens (default: the
+    batch's lens, updated)."""
+    if new_lens is None:
+        new_lens = batch.lens
+    if new_table is None:
+        new_table = batch.table
+    if new_table.dim() != 2 or new_table.shape[0] != batch.B or (new_table.shape[1] > 1 and new_table.stride(1) != 1) \
+            or new_table.dtype not in _i32_types() or not new_table.is_cuda:
+        raise ValueError("new_table must be an int32 CUDA tensor B x pages with contiguous rows")
+    _check(_lib.pvmvmd_kv_evict(pool.ref, batch.ref, budget, recent, new_table.data_ptr(), new_table.stride(0),
+                                new_table.shape[1], _dev_ptr(new_lens, "new_lens", _i32_types(), batch.B),
+                                _stream_ptr(stream)), "pvmvmd_kv_evict")
+    return new_lens
 
 
 PVMVMD_DEBUG_WAIT_OFF = 0

@@ -1,0 +1,46 @@
+// Host-side launchers of the client's attention (internal to the library).
+#pragma once
+
+#include "launch.h"
+
+namespace pv {
+
+struct KvView;
+
+// Heads of one tensor: strides in elements.
+struct RopePart {
+    const void *src;
+    void *dst;  // part 0 alone; parts 1 and 2 go to the cache
+    int64_t src_token, src_head, dst_token, dst_head;
+    int heads;
+};
+struct RopeJob {
+    const uint64_t *turns;
+    const int32_t *pos;  // null: cache indexes
+    RopePart part[3];    // q (or x), k, v
+    int T, dim, rot, interleaved, in_type, out_type;
+    float magnitude, scale;
+    bool cached;  // parts 1 and 2 are there
+};
+cudaError_t launch_rope(const RopeJob &j, const KvView *kv, cudaStream_t s);
+
+struct AttendJob {
+    const void *q;
+    void *out;
+    float *lse;                              // may be null
+    int64_t q_token, q_head, o_token, o_head;  // bytes
+    int Hq, window, type, max_new;           // window 0: none
+    float scale;
+    bool causal, accumulate;
+};
+cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t s);
+
+struct EvictJob {
+    int budget, recent;
+    const int32_t *new_table;
+    int64_t new_stride;
+    int32_t *new_lens;
+};
+cudaError_t launch_evict(const EvictJob &j, const KvView &kv, cudaStream_t s);
+
+}  // namespace pv

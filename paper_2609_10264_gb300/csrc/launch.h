@@ -189,7 +189,10 @@ cudaError_t launch_batched_grouped(const BatchJob *jobs, int count, uint32_t *er
 
 // Grow-only scratch of at least `need` bytes for `purpose` on the current
 // device, one buffer per stream (see scratch.cu).
-enum ScratchPurpose { kScratchDigits = 0 };  // digit tiles or planes of the batched products
+enum ScratchPurpose {
+    kScratchDigits = 0,     // digit tiles or planes of the batched products
+    kScratchAttention = 1,  // partial results of attention, lists of eviction
+};
 cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out);
 // Whether stream_scratch would return a buffer here: one that is large enough
 // already, or a stream that is not being captured.
