@@ -49,6 +49,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_attend_rows(const __grid_consta
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int t = blockIdx.x / j.Hq, h = blockIdx.x % j.Hq, hk = h / (j.Hq / kv.heads);
     const int b = kv.seq(t), len = kv.len(b);
+    if (kv.news(b) * (j.Hq / kv.heads) <= kFewRows) return;
     int lo, hi;
     reach(j, len, len - kv.news(b) + t - kv.first(b), lo, hi);
     float q[kPer], o[kPer] = {}, m = -INFINITY, l = 0.0f;
@@ -95,6 +96,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_mass_keys(const __grid_constant
     int page, slot;
     if (k >= len || !kv.place(b, k, page, slot)) return;
     const int G = j.Hq / kv.heads, t0 = kv.first(b), n = kv.news(b);
+    if (n * G <= kFewRows) return;
     float x[kPer], q[kPer], sum = 0.0f;
     load_row<T>(kv.K + page * kv.k_page + slot * kv.k_slot + hk * kv.k_head, kv.dim, lane, x);
     for (int t = 0; t < n; ++t) {
@@ -133,6 +135,11 @@ cudaError_t attend(const AttendJob &j, const KvView &kv, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    const int G = j.Hq / kv.heads;
+    if (G <= kFewRows) {
+        const cudaError_t e = launch_attention_few(j, kv, s);
+        if (e != cudaSuccess || j.max_new <= kFewRows / G) return e;
+    }
     return j.type == PVMVMD_BF16 ? attend<__nv_bfloat16>(j, kv, s) : attend<__half>(j, kv, s);
 }
 

@@ -34,6 +34,10 @@ struct AttendJob {
     bool causal, accumulate;
 };
 cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t s);
+// Of the sequences with at most kFewRows new rows per key head (tokens x query
+// heads of it); the others are left alone.
+constexpr int kFewRows = 16;
+cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
 
 struct EvictJob {
     int budget, recent;

@@ -1,0 +1,559 @@
+// Attention of sequences with few new rows (new tokens x query heads of a key head):
+// single generated tokens above all.  Bound by the reading of K and V.
+//
+// Work.  The keys of a (sequence, key head) come in tiles of 64.  All tiles of all
+// of them, one after the other, are dealt out evenly to the CTAs, whatever the
+// sequences' lengths: CTA c of C takes tiles [N c / C, N (c + 1) / C).  A sequence
+// that one CTA has whole is finished there; parts go to scratch as (maximum, sum,
+// unnormalised output), and k_few_join puts them together in order.
+//
+// A warp takes 16 of a tile's 64 keys through its own ring of asynchronous copies
+// and keeps its own running maximum and sum, so that nothing but the end of a
+// sequence waits for another warp.  Both products are m16n8k16 MMAs with the rows
+// padded to 16 (tcgen05 would pad them to 128, and its operands would all pass
+// through one barrier per tile).  P is split into two 16-bit parts, which leaves its
+// rounding at 2^-17: the MMAs are not what bounds this.
+#include <algorithm>
+
+#include "attention.h"
+#include "kv.cuh"
+
+namespace pv {
+namespace {
+
+constexpr int kFewWarps = 4;
+constexpr int kFewThreads = 32 * kFewWarps;
+constexpr int kSub = 16;                  // keys per warp and step
+constexpr int kTile = kFewWarps * kSub;   // keys per tile
+constexpr int kRows = kFewRows;           // rows per item, of one MMA
+
+struct FewArgs {
+    AttendJob j;
+    KvView kv;
+    float *part;     // [2 C][kRows][DP] unnormalised partial outputs
+    float2 *stat;    // [2 C][kRows] their maximum and sum
+    float2 *norm;    // [T][Hq] maximum and 1 / sum, where mass is accumulated
+    float *scores;   // [B][heads][max tiles x 64][rows] where mass is accumulated
+    int score_rows, max_tiles;
+    float scale2;    // scale x log2(e)
+    int G, C;
+};
+
+template <int DP>
+struct Few {
+    static constexpr int kStages = DP == 128 ? 3 : 4;
+    static constexpr int kRow = 2 * DP;  // bytes
+    static constexpr int kHalf = kSub * kRow;
+    static constexpr int kStage = 2 * kHalf;
+    static constexpr int kRing = kFewWarps * kStages * kStage;
+    static constexpr int kSmem = kRing + kRows * kRow;
+    static constexpr int kChunks = DP / 8;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (sizeof(T) == 2 && __is_same(T, __half))
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack(float x, float y, __half) {
+    const __half2 v = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack(float x, float y, __nv_bfloat16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// two values as a 16-bit pair and the pair of what that leaves
+template <typename T>
+__device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &lo) {
+    const T a = from_f32<T>(x), b = from_f32<T>(y);
+    hi = pack(x, y, T{});
+    lo = pack(x - to_f32(a), y - to_f32(b), T{});
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---------------------------------------------------------------- work
+// One sequence's share: `items` key heads of `tiles` tiles from key `first` on.
+struct Share {
+    int rows, first, tiles;
+    int64_t work;  // tiles over all key heads
+};
+__device__ __forceinline__ Share share(const FewArgs &a, int b) {
+    Share s;
+    const int n = a.kv.news(b), len = a.kv.len(b);
+    s.rows = n * a.G;
+    s.first = s.tiles = 0;
+    s.work = 0;
+    if (s.rows <= 0 || s.rows > kRows) return s;
+    if (a.j.window > 0) s.first = max(0, len - n - a.j.window + 1) / kTile * kTile;
+    s.tiles = max(1, (len - s.first + kTile - 1) / kTile);
+    s.work = (int64_t)s.tiles * a.kv.heads;
+    return s;
+}
+// Work before sequence `at` (p < 0), or the sequence that holds position p and the
+// work before it; and all the work.  By all threads of the CTA.
+struct Found {
+    int64_t total, before;
+    int b;
+};
+template <int kThreads>
+__device__ __forceinline__ Found find(const FewArgs &a, int at, int c) {
+    __shared__ int64_t s_warp[kThreads / 32], s_before;
+    __shared__ int s_b;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.kv.B + kThreads - 1) / kThreads, b0 = min(a.kv.B, tid * per), b1 = min(a.kv.B, b0 + per);
+    int64_t sum = 0;
+    for (int b = b0; b < b1; ++b) sum += share(a, b).work;
+    int64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(kFull, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    int64_t total = 0, base = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) base += s_warp[w];
+        total += s_warp[w];
+    }
+    int64_t pre = base + incl - sum;
+    const int64_t C = min((int64_t)a.C, total);
+    const int64_t p = at >= 0 ? -1 : c < C ? total * c / C : -1;
+    for (int b = b0; b < b1; ++b) {
+        const int64_t w = share(a, b).work;
+        if (at >= 0 ? b == at : p >= pre && p < pre + w) s_before = pre, s_b = b;
+        pre += w;
+    }
+    __syncthreads();
+    Found f;
+    f.total = total;
+    f.before = s_before;
+    f.b = s_b;
+    return f;
+}
+// The CTA that takes position p of N, among C <= N.
+__device__ __forceinline__ int owner(int64_t p, int64_t N, int64_t C) { return (int)(((p + 1) * C - 1) / N); }
+
+// ---------------------------------------------------------------- main kernel
+template <typename T, int DP>
+__global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ FewArgs a) {
+    using F = Few<DP>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float2 s_stat[kFewWarps][kRows];
+    const AttendJob &j = a.j;
+    const KvView &kv = a.kv;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, grp = lane >> 2;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const Found f = find<kFewThreads>(a, -1, blockIdx.x);
+    const int64_t C = min((int64_t)a.C, f.total);
+    if ((int64_t)blockIdx.x >= C) return;
+    const int64_t p1 = f.total * (blockIdx.x + 1) / C;
+    int64_t p = f.total * blockIdx.x / C, before = f.before;
+    int b = f.b;
+    Share sh = share(a, b);
+    const uint32_t ring = smem_u32(smem) + warp * F::kStages * F::kStage, qs = smem_u32(smem) + F::kRing;
+    const bool one_page = kv.ps.d % kSub == 0;
+    const int chunks = kv.dim / 8;
+
+    while (p < p1) {
+        while (p >= before + sh.work) {
+            before += sh.work;
+            sh = share(a, ++b);
+        }
+        const int item = (int)((p - before) / sh.tiles), t0 = (int)((p - before) % sh.tiles);
+        const int nt = (int)min((int64_t)(sh.tiles - t0), p1 - p);
+        const int hk = item, len = kv.len(b), n = kv.news(b), row0 = kv.first(b);
+        // ---- this warp's step i: keys from key0(i) on
+        auto key0 = [&](int i) { return sh.first + (t0 + i) * kTile + warp * kSub; };
+        int page_next = 0;
+        auto fetch_page = [&](int i) {  // of the step's keys, a lane each
+            const int k = key0(i) + (one_page ? 0 : lane & 15);
+            if (i < nt && k < len) {
+                uint32_t q, r;
+                kv.ps.divmod((uint32_t)k, q, r);
+                page_next = kv.table[b * kv.table_stride + q];
+            } else {
+                page_next = -1;
+            }
+        };
+        uint64_t seen = 0;  // of the steps loaded last, 16 bits each: the keys that are there
+        auto load = [&](int i) {  // step i's copies (its pages have been fetched)
+            unsigned there = 0;
+            if (i < nt) {
+                const int k0 = key0(i), ch = lane % F::kChunks, r0 = lane / F::kChunks;
+                const bool mine = (one_page || lane < kSub) && page_next >= 0 && page_next < kv.pages &&
+                                  k0 + (lane & 15) < len;
+                there = __ballot_sync(kFull, mine) & 0xffffu;
+                uint32_t d = ring + (i % F::kStages) * F::kStage + r0 * F::kRow, q, o;
+                kv.ps.divmod((uint32_t)(k0 + r0), q, o);
+                const char *ks = kv.K + page_next * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
+                const char *vs = kv.V + page_next * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
+                // a row's chunks by neighbouring lanes; rows of K, and of V behind them
+#pragma unroll
+                for (int u = 0; u < kSub * F::kChunks / 32; ++u) {
+                    const int r = u * (32 / F::kChunks) + r0;
+                    if (!one_page) {
+                        const int pg = __shfl_sync(kFull, page_next, r);
+                        kv.ps.divmod((uint32_t)(k0 + r), q, o);
+                        ks = kv.K + pg * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
+                        vs = kv.V + pg * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
+                    }
+                    const bool real = (there >> r & 1) && ch < chunks;
+                    copy16(d + ((ch ^ (r & 7)) << 4), real ? ks : kv.K, real);
+                    copy16(d + F::kHalf + ((ch ^ (r & 7)) << 4), real ? vs : kv.V, real);
+                    ks += (32 / F::kChunks) * kv.k_slot;
+                    vs += (32 / F::kChunks) * kv.v_slot;
+                    d += (32 / F::kChunks) * F::kRow;
+                }
+            }
+            seen = seen << 16 | there;
+            copy_commit();
+        };
+        // rows of Q, zero beyond the real ones
+        for (int id = tid; id < kRows * F::kChunks; id += kFewThreads) {
+            const int r = id / F::kChunks, ch = id % F::kChunks;
+            const bool real = r < sh.rows && ch < chunks;
+            const char *src = static_cast<const char *>(j.q);
+            if (real) src += (int64_t)(row0 + r / a.G) * j.q_token + (int64_t)(hk * a.G + r % a.G) * j.q_head + ch * 16;
+            copy16(qs + r * F::kRow + ((ch ^ (r & 7)) << 4), src, real);
+        }
+        copy_commit();
+        fetch_page(0);
+#pragma unroll
+        for (int i = 0; i < F::kStages - 1; ++i) {
+            load(i);
+            fetch_page(i + 1);
+        }
+        copy_wait<F::kStages - 1>();
+        __syncthreads();
+        uint32_t qf[DP / 16][4];
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+            const int r = lane & 15, ch = 2 * k + (lane >> 4);
+            ldsm4(qs + r * F::kRow + ((ch ^ (r & 7)) << 4), qf[k]);
+        }
+        // keys that rows grp and grp + 8 see
+        int lo[2], hi[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = grp + 8 * h, at = len - n + r / a.G;
+            hi[h] = r < sh.rows ? (j.causal ? min(len, at + 1) : len) : 0;
+            lo[h] = j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
+        }
+        float o[DP / 8][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+        for (int i = 0; i < nt; ++i) {
+            copy_wait<F::kStages - 2>();
+            __syncwarp();
+            load(i + F::kStages - 1);
+            fetch_page(i + F::kStages);
+            const uint32_t st = ring + (i % F::kStages) * F::kStage;
+            const int k0 = key0(i);
+            if (k0 >= len) continue;  // the same for the whole warp
+            const unsigned there = (unsigned)(seen >> 16 * (F::kStages - 1)) & 0xffffu;
+            float s[2][4] = {};
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                uint32_t kf[4];
+                const int r = (lane & 7) + ((lane >> 4) << 3), ch = 2 * k + ((lane >> 3) & 1);
+                ldsm4(st + r * F::kRow + ((ch ^ (r & 7)) << 4), kf);
+                mma<T>(s[0], qf[k], kf[0], kf[1]);
+                mma<T>(s[1], qf[k], kf[2], kf[3]);
+            }
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i16 = 8 * t + 2 * quad + (e & 1), key = k0 + i16, h = e >> 1;
+                    s[t][e] = key >= lo[h] && key < hi[h] && (there >> i16 & 1) ? s[t][e] * a.scale2 : -INFINITY;
+                    mx[h] = fmaxf(mx[h], s[t][e]);
+                }
+            if (a.scores) {
+                float *sc = a.scores + (((int64_t)b * kv.heads + hk) * a.max_tiles * kTile + k0 - sh.first) * a.score_rows;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = 8 * t + 2 * quad + (e & 1), r = grp + 8 * (e >> 1);
+                        if (r < sh.rows) sc[key * a.score_rows + r] = s[t][e];
+                    }
+            }
+            float shift[2];
+            bool moved = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                mx[h] = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 1));
+                mx[h] = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 2));
+                mx[h] = fmaxf(m[h], mx[h]);
+                moved |= mx[h] != m[h];
+                shift[h] = mx[h] == -INFINITY ? 0.0f : mx[h];
+            }
+            if (__any_sync(kFull, moved)) {
+                float w[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    w[h] = exp2_fast(m[h] - shift[h]);
+                    l[h] *= w[h];
+                    m[h] = mx[h];
+                }
+#pragma unroll
+                for (int d = 0; d < DP / 8; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[d][e] *= w[e >> 1];
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[t][e] = exp2_fast(s[t][e] - shift[e >> 1]);
+                    l[e >> 1] += s[t][e];
+                }
+            uint32_t ph[4], pl[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                split<T>(s[t][0], s[t][1], ph[2 * t], pl[2 * t]);
+                split<T>(s[t][2], s[t][3], ph[2 * t + 1], pl[2 * t + 1]);
+            }
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                uint32_t vf[4];
+                const int r = lane & 15, ch = 2 * d + (lane >> 4);
+                ldsm4_t(st + F::kHalf + r * F::kRow + ((ch ^ (r & 7)) << 4), vf);
+                mma<T>(o[2 * d], ph, vf[0], vf[1]);
+                mma<T>(o[2 * d + 1], ph, vf[2], vf[3]);
+                mma<T>(o[2 * d], pl, vf[0], vf[1]);
+                mma<T>(o[2 * d + 1], pl, vf[2], vf[3]);
+            }
+        }
+        copy_wait<0>();
+        // ---- join the warps through shared memory (the ring is empty)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            l[h] += __shfl_xor_sync(kFull, l[h], 1);
+            l[h] += __shfl_xor_sync(kFull, l[h], 2);
+            if (quad == 0) s_stat[warp][grp + 8 * h] = make_float2(m[h], l[h]);
+        }
+        __syncthreads();
+        float *all = reinterpret_cast<float *>(smem);
+        constexpr int kPitch = DP + 8;
+#pragma unroll
+        for (int d = 0; d < DP / 8; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<float2 *>(all + (warp * kRows + grp + 8 * h) * kPitch + 8 * d + 2 * quad) =
+                    make_float2(o[d][2 * h], o[d][2 * h + 1]);
+        __syncthreads();
+        const bool whole = nt == sh.tiles;
+        const int slot = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
+        for (int id = tid; id < sh.rows * (DP / 4); id += kFewThreads) {
+            const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
+            float M = -INFINITY, L = 0.0f;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, s_stat[w][r].x);
+            const float ref = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const float2 z = s_stat[w][r];
+                const float e = exp2_fast(z.x - ref);
+                const float4 x = *reinterpret_cast<const float4 *>(all + (w * kRows + r) * kPitch + d);
+                L += z.y * e;
+                v.x += x.x * e;
+                v.y += x.y * e;
+                v.z += x.z * e;
+                v.w += x.w * e;
+            }
+            if (!whole) {
+                *reinterpret_cast<float4 *>(a.part + ((int64_t)slot * kRows + r) * DP + d) = v;
+                if (d == 0) a.stat[(int64_t)slot * kRows + r] = make_float2(M, L);
+                continue;
+            }
+            const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
+            const float inv = M == -INFINITY ? 0.0f : 1.0f / L;
+            if (d < kv.dim) {
+                uint2 x;
+                x.x = pack(v.x * inv, v.y * inv, T{});
+                x.y = pack(v.z * inv, v.w * inv, T{});
+                *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
+            }
+            if (d == 0) {
+                if (j.lse) j.lse[(int64_t)t * j.Hq + h] = 0.6931471805599453f * (M + log2f(L));
+                if (a.norm) a.norm[(int64_t)t * j.Hq + h] = make_float2(M, inv);
+            }
+        }
+        __syncthreads();
+        p += nt;
+    }
+}
+
+// Sequences that several CTAs had: their parts, in the order of the keys.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kFewThreads) k_few_join(const __grid_constant__ FewArgs a) {
+    const AttendJob &j = a.j;
+    const KvView &kv = a.kv;
+    const int b = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x;
+    const Found f = find<kFewThreads>(a, b, 0);
+    const Share sh = share(a, b);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!sh.work) return;
+    const int64_t C = min((int64_t)a.C, f.total), i0 = f.before + (int64_t)hk * sh.tiles, i1 = i0 + sh.tiles;
+    const int c0 = owner(i0, f.total, C), c1 = owner(i1 - 1, f.total, C);
+    if (c0 == c1) return;
+    const int row0 = kv.first(b);
+    for (int id = tid; id < sh.rows * (DP / 4); id += kFewThreads) {
+        const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
+        auto stat = [&](int c) { return a.stat[(int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows + r]; };
+        float M = -INFINITY, L = 0.0f;
+        for (int c = c0; c <= c1; ++c) M = fmaxf(M, stat(c).x);
+        const float ref = M == -INFINITY ? 0.0f : M;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int c = c0; c <= c1; ++c) {
+            const float2 z = stat(c);
+            const float e = exp2_fast(z.x - ref);
+            const float4 x = *reinterpret_cast<const float4 *>(
+                a.part + ((int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows + r) * DP + d);
+            L += z.y * e;
+            v.x += x.x * e;
+            v.y += x.y * e;
+            v.z += x.z * e;
+            v.w += x.w * e;
+        }
+        const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
+        const float inv = M == -INFINITY ? 0.0f : 1.0f / L;
+        if (d < kv.dim) {
+            uint2 x;
+            x.x = pack(v.x * inv, v.y * inv, T{});
+            x.y = pack(v.z * inv, v.w * inv, T{});
+            *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
+        }
+        if (d == 0) {
+            if (j.lse) j.lse[(int64_t)t * j.Hq + h] = 0.6931471805599453f * (M + log2f(L));
+            if (a.norm) a.norm[(int64_t)t * j.Hq + h] = make_float2(M, inv);
+        }
+    }
+}
+
+// mass += sum over the rows of exp2(score - maximum) / sum, a thread per key.
+__global__ void __launch_bounds__(256) k_few_mass(const __grid_constant__ FewArgs a) {
+    const KvView &kv = a.kv;
+    const int b = blockIdx.z, hk = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+    const Share sh = share(a, b);
+    const int key = sh.first + i;
+    int page, slot;
+    if (!sh.work || key >= kv.len(b) || !kv.place(b, key, page, slot)) return;
+    const float *sc = a.scores + (((int64_t)b * kv.heads + hk) * a.max_tiles * kTile + i) * a.score_rows;
+    const int row0 = kv.first(b);
+    float sum = 0.0f;
+    for (int r = 0; r < sh.rows; ++r) {
+        const float2 z = a.norm[(int64_t)(row0 + r / a.G) * a.j.Hq + hk * a.G + r % a.G];
+        if (z.x != -INFINITY) sum += exp2_fast(sc[r] - z.x) * z.y;
+    }
+    *kv.mass_at(page, slot, hk) += sum;
+}
+
+int few_ctas() {
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return 2 * sms;
+}
+
+template <typename K>
+cudaError_t dependent(K kern, dim3 grid, int threads, const FewArgs &a, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return counted_launch(cudaLaunchKernelEx(&cfg, kern, a));
+}
+
+template <typename T, int DP>
+cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    FewArgs a{};
+    a.j = j;
+    a.kv = kv;
+    a.G = j.Hq / kv.heads;
+    a.C = few_ctas();
+    a.scale2 = j.scale * 1.4426950408889634f;
+    const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
+    a.max_tiles = (int)((room + kTile - 1) / kTile);
+    a.score_rows = (int)std::min<int64_t>(kRows, (int64_t)j.max_new * a.G);
+    auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+    const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
+    const size_t norms = j.accumulate ? up((size_t)kv.T * j.Hq * sizeof(float2)) : 0;
+    const size_t scores =
+        j.accumulate ? (size_t)kv.B * kv.heads * a.max_tiles * kTile * a.score_rows * sizeof(float) : 0;
+    void *buf = nullptr;
+    cudaError_t e = stream_scratch(kScratchAttention, parts + stats + norms + scores, s, &buf);
+    if (e != cudaSuccess) return e;
+    char *at = static_cast<char *>(buf);
+    a.part = reinterpret_cast<float *>(at);
+    a.stat = reinterpret_cast<float2 *>(at + parts);
+    if (j.accumulate) {
+        a.norm = reinterpret_cast<float2 *>(at + parts + stats);
+        a.scores = reinterpret_cast<float *>(at + parts + stats + norms);
+    }
+    e = func_attr(reinterpret_cast<const void *>(k_few<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                  Few<DP>::kSmem);
+    if (e != cudaSuccess) return e;
+    k_few<T, DP><<<(unsigned)a.C, kFewThreads, Few<DP>::kSmem, s>>>(a);
+    e = counted_launch(cudaGetLastError());
+    if (e == cudaSuccess && a.max_tiles > 1)
+        e = dependent(k_few_join<T, DP>, dim3((unsigned)kv.heads, (unsigned)kv.B), kFewThreads, a, s);
+    if (e == cudaSuccess && j.accumulate) {
+        const dim3 grid((unsigned)((room + 255) / 256), (unsigned)kv.heads, (unsigned)kv.B);
+        k_few_mass<<<grid, 256, 0, s>>>(a);
+        e = counted_launch(cudaGetLastError());
+    }
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    if (j.type == PVMVMD_BF16) return kv.dim <= 64 ? few<__nv_bfloat16, 64>(j, kv, s) : few<__nv_bfloat16, 128>(j, kv, s);
+    return kv.dim <= 64 ? few<__half, 64>(j, kv, s) : few<__half, 128>(j, kv, s);
+}
+
+}  // namespace pv
