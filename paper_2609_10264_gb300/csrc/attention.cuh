@@ -1,0 +1,123 @@
+// What the kernels of the client's attention share.
+#pragma once
+
+#include "attention.h"
+#include "kv.cuh"
+#include "tensor.cuh"
+
+namespace pv {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// 16 bytes, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint32_t pack(float x, float y, __half) {
+    const __half2 v = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack(float x, float y, __nv_bfloat16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+
+// Where a share of work lies among the sequences' works.  By all threads of the CTA.
+struct Found {
+    int64_t total, before;  // all the work, and that of the sequences before b
+    int b;
+};
+// The sequence that holds position pos(total) of all the work (a negative one: none).
+template <int kThreads, typename Work, typename Pos>
+__device__ __forceinline__ Found find(int B, Work work, Pos pos) {
+    __shared__ int64_t s_warp[kThreads / 32], s_before;
+    __shared__ int s_b;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    int64_t sum = 0;
+    for (int b = b0; b < b1; ++b) sum += work(b);
+    int64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(kFull, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) s_warp[warp] = incl;
+    if (tid == 0) s_before = 0, s_b = -1;
+    __syncthreads();
+    int64_t total = 0, base = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) base += s_warp[w];
+        total += s_warp[w];
+    }
+    int64_t pre = base + incl - sum;
+    const int64_t p = pos(total);
+    if (p >= pre && p < pre + sum)
+        for (int b = b0; b < b1; ++b) {
+            const int64_t w = work(b);
+            if (p >= pre && p < pre + w) s_before = pre, s_b = b;
+            pre += w;
+        }
+    __syncthreads();
+    return Found{total, s_before, s_b};
+}
+// The work before sequence at, which holds any, and all of it.
+template <int kThreads, typename Work>
+__device__ __forceinline__ Found before(int B, Work work, int at) {
+    __shared__ int64_t s_sum[2][kThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int64_t sum = 0, pre = 0;
+    for (int b = tid; b < B; b += kThreads) {
+        const int64_t w = work(b);
+        sum += w;
+        if (b < at) pre += w;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        sum += __shfl_xor_sync(kFull, sum, o);
+        pre += __shfl_xor_sync(kFull, pre, o);
+    }
+    if (lane == 0) s_sum[0][warp] = sum, s_sum[1][warp] = pre;
+    __syncthreads();
+    Found f{0, 0, at};
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        f.total += s_sum[0][w];
+        f.before += s_sum[1][w];
+    }
+    return f;
+}
+
+// Launched as soon as the kernel before lets it, which it waits for itself.
+template <typename K, typename A>
+cudaError_t launch_dependent(K kern, dim3 grid, int threads, const A &a, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return counted_launch(cudaLaunchKernelEx(&cfg, kern, a));
+}
+
+// 1 / L for a row's sum, 0 for one that sees nothing (M its maximum).
+__device__ __forceinline__ float inverse(float M, float L) { return M == -INFINITY ? 0.0f : 1.0f / L; }
+
+}  // namespace
+}  // namespace pv

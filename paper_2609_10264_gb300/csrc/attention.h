@@ -38,6 +38,8 @@ cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t 
 // heads of it); the others are left alone.
 constexpr int kFewRows = 16;
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
+// Of the others.
+cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s);
 
 struct EvictJob {
     int budget, recent;

@@ -1,0 +1,535 @@
+// Attention of many new rows (tokens of a chunk x query heads of a key head) over a
+// paged cache, on the tensor cores.
+//
+// A CTA takes 256 rows of one sequence and key head, token by token with the heads
+// of a token side by side, as two tiles of 128, and walks the keys that they see in
+// tiles of 128:
+//     S = Q K^T  (128 x 128, fp32 in TMEM),  P = exp2(scale2 (S - m)),  O += P V.
+// P goes back to TMEM as 16-bit values in the place of its S, from where the second
+// product reads it as its A operand; O (128 x D) stays in TMEM.
+//
+// Warps (384 threads):
+//   0-3, 4-7  the softmax of tile 0, of tile 1: a thread holds one row of S.  While
+//             one tile's is under way the tensor cores work for the other.
+//   8         issues the MMAs
+//   9-11      copy Q, then tiles of K and V through a ring, gathering the rows of
+//             their pages
+// The running maximum m is raised only where S exceeds it by more than 2^8 (in
+// steps of exp2), so that O is rescaled seldom, by the softmax warps themselves:
+// P stays below 2^8, and its sum and O are exact multiples of what they would be.
+// P is rounded to the cache's 16-bit type (2^-9 of each at most, for bf16), as the
+// MMA takes both operands in one type; the sum of a row is that of the 32-bit values.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+
+#include "attention.cuh"
+
+namespace pv {
+namespace {
+
+constexpr int kCM = 128;             // rows per tile
+constexpr int kCRows = 2 * kCM;      // rows per CTA
+constexpr int kCN = 128;             // keys per tile
+constexpr int kCThreads = 384;
+constexpr int kCLoaders = 3;         // warps 9-11
+constexpr int kCLag = 3;             // tiles that a loader keeps in flight
+constexpr int kCSoftRegs = 208, kCOtherRegs = 80;
+constexpr float kCHeadroom = 8.0f;   // log2 of the largest P
+
+struct ChunkArgs {
+    AttendJob j;
+    KvView kv;
+    float *part;    // [items][splits][256][DP] normalised partial outputs
+    float *stat;    // [items][splits][256] log2 of their sums
+    float scale2;   // |scale| log2(e)
+    int G, splits, negative;
+};
+
+template <int DP>
+struct Chunk {
+    static constexpr int kSlabs = DP / 64;             // 128-byte wide parts of a tile's rows
+    static constexpr int kSlab = kCN * 128;            // bytes
+    static constexpr int kTileBytes = kSlabs * kSlab;  // of Q, K and V alike
+    static constexpr int kStages = DP == 128 ? 5 : 8;
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
+    static constexpr int kO = 2 * kCN;                 // TMEM column of O
+    static constexpr int kPerRow = DP / 8;             // 16-byte chunks
+};
+
+// rows that loader warp w copies of a tile: 44, 44, 40
+__device__ __forceinline__ int loader_first(int w) { return 44 * w; }
+__device__ __forceinline__ int loader_rows(int w) { return w == 2 ? 40 : 44; }
+
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t chunk_idesc(int n) {
+    const uint32_t f = __is_same(T, __half) ? 0u : 1u;
+    return (1u << 4) | (f << 7) | (f << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kCM >> 4) << 24);
+}
+// V as the B operand: D (the N dimension) is contiguous.  64 values of D are a
+// swizzled 128-byte row, 8 keys 1024 bytes (stride offset), the next 64 values a
+// slab further (leading offset).
+__device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr, uint32_t slab) {
+    return (sw128_desc(saddr) & ~((uint64_t)0x3FFFu << 16)) | (uint64_t)(slab >> 4) << 16;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+          "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
+          "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
+          "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// ---------------------------------------------------------------- work
+__device__ __forceinline__ int chunk_tiles(const ChunkArgs &a, int b) {
+    const int rows = a.kv.news(b) * a.G;
+    return a.G <= kFewRows && rows <= kFewRows ? 0 : (rows + kCRows - 1) / kCRows;
+}
+// Item `idx` (row tile and key head of a sequence; the last tiles, which see most
+// keys, come first) and its share of the keys.
+struct ChunkItem {
+    int b, hk, row0, rows;       // rows of the sequence and key head, of this item
+    int len, n;                  // cached and new tokens
+    int kt0, kt1;                // key tiles of the item
+    int per, parts;              // key tiles of a split, splits that have any
+    int64_t slot;                // of the item, for partial results
+};
+__device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int idx, ChunkItem &it) {
+    const KvView &kv = a.kv;
+    const int hk = idx % kv.heads;
+    const int64_t rank = idx / kv.heads;
+    const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)chunk_tiles(a, b); },
+                                    [&](int64_t total) { return total - 1 - rank; });
+    if (f.b < 0) return false;
+    it.b = f.b;
+    it.hk = hk;
+    it.len = kv.len(f.b);
+    it.n = kv.news(f.b);
+    it.row0 = (int)(f.total - 1 - rank - f.before) * kCRows;
+    it.rows = min(kCRows, it.n * a.G - it.row0);
+    const int at0 = it.len - it.n + it.row0 / a.G, at1 = it.len - it.n + (it.row0 + it.rows - 1) / a.G;
+    const int hi = a.j.causal ? max(0, min(it.len, at1 + 1)) : it.len;
+    const int lo = a.j.window > 0 && at0 >= a.j.window ? at0 - a.j.window + 1 : 0;
+    it.kt0 = min(lo, hi) / kCN;
+    it.kt1 = max(it.kt0 + 1, (hi + kCN - 1) / kCN);  // a tile at least, if all of it is hidden
+    const int n = it.kt1 - it.kt0;
+    it.per = (n + a.splits - 1) / a.splits;
+    it.parts = (n + it.per - 1) / it.per;
+    it.slot = (int64_t)idx * a.splits;
+    return true;
+}
+
+// ---------------------------------------------------------------- main kernel
+template <typename T, int DP>
+__global__ void __launch_bounds__(kCThreads, 1)
+    k_chunk(const __grid_constant__ ChunkArgs a, uint32_t *__restrict__ err) {
+    using C = Chunk<DP>;
+    constexpr int kSt = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t q_full, kv_full[kSt], kv_empty[kSt], s_full[2], p_full[2], o_done[2], mma_done;
+    __shared__ uint32_t s_tmem;
+    __shared__ bool s_gap[4][kCLoaders];  // whether keys of a tile are not there, as each loader saw it
+    const AttendJob &j = a.j;
+    const KvView &kv = a.kv;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(kFull, tid >> 5, 0);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    ChunkItem it;
+    if (!chunk_item(a, blockIdx.x, it)) return;
+    const int split = blockIdx.y;
+    if (split >= it.parts) return;
+    const int kt0 = it.kt0 + split * it.per, nk = min(it.kt1, kt0 + it.per) - kt0;
+
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t qbase = base, ring = base + 2 * C::kTileBytes;
+    if (tid == 0) {
+        mbar_init(&q_full, kCLoaders);
+        mbar_init(&mma_done, 1);
+        for (int s = 0; s < kSt; ++s) {
+            mbar_init(&kv_full[s], kCLoaders);
+            mbar_init(&kv_empty[s], 1);
+        }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&s_full[t], 1);
+            mbar_init(&p_full[t], 4);
+            mbar_init(&o_done[t], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    // ring places of the tiles: K0, K1, V0, K2, V1, ..., the last V
+    const int places = 2 * nk;
+    auto place_k = [&](int i) { return i == 0 ? 0 : 2 * i - 1; };
+    auto place_v = [&](int i) { return min(2 * i + 2, places - 1); };
+
+    if (warp < 8) {
+        // ------------------------------------------------ softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCSoftRegs));
+        const int tile = warp >> 2, r = tile * kCM + (warp & 3) * 32 + lane;
+        const bool real = r < it.rows;
+        const int at = it.len - it.n + (it.row0 + r) / a.G;
+        const int hi = !real ? INT_MAX : j.causal ? min(it.len, at + 1) : it.len;
+        const int lo = real && j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t ts = tmem + lanes + (uint32_t)(tile * kCN), to = tmem + lanes + (uint32_t)(C::kO + tile * DP);
+        float m = -INFINITY, l = 0.0f;
+        bool ok = true;
+        for (int i = 0; i < nk; ++i) {
+            if (!mbar_wait_warp(&s_full[tile], i & 1, err, kWaitNs)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            float s[kCN];
+#pragma unroll
+            for (int c = 0; c < kCN / 32; ++c) tmem_ld32_async(ts + 32 * c, s + 32 * c);
+            const int k0 = (kt0 + i) * kCN;
+            const bool gap = s_gap[i & 3][0] || s_gap[i & 3][1] || s_gap[i & 3][2];
+            tmem_ld_wait();
+            if (__any_sync(kFull, k0 < lo || k0 + kCN > hi) || gap) {
+#pragma unroll
+                for (int c = 0; c < kCN / 32; ++c) {
+                    uint32_t there = kFull;
+                    if (gap) {
+                        const int key = k0 + 32 * c + lane;
+                        int page, slot;
+                        there = __ballot_sync(kFull, key < it.len && kv.place(it.b, key, page, slot));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int key = k0 + 32 * c + e;
+                        if (key < lo || key >= hi || !(there >> e & 1)) s[32 * c + e] = -INFINITY;
+                    }
+                }
+            }
+            float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+            for (int e = 4; e < kCN; ++e) mx[e & 3] = fmaxf(mx[e & 3], s[e]);
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            if (__any_sync(kFull, (top - m) * a.scale2 > kCHeadroom)) {  // -inf - -inf: not
+                const float mn = fmaxf(m, top), w = m == -INFINITY ? 0.0f : exp2_fast((m - mn) * a.scale2);
+                m = mn;
+                l *= w;
+                if (i > 0) {
+                    if (!mbar_wait_warp(&o_done[tile], (i - 1) & 1, err, kWaitNs)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32(to + 32 * c, o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * w);
+                        tmem_st32(to + 32 * c, o);
+                    }
+                }
+            }
+            const float shift = m == -INFINITY ? 0.0f : -m * a.scale2;
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float x = exp2_fast(fmaf(s[64 * c + 2 * e], a.scale2, shift));
+                    const float y = exp2_fast(fmaf(s[64 * c + 2 * e + 1], a.scale2, shift));
+                    sum[(2 * e) & 3] += x;
+                    sum[(2 * e + 1) & 3] += y;
+                    p[e] = pack(x, y, T{});
+                }
+                tmem_st32(ts + 32 * c, p);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[tile]);
+        }
+        // ------------------------------------------------ output
+        if (ok && mbar_wait_warp(&o_done[tile], (nk - 1) & 1, err, kWaitNs)) {
+            tc_fence_after();
+            const int t = kv.first(it.b) + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
+            const float inv = inverse(m, l), lse2 = m == -INFINITY ? (l != l ? l : m) : m * a.scale2 + log2f(l);
+            const int64_t prow = (it.slot + split) * kCRows + r;
+            char *orow = static_cast<char *>(j.out) + t * j.o_token + h * j.o_head;
+#pragma unroll 1
+            for (int c = 0; c < DP / 32; ++c) {
+                float o[32];
+                tmem_ld32_async(to + 32 * c, o);
+                tmem_ld_wait();
+                if (!real) continue;
+                if (it.parts > 1) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4 *>(a.part + prow * DP + 32 * c + e) =
+                            make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        if (32 * c + e < kv.dim)
+                            *reinterpret_cast<uint4 *>(orow + 2 * (32 * c + e)) =
+                                make_uint4(pack(o[e] * inv, o[e + 1] * inv, T{}), pack(o[e + 2] * inv, o[e + 3] * inv, T{}),
+                                           pack(o[e + 4] * inv, o[e + 5] * inv, T{}),
+                                           pack(o[e + 6] * inv, o[e + 7] * inv, T{}));
+                }
+            }
+            if (real) {
+                if (it.parts > 1)
+                    a.stat[prow] = lse2;
+                else if (j.lse)
+                    j.lse[(int64_t)t * j.Hq + h] = kLn2 * lse2;
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCOtherRegs));
+        if (warp == 8) {
+            // ------------------------------------------------ MMA issuer
+            const uint32_t id_s = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u), id_o = chunk_idesc<T>(DP) | 1u << 16;
+            auto stage = [&](int place) { return ring + (uint32_t)(place % kSt) * C::kTileBytes; };
+            auto full = [&](int place) { return mbar_wait_warp(&kv_full[place % kSt], (place / kSt) & 1, err, kWaitNs); };
+            auto scores = [&](int t, int i) {  // S = Q K^T
+                const uint64_t ad = sw128_desc(qbase + t * C::kTileBytes), bd = sw128_desc(stage(place_k(i)));
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const uint32_t off = (uint32_t)((k >> 2) * (C::kSlab >> 4) + (k & 3) * 2);
+                        mma_ss(tmem + t * kCN, ad + off, bd + off, id_s, k > 0);
+                    }
+                    commit(&s_full[t]);
+                }
+                __syncwarp();
+            };
+            auto output = [&](int t, int i) {  // O += P V
+                const uint64_t bd = sw128_desc_mn(stage(place_v(i)), C::kSlab);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kCN / 16; ++k)
+                        mma_ts(tmem + C::kO + t * DP, tmem + t * kCN + 8 * k, bd + (uint32_t)(k * (2048 >> 4)), id_o,
+                               i > 0 || k > 0);
+                    commit(&o_done[t]);
+                }
+                __syncwarp();
+            };
+            auto release = [&](int place) {
+                if (elect_one()) commit(&kv_empty[place % kSt]);
+                __syncwarp();
+            };
+            bool ok = mbar_wait_warp(&q_full, 0, err, kWaitNs) && full(0);
+            if (ok) {
+                tc_fence_after();
+                scores(0, 0);
+                scores(1, 0);
+                release(0);
+            }
+            for (int i = 0; i < nk && ok; ++i) {
+                const bool more = i + 1 < nk;
+                for (int t = 0; t < 2 && ok; ++t) {
+                    ok = (t || full(place_v(i))) && mbar_wait_warp(&p_full[t], i & 1, err, kWaitNs);
+                    if (!ok) break;
+                    tc_fence_after();
+                    output(t, i);
+                    if (!more) continue;
+                    ok = t || full(place_k(i + 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(t, i + 1);
+                }
+                if (!ok) break;
+                if (more) release(place_k(i + 1));
+                release(place_v(i));
+            }
+            // every MMA is through before the memory that it reads goes
+            if (elect_one()) commit(&mma_done);
+            __syncwarp();
+            mbar_wait_warp(&mma_done, 0, err, kWaitNs);
+        } else {
+            // ------------------------------------------------ copies
+            const int w = warp - 9, r0 = loader_first(w), nr = loader_rows(w);
+            constexpr int kPer = 32 / C::kPerRow;  // rows per instruction
+            const int ch = lane % C::kPerRow, sub = lane / C::kPerRow;
+            const uint32_t chunk_off = (uint32_t)(ch >> 3) * C::kSlab;
+            const bool chunk_real = ch * 8 < kv.dim;
+            bool ok = true;
+            // Q: both tiles' rows, token by token
+            for (int t = 0; t < 2; ++t)
+                for (int u = 0; u < nr; u += kPer) {
+                    const int rr = r0 + u + sub, r = t * kCM + rr;
+                    if (u + sub < nr) {
+                        const bool real = r < it.rows && chunk_real;
+                        const char *src = static_cast<const char *>(j.q);
+                        if (real)
+                            src += (int64_t)(kv.first(it.b) + (it.row0 + r) / a.G) * j.q_token +
+                                   (int64_t)(it.hk * a.G + (it.row0 + r) % a.G) * j.q_head + ch * 16;
+                        copy16(qbase + t * C::kTileBytes + chunk_off + sw128_off(rr, ch & 7), src, real);
+                    }
+                }
+            copy_commit();
+            for (int x = 0; x < places + kCLag && ok; ++x) {
+                if (x < places) {
+                    const bool values = (x > 0 && x % 2 == 0) || x == places - 1;
+                    const int i = !values ? (x + 1) / 2 : x == places - 1 ? nk - 1 : x / 2 - 1;
+                    if (x >= kSt && !mbar_wait_warp(&kv_empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
+                        ok = false;
+                        break;
+                    }
+                    // where this warp's rows are: a lane each, and some a second one
+                    int64_t off[2];
+                    unsigned there[2];
+                    bool gap = false;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int rr = 32 * y + lane, key = (kt0 + i) * kCN + r0 + rr;
+                        const bool wanted = rr < nr && key < it.len;
+                        int page = 0, slot = 0;
+                        const bool is = wanted && kv.place(it.b, key, page, slot);
+                        off[y] = !is ? 0
+                                 : values ? page * kv.v_page + slot * kv.v_slot + it.hk * kv.v_head
+                                          : page * kv.k_page + slot * kv.k_slot + it.hk * kv.k_head;
+                        there[y] = __ballot_sync(kFull, is);
+                        gap |= __any_sync(kFull, wanted && !is);
+                    }
+                    if (!values && lane == 0) s_gap[i & 3][w] = gap;
+                    const char *src = (values ? kv.V : kv.K) + ch * 16;
+                    const uint32_t dst = ring + (uint32_t)(x % kSt) * C::kTileBytes + chunk_off;
+#pragma unroll
+                    for (int u = 0; u < 44 / kPer; ++u) {
+                        const int rr = u * kPer + sub;
+                        const int64_t o = __shfl_sync(kFull, off[u * kPer / 32], rr & 31);
+                        if (rr < nr) {
+                            const bool real = chunk_real && (there[u * kPer / 32] >> (rr & 31) & 1);
+                            copy16(dst + sw128_off(r0 + rr, ch & 7), src + o, real);
+                        }
+                    }
+                }
+                copy_commit();
+                copy_wait<kCLag>();
+                if (x >= kCLag - 1) {  // Q, then tile x - kCLag
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(x < kCLag ? &q_full : &kv_full[(x - kCLag) % kSt]);
+                }
+            }
+            copy_wait<0>();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+// Items of several splits: their parts, in the order of the keys.  32 rows a CTA.
+constexpr int kJoinRows = 32;
+template <typename T, int DP>
+__global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant__ ChunkArgs a) {
+    ChunkItem it;
+    const bool is = chunk_item(a, blockIdx.x, it);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!is || it.parts == 1) return;
+    const int r0 = blockIdx.y * kJoinRows, rows = min(kJoinRows, it.rows - r0);
+    const int t0 = a.kv.first(it.b);
+    for (int id = threadIdx.x; id < rows * (DP / 4); id += kCThreads) {
+        const int r = r0 + id / (DP / 4), d = 4 * (id % (DP / 4));
+        float M = -INFINITY, L = 0.0f;
+        for (int p = 0; p < it.parts; ++p) M = fmaxf(M, a.stat[(it.slot + p) * kCRows + r]);
+        const float ref = M == -INFINITY ? 0.0f : M;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int p = 0; p < it.parts; ++p) {
+            const int64_t row = (it.slot + p) * kCRows + r;
+            const float e = exp2_fast(a.stat[row] - ref);
+            const float4 x = *reinterpret_cast<const float4 *>(a.part + row * DP + d);
+            L += e;
+            v.x += x.x * e;
+            v.y += x.y * e;
+            v.z += x.z * e;
+            v.w += x.w * e;
+        }
+        const int t = t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
+        const float inv = inverse(M, L);
+        if (d < a.kv.dim)
+            *reinterpret_cast<uint2 *>(static_cast<char *>(a.j.out) + t * a.j.o_token + h * a.j.o_head + 2 * d) =
+                make_uint2(pack(v.x * inv, v.y * inv, T{}), pack(v.z * inv, v.w * inv, T{}));
+        if (d == 0 && a.j.lse) a.j.lse[(int64_t)t * a.j.Hq + h] = kLn2 * (M + log2f(L));
+    }
+}
+
+template <typename T, int DP>
+cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    ChunkArgs a{};
+    a.j = j;
+    a.kv = kv;
+    a.G = j.Hq / kv.heads;
+    a.negative = j.scale < 0.0f;
+    // (a scale of 0 stays above it, so that hidden scores stay -infinity)
+    a.scale2 = std::max(std::fabs(j.scale) * kLog2e, 1e-37f);
+    uint32_t *err = library_error_word();
+    if (!err) return cudaErrorUnknown;
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    // at most as many row tiles as full ones and one more for each sequence of any
+    const int64_t rows = (int64_t)kv.T * a.G;
+    const int64_t tiles = rows / kCRows + std::min<int64_t>(kv.B, kv.T), items = tiles * kv.heads;
+    const int64_t room = (int64_t)kv.max_pages * kv.ps.d, keys = (room + kCN - 1) / kCN;
+    // keys are split where the items alone would leave SMs without work
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(sms / items, keys / 4));
+    if (items > INT_MAX) return cudaErrorInvalidValue;
+    if (a.splits > 1) {
+        auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+        const size_t n = (size_t)items * a.splits * kCRows, parts = up(n * DP * sizeof(float));
+        void *buf = nullptr;
+        const cudaError_t e = stream_scratch(kScratchAttention, parts + n * sizeof(float), s, &buf);
+        if (e != cudaSuccess) return e;
+        a.part = static_cast<float *>(buf);
+        a.stat = reinterpret_cast<float *>(static_cast<char *>(buf) + parts);
+    }
+    cudaError_t e = func_attr(reinterpret_cast<const void *>(k_chunk<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Chunk<DP>::kSmem);
+    if (e != cudaSuccess) return e;
+    k_chunk<T, DP><<<dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s>>>(a, err);
+    e = counted_launch(cudaGetLastError());
+    if (e == cudaSuccess && a.splits > 1)
+        e = launch_dependent(k_chunk_join<T, DP>, dim3((unsigned)items, kCRows / kJoinRows), kCThreads, a, s);
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    if (j.type == PVMVMD_BF16) return kv.dim <= 64 ? chunk<__nv_bfloat16, 64>(j, kv, s) : chunk<__nv_bfloat16, 128>(j, kv, s);
+    return kv.dim <= 64 ? chunk<__half, 64>(j, kv, s) : chunk<__half, 128>(j, kv, s);
+}
+
+}  // namespace pv

@@ -16,7 +16,7 @@
 #include <algorithm>
 
 #include "attention.h"
-#include "kv.cuh"
+#include "attention.cuh"
 
 namespace pv {
 namespace {
@@ -50,16 +50,6 @@ struct Few {
     static constexpr int kChunks = DP / 8;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes, or zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -85,14 +75,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack(float x, float y, __half) {
-    const __half2 v = __floats2half2_rn(x, y);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t pack(float x, float y, __nv_bfloat16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
 // two values as a 16-bit pair and the pair of what that leaves
 template <typename T>
 __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &lo) {
@@ -100,12 +82,6 @@ __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &
     hi = pack(x, y, T{});
     lo = pack(x - to_f32(a), y - to_f32(b), T{});
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // ---------------------------------------------------------------- work
 // One sequence's share: `items` key heads of `tiles` tiles from key `first` on.
 struct Share {
@@ -124,49 +100,6 @@ __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     s.work = (int64_t)s.tiles * a.kv.heads;
     return s;
 }
-// Work before sequence `at` (p < 0), or the sequence that holds position p and the
-// work before it; and all the work.  By all threads of the CTA.
-struct Found {
-    int64_t total, before;
-    int b;
-};
-template <int kThreads>
-__device__ __forceinline__ Found find(const FewArgs &a, int at, int c) {
-    __shared__ int64_t s_warp[kThreads / 32], s_before;
-    __shared__ int s_b;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (a.kv.B + kThreads - 1) / kThreads, b0 = min(a.kv.B, tid * per), b1 = min(a.kv.B, b0 + per);
-    int64_t sum = 0;
-    for (int b = b0; b < b1; ++b) sum += share(a, b).work;
-    int64_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(kFull, incl, o);
-        if (lane >= o) incl += v;
-    }
-    if (lane == 31) s_warp[warp] = incl;
-    __syncthreads();
-    int64_t total = 0, base = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) base += s_warp[w];
-        total += s_warp[w];
-    }
-    int64_t pre = base + incl - sum;
-    const int64_t C = min((int64_t)a.C, total);
-    const int64_t p = at >= 0 ? -1 : c < C ? total * c / C : -1;
-    for (int b = b0; b < b1; ++b) {
-        const int64_t w = share(a, b).work;
-        if (at >= 0 ? b == at : p >= pre && p < pre + w) s_before = pre, s_b = b;
-        pre += w;
-    }
-    __syncthreads();
-    Found f;
-    f.total = total;
-    f.before = s_before;
-    f.b = s_b;
-    return f;
-}
 // The CTA that takes position p of N, among C <= N.
 __device__ __forceinline__ int owner(int64_t p, int64_t N, int64_t C) { return (int)(((p + 1) * C - 1) / N); }
 
@@ -180,23 +113,28 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, grp = lane >> 2;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const Found f = find<kFewThreads>(a, -1, blockIdx.x);
+    const Found f = find<kFewThreads>(
+        kv.B, [&](int b) { return share(a, b).work; },
+        [&](int64_t total) {
+            const int64_t C = min((int64_t)a.C, total);
+            return (int64_t)blockIdx.x < C ? total * blockIdx.x / C : -1;
+        });
     const int64_t C = min((int64_t)a.C, f.total);
     if ((int64_t)blockIdx.x >= C) return;
     const int64_t p1 = f.total * (blockIdx.x + 1) / C;
-    int64_t p = f.total * blockIdx.x / C, before = f.before;
+    int64_t p = f.total * blockIdx.x / C, done = f.before;
     int b = f.b;
     Share sh = share(a, b);
-    const uint32_t ring = smem_u32(smem) + warp * F::kStages * F::kStage, qs = smem_u32(smem) + F::kRing;
+    const uint32_t ring = smem_addr(smem) + warp * F::kStages * F::kStage, qs = smem_addr(smem) + F::kRing;
     const bool one_page = kv.ps.d % kSub == 0;
     const int chunks = kv.dim / 8;
 
     while (p < p1) {
-        while (p >= before + sh.work) {
-            before += sh.work;
+        while (p >= done + sh.work) {
+            done += sh.work;
             sh = share(a, ++b);
         }
-        const int item = (int)((p - before) / sh.tiles), t0 = (int)((p - before) % sh.tiles);
+        const int item = (int)((p - done) / sh.tiles), t0 = (int)((p - done) % sh.tiles);
         const int nt = (int)min((int64_t)(sh.tiles - t0), p1 - p);
         const int hk = item, len = kv.len(b), n = kv.news(b), row0 = kv.first(b);
         // ---- this warp's step i: keys from key0(i) on
@@ -405,7 +343,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                 continue;
             }
             const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
-            const float inv = M == -INFINITY ? 0.0f : 1.0f / L;
+            const float inv = inverse(M, L);
             if (d < kv.dim) {
                 uint2 x;
                 x.x = pack(v.x * inv, v.y * inv, T{});
@@ -413,7 +351,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                 *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
             }
             if (d == 0) {
-                if (j.lse) j.lse[(int64_t)t * j.Hq + h] = 0.6931471805599453f * (M + log2f(L));
+                if (j.lse) j.lse[(int64_t)t * j.Hq + h] = kLn2 * (M + log2f(L));
                 if (a.norm) a.norm[(int64_t)t * j.Hq + h] = make_float2(M, inv);
             }
         }
@@ -428,7 +366,7 @@ __global__ void __launch_bounds__(kFewThreads) k_few_join(const __grid_constant_
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int b = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x;
-    const Found f = find<kFewThreads>(a, b, 0);
+    const Found f = before<kFewThreads>(kv.B, [&](int i) { return share(a, i).work; }, b);
     const Share sh = share(a, b);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!sh.work) return;
@@ -455,7 +393,7 @@ __global__ void __launch_bounds__(kFewThreads) k_few_join(const __grid_constant_
             v.w += x.w * e;
         }
         const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
-        const float inv = M == -INFINITY ? 0.0f : 1.0f / L;
+        const float inv = inverse(M, L);
         if (d < kv.dim) {
             uint2 x;
             x.x = pack(v.x * inv, v.y * inv, T{});
@@ -463,7 +401,7 @@ __global__ void __launch_bounds__(kFewThreads) k_few_join(const __grid_constant_
             *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
         }
         if (d == 0) {
-            if (j.lse) j.lse[(int64_t)t * j.Hq + h] = 0.6931471805599453f * (M + log2f(L));
+            if (j.lse) j.lse[(int64_t)t * j.Hq + h] = kLn2 * (M + log2f(L));
             if (a.norm) a.norm[(int64_t)t * j.Hq + h] = make_float2(M, inv);
         }
     }
@@ -494,20 +432,6 @@ int few_ctas() {
     return 2 * sms;
 }
 
-template <typename K>
-cudaError_t dependent(K kern, dim3 grid, int threads, const FewArgs &a, cudaStream_t s) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    return counted_launch(cudaLaunchKernelEx(&cfg, kern, a));
-}
-
 template <typename T, int DP>
 cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     FewArgs a{};
@@ -515,7 +439,7 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     a.kv = kv;
     a.G = j.Hq / kv.heads;
     a.C = few_ctas();
-    a.scale2 = j.scale * 1.4426950408889634f;
+    a.scale2 = j.scale * kLog2e;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
     a.max_tiles = (int)((room + kTile - 1) / kTile);
     a.score_rows = (int)std::min<int64_t>(kRows, (int64_t)j.max_new * a.G);
@@ -540,7 +464,7 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     k_few<T, DP><<<(unsigned)a.C, kFewThreads, Few<DP>::kSmem, s>>>(a);
     e = counted_launch(cudaGetLastError());
     if (e == cudaSuccess && a.max_tiles > 1)
-        e = dependent(k_few_join<T, DP>, dim3((unsigned)kv.heads, (unsigned)kv.B), kFewThreads, a, s);
+        e = launch_dependent(k_few_join<T, DP>, dim3((unsigned)kv.heads, (unsigned)kv.B), kFewThreads, a, s);
     if (e == cudaSuccess && j.accumulate) {
         const dim3 grid((unsigned)((room + 255) / 256), (unsigned)kv.heads, (unsigned)kv.B);
         k_few_mass<<<grid, 256, 0, s>>>(a);

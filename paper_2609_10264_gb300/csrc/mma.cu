@@ -51,6 +51,7 @@
 
 #include "common.cuh"
 #include "launch.h"
+#include "tensor.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -75,64 +76,6 @@ constexpr int kWarpLoader = 16, kWarpMma = 17, kWarpWLoad = 18;
 constexpr int kRawTile = kBM * kBK;     // 8 KiB: rows of 64 bytes, unswizzled
 constexpr int kRawOff = kStages * kStageBytes;
 constexpr int kMmaSmem = kRawOff + kRaw * kRawTile + 1024;  // + alignment slack
-constexpr uint32_t kWaitLimit = 1u << 24;
-
-__device__ __forceinline__ uint32_t smem_addr(const void *p) {
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
-
-// ---------------------------------------------------------------- mbarrier
-__device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count));
-}
-// Arrivals discard the barrier state (sink `_`): the thread does not wait
-// for it.
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_tx(uint64_t *bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes)
-                 : "memory");
-}
-// mbarrier.try_wait suspends the thread until the phase completes or a
-// hardware time limit passes, so a waiting warp costs no issue slots and
-// resumes as soon as the phase flips.
-__device__ __forceinline__ bool mbar_try(uint64_t *bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        " selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ uint64_t global_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-// Bounded wait for the phase of parity `parity`: false (and an error bit)
-// after wait_ns nanoseconds (kWaitNs unless a test shortens it) or kWaitLimit
-// attempts, whichever comes first.
-constexpr uint64_t kWaitNs = 1000000000ull;
-__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, uint32_t *err, uint64_t wait_ns) {
-    if (mbar_try(bar, parity)) return true;
-    const uint64_t t0 = global_ns();
-    for (uint32_t i = 0; i < kWaitLimit; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        if (global_ns() - t0 > wait_ns) break;
-    }
-    record_error(err, kErrMmaTimeout);
-    return false;
-}
-
-// The same wait taken by a whole warp: every lane polls, and the warp goes on
-// only if every lane saw the phase, so the lanes stay converged for the
-// .sync.aligned tcgen05 instructions and the warp-level arrivals that follow.
-__device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, uint32_t *err, uint64_t wait_ns) {
-    return __all_sync(kFull, mbar_wait(bar, parity, err, wait_ns));
-}
 
 // Arrival on a barrier of any CTA of the cluster (address from mapa).
 __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
@@ -142,19 +85,6 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
-}
-
-// One lane of the converged warp (the same one each time).  MMAs are issued
-// under this by a warp that runs its loop together: their operands are then
-// uniform, and an MMA takes the warp 16 cycles.  Under `if (lane == 0)` it took
-// 61 alone on an SM and about 110 beside the other roles, so issuing bounded
-// the kernels (one MMA of N = 256 lasts 128; a 64-vector 8B-class layer 86
-// -> 80 us, a 256-vector 70B-class layer 1115 -> 1030, and at the power cap
-// of a long run 88.6 -> 84.7 and 1116 -> 1092).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
-    return p != 0;
 }
 
 // ---------------------------------------------------------------- async copies, fences
@@ -174,28 +104,7 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, i
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_addr(bar))
         : "memory");
 }
-__device__ __forceinline__ void fence_async_smem() {
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_before() {
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_after() {
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-}
-
 // ---------------------------------------------------------------- tcgen05
-// Shared-memory matrix descriptor: K-major, 128-byte swizzle, 8-row groups
-// 1024 bytes apart (stride byte offset), start address in 16-byte units.
-__device__ __forceinline__ uint64_t sw128_desc(uint32_t saddr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
-    d |= (uint64_t)1u << 16;                      // leading byte offset (unused here)
-    d |= (uint64_t)(1024u >> 4) << 32;            // stride byte offset
-    d |= (uint64_t)1u << 46;                      // descriptor version
-    d |= (uint64_t)2u << 61;                      // 128-byte swizzle
-    return d;
-}
 // Instruction descriptor, kind::f16: fp16 A and B (format 0), f32 D (1),
 // both K-major, N = 256, M = 256 (the pair's two 128-row halves).
 constexpr uint32_t kIdesc = (1u << 4) | (0u << 7) | (0u << 10) | ((uint32_t)(kBN >> 3) << 17) |
@@ -221,24 +130,6 @@ __device__ __forceinline__ void warp_commit_pair(uint64_t *bar, uint16_t mask) {
     if (elect_one()) mma_commit_pair(bar, mask);
     __syncwarp();
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
-        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-          "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-// Byte offset of (row, 16-byte chunk) inside a K-major 128-byte-swizzled tile.
-__device__ __forceinline__ uint32_t sw128_off(uint32_t row, uint32_t chunk) {
-    return (row >> 3) * 1024u + (row & 7u) * 128u + ((chunk ^ (row & 7u)) << 4);
-}
-
 // Four signed bytes -> two fp16x2 words holding the same integers: with
 // u = b + 128 (the byte xor 0x80), the fp16 pattern 0x6400 | u is 1024 + u,
 // and subtracting 1152 leaves b exactly.
@@ -821,18 +712,6 @@ __device__ __forceinline__ void mma_pair_ta(uint32_t tmem_d, uint32_t tmem_a, ui
         "r"(tmem_a), "l"(bdesc), "r"(IDESC), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
-        "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
-        "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-
 struct GroupJob {
     const uint8_t *D;         // digit tiles: nvt x nkb blocks of GTile<V>::kBTile bytes
     uint32_t *Y;              // B x m, written directly when split == 1
