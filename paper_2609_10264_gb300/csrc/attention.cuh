@@ -116,6 +116,54 @@ cudaError_t launch_dependent(K kern, dim3 grid, int threads, const A &a, cudaStr
     return counted_launch(cudaLaunchKernelEx(&cfg, kern, a));
 }
 
+// ---------------------------------------------------------------- tensor cores
+// What the chunk kernels share: CTAs of three warpgroups, two that compute and one of
+// which a warp issues MMAs and three copy tiles of 128 rows.
+constexpr int kCM = 128;             // rows per tile
+constexpr int kCN = 128;             // keys per tile
+constexpr int kCThreads = 384;
+constexpr int kCLoaders = 3;         // warps 9-11
+constexpr int kCLag = 3;             // tiles that a loader keeps in flight
+constexpr int kCSoftRegs = 208, kCOtherRegs = 80;
+// rows that loader warp w copies of a tile: 44, 44, 40
+__device__ __forceinline__ int loader_first(int w) { return 44 * w; }
+__device__ __forceinline__ int loader_rows(int w) { return w == 2 ? 40 : 44; }
+
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t chunk_idesc(int n) {
+    const uint32_t f = __is_same(T, __half) ? 0u : 1u;
+    return (1u << 4) | (f << 7) | (f << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kCM >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+          "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
+          "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
+          "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+
+// New rows of sequence b per key head, where they are too many for the kernel of few.
+__device__ __forceinline__ int many_rows(const KvView &kv, int G, int b) {
+    const int rows = kv.news(b) * G;
+    return G <= kFewRows && rows <= kFewRows ? 0 : rows;
+}
+
 // 1 / L for a row's sum, 0 for one that sees nothing (M its maximum).
 __device__ __forceinline__ float inverse(float M, float L) { return M == -INFINITY ? 0.0f : 1.0f / L; }
 

@@ -28,6 +28,7 @@ struct AttendJob {
     const void *q;
     void *out;
     float *lse;                              // may be null
+    float *lse2;                             // scratch: log2 of the rows' sums (see row_sum), may be null
     int64_t q_token, q_head, o_token, o_head;  // bytes
     int Hq, window, type, max_new;           // window 0: none
     float scale;
@@ -40,6 +41,8 @@ constexpr int kFewRows = 16;
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
 // Of the others.
 cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s);
+// Their keys' mass, from lse2.
+cudaError_t launch_attention_mass(const AttendJob &j, const KvView &kv, cudaStream_t s);
 
 struct EvictJob {
     int budget, recent;

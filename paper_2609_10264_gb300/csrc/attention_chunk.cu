@@ -28,13 +28,7 @@
 namespace pv {
 namespace {
 
-constexpr int kCM = 128;             // rows per tile
 constexpr int kCRows = 2 * kCM;      // rows per CTA
-constexpr int kCN = 128;             // keys per tile
-constexpr int kCThreads = 384;
-constexpr int kCLoaders = 3;         // warps 9-11
-constexpr int kCLag = 3;             // tiles that a loader keeps in flight
-constexpr int kCSoftRegs = 208, kCOtherRegs = 80;
 constexpr float kCHeadroom = 8.0f;   // log2 of the largest P
 
 struct ChunkArgs {
@@ -57,27 +51,11 @@ struct Chunk {
     static constexpr int kPerRow = DP / 8;             // 16-byte chunks
 };
 
-// rows that loader warp w copies of a tile: 44, 44, 40
-__device__ __forceinline__ int loader_first(int w) { return 44 * w; }
-__device__ __forceinline__ int loader_rows(int w) { return w == 2 ? 40 : 44; }
-
-template <typename T>
-__device__ __forceinline__ constexpr uint32_t chunk_idesc(int n) {
-    const uint32_t f = __is_same(T, __half) ? 0u : 1u;
-    return (1u << 4) | (f << 7) | (f << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kCM >> 4) << 24);
-}
 // V as the B operand: D (the N dimension) is contiguous.  64 values of D are a
 // swizzled 128-byte row, 8 keys 1024 bytes (stride offset), the next 64 values a
 // slab further (leading offset).
 __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr, uint32_t slab) {
     return (sw128_desc(saddr) & ~((uint64_t)0x3FFFu << 16)) | (uint64_t)(slab >> 4) << 16;
-}
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(acc)
-        : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     asm volatile(
@@ -86,26 +64,17 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(idesc), "r"(acc)
         : "memory");
 }
-__device__ __forceinline__ void commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
-                 : "memory");
+// A row's log2 of its sum.  The scratch copy, which scores are compared with, has
+// +infinity for a row that sees nothing.
+__device__ __forceinline__ void row_sum(const AttendJob &j, int64_t row, float lse2) {
+    if (j.lse) j.lse[row] = kLn2 * lse2;
+    if (j.lse2) j.lse2[row] = lse2 == -INFINITY ? INFINITY : lse2;
 }
-__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
-        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
-          "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
-          "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
-          "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
-        : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------- work
 __device__ __forceinline__ int chunk_tiles(const ChunkArgs &a, int b) {
-    const int rows = a.kv.news(b) * a.G;
-    return a.G <= kFewRows && rows <= kFewRows ? 0 : (rows + kCRows - 1) / kCRows;
+    const int rows = many_rows(a.kv, a.G, b);
+    return (rows + kCRows - 1) / kCRows;
 }
 // Item `idx` (row tile and key head of a sequence; the last tiles, which see most
 // keys, come first) and its share of the keys.
@@ -306,8 +275,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
             if (real) {
                 if (it.parts > 1)
                     a.stat[prow] = lse2;
-                else if (j.lse)
-                    j.lse[(int64_t)t * j.Hq + h] = kLn2 * lse2;
+                else
+                    row_sum(j, (int64_t)t * j.Hq + h, lse2);
             }
         }
     } else {
@@ -481,7 +450,7 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
         if (d < a.kv.dim)
             *reinterpret_cast<uint2 *>(static_cast<char *>(a.j.out) + t * a.j.o_token + h * a.j.o_head + 2 * d) =
                 make_uint2(pack(v.x * inv, v.y * inv, T{}), pack(v.z * inv, v.w * inv, T{}));
-        if (d == 0 && a.j.lse) a.j.lse[(int64_t)t * a.j.Hq + h] = kLn2 * (M + log2f(L));
+        if (d == 0) row_sum(a.j, (int64_t)t * a.j.Hq + h, M + log2f(L));
     }
 }
 

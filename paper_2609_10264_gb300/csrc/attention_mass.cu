@@ -1,0 +1,262 @@
+// The attention weight that keys gather from many new rows: mass_j += sum over the
+// rows that see key j of exp2(scale2 q.k_j - lse2), after the attention itself has
+// written lse2, each row's log2 of the sum.
+//
+// Keys are the rows of the product here, so that a thread holds a key and its sum
+// needs no other thread, and no atomics: S^T = K Q^T.  A CTA keeps two tiles of 128
+// keys and walks the rows that see them in tiles of 128 through a ring; each of the
+// two has two accumulators in TMEM, so that the tensor cores work on the next tile
+// while one is summed.  One exp2 a score bounds it.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+
+#include "attention.cuh"
+
+namespace pv {
+namespace {
+
+constexpr int kMKeys = 2 * kCM;  // keys per CTA
+constexpr int kShifts = 8;       // ring of the rows' lse2, longer than that of their tiles
+
+struct MassArgs {
+    AttendJob j;
+    KvView kv;
+    float scale2;
+    int G, negative;
+};
+
+template <int DP>
+struct Mass {
+    static constexpr int kSlabs = DP / 64, kSlab = kCM * 128, kTileBytes = kSlabs * kSlab;
+    static constexpr int kStages = 4;
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
+    static constexpr int kPerRow = DP / 8;
+};
+
+// Keys [first, len) of a sequence that some new row may see, in CTAs' shares.
+__device__ __forceinline__ int mass_first(const MassArgs &a, int b) {
+    const int at = a.kv.len(b) - a.kv.news(b);
+    return a.j.window > 0 && at >= a.j.window ? (at - a.j.window + 1) / kMKeys * kMKeys : 0;
+}
+__device__ __forceinline__ int mass_shares(const MassArgs &a, int b) {
+    return many_rows(a.kv, a.G, b) ? (a.kv.len(b) - mass_first(a, b) + kMKeys - 1) / kMKeys : 0;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kCThreads, 1)
+    k_mass(const __grid_constant__ MassArgs a, uint32_t *__restrict__ err) {
+    using C = Mass<DP>;
+    constexpr int kSt = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], mma_done;
+    __shared__ __align__(16) float s_shift[kShifts][kCM];
+    __shared__ uint32_t s_tmem;
+    const AttendJob &j = a.j;
+    const KvView &kv = a.kv;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(kFull, tid >> 5, 0);
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t ring = base + 2 * C::kTileBytes;
+    if (tid == 0) {
+        for (int s = 0; s < kSt; ++s) {
+            mbar_init(&full[s], kCLoaders);
+            mbar_init(&empty[s], 1);
+        }
+        for (int t = 0; t < 4; ++t) {
+            mbar_init(&s_full[t >> 1][t & 1], 1);
+            mbar_init(&s_empty[t >> 1][t & 1], 4);
+        }
+        mbar_init(&mma_done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    if (warp < 8)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCSoftRegs));
+    else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCOtherRegs));
+
+    uint32_t g = 0;  // tiles of rows of the items before, the same in every warp
+    uint32_t items = 0;
+    bool ok = true;
+    for (int64_t idx = blockIdx.x;; idx += gridDim.x, ++items) {
+        const int hk = (int)(idx % kv.heads);
+        __syncthreads();  // the item before is through
+        const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
+                                        [&](int64_t) { return idx / kv.heads; });
+        if (f.b < 0) break;
+        const int b = f.b, len = kv.len(b), n = kv.news(b), rows = n * a.G, old = len - n;
+        const int k0 = mass_first(a, b) + (int)(idx / kv.heads - f.before) * kMKeys;
+        // rows that see any of the keys: [from, to)
+        auto first_row = [&](int key) { return j.causal && key > old ? (int)min((int64_t)rows, (int64_t)(key - old) * a.G) : 0; };
+        auto last_row = [&](int key) {
+            const int64_t t = j.window > 0 ? (int64_t)key + j.window - old : n;
+            return t >= n ? rows : t <= 0 ? 0 : (int)t * a.G;
+        };
+        const int r0 = first_row(k0) / kCM * kCM, r1 = last_row(min(k0 + kMKeys, len) - 1);
+        const int nt = r1 > r0 ? (r1 - r0 + kCM - 1) / kCM : 0;
+        if (warp < 8) {
+            // ------------------------------------------------ sums
+            const int tile = warp >> 2, key = k0 + tile * kCM + (warp & 3) * 32 + lane;
+            int page, slot;
+            const bool real = key < len && kv.place(b, key, page, slot);
+            const int lo = real ? first_row(key) : 0, hi = real ? last_row(key) : INT_MAX;
+            const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < nt && ok; ++i) {
+                const uint32_t x = g + i;
+                ok = mbar_wait_warp(&s_full[tile][x & 1], (x >> 1) & 1, err, kWaitNs);
+                if (!ok) break;
+                tc_fence_after();
+                float s[kCN];
+#pragma unroll
+                for (int c = 0; c < kCN / 32; ++c) tmem_ld32_async(ts + (x & 1) * kCN + 32 * c, s + 32 * c);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[tile][x & 1]);
+                const int q0 = r0 + i * kCM;
+                const float4 *sh = reinterpret_cast<const float4 *>(s_shift[x % kShifts]);
+                if (__any_sync(kFull, q0 < lo || hi - kCM < q0)) {
+#pragma unroll
+                    for (int e = 0; e < kCN; ++e)
+                        if (q0 + e < lo || q0 + e >= hi) s[e] = -INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < kCN; e += 4) {
+                    const float4 z = sh[e / 4];
+                    sum[0] += exp2_fast(fmaf(s[e], a.scale2, z.x));
+                    sum[1] += exp2_fast(fmaf(s[e + 1], a.scale2, z.y));
+                    sum[2] += exp2_fast(fmaf(s[e + 2], a.scale2, z.z));
+                    sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, z.w));
+                }
+            }
+            if (ok && real && nt) *kv.mass_at(page, slot, hk) += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        } else if (warp == 8) {
+            // ------------------------------------------------ MMA issuer
+            const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
+            for (int i = 0; i < nt && ok; ++i) {
+                const uint32_t x = g + i;
+                ok = mbar_wait_warp(&full[x % kSt], (x / kSt) & 1, err, kWaitNs);
+                const uint64_t bd = sw128_desc(ring + (x % kSt) * C::kTileBytes);
+                for (int t = 0; t < 2 && ok; ++t) {
+                    ok = mbar_wait_warp(&s_empty[t][x & 1], ((x >> 1) & 1) ^ 1, err, kWaitNs);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t ad = sw128_desc(base + t * C::kTileBytes);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < DP / 16; ++k) {
+                            const uint32_t off = (uint32_t)((k >> 2) * (C::kSlab >> 4) + (k & 3) * 2);
+                            mma_ss(tmem + (2 * t + (x & 1)) * kCN, ad + off, bd + off, idesc, k > 0);
+                        }
+                        commit(&s_full[t][x & 1]);
+                    }
+                    __syncwarp();
+                }
+                if (elect_one()) commit(&empty[x % kSt]);
+                __syncwarp();
+            }
+            // the next item's keys go where these are
+            if (elect_one()) commit(&mma_done);
+            __syncwarp();
+            mbar_wait_warp(&mma_done, items & 1, err, kWaitNs);
+        } else {
+            // ------------------------------------------------ copies: the keys with the first tile of rows
+            const int w = warp - 9, w0 = loader_first(w), nr = loader_rows(w);
+            constexpr int kPer = 32 / C::kPerRow;
+            const int ch = lane % C::kPerRow, sub = lane / C::kPerRow;
+            const uint32_t chunk_off = (uint32_t)(ch >> 3) * C::kSlab;
+            const bool chunk_real = ch * 8 < kv.dim;
+            if (nt)
+                for (int t = 0; t < 2; ++t)
+                    for (int u = 0; u < nr; u += kPer) {
+                        const int rr = w0 + u + sub, key = k0 + t * kCM + rr;
+                        int page, slot;
+                        if (u + sub < nr) {
+                            const bool real = chunk_real && key < len && kv.place(b, key, page, slot);
+                            const char *src = kv.K;
+                            if (real) src += page * kv.k_page + slot * kv.k_slot + hk * kv.k_head + ch * 16;
+                            copy16(base + t * C::kTileBytes + chunk_off + sw128_off(rr, ch & 7), src, real);
+                        }
+                    }
+            const int t0 = kv.first(b);
+            for (int i = 0; i < nt + kCLag && ok; ++i) {
+                const uint32_t x = g + i;
+                if (i < nt) {
+                    if (x >= kSt && !mbar_wait_warp(&empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t dst = ring + (x % kSt) * C::kTileBytes + chunk_off;
+                    const int q0 = r0 + i * kCM + w0;
+                    for (int u = 0; u < nr; u += kPer) {
+                        const int rr = u + sub, r = q0 + rr;
+                        if (rr < nr) {
+                            const bool real = chunk_real && r < rows;
+                            const char *src = static_cast<const char *>(j.q);
+                            if (real)
+                                src += (int64_t)(t0 + r / a.G) * j.q_token + (int64_t)(hk * a.G + r % a.G) * j.q_head + ch * 16;
+                            copy16(dst + sw128_off(w0 + rr, ch & 7), src, real);
+                        }
+                    }
+                    for (int rr = lane; rr < nr; rr += 32) {
+                        const int r = q0 + rr;
+                        s_shift[x % kShifts][w0 + rr] =
+                            r < rows ? -j.lse2[(int64_t)(t0 + r / a.G) * j.Hq + hk * a.G + r % a.G] : -INFINITY;
+                    }
+                }
+                copy_commit();
+                copy_wait<kCLag>();
+                if (i >= kCLag) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full[(x - kCLag) % kSt]);
+                }
+            }
+            copy_wait<0>();
+        }
+        g += (uint32_t)nt;
+        ok = __syncthreads_and(ok);
+        if (!ok) break;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+template <typename T, int DP>
+cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    MassArgs a{j, kv, std::max(std::fabs(j.scale) * kLog2e, 1e-37f), j.Hq / kv.heads, j.scale < 0.0f};
+    uint32_t *err = library_error_word();
+    if (!err) return cudaErrorUnknown;
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
+    const int64_t items = (int64_t)kv.B * kv.heads * ((room + kMKeys - 1) / kMKeys);
+    const cudaError_t e = func_attr(reinterpret_cast<const void *>(k_mass<T, DP>),
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, Mass<DP>::kSmem);
+    if (e != cudaSuccess) return e;
+    k_mass<T, DP><<<(unsigned)std::min<int64_t>(items, sms), kCThreads, Mass<DP>::kSmem, s>>>(a, err);
+    return counted_launch(cudaGetLastError());
+}
+
+}  // namespace
+
+cudaError_t launch_attention_mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    if (j.type == PVMVMD_BF16) return kv.dim <= 64 ? mass<__nv_bfloat16, 64>(j, kv, s) : mass<__nv_bfloat16, 128>(j, kv, s);
+    return kv.dim <= 64 ? mass<__half, 64>(j, kv, s) : mass<__half, 128>(j, kv, s);
+}
+
+}  // namespace pv

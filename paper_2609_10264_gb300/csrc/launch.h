@@ -192,7 +192,7 @@ cudaError_t launch_batched_grouped(const BatchJob *jobs, int count, uint32_t *er
 enum ScratchPurpose {
     kScratchDigits = 0,     // digit tiles or planes of the batched products
     kScratchAttention = 1,  // partial results of attention, lists of eviction
-    kScratchLse = 2,        // rows' log sums, where the caller does not take them
+    kScratchLse = 2,        // rows' log sums, for the accumulation of mass
 };
 cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out);
 // Whether stream_scratch would return a buffer here: one that is large enough
