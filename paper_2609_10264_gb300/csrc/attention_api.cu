@@ -37,7 +37,7 @@ int view(const pvmvmd_kv_pool *p, const pvmvmd_kv_batch *b, KvView &v) {
         return PVMVMD_E_ARG;
     if (p->pages < 1 || p->page_size < 1 || p->heads < 1 || p->dim < 8 || p->dim > PVMVMD_MAX_HEAD || p->dim % 8)
         return PVMVMD_E_SHAPE;
-    if (b->B < 1 || b->T < 0 || b->max_pages < 1 || b->max_new < 0) return PVMVMD_E_SHAPE;
+    if (b->B < 1 || b->B > 65535 || p->heads > 65535 || b->T < 0 || b->max_pages < 1 || b->max_new < 0) return PVMVMD_E_SHAPE;
     if ((int64_t)b->max_pages * p->page_size > 1 << 30) return PVMVMD_E_SHAPE;  // cache indexes are ints
     v.K = static_cast<char *>(p->K_dev);
     v.V = static_cast<char *>(p->V_dev);

@@ -681,7 +681,7 @@ def kept_indexes(w, L, budget, recent):
     ([5, 0, 64, 65, 200], 2, 64, 16, 64, 10, "hnd", "f16"), ([3000, 100], 2, 128, 100, 1000, 0, "fused", "bf16"),
     ([1025, 2049], 4, 80, 7, 1, 0, "nhd", "bf16"), ([300], 1, 64, 64, 50, 90, "nhd", "f16"),
     ([513, 40], 3, 40, 24, 5000, 3, "nhd", "bf16"), ([20000], 1, 64, 32, 19999, 1, "nhd", "bf16")])
-@pytest.mark.parametrize("where", ["own", "new"])
+@pytest.mark.parametrize("where", ["own", "copy", "new"])
 @pytest.mark.parametrize("values", ["any", "ties", "odd"])
 def test_evict(pv, lens, H, D, page, budget, recent, layout, kind, where, values):
     import torch
@@ -705,6 +705,8 @@ def test_evict(pv, lens, H, D, page, budget, recent, layout, kind, where, values
         table = _dev(tab, "field")
         pv.pvmvmd_kv_evict(c.pool, c.batch, budget, recent, new_lens=new_lens, new_table=table)
         assert c.dlens.tolist() == lens
+    elif where == "copy":  # the same pages, under a table of its own
+        pv.pvmvmd_kv_evict(c.pool, c.batch, budget, recent, new_lens=new_lens, new_table=table.clone())
     else:
         pv.pvmvmd_kv_evict(c.pool, c.batch, budget, recent)
         new_lens = c.dlens
