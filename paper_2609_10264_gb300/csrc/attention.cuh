@@ -14,6 +14,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src, bool real) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
+}
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() {
@@ -123,11 +126,46 @@ constexpr int kCM = 128;             // rows per tile
 constexpr int kCN = 128;             // keys per tile
 constexpr int kCThreads = 384;
 constexpr int kCLoaders = 3;         // warps 9-11
-constexpr int kCLag = 3;             // tiles that a loader keeps in flight
 constexpr int kCSoftRegs = 208, kCOtherRegs = 80;
-// rows that loader warp w copies of a tile: 44, 44, 40
-__device__ __forceinline__ int loader_first(int w) { return 44 * w; }
-__device__ __forceinline__ int loader_rows(int w) { return w == 2 ? 40 : 44; }
+
+// The copy of a tile of 128 rows of up to DP 16-bit values by one warp, into the
+// 128-byte-swizzled layout: slabs of 64 values, 16 KiB each.
+template <int DP>
+struct TileCopy {
+    static constexpr int kPerRow = DP / 8, kRowsAt = 32 / kPerRow;  // 16-byte chunks, rows per instruction
+    int lane, ch, sub;
+    bool real;  // this lane's chunk is one of the row's
+    __device__ __forceinline__ TileCopy(int lane_, int dim)
+        : lane(lane_), ch(lane_ % kPerRow), sub(lane_ / kPerRow), real(lane_ % kPerRow * 8 < dim) {}
+    // row(rr, off): whether row rr is there, and its place from src on; else zeros
+    template <typename Row>
+    __device__ __forceinline__ void copy(uint32_t dst, const char *src, Row row) const {
+        int64_t off[kCM / 32];
+        unsigned there[kCM / 32];
+#pragma unroll
+        for (int x = 0; x < kCM / 32; ++x) {
+            const bool is = row(32 * x + lane, off[x]);
+            if (!is) off[x] = 0;
+            there[x] = __ballot_sync(kFull, is);
+        }
+        src += real ? ch * 16 : 0;
+        dst += (uint32_t)(ch >> 3) * (kCM * 128);
+#pragma unroll
+        for (int u = 0; u < kCM / kRowsAt; ++u) {
+            const int rr = u * kRowsAt + sub, x = u * kRowsAt / 32;
+            const int64_t o = __shfl_sync(kFull, off[x], rr & 31);
+            copy16(dst + sw128_off(rr, ch & 7), src + o, real && (there[x] >> (rr & 31) & 1));
+        }
+        copy_commit();
+    }
+    // Once it is all there, for the MMAs.
+    __device__ __forceinline__ void arrive(uint64_t *bar) const {
+        copy_wait<0>();
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ constexpr uint32_t chunk_idesc(int n) {

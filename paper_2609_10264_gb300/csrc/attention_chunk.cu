@@ -13,7 +13,9 @@
 //             one tile's is under way the tensor cores work for the other.
 //   8         issues the MMAs
 //   9-11      copy Q, then tiles of K and V through a ring, gathering the rows of
-//             their pages
+//             their pages.  Each takes whole tiles: the fence that shows a tile to
+//             the MMAs waits for all that its warp has in flight (a third of every
+//             tile each, three tiles ahead, took 3.6 us for 256 rows and 128 keys)
 // The running maximum m is raised only where S exceeds it by more than 2^8 (in
 // steps of exp2), so that O is rescaled seldom, by the softmax warps themselves:
 // P stays below 2^8, and its sum and O are exact multiples of what they would be.
@@ -48,7 +50,6 @@ struct Chunk {
     static constexpr int kStages = DP == 128 ? 5 : 8;
     static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
     static constexpr int kO = 2 * kCN;                 // TMEM column of O
-    static constexpr int kPerRow = DP / 8;             // 16-byte chunks
 };
 
 // V as the B operand: D (the N dimension) is contiguous.  64 values of D are a
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t q_full, kv_full[kSt], kv_empty[kSt], s_full[2], p_full[2], o_done[2], mma_done;
     __shared__ uint32_t s_tmem;
-    __shared__ bool s_gap[4][kCLoaders];  // whether keys of a tile are not there, as each loader saw it
+    __shared__ bool s_gap[4];  // whether keys of a tile are not there
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31;
@@ -134,10 +135,10 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t qbase = base, ring = base + 2 * C::kTileBytes;
     if (tid == 0) {
-        mbar_init(&q_full, kCLoaders);
+        mbar_init(&q_full, 2);
         mbar_init(&mma_done, 1);
         for (int s = 0; s < kSt; ++s) {
-            mbar_init(&kv_full[s], kCLoaders);
+            mbar_init(&kv_full[s], 1);
             mbar_init(&kv_empty[s], 1);
         }
         for (int t = 0; t < 2; ++t) {
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
 #pragma unroll
             for (int c = 0; c < kCN / 32; ++c) tmem_ld32_async(ts + 32 * c, s + 32 * c);
             const int k0 = (kt0 + i) * kCN;
-            const bool gap = s_gap[i & 3][0] || s_gap[i & 3][1] || s_gap[i & 3][2];
+            const bool gap = s_gap[i & 3];
             tmem_ld_wait();
             if (__any_sync(kFull, k0 < lo || k0 + kCN > hi) || gap) {
 #pragma unroll
@@ -343,72 +344,38 @@ __global__ void __launch_bounds__(kCThreads, 1)
             mbar_wait_warp(&mma_done, 0, err, kWaitNs);
         } else {
             // ------------------------------------------------ copies
-            const int w = warp - 9, r0 = loader_first(w), nr = loader_rows(w);
-            constexpr int kPer = 32 / C::kPerRow;  // rows per instruction
-            const int ch = lane % C::kPerRow, sub = lane / C::kPerRow;
-            const uint32_t chunk_off = (uint32_t)(ch >> 3) * C::kSlab;
-            const bool chunk_real = ch * 8 < kv.dim;
-            bool ok = true;
-            // Q: both tiles' rows, token by token
-            for (int t = 0; t < 2; ++t)
-                for (int u = 0; u < nr; u += kPer) {
-                    const int rr = r0 + u + sub, r = t * kCM + rr;
-                    if (u + sub < nr) {
-                        const bool real = r < it.rows && chunk_real;
-                        const char *src = static_cast<const char *>(j.q);
-                        if (real)
-                            src += (int64_t)(kv.first(it.b) + (it.row0 + r) / a.G) * j.q_token +
-                                   (int64_t)(it.hk * a.G + (it.row0 + r) % a.G) * j.q_head + ch * 16;
-                        copy16(qbase + t * C::kTileBytes + chunk_off + sw128_off(rr, ch & 7), src, real);
-                    }
-                }
-            copy_commit();
-            for (int x = 0; x < places + kCLag && ok; ++x) {
-                if (x < places) {
-                    const bool values = (x > 0 && x % 2 == 0) || x == places - 1;
-                    const int i = !values ? (x + 1) / 2 : x == places - 1 ? nk - 1 : x / 2 - 1;
-                    if (x >= kSt && !mbar_wait_warp(&kv_empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
-                        ok = false;
-                        break;
-                    }
-                    // where this warp's rows are: a lane each, and some a second one
-                    int64_t off[2];
-                    unsigned there[2];
-                    bool gap = false;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int rr = 32 * y + lane, key = (kt0 + i) * kCN + r0 + rr;
-                        const bool wanted = rr < nr && key < it.len;
-                        int page = 0, slot = 0;
-                        const bool is = wanted && kv.place(it.b, key, page, slot);
-                        off[y] = !is ? 0
-                                 : values ? page * kv.v_page + slot * kv.v_slot + it.hk * kv.v_head
-                                          : page * kv.k_page + slot * kv.k_slot + it.hk * kv.k_head;
-                        there[y] = __ballot_sync(kFull, is);
-                        gap |= __any_sync(kFull, wanted && !is);
-                    }
-                    if (!values && lane == 0) s_gap[i & 3][w] = gap;
-                    const char *src = (values ? kv.V : kv.K) + ch * 16;
-                    const uint32_t dst = ring + (uint32_t)(x % kSt) * C::kTileBytes + chunk_off;
-#pragma unroll
-                    for (int u = 0; u < 44 / kPer; ++u) {
-                        const int rr = u * kPer + sub;
-                        const int64_t o = __shfl_sync(kFull, off[u * kPer / 32], rr & 31);
-                        if (rr < nr) {
-                            const bool real = chunk_real && (there[u * kPer / 32] >> (rr & 31) & 1);
-                            copy16(dst + sw128_off(r0 + rr, ch & 7), src + o, real);
-                        }
-                    }
-                }
-                copy_commit();
-                copy_wait<kCLag>();
-                if (x >= kCLag - 1) {  // Q, then tile x - kCLag
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(x < kCLag ? &q_full : &kv_full[(x - kCLag) % kSt]);
-                }
+            const int w = warp - 9;
+            const TileCopy<DP> tile(lane, kv.dim);
+            // Q: token by token, a tile each by the first two
+            if (w < 2) {
+                tile.copy(qbase + w * C::kTileBytes, static_cast<const char *>(j.q), [&](int rr, int64_t &off) {
+                    const int r = w * kCM + rr;
+                    off = (int64_t)(kv.first(it.b) + (it.row0 + r) / a.G) * j.q_token +
+                          (int64_t)(it.hk * a.G + (it.row0 + r) % a.G) * j.q_head;
+                    return r < it.rows;
+                });
+                tile.arrive(&q_full);
             }
-            copy_wait<0>();
+            // tiles of K and V in turn
+            for (int x = w; x < places; x += kCLoaders) {
+                const bool values = (x > 0 && x % 2 == 0) || x == places - 1;
+                const int i = !values ? (x + 1) / 2 : x == places - 1 ? nk - 1 : x / 2 - 1;
+                if (x >= kSt && !mbar_wait_warp(&kv_empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) break;
+                const int64_t ps = values ? kv.v_page : kv.k_page, ss = values ? kv.v_slot : kv.k_slot,
+                              hs = it.hk * (values ? kv.v_head : kv.k_head);
+                bool gap = false;
+                tile.copy(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? kv.V : kv.K, [&](int rr, int64_t &off) {
+                    const int key = (kt0 + i) * kCN + rr;
+                    int page = 0, slot = 0;
+                    const bool is = key < it.len && kv.place(it.b, key, page, slot);
+                    gap |= key < it.len && !is;
+                    off = page * ps + slot * ss + hs;
+                    return is;
+                });
+                gap = __any_sync(kFull, gap);
+                if (!values && lane == 0) s_gap[i & 3] = gap;
+                tile.arrive(&kv_full[x % kSt]);
+            }
         }
     }
     tc_fence_before();

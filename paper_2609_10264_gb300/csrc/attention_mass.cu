@@ -17,7 +17,7 @@ namespace pv {
 namespace {
 
 constexpr int kMKeys = 2 * kCM;  // keys per CTA
-constexpr int kShifts = 8;       // ring of the rows' lse2, longer than that of their tiles
+constexpr int kShifts = 8;       // ring of the rows' lse2, which are read after their tiles are let go
 
 struct MassArgs {
     AttendJob j;
@@ -31,7 +31,6 @@ struct Mass {
     static constexpr int kSlabs = DP / 64, kSlab = kCM * 128, kTileBytes = kSlabs * kSlab;
     static constexpr int kStages = 4;
     static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
-    static constexpr int kPerRow = DP / 8;
 };
 
 // Keys [first, len) of a sequence that some new row may see, in CTAs' shares.
@@ -49,7 +48,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     using C = Mass<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], mma_done;
+    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full, mma_done;
     __shared__ __align__(16) float s_shift[kShifts][kCM];
     __shared__ uint32_t s_tmem;
     const AttendJob &j = a.j;
@@ -60,13 +59,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const uint32_t ring = base + 2 * C::kTileBytes;
     if (tid == 0) {
         for (int s = 0; s < kSt; ++s) {
-            mbar_init(&full[s], kCLoaders);
+            mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
         for (int t = 0; t < 4; ++t) {
             mbar_init(&s_full[t >> 1][t & 1], 1);
             mbar_init(&s_empty[t >> 1][t & 1], 4);
         }
+        mbar_init(&k_full, 2);
         mbar_init(&mma_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCOtherRegs));
 
     uint32_t g = 0;  // tiles of rows of the items before, the same in every warp
-    uint32_t items = 0;
+    uint32_t items = 0, loaded = 0;  // of them, those with rows
     bool ok = true;
     for (int64_t idx = blockIdx.x;; idx += gridDim.x, ++items) {
         const int hk = (int)(idx % kv.heads);
@@ -132,16 +132,17 @@ __global__ void __launch_bounds__(kCThreads, 1)
 #pragma unroll
                 for (int e = 0; e < kCN; e += 4) {
                     const float4 z = sh[e / 4];
-                    sum[0] += exp2_fast(fmaf(s[e], a.scale2, z.x));
-                    sum[1] += exp2_fast(fmaf(s[e + 1], a.scale2, z.y));
-                    sum[2] += exp2_fast(fmaf(s[e + 2], a.scale2, z.z));
-                    sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, z.w));
+                    sum[0] += exp2_fast(fmaf(s[e], a.scale2, -z.x));
+                    sum[1] += exp2_fast(fmaf(s[e + 1], a.scale2, -z.y));
+                    sum[2] += exp2_fast(fmaf(s[e + 2], a.scale2, -z.z));
+                    sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, -z.w));
                 }
             }
             if (ok && real && nt) *kv.mass_at(page, slot, hk) += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         } else if (warp == 8) {
             // ------------------------------------------------ MMA issuer
             const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
+            if (nt) ok = mbar_wait_warp(&k_full, loaded & 1, err, kWaitNs);
             for (int i = 0; i < nt && ok; ++i) {
                 const uint32_t x = g + i;
                 ok = mbar_wait_warp(&full[x % kSt], (x / kSt) & 1, err, kWaitNs);
@@ -169,61 +170,41 @@ __global__ void __launch_bounds__(kCThreads, 1)
             __syncwarp();
             mbar_wait_warp(&mma_done, items & 1, err, kWaitNs);
         } else {
-            // ------------------------------------------------ copies: the keys with the first tile of rows
-            const int w = warp - 9, w0 = loader_first(w), nr = loader_rows(w);
-            constexpr int kPer = 32 / C::kPerRow;
-            const int ch = lane % C::kPerRow, sub = lane / C::kPerRow;
-            const uint32_t chunk_off = (uint32_t)(ch >> 3) * C::kSlab;
-            const bool chunk_real = ch * 8 < kv.dim;
-            if (nt)
-                for (int t = 0; t < 2; ++t)
-                    for (int u = 0; u < nr; u += kPer) {
-                        const int rr = w0 + u + sub, key = k0 + t * kCM + rr;
-                        int page, slot;
-                        if (u + sub < nr) {
-                            const bool real = chunk_real && key < len && kv.place(b, key, page, slot);
-                            const char *src = kv.K;
-                            if (real) src += page * kv.k_page + slot * kv.k_slot + hk * kv.k_head + ch * 16;
-                            copy16(base + t * C::kTileBytes + chunk_off + sw128_off(rr, ch & 7), src, real);
-                        }
-                    }
-            const int t0 = kv.first(b);
-            for (int i = 0; i < nt + kCLag && ok; ++i) {
-                const uint32_t x = g + i;
-                if (i < nt) {
-                    if (x >= kSt && !mbar_wait_warp(&empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t dst = ring + (x % kSt) * C::kTileBytes + chunk_off;
-                    const int q0 = r0 + i * kCM + w0;
-                    for (int u = 0; u < nr; u += kPer) {
-                        const int rr = u + sub, r = q0 + rr;
-                        if (rr < nr) {
-                            const bool real = chunk_real && r < rows;
-                            const char *src = static_cast<const char *>(j.q);
-                            if (real)
-                                src += (int64_t)(t0 + r / a.G) * j.q_token + (int64_t)(hk * a.G + r % a.G) * j.q_head + ch * 16;
-                            copy16(dst + sw128_off(w0 + rr, ch & 7), src, real);
-                        }
-                    }
-                    for (int rr = lane; rr < nr; rr += 32) {
-                        const int r = q0 + rr;
-                        s_shift[x % kShifts][w0 + rr] =
-                            r < rows ? -j.lse2[(int64_t)(t0 + r / a.G) * j.Hq + hk * a.G + r % a.G] : -INFINITY;
-                    }
-                }
-                copy_commit();
-                copy_wait<kCLag>();
-                if (i >= kCLag) {
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&full[(x - kCLag) % kSt]);
-                }
+            // ------------------------------------------------ copies: the keys, then tiles of rows in turn
+            const int w = warp - 9;
+            const TileCopy<DP> tile(lane, kv.dim);
+            if (nt && w < 2) {
+                tile.copy(base + w * C::kTileBytes, kv.K, [&](int rr, int64_t &off) {
+                    const int key = k0 + w * kCM + rr;
+                    int page = 0, slot = 0;
+                    const bool is = key < len && kv.place(b, key, page, slot);
+                    off = page * kv.k_page + slot * kv.k_slot + hk * kv.k_head;
+                    return is;
+                });
+                tile.arrive(&k_full);
             }
-            copy_wait<0>();
+            const int t0 = kv.first(b);
+            for (int i = w; i < nt; i += kCLoaders) {
+                const uint32_t x = g + i;
+                if (x >= kSt && !mbar_wait_warp(&empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
+                    ok = false;
+                    break;
+                }
+                const int q0 = r0 + i * kCM;
+                // the rows' lse2 with them (rows past the end are masked)
+                const float *lse2 = j.lse2 + (int64_t)t0 * j.Hq + hk * a.G;
+                const uint32_t sh = smem_addr(s_shift[x % kShifts]);
+                tile.copy(ring + (x % kSt) * C::kTileBytes, static_cast<const char *>(j.q), [&](int rr, int64_t &off) {
+                    const int r = q0 + rr, t = r / a.G, h = r % a.G;
+                    off = (int64_t)(t0 + t) * j.q_token + (int64_t)(hk * a.G + h) * j.q_head;
+                    copy4(sh + 4 * rr, r < rows ? lse2 + (int64_t)t * j.Hq + h : lse2, r < rows);
+                    return r < rows;
+                });
+                tile.arrive(&full[x % kSt]);
+            }
         }
         g += (uint32_t)nt;
+        loaded += nt > 0;
         ok = __syncthreads_and(ok);
         if (!ok) break;
     }
