@@ -150,13 +150,39 @@ struct TileCopy {
         }
         src += real ? ch * 16 : 0;
         dst += (uint32_t)(ch >> 3) * (kCM * 128);
+        // some places at a time, then their copies, which the compiler keeps in order
+        constexpr int kBatch = 4;
 #pragma unroll
-        for (int u = 0; u < kCM / kRowsAt; ++u) {
-            const int rr = u * kRowsAt + sub, x = u * kRowsAt / 32;
-            const int64_t o = __shfl_sync(kFull, off[x], rr & 31);
-            copy16(dst + sw128_off(rr, ch & 7), src + o, real && (there[x] >> (rr & 31) & 1));
+        for (int u0 = 0; u0 < kCM / kRowsAt; u0 += kBatch) {
+            int64_t o[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int first = (u0 + u) * kRowsAt;
+                o[u] = __shfl_sync(kFull, off[first / 32], (first + sub) & 31);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int first = (u0 + u) * kRowsAt;
+                copy16(dst + sw128_off(first + sub, ch & 7), src + o[u], real && (there[first / 32] >> ((first + sub) & 31) & 1));
+            }
         }
         copy_commit();
+    }
+    // The same from pages, by the tensor memory accelerator: boxes of `box` keys that
+    // lie on one page, a lane each; map: (values, slots, heads, pages).  page: of the
+    // lane's box.
+    __device__ __forceinline__ void fetch(uint32_t dst, const CUtensorMap *map, int box, int slot, int hk, int page,
+                                          uint64_t *bar) const {
+        if (lane == 0) mbar_arrive_tx(bar, DP / 64 * kCM * 128);
+        __syncwarp();
+        if (lane * box < kCM)
+#pragma unroll
+            for (int s = 0; s < DP / 64; ++s)
+                asm volatile(
+                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+                    "%4, %5}], [%6];" ::"r"(dst + s * (kCM * 128) + lane * box * 128),
+                    "l"(reinterpret_cast<uint64_t>(map)), "r"(64 * s), "r"(slot), "r"(hk), "r"(page), "r"(smem_addr(bar))
+                    : "memory");
     }
     // Once it is all there, for the MMAs.
     __device__ __forceinline__ void arrive(uint64_t *bar) const {
@@ -195,6 +221,22 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *r) {
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+
+// Keys or values as a tensor of (values, slots, heads, pages), for boxes of 64 values
+// x `box` slots.
+inline cudaError_t page_map(CUtensorMap *map, const KvView &kv, bool values, int type, int box) {
+    PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dim[4] = {(cuuint64_t)kv.dim, kv.ps.d, (cuuint64_t)kv.heads, (cuuint64_t)kv.pages};
+    const cuuint64_t stride[3] = {(cuuint64_t)(values ? kv.v_slot : kv.k_slot), (cuuint64_t)(values ? kv.v_head : kv.k_head),
+                                  (cuuint64_t)(values ? kv.v_page : kv.k_page)};
+    const cuuint32_t part[4] = {64, (cuuint32_t)box, 1, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = encode(map, type == PVMVMD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              4, values ? kv.V : kv.K, dim, stride, part, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
 
 // New rows of sequence b per key head, where they are too many for the kernel of few.
 __device__ __forceinline__ int many_rows(const KvView &kv, int G, int b) {

@@ -40,6 +40,7 @@ struct ChunkArgs {
     float *stat;    // [items][splits][256] log2 of their sums
     float scale2;   // |scale| log2(e)
     int G, splits, negative;
+    int box;        // keys per TMA box, 0: the pages are not such that boxes fit them
 };
 
 template <int DP>
@@ -65,6 +66,32 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(idesc), "r"(acc)
         : "memory");
 }
+// ---------------------------------------------------------------- pairs of 32-bit values
+// (half the instructions of the softmax's multiply-adds and sums)
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &x, float &y) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // A row's log2 of its sum.  The scratch copy, which scores are compared with, has
 // +infinity for a row that sees nothing.
 __device__ __forceinline__ void row_sum(const AttendJob &j, int64_t row, float lse2) {
@@ -114,11 +141,12 @@ __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int idx, ChunkIte
 // ---------------------------------------------------------------- main kernel
 template <typename T, int DP>
 __global__ void __launch_bounds__(kCThreads, 1)
-    k_chunk(const __grid_constant__ ChunkArgs a, uint32_t *__restrict__ err) {
+    k_chunk(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap k_map,
+            const __grid_constant__ CUtensorMap v_map, uint32_t *__restrict__ err) {
     using C = Chunk<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t q_full, kv_full[kSt], kv_empty[kSt], s_full[2], p_full[2], o_done[2], mma_done;
+    __shared__ __align__(8) uint64_t q_full, kv_full[kSt], kv_empty[kSt], s_full[2], p_full[2][2], o_done[2], mma_done;
     __shared__ uint32_t s_tmem;
     __shared__ bool s_gap[4];  // whether keys of a tile are not there
     const AttendJob &j = a.j;
@@ -143,7 +171,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&s_full[t], 1);
-            mbar_init(&p_full[t], 4);
+            mbar_init(&p_full[t][0], 4);
+            mbar_init(&p_full[t][1], 4);
             mbar_init(&o_done[t], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -203,8 +232,10 @@ __global__ void __launch_bounds__(kCThreads, 1)
             }
             float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-            for (int e = 4; e < kCN; ++e) mx[e & 3] = fmaxf(mx[e & 3], s[e]);
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            for (int e = 4; e < kCN; e += 8)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = e + 2 * k + 1 < kCN ? max3(mx[k], s[e + 2 * k], s[e + 2 * k + 1]) : mx[k];
+            const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
             if (__any_sync(kFull, (top - m) * a.scale2 > kCHeadroom)) {  // -inf - -inf: not
                 const float mn = fmaxf(m, top), w = m == -INFINITY ? 0.0f : exp2_fast((m - mn) * a.scale2);
                 m = mn;
@@ -226,24 +257,29 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 }
             }
             const float shift = m == -INFINITY ? 0.0f : -m * a.scale2;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const uint64_t scale_2 = pair(a.scale2, a.scale2), shift_2 = pair(shift, shift);
+            uint64_t sum[2] = {0u, 0u};
+            // P in two halves, so that the MMAs on the first run while the second is formed
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 uint32_t p[32];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
-                    const float x = exp2_fast(fmaf(s[64 * c + 2 * e], a.scale2, shift));
-                    const float y = exp2_fast(fmaf(s[64 * c + 2 * e + 1], a.scale2, shift));
-                    sum[(2 * e) & 3] += x;
-                    sum[(2 * e + 1) & 3] += y;
+                    float x, y;
+                    unpair(fma2(pair(s[64 * c + 2 * e], s[64 * c + 2 * e + 1]), scale_2, shift_2), x, y);
+                    x = exp2_fast(x);
+                    y = exp2_fast(y);
+                    sum[e & 1] = add2(sum[e & 1], pair(x, y));
                     p[e] = pack(x, y, T{});
                 }
                 tmem_st32(ts + 32 * c, p);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[tile][c]);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[tile]);
+            float x, y;
+            unpair(add2(sum[0], sum[1]), x, y);
+            l += x + y;
         }
         // ------------------------------------------------ output
         if (ok && mbar_wait_warp(&o_done[tile], (nk - 1) & 1, err, kWaitNs)) {
@@ -299,14 +335,16 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 }
                 __syncwarp();
             };
-            auto output = [&](int t, int i) {  // O += P V
+            auto output = [&](int t, int i, int half) {  // O += P V, 64 keys
                 const uint64_t bd = sw128_desc_mn(stage(place_v(i)), C::kSlab);
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < kCN / 16; ++k)
-                        mma_ts(tmem + C::kO + t * DP, tmem + t * kCN + 8 * k, bd + (uint32_t)(k * (2048 >> 4)), id_o,
-                               i > 0 || k > 0);
-                    commit(&o_done[t]);
+                    for (int k = 0; k < kCN / 32; ++k) {
+                        const int kk = half * (kCN / 32) + k;
+                        mma_ts(tmem + C::kO + t * DP, tmem + t * kCN + 8 * kk, bd + (uint32_t)(kk * (2048 >> 4)), id_o,
+                               i > 0 || kk > 0);
+                    }
+                    if (half) commit(&o_done[t]);
                 }
                 __syncwarp();
             };
@@ -324,10 +362,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
             for (int i = 0; i < nk && ok; ++i) {
                 const bool more = i + 1 < nk;
                 for (int t = 0; t < 2 && ok; ++t) {
-                    ok = (t || full(place_v(i))) && mbar_wait_warp(&p_full[t], i & 1, err, kWaitNs);
+                    ok = t || full(place_v(i));
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        ok = mbar_wait_warp(&p_full[t][half], i & 1, err, kWaitNs);
+                        if (!ok) break;
+                        tc_fence_after();
+                        output(t, i, half);
+                    }
                     if (!ok) break;
-                    tc_fence_after();
-                    output(t, i);
                     if (!more) continue;
                     ok = t || full(place_k(i + 1));
                     if (!ok) break;
@@ -357,15 +399,28 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 tile.arrive(&q_full);
             }
             // tiles of K and V in turn
-            for (int x = w; x < places; x += kCLoaders) {
+            int x = w;
+            for (; x < places; x += kCLoaders) {
                 const bool values = (x > 0 && x % 2 == 0) || x == places - 1;
                 const int i = !values ? (x + 1) / 2 : x == places - 1 ? nk - 1 : x / 2 - 1;
                 if (x >= kSt && !mbar_wait_warp(&kv_empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) break;
                 const int64_t ps = values ? kv.v_page : kv.k_page, ss = values ? kv.v_slot : kv.k_slot,
                               hs = it.hk * (values ? kv.v_head : kv.k_head);
+                const int key0 = (kt0 + i) * kCN;
+                if (a.box && key0 + kCN <= it.len) {
+                    int page = 0, slot = 0;
+                    const bool is = lane * a.box >= kCN || kv.place(it.b, key0 + lane * a.box, page, slot);
+                    if (__all_sync(kFull, is)) {
+                        if (!values && lane == 0) s_gap[i & 3] = false;
+                        __syncwarp();
+                        tile.fetch(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? &v_map : &k_map, a.box, slot, it.hk,
+                                   page, &kv_full[x % kSt]);
+                        continue;
+                    }
+                }
                 bool gap = false;
                 tile.copy(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? kv.V : kv.K, [&](int rr, int64_t &off) {
-                    const int key = (kt0 + i) * kCN + rr;
+                    const int key = key0 + rr;
                     int page = 0, slot = 0;
                     const bool is = key < it.len && kv.place(it.b, key, page, slot);
                     gap |= key < it.len && !is;
@@ -376,6 +431,10 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 if (!values && lane == 0) s_gap[i & 3] = gap;
                 tile.arrive(&kv_full[x % kSt]);
             }
+            // copies in flight complete before the CTA may exit (a tile whose place has
+            // been filled again was read, and its barrier is a phase ahead)
+            for (int y = x - kCLoaders; y >= 0 && y + kSt >= min(places, x); y -= kCLoaders)
+                mbar_wait_warp(&kv_full[y % kSt], (y / kSt) & 1, err, kWaitNs);
         }
     }
     tc_fence_before();
@@ -421,6 +480,18 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
     }
 }
 
+// Keys per box: the largest power of two, up to a tile, that divides the page size;
+// of less than 8 (a swizzle's rows) none, and none where a stride is not one that a
+// tensor map can have (64 bits wide, but not negative, nor zero where it is used).
+int page_box(const KvView &kv) {
+    int box = 1;
+    while (box < kCN && kv.ps.d % (2 * box) == 0) box *= 2;
+    const int64_t most = (int64_t)1 << 40;
+    for (int64_t st : {kv.k_slot, kv.k_head, kv.k_page, kv.v_slot, kv.v_head, kv.v_page})
+        if (st <= 0 || st >= most) return 0;
+    return box >= 8 ? box : 0;
+}
+
 template <typename T, int DP>
 cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     ChunkArgs a{};
@@ -451,10 +522,14 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
         a.part = static_cast<float *>(buf);
         a.stat = reinterpret_cast<float *>(static_cast<char *>(buf) + parts);
     }
+    CUtensorMap maps[2] = {};
+    a.box = page_box(kv);
+    for (int v = 0; a.box && v < 2; ++v)
+        if (page_map(&maps[v], kv, v, j.type, a.box) != cudaSuccess) a.box = 0;
     cudaError_t e = func_attr(reinterpret_cast<const void *>(k_chunk<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
                               Chunk<DP>::kSmem);
     if (e != cudaSuccess) return e;
-    k_chunk<T, DP><<<dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s>>>(a, err);
+    k_chunk<T, DP><<<dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s>>>(a, maps[0], maps[1], err);
     e = counted_launch(cudaGetLastError());
     if (e == cudaSuccess && a.splits > 1)
         e = launch_dependent(k_chunk_join<T, DP>, dim3((unsigned)items, kCRows / kJoinRows), kCThreads, a, s);

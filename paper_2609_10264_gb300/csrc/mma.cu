@@ -548,22 +548,6 @@ int choose_split(const void *kern, int pairs, int nkb) {
     return best;
 }
 
-// cuTensorMapEncodeTiled from the driver, looked up once.
-PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
-                cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    }();
-    return fn;
-}
-
 cudaError_t batched_launch(const int8_t *W, int m, int K, const uint32_t *Xhat, int B, uint32_t *Yhat,
                            uint32_t *err, uint8_t *D, cudaStream_t s) {
     const int nkb = (K + kBK - 1) / kBK;
