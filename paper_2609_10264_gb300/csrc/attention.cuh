@@ -106,10 +106,11 @@ __device__ __forceinline__ Found before(int B, Work work, int at) {
 
 // Launched as soon as the kernel before lets it, which it waits for itself.
 template <typename K, typename A>
-cudaError_t launch_dependent(K kern, dim3 grid, int threads, const A &a, cudaStream_t s) {
+cudaError_t launch_dependent(K kern, dim3 grid, int threads, const A &a, cudaStream_t s, int smem = 0) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -1,26 +1,29 @@
 // Eviction from a paged cache by accumulated attention weight (pvmvmd_kv_evict).
 //
 // k_evict_select, a CTA per (sequence, head): the kept tokens' indexes, ascending.
-// Masses map to integers of the same order, and the value of the last one kept is
-// found two bits at a time: three counts of the keys not below a bound.  Keys stay
-// in registers (up to 32768 of them; longer sequences are read again for each of
-// four passes of 8 bits).  A scan over the counts of every warp's keys then gives
-// each kept one its place.
+// Masses map to integers of the same order, held in registers (up to 32768 of them;
+// those of longer sequences are read again for every pass).  The value of the last
+// one kept is found in three passes of 11, 11 and 10 bits: a histogram of the keys
+// that share the digits found, and a scan of its bins.  Another scan over the counts
+// of every warp's keys gives each kept one its place.
 //
 // k_evict_move: the rows of a list, 16 KiB of keys and as many of values a CTA.  A row
 // never moves to a higher index, so in place the rows that lie where a CTA writes are
 // its own or those of CTAs before it: it reports its rows read and waits for their
 // reports before it writes.  Blocks start in the order of their index (as the other
 // kernels that chain blocks rest on); the wait is bounded.
+#include <algorithm>
+
 #include "attention.cuh"
 
 namespace pv {
 namespace {
 
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
-constexpr int kSelPer = 64;   // keys per thread in registers
-constexpr int kMoveThreads = 256;
-constexpr int kMoveChunks = 8;  // 16-byte chunks per thread
+constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32;
+constexpr int kSelPer = 32;   // keys per thread in registers
+constexpr int kBins = 2048;
+constexpr int kMoveThreads = 128;
+constexpr int kMoveBytes = 32 << 10;  // of keys and values per CTA
 
 struct EvictArgs {
     EvictJob j;
@@ -43,66 +46,71 @@ __device__ __forceinline__ uint32_t key_at(const KvView &kv, int b, int h, int i
     return kv.place(b, i, page, slot) ? mass_key(*kv.mass_at(page, slot, h)) : 0u;
 }
 
-// The largest value of which at least `want` of `cand` keys are not below, and how
-// many of those equal to it are among the first `want`: keys in registers, thread
-// i's x-th one number i + x kSelThreads; those past the end are 0 and not counted.
-__device__ __forceinline__ uint32_t select_held(const uint32_t (&key)[kSelPer], int cand, int want, int &equal) {
-    __shared__ int s_count[2][3][kSelWarps];
+// Sum of v over the threads before this one, and over all.
+template <typename V>
+__device__ __forceinline__ V scan_before(V v, V &total) {
+    __shared__ V s_warp[kSelWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t value = 0;  // at least `want` keys are not below it
-    int above = 0;       // keys not below value + 2^(shift + 2)
-    for (int shift = 30, round = 0; shift >= 0; shift -= 2, round ^= 1) {
-        int n[3] = {0, 0, 0};
+    V incl = v;
 #pragma unroll
-        for (int x = 0; x < kSelPer; ++x) {
-            if (x % 8 == 0 && x * kSelThreads >= cand) break;
-#pragma unroll
-            for (int d = 0; d < 3; ++d) n[d] += key[x] >= value + ((uint32_t)(d + 1) << shift);
-        }
-#pragma unroll
-        for (int d = 0; d < 3; ++d) {
-            n[d] = __reduce_add_sync(kFull, n[d]);
-            if (lane == 0) s_count[round][d][warp] = n[d];
-        }
-        __syncthreads();
-        int digit = 0;
-#pragma unroll
-        for (int d = 0; d < 3; ++d) {
-            n[d] = __reduce_add_sync(kFull, lane < kSelWarps ? s_count[round][d][lane] : 0);
-            if (n[d] >= want) digit = d + 1;
-        }
-        if (digit < 3) above = n[digit];
-        value += (uint32_t)digit << shift;
+    for (int o = 1; o < 32; o <<= 1) {
+        const V x = __shfl_up_sync(kFull, incl, o);
+        if (lane >= o) incl += x;
     }
-    equal = want - above;
-    return value;
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    V w = s_warp[lane];
+    static_assert(kSelWarps == 32, "a lane per warp");
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const V x = __shfl_up_sync(kFull, w, o);
+        if (lane >= o) w += x;
+    }
+    total = __shfl_sync(kFull, w, 31);
+    const V before = __shfl_sync(kFull, w, warp ? warp - 1 : 0);
+    __syncthreads();
+    return (warp ? before : V(0)) + incl - v;
 }
 
-// The same by passes over the masses.
-__device__ __forceinline__ uint32_t select_read(const KvView &kv, int b, int h, int cand, int want, int &equal) {
-    __shared__ int hist[256], s_left;
+// A key into its bin; by whole warps.  Lanes of one bin (equal masses) add once.
+__device__ __forceinline__ void count_key(int *hist, bool in, int bin) {
+    int same;
+    __match_all_sync(kFull, in ? bin : -1, &same);
+    if (in && (!same || (threadIdx.x & 31) == 0)) atomicAdd(&hist[bin], same ? 32 : 1);
+}
+
+// The largest value of which at least `want` of the keys are not below, and how many
+// of those equal to it are among them: those that `each` shows, want at least one.
+template <typename Each>
+__device__ __forceinline__ uint32_t select(Each each, int want, int &equal) {
+    __shared__ int hist[kBins];
     __shared__ uint32_t s_value;
+    __shared__ int s_left;
     const int tid = threadIdx.x;
     uint32_t value = 0, mask = 0;
     int left = want;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
         __syncthreads();
-        for (int i = tid; i < cand; i += kSelThreads) {
-            const uint32_t k = key_at(kv, b, h, i);
-            if ((k & mask) == value) atomicAdd(&hist[(k >> shift) & 255u], 1);
-        }
+        const uint32_t bits = pass == 2 ? 0x3ffu : kBins - 1u;
+        each([&](bool in, uint32_t key) { count_key(hist, in && (key & mask) == value, (int)((key >> shift) & bits)); });
         __syncthreads();
-        if (tid == 0) {
-            int d = 255, above = 0;
-            while (d > 0 && above + hist[d] < left) above += hist[d--];
-            s_value = value | (uint32_t)d << shift;
-            s_left = left - above;
+        // bins from the top
+        const int b0 = kBins - 1 - 2 * tid;
+        const int c0 = hist[b0], c1 = hist[b0 - 1];
+        int total;
+        const int above = scan_before(c0 + c1, total);
+        if (above < left && left <= above + c0 + c1) {
+            const bool second = left > above + c0;
+            s_value = value | (uint32_t)(second ? b0 - 1 : b0) << shift;
+            s_left = left - above - (second ? c0 : 0);
         }
         __syncthreads();
         value = s_value;
         left = s_left;
-        mask |= 255u << shift;
+        mask |= bits << shift;
     }
     equal = left;
     return value;
@@ -125,61 +133,54 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
     for (int i = tid; i < fixed; i += kSelThreads) list[want + i] = cand + i;
     if (want == 0) return;
     // kept: the keys above value, and the first `equal` equal to it
-    __shared__ uint32_t s_warp[kSelPer * kSelWarps];  // of each warp's turn: above, equal << 16
-    __shared__ uint2 s_total[kSelWarps];
     if (cand <= kSelPer * kSelThreads) {
+        __shared__ uint32_t s_turn[kSelPer * kSelWarps];  // of a warp's turn: above, equal << 16; then their places
+        __shared__ int2 s_place[kSelPer * kSelWarps];
         uint32_t key[kSelPer];
+        const int turns = (cand + kSelThreads - 1) / kSelThreads;
 #pragma unroll
-        for (int x = 0; x < kSelPer; ++x) {
-            if (x % 8 == 0 && x * kSelThreads >= cand) break;
-            const int i = tid + x * kSelThreads;
-            key[x] = i < cand ? key_at(kv, b, h, i) : 0u;
+        for (int x = 0; x < kSelPer; x += 4) {
+            if (x >= turns) break;
+            int page[4], slot[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {  // (one past the end looks where the last one does)
+                const int i = min(tid + (x + y) * kSelThreads, cand - 1);
+                if (!kv.place(b, i, page[y], slot[y])) page[y] = -1;
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float v = *kv.mass_at(max(page[y], 0), slot[y], h);
+                key[x + y] = page[y] >= 0 ? mass_key(v) : 0u;
+            }
         }
         int equal;
-        const uint32_t value = select_held(key, cand, want, equal);
+        const uint32_t value = select(
+            [&](auto count) {
+#pragma unroll
+                for (int x = 0; x < kSelPer; ++x) {
+                    if (x >= turns) break;
+                    count(tid + x * kSelThreads < cand, key[x]);
+                }
+            },
+            want, equal);
 #pragma unroll
         for (int x = 0; x < kSelPer; ++x) {
-            if (x % 8 == 0 && x * kSelThreads >= cand) break;
+            if (x >= turns) break;
             const bool in = tid + x * kSelThreads < cand;
             const uint32_t gt = __popc(__ballot_sync(kFull, in && key[x] > value));
             const uint32_t eq = __popc(__ballot_sync(kFull, in && key[x] == value));
-            if (lane == 0) s_warp[x * kSelWarps + warp] = gt | eq << 16;
+            if (lane == 0) s_turn[x * kSelWarps + warp] = gt | eq << 16;
         }
         __syncthreads();
-        // exclusive scan of all the turns' counts, two a thread
-        const int turns = (cand + 8 * kSelThreads - 1) / (8 * kSelThreads) * 8 * kSelWarps;
-        uint2 v[2], sum = make_uint2(0u, 0u);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t c = 2 * tid + e < turns ? s_warp[2 * tid + e] : 0u;
-            v[e] = make_uint2(c & 0xffffu, c >> 16);
-            sum.x += v[e].x;
-            sum.y += v[e].y;
-        }
-        uint2 incl = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(kFull, incl.x, o), y = __shfl_up_sync(kFull, incl.y, o);
-            if (lane >= o) incl.x += x, incl.y += y;
-        }
-        if (lane == 31) s_total[warp] = incl;
-        __syncthreads();
-        uint2 pre = make_uint2(incl.x - sum.x, incl.y - sum.y);
-        for (int w = 0; w < warp; ++w) pre.x += s_total[w].x, pre.y += s_total[w].y;
-        // place of a turn's first key that stays: those above before it, and the equal ones up to their number;
-        // and how many of its equal ones stay
-        __syncthreads();
-        __shared__ int2 s_place[kSelPer * kSelWarps];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            s_place[2 * tid + e] = make_int2((int)pre.x, (int)pre.y);
-            pre.x += v[e].x;
-            pre.y += v[e].y;
-        }
+        const uint32_t c = tid < turns * kSelWarps ? s_turn[tid] : 0u;
+        unsigned long long total;
+        const unsigned long long pre =
+            scan_before((unsigned long long)(c & 0xffffu) | (unsigned long long)(c >> 16) << 32, total);
+        s_place[tid] = make_int2((int)(uint32_t)pre, (int)(pre >> 32));
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < kSelPer; ++x) {
-            if (x % 8 == 0 && x * kSelThreads >= cand) break;
+            if (x >= turns) break;
             const int i = tid + x * kSelThreads;
             const bool in = i < cand, above = in && key[x] > value, same = in && key[x] == value;
             const unsigned gt = __ballot_sync(kFull, above), eq = __ballot_sync(kFull, same);
@@ -190,69 +191,69 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
         return;
     }
     int equal;
-    const uint32_t value = select_read(kv, b, h, cand, want, equal);
+    const uint32_t value = select(
+        [&](auto count) {
+            for (int i0 = 0; i0 < cand; i0 += kSelThreads) count(i0 + tid < cand, i0 + tid < cand ? key_at(kv, b, h, i0 + tid) : 0u);
+        },
+        want, equal);
     int gt0 = 0, eq0 = 0;
     for (int i0 = 0; i0 < cand; i0 += kSelThreads) {
         const int i = i0 + tid;
         const uint32_t k = i < cand ? key_at(kv, b, h, i) : 0u;
-        const unsigned gt = __ballot_sync(kFull, i < cand && k > value), eq = __ballot_sync(kFull, i < cand && k == value);
-        if (lane == 0) s_warp[warp] = __popc(gt) | __popc(eq) << 16;
-        __syncthreads();
-        int g = gt0 + __popc(gt & lanemask_lt()), e = eq0 + __popc(eq & lanemask_lt());
-        for (int w = 0; w < kSelWarps; ++w) {
-            if (w < warp) g += s_warp[w] & 0xffffu, e += s_warp[w] >> 16;
-            gt0 += s_warp[w] & 0xffffu, eq0 += s_warp[w] >> 16;
-        }
-        if (i < cand && (k > value || (k == value && e < equal))) list[g + min(e, equal)] = i;
-        __syncthreads();
+        const bool above = i < cand && k > value, same = i < cand && k == value;
+        unsigned long long total;
+        const unsigned long long pre =
+            scan_before((unsigned long long)above | (unsigned long long)same << 32, total);
+        const int g = gt0 + (int)(uint32_t)pre, e = eq0 + (int)(pre >> 32);
+        if (above || (same && e < equal)) list[g + min(e, equal)] = i;
+        gt0 += (int)(uint32_t)total;
+        eq0 += (int)(total >> 32);
     }
 }
 
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_constant__ EvictArgs a) {
     const KvView &kv = a.kv;
     const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int n = a.kept[b], per_part = kv.dim / 8, per = 2 * per_part;
-    if (chunk == 0 && h == 0 && tid == 0) a.j.new_lens[b] = n;
-    const int r0 = chunk * a.rows, m = min(a.rows, n - r0);
-    if (m <= 0) return;
+    extern __shared__ __align__(16) uint8_t smem[];
+    // where each row is and goes
+    __shared__ int64_t s_from[2][kMoveThreads], s_to[2][kMoveThreads];
+    const int r0 = chunk * a.rows, per_part = kv.dim / 8, per = 2 * per_part;
     const int64_t at = (int64_t)b * kv.heads + h;
-    const int32_t *list = a.list + at * a.j.budget + r0;
-    uint4 x[kMoveChunks];
-    char *to[kMoveChunks];
-    // of a row, chunks of its key, then of its value
-#pragma unroll
-    for (int c = 0; c < kMoveChunks; ++c) {
-        const int id = tid + c * kMoveThreads, r = id / per, part = id % per;
-        to[c] = nullptr;
-        if (r >= m) continue;
-        const bool v = part >= per_part;
-        const int64_t off = (int64_t)(v ? part - per_part : part) * 16;
-        const int from = list[r];
-        int sp, ss, dp;
-        uint32_t q, ds;
-        if (!kv.place(b, from, sp, ss)) continue;
-        kv.ps.divmod((uint32_t)(r0 + r), q, ds);
-        dp = a.j.new_table[b * a.j.new_stride + q];
-        if (dp < 0 || dp >= kv.pages) continue;
-        if (dp == sp && (int)ds == ss) continue;  // where it is already
-        to[c] = (v ? kv.V + dp * kv.v_page + ds * kv.v_slot + h * kv.v_head
-                   : kv.K + dp * kv.k_page + ds * kv.k_slot + h * kv.k_head) + off;
-        x[c] = *reinterpret_cast<const uint4 *>((v ? kv.V + sp * kv.v_page + ss * kv.v_slot + h * kv.v_head
-                                                   : kv.K + sp * kv.k_page + ss * kv.k_slot + h * kv.k_head) + off);
-    }
+    uint32_t q, o;
+    kv.ps.divmod((uint32_t)(r0 + tid), q, o);
+    const int ds = (int)o;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n = a.kept[b];
+    const int from = tid < a.rows && r0 + tid < a.j.budget ? a.list[at * a.j.budget + r0 + tid] : 0;
+    if (chunk == 0 && h == 0 && tid == 0) a.j.new_lens[b] = n;
+    const int m = min(a.rows, n - r0);
+    if (m <= 0) return;
     float w = 0.0f, *wto = nullptr;
     if (tid < m) {
-        const int from = list[tid];
-        int sp, ss, dp;
-        uint32_t q, ds;
-        kv.ps.divmod((uint32_t)(r0 + tid), q, ds);
-        dp = a.j.new_table[b * a.j.new_stride + q];
-        if (kv.place(b, from, sp, ss) && dp >= 0 && dp < kv.pages) {
+        const int dp = a.j.new_table[b * a.j.new_stride + q];
+        int sp = 0, ss = 0;
+        const bool moves = kv.place(b, from, sp, ss) && dp >= 0 && dp < kv.pages && (dp != sp || ds != ss);
+        if (moves) {
             w = *kv.mass_at(sp, ss, h);
-            wto = kv.mass_at(dp, (int)ds, h);
+            wto = kv.mass_at(dp, ds, h);
         }
+        s_from[0][tid] = moves ? sp * kv.k_page + ss * kv.k_slot : -1;
+        s_from[1][tid] = sp * kv.v_page + ss * kv.v_slot;
+        s_to[0][tid] = dp * kv.k_page + ds * kv.k_slot;
+        s_to[1][tid] = dp * kv.v_page + ds * kv.v_slot;
     }
+    __syncthreads();
+    // of a row, chunks of its key, then of its value
+    const int chunks = m * per;
+    for (int id = tid; id < chunks; id += kMoveThreads) {
+        const int r = id / per, part = id - r * per;
+        const bool v = part >= per_part;
+        if (s_from[0][r] == -1) continue;
+        const int64_t off = (int64_t)(v ? part - per_part : part) * 16 + h * (v ? kv.v_head : kv.k_head);
+        copy16(smem_addr(smem) + 16 * id, (v ? kv.V : kv.K) + s_from[v][r] + off, true);
+    }
+    copy_commit();
+    copy_wait<0>();
     uint32_t *loaded = a.loaded + at * a.chunks;
     __threadfence();  // the rows are read before the report
     __syncthreads();
@@ -266,9 +267,13 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
         if (tid == 0) record_error(a.err, kErrScanTimeout);
         return;
     }
-#pragma unroll
-    for (int c = 0; c < kMoveChunks; ++c)
-        if (to[c]) *reinterpret_cast<uint4 *>(to[c]) = x[c];
+    for (int id = tid; id < chunks; id += kMoveThreads) {
+        const int r = id / per, part = id - r * per;
+        const bool v = part >= per_part;
+        if (s_from[0][r] == -1) continue;
+        const int64_t off = (int64_t)(v ? part - per_part : part) * 16 + h * (v ? kv.v_head : kv.k_head);
+        *reinterpret_cast<uint4 *>((v ? kv.V : kv.K) + s_to[v][r] + off) = *reinterpret_cast<const uint4 *>(smem + 16 * id);
+    }
     if (wto) *wto = w;
 }
 
@@ -283,8 +288,7 @@ cudaError_t launch_evict(const EvictJob &j, const KvView &kv, cudaStream_t s) {
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
     if (a.j.budget > room) a.j.budget = (int)room;  // no sequence is longer
     // rows of a CTA: whole ones, no more than it has threads for their masses
-    a.rows = kMoveThreads * kMoveChunks / (kv.dim / 4);
-    if (a.rows > kMoveThreads) a.rows = kMoveThreads;
+    a.rows = std::min(kMoveBytes / (4 * kv.dim), kMoveThreads);
     a.chunks = (a.j.budget + a.rows - 1) / a.rows;
     void *p = nullptr;
     const size_t lists = (size_t)kv.B * kv.heads * a.j.budget;
@@ -297,7 +301,8 @@ cudaError_t launch_evict(const EvictJob &j, const KvView &kv, cudaStream_t s) {
     k_evict_select<<<dim3((unsigned)kv.heads, (unsigned)kv.B), kSelThreads, 0, s>>>(a);
     const cudaError_t e1 = counted_launch(cudaGetLastError());
     if (e1 != cudaSuccess) return e1;
-    return launch_dependent(k_evict_move, dim3((unsigned)a.chunks, (unsigned)kv.heads, (unsigned)kv.B), kMoveThreads, a, s);
+    return launch_dependent(k_evict_move, dim3((unsigned)a.chunks, (unsigned)kv.heads, (unsigned)kv.B), kMoveThreads, a, s,
+                            kMoveBytes);
 }
 
 }  // namespace pv
