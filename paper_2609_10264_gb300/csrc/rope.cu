@@ -31,11 +31,11 @@ __device__ __forceinline__ void sincos_at(const RopeJob &j, int pair, int pos, f
     s *= j.magnitude;
 }
 
-// Source and destination of head h (of all three parts) of token t; null where
-// there is nothing to write.
+// Source and destination of head h (of all three parts) of token t, which goes to
+// the slot of the page; null where there is nothing to write (page < 0).
 template <typename In, typename Out>
-__device__ __forceinline__ void head_rows(const RopeArgs &a, int t, int h, int b, int page, int slot, bool placed,
-                                          const In *&src, Out *&dst, bool &rotate) {
+__device__ __forceinline__ void head_rows(const RopeArgs &a, int t, int h, int page, int slot, const In *&src, Out *&dst,
+                                          bool &rotate) {
     const RopeJob &j = a.j;
     if (h < j.part[0].heads) {
         src = static_cast<const In *>(j.part[0].src) + t * j.part[0].src_token + h * j.part[0].src_head;
@@ -50,7 +50,7 @@ __device__ __forceinline__ void head_rows(const RopeArgs &a, int t, int h, int b
     src = static_cast<const In *>(p.src) + t * p.src_token + h * p.src_head;
     rotate = !v && j.rot > 0;
     dst = nullptr;
-    if (placed)
+    if (page >= 0)
         dst = reinterpret_cast<Out *>(v ? a.kv.V + page * a.kv.v_page + slot * a.kv.v_slot + h * a.kv.v_head
                                         : a.kv.K + page * a.kv.k_page + slot * a.kv.k_slot + h * a.kv.k_head);
 }
@@ -66,18 +66,17 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope_any(const __grid_constant
     const int h = (int)(th % a.heads);
     if (th / a.heads >= j.T) return;
     const int t = (int)(th / a.heads);
-    int b = 0, page = 0, slot = 0, idx = 0;
-    bool placed = false;
+    int b = 0, page = -1, slot = 0, idx = 0;
     if (j.cached) {
         b = a.kv.seq(t);
         idx = a.kv.len(b) - a.kv.news(b) + t - a.kv.first(b);
-        placed = idx >= 0 && a.kv.place(b, idx, page, slot);
+        if (idx < 0 || !a.kv.place(b, idx, page, slot)) page = -1;
     }
     const In *src;
     Out *dst;
     bool rotate;
-    head_rows(a, t, h, b, page, slot, placed, src, dst, rotate);
-    if (j.cached && a.kv.mass && placed && u == 0 && h >= j.part[0].heads && h < j.part[0].heads + j.part[1].heads)
+    head_rows(a, t, h, page, slot, src, dst, rotate);
+    if (j.cached && a.kv.mass && page >= 0 && u == 0 && h >= j.part[0].heads && h < j.part[0].heads + j.part[1].heads)
         *a.kv.mass_at(page, slot, h - j.part[0].heads) = 0.0f;
     if (!dst) return;
     if (u >= half) {
@@ -106,18 +105,15 @@ struct __align__(sizeof(T) * N) Vec {
 constexpr int kGroup = 8;  // values that a thread takes at a time
 
 template <typename T>
-struct Raw {
-    static constexpr int kN = 16 / sizeof(T);
-    Vec<T, kN> u[kGroup / kN];
-    __device__ __forceinline__ void load(const T *p) {
+__device__ __forceinline__ void load8(const T *p, float scale, float (&x)[kGroup]) {
+    constexpr int kN = 16 / sizeof(T);
 #pragma unroll
-        for (int i = 0; i < kGroup / kN; ++i) u[i] = *reinterpret_cast<const Vec<T, kN> *>(p + i * kN);
-    }
-    __device__ __forceinline__ void get(float scale, float (&x)[kGroup]) const {
+    for (int i = 0; i < kGroup; i += kN) {
+        const Vec<T, kN> u = *reinterpret_cast<const Vec<T, kN> *>(p + i);
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) x[i] = to_f32(u[i / kN].v[i % kN]) * scale;
+        for (int e = 0; e < kN; ++e) x[i + e] = to_f32(u.v[e]) * scale;
     }
-};
+}
 template <typename T>
 __device__ __forceinline__ void store8(T *p, const float (&x)[kGroup]) {
     constexpr int kN = 16 / sizeof(T);
@@ -130,81 +126,81 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[kGroup]) {
     }
 }
 
-// 16 bytes at a time, for rows on 16-byte boundaries.  A thread owns 8 values of a
-// token, or the two groups of 8 that make pairs, and takes them through several
-// heads, so that it forms their angles once: without that the sines bound it (a chunk
-// of 6001 tokens, 80 heads of 128, took 283 us with them formed for every head).
+// 16 bytes at a time, for rows on 16-byte boundaries.  A CTA takes some tokens
+// through some heads: it forms the tokens' sines and places once, in shared memory,
+// and then every thread 8 values of a head, or the two groups of 8 that make pairs
+// (more of them at a time cost registers, and with them warps in flight).  Bound by
+// the copy: 6001 tokens of 80 heads of 128 took 283 us with sines formed for every
+// head, 95 with a token's formed by each thread.
 // kHalves: pairs are half a rotation apart, not side by side.
+constexpr int kRowThreads = 256;
+constexpr int kMostTokens = 8;
+constexpr int kMostSines = 1024;  // tokens x pairs of a CTA
+struct RowPlan {
+    int tokens, heads;  // of a CTA
+    FastDiv units, per; // threads per head; heads
+};
 template <typename In, typename Out, bool kHalves>
-__global__ void __launch_bounds__(kRopeThreads) k_rope_rows(const __grid_constant__ RopeArgs a, int units, int split,
-                                                           int per) {
+__global__ void __launch_bounds__(kRowThreads, 8) k_rope_rows(const __grid_constant__ RopeArgs a,
+                                                          const __grid_constant__ RowPlan plan) {
     const RopeJob &j = a.j;
-    const int64_t id = (int64_t)blockIdx.x * kRopeThreads + threadIdx.x;
-    const int u = (int)(id % units);
-    const int64_t ts = id / units;
-    const int t = (int)(ts / split), h0 = (int)(ts % split) * per, h1 = min(a.heads, h0 + per);
-    if (ts / split >= j.T) return;
-    int b = 0, page = 0, slot = 0, idx = 0;
-    bool placed = false;
-    if (j.cached) {
+    __shared__ __align__(16) float s_cos[kMostSines], s_sin[kMostSines];
+    __shared__ int s_page[kMostTokens], s_slot[kMostTokens];  // page -1: nowhere
+    const int tid = threadIdx.x, half = j.rot / 2;
+    const int t0 = blockIdx.x * plan.tokens, nt = min(plan.tokens, j.T - t0);
+    const int h0 = blockIdx.y * plan.heads, nh = min(plan.heads, a.heads - h0);
+    const int turned = j.part[0].heads + j.part[1].heads;  // heads that are rotated
+    auto index_of = [&](int t, int &b) {  // the token's cache index
         b = a.kv.seq(t);
-        idx = a.kv.len(b) - a.kv.news(b) + t - a.kv.first(b);
-        placed = idx >= 0 && a.kv.place(b, idx, page, slot);
+        return a.kv.len(b) - a.kv.news(b) + t - a.kv.first(b);
+    };
+    if (j.cached && tid < nt) {
+        int b, page, slot;
+        const int idx = index_of(t0 + tid, b);
+        const bool placed = idx >= 0 && a.kv.place(b, idx, page, slot);
+        s_page[tid] = placed ? page : -1;
+        s_slot[tid] = placed ? slot : 0;
     }
-    const int turning = kHalves ? j.rot / (2 * kGroup) : j.rot / kGroup;  // units that are rotated
-    const bool mine = u < turning;
-    const int d0 = mine || !kHalves ? u * kGroup : j.rot + (u - turning) * kGroup, d1 = d0 + j.rot / 2;
-    float c[kGroup], s[kGroup];
-    if (mine && h0 < j.part[0].heads + j.part[1].heads) {
-        const int pos = j.pos ? j.pos[t] : idx;
-#pragma unroll
-        for (int e = 0; e < (kHalves ? kGroup : kGroup / 2); ++e) sincos_at(j, kHalves ? d0 + e : d0 / 2 + e, pos, c[e], s[e]);
-    }
-    // some heads' loads in flight before the first is stored (out may be x itself)
-    constexpr int kAhead = sizeof(In) == 2 ? 4 : 2;
-    for (int hb = h0; hb < h1; hb += kAhead) {
-        Raw<In> raw0[kAhead], raw1[kAhead];
-        Out *to[kAhead];
-        bool turn[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int h = hb + i;
-            const In *src;
-            to[i] = nullptr;
-            if (h >= h1) continue;
-            head_rows(a, t, h, b, page, slot, placed, src, to[i], turn[i]);
-            if (j.cached && a.kv.mass && placed && u == 0 && h >= j.part[0].heads &&
-                h < j.part[0].heads + j.part[1].heads)
-                *a.kv.mass_at(page, slot, h - j.part[0].heads) = 0.0f;
-            if (!to[i]) continue;
-            raw0[i].load(src + d0);
-            if (kHalves && mine) raw1[i].load(src + d1);
+    if (h0 < turned)
+        for (int i = tid; i < nt * half; i += kRowThreads) {
+            const int t = i / half, e = i - t * half;
+            int b;
+            const int pos = j.pos ? j.pos[t0 + t] : index_of(t0 + t, b);
+            sincos_at(j, e, pos, s_cos[i], s_sin[i]);
         }
+    __syncthreads();
+    const int turning = kHalves ? half / kGroup : j.rot / kGroup;  // units that are rotated
+    const int units = (int)plan.units.d, all = nt * nh * units;
+    for (int i = tid; i < all; i += kRowThreads) {
+        uint32_t row, u, t, h;
+        plan.units.divmod((uint32_t)i, row, u);
+        plan.per.divmod(row, t, h);
+        h += h0;
+        const int page = j.cached ? s_page[t] : -1, slot = j.cached ? s_slot[t] : 0;
+        const In *src;
+        Out *dst;
+        bool rotate;
+        head_rows(a, t0 + (int)t, (int)h, page, slot, src, dst, rotate);
+        if (j.cached && a.kv.mass && page >= 0 && u == 0 && (int)h >= j.part[0].heads && (int)h < turned)
+            *a.kv.mass_at(page, slot, (int)h - j.part[0].heads) = 0.0f;
+        if (!dst) continue;
+        const bool mine = (int)u < turning;
+        const int d0 = mine || !kHalves ? (int)u * kGroup : j.rot + ((int)u - turning) * kGroup;
+        float x[kGroup], y[kGroup];
+        load8(src + d0, j.scale, x);
+        if (kHalves && mine) load8(src + d0 + half, j.scale, y);
+        if (mine && rotate) {
+            const int at = (int)t * half + (kHalves ? d0 : d0 / 2);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (!to[i]) continue;
-            float x[kGroup], y[kGroup];
-            raw0[i].get(j.scale, x);
-            if (kHalves && mine) {
-                raw1[i].get(j.scale, y);
-                if (turn[i])
-#pragma unroll
-                    for (int e = 0; e < kGroup; ++e) {
-                        const float p = x[e], q = y[e];
-                        x[e] = p * c[e] - q * s[e];
-                        y[e] = p * s[e] + q * c[e];
-                    }
-                store8(to[i] + d1, y);
-            } else if (!kHalves && mine && turn[i]) {
-#pragma unroll
-                for (int e = 0; e < kGroup / 2; ++e) {
-                    const float p = x[2 * e], q = x[2 * e + 1];
-                    x[2 * e] = p * c[e] - q * s[e];
-                    x[2 * e + 1] = p * s[e] + q * c[e];
-                }
+            for (int e = 0; e < (kHalves ? kGroup : kGroup / 2); ++e) {
+                float &p = kHalves ? x[e] : x[2 * e], &q = kHalves ? y[e] : x[2 * e + 1];
+                const float c = s_cos[at + e], s = s_sin[at + e], px = p, qx = q;
+                p = px * c - qx * s;
+                q = px * s + qx * c;
             }
-            store8(to[i] + d0, x);
         }
+        if (kHalves && mine) store8(dst + d0 + half, y);
+        store8(dst + d0, x);
     }
 }
 
@@ -212,7 +208,7 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope_rows(const __grid_constan
 template <typename In, typename Out>
 bool rows_ok(const RopeArgs &a) {
     const RopeJob &j = a.j;
-    if (j.dim % kGroup || j.rot % (j.interleaved ? kGroup : 2 * kGroup)) return false;
+    if (j.dim % kGroup || j.rot % (j.interleaved ? kGroup : 2 * kGroup) || j.rot / 2 > kMostSines) return false;
     for (const RopePart &p : j.part) {
         if (!p.heads) continue;
         if (reinterpret_cast<uintptr_t>(p.src) % 16 || p.src_token * sizeof(In) % 16 || p.src_head * sizeof(In) % 16)
@@ -229,15 +225,21 @@ cudaError_t rope_launch(const RopeArgs &a, cudaStream_t s) {
     const RopeJob &j = a.j;
     if (rows_ok<In, Out>(a)) {
         const int units = j.interleaved ? j.dim / kGroup : j.rot / (2 * kGroup) + (j.dim - j.rot) / kGroup;
-        // heads a thread: few while that leaves SMs without threads, at most 16
-        const int64_t threads = (int64_t)j.T * units * a.heads;
-        const int per = (int)std::max<int64_t>(1, std::min<int64_t>(16, threads / (152 * 1024)));
-        const int split = (a.heads + per - 1) / per;
-        const unsigned grid = (unsigned)(((int64_t)j.T * units * split + kRopeThreads - 1) / kRopeThreads);
+        // Heads a CTA: all, or as many as four turns of its threads take where the
+        // tokens alone would leave SMs without one.  Tokens a CTA: up to eight turns.
+        const int turn = std::max(1, kRowThreads / units), sms = 152;
+        RowPlan plan;
+        plan.heads = j.T >= 4 * sms ? a.heads : std::min(a.heads, j.T >= sms ? 4 * turn : turn);
+        plan.tokens = std::max(1, std::min({kMostTokens, kMostSines / std::max(1, j.rot / 2), 8 * turn / plan.heads,
+                                            j.T / (4 * sms)}));
+        plan.units = FastDiv((uint32_t)units);
+        plan.per = FastDiv((uint32_t)plan.heads);
+        const dim3 grid((unsigned)((j.T + plan.tokens - 1) / plan.tokens),
+                        (unsigned)((a.heads + plan.heads - 1) / plan.heads));
         if (j.interleaved)
-            k_rope_rows<In, Out, false><<<grid, kRopeThreads, 0, s>>>(a, units, split, per);
+            k_rope_rows<In, Out, false><<<grid, kRowThreads, 0, s>>>(a, plan);
         else
-            k_rope_rows<In, Out, true><<<grid, kRopeThreads, 0, s>>>(a, units, split, per);
+            k_rope_rows<In, Out, true><<<grid, kRowThreads, 0, s>>>(a, plan);
         return counted_launch(cudaGetLastError());
     }
     const int64_t n = (int64_t)j.T * a.heads * (j.rot / 2 + j.dim - j.rot);
