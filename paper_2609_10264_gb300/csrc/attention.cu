@@ -12,9 +12,10 @@ namespace pv {
 cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_t s) {
     AttendJob j = job;
     const int G = j.Hq / kv.heads;
-    if (G <= kFewRows) {
+    const bool one = kv.B == 1;  // which has all the new tokens
+    if (G <= kFewRows && !(one && (int64_t)kv.T * G > kFewRows)) {
         const cudaError_t e = launch_attention_few(j, kv, s);
-        if (e != cudaSuccess || j.max_new <= kFewRows / G) return e;
+        if (e != cudaSuccess || one || j.max_new <= kFewRows / G) return e;
     }
     if (j.accumulate) {
         void *p = nullptr;

@@ -138,14 +138,15 @@ struct TileCopy {
     bool real;  // this lane's chunk is one of the row's
     __device__ __forceinline__ TileCopy(int lane_, int dim)
         : lane(lane_), ch(lane_ % kPerRow), sub(lane_ / kPerRow), real(lane_ % kPerRow * 8 < dim) {}
-    // row(rr, off): whether row rr is there, and its place from src on; else zeros
-    template <typename Row>
-    __device__ __forceinline__ void copy(uint32_t dst, const char *src, Row row) const {
-        int64_t off[kCM / 32];
-        unsigned there[kCM / 32];
+    // Rows first .. first + 32 kBlocks - 1.  row(rr, off): whether row rr is there, and
+    // its place from src on; else zeros.
+    template <int kBlocks = kCM / 32, typename Row>
+    __device__ __forceinline__ void copy(uint32_t dst, const char *src, Row row, int first = 0) const {
+        int64_t off[kBlocks];
+        unsigned there[kBlocks];
 #pragma unroll
-        for (int x = 0; x < kCM / 32; ++x) {
-            const bool is = row(32 * x + lane, off[x]);
+        for (int x = 0; x < kBlocks; ++x) {
+            const bool is = row(first + 32 * x + lane, off[x]);
             if (!is) off[x] = 0;
             there[x] = __ballot_sync(kFull, is);
         }
@@ -154,17 +155,17 @@ struct TileCopy {
         // some places at a time, then their copies, which the compiler keeps in order
         constexpr int kBatch = 4;
 #pragma unroll
-        for (int u0 = 0; u0 < kCM / kRowsAt; u0 += kBatch) {
+        for (int u0 = 0; u0 < 32 * kBlocks / kRowsAt; u0 += kBatch) {
             int64_t o[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                const int first = (u0 + u) * kRowsAt;
-                o[u] = __shfl_sync(kFull, off[first / 32], (first + sub) & 31);
+                const int rr = (u0 + u) * kRowsAt;
+                o[u] = __shfl_sync(kFull, off[rr / 32], (rr + sub) & 31);
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                const int first = (u0 + u) * kRowsAt;
-                copy16(dst + sw128_off(first + sub, ch & 7), src + o[u], real && (there[first / 32] >> ((first + sub) & 31) & 1));
+                const int rr = (u0 + u) * kRowsAt;
+                copy16(dst + sw128_off(first + rr + sub, ch & 7), src + o[u], real && (there[rr / 32] >> ((rr + sub) & 31) & 1));
             }
         }
         copy_commit();
@@ -237,6 +238,16 @@ inline cudaError_t page_map(CUtensorMap *map, const KvView &kv, bool values, int
                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// Cache index i of sequence b, of length len: whether it is there, and its place in
+// K or V (strides in bytes).  No branch, so that several look-ups run at a time.
+__device__ __forceinline__ bool key_place(const KvView &kv, int b, int len, int i, int64_t page_stride,
+                                          int64_t slot_stride, int64_t &off) {
+    int page, slot;
+    const bool is = kv.place(b, max(min(i, len - 1), 0), page, slot) && i < len;
+    off = page * page_stride + slot * slot_stride;
+    return is;
 }
 
 // New rows of sequence b per key head, where they are too many for the kernel of few.

@@ -108,7 +108,7 @@ __device__ __forceinline__ int chunk_tiles(const ChunkArgs &a, int b) {
 // keys, come first) and its share of the keys.
 struct ChunkItem {
     int b, hk, row0, rows;       // rows of the sequence and key head, of this item
-    int len, n;                  // cached and new tokens
+    int len, n, t0;              // cached and new tokens, the first of these
     int kt0, kt1;                // key tiles of the item
     int per, parts;              // key tiles of a split, splits that have any
     int64_t slot;                // of the item, for partial results
@@ -124,6 +124,7 @@ __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int idx, ChunkIte
     it.hk = hk;
     it.len = kv.len(f.b);
     it.n = kv.news(f.b);
+    it.t0 = kv.first(f.b);
     it.row0 = (int)(f.total - 1 - rank - f.before) * kCRows;
     it.rows = min(kCRows, it.n * a.G - it.row0);
     const int at0 = it.len - it.n + it.row0 / a.G, at1 = it.len - it.n + (it.row0 + it.rows - 1) / a.G;
@@ -159,11 +160,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const int split = blockIdx.y;
     if (split >= it.parts) return;
     const int kt0 = it.kt0 + split * it.per, nk = min(it.kt1, kt0 + it.per) - kt0;
+    const int used = it.rows > kCM ? 2 : 1;  // tiles with rows
 
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t qbase = base, ring = base + 2 * C::kTileBytes;
     if (tid == 0) {
-        mbar_init(&q_full, 2);
+        mbar_init(&q_full, 8);
         mbar_init(&mma_done, 1);
         for (int s = 0; s < kSt; ++s) {
             mbar_init(&kv_full[s], 1);
@@ -199,10 +201,20 @@ __global__ void __launch_bounds__(kCThreads, 1)
         const int hi = !real ? INT_MAX : j.causal ? min(it.len, at + 1) : it.len;
         const int lo = real && j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        // the warp's rows of Q
+        {
+            const TileCopy<DP> q(lane, kv.dim);
+            q.template copy<1>(qbase + tile * C::kTileBytes, static_cast<const char *>(j.q), [&](int, int64_t &off) {
+                off = (int64_t)(it.t0 + (it.row0 + r) / a.G) * j.q_token +
+                      (int64_t)(it.hk * a.G + (it.row0 + r) % a.G) * j.q_head;
+                return real;
+            }, (warp & 3) * 32);
+            q.arrive(&q_full);
+        }
         const uint32_t ts = tmem + lanes + (uint32_t)(tile * kCN), to = tmem + lanes + (uint32_t)(C::kO + tile * DP);
         float m = -INFINITY, l = 0.0f;
         bool ok = true;
-        for (int i = 0; i < nk; ++i) {
+        for (int i = 0; i < nk && tile < used; ++i) {
             if (!mbar_wait_warp(&s_full[tile], i & 1, err, kWaitNs)) {
                 ok = false;
                 break;
@@ -282,9 +294,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
             l += x + y;
         }
         // ------------------------------------------------ output
-        if (ok && mbar_wait_warp(&o_done[tile], (nk - 1) & 1, err, kWaitNs)) {
+        if (ok && tile < used && mbar_wait_warp(&o_done[tile], (nk - 1) & 1, err, kWaitNs)) {
             tc_fence_after();
-            const int t = kv.first(it.b) + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
+            const int t = it.t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
             const float inv = inverse(m, l), lse2 = m == -INFINITY ? (l != l ? l : m) : m * a.scale2 + log2f(l);
             const int64_t prow = (it.slot + split) * kCRows + r;
             char *orow = static_cast<char *>(j.out) + t * j.o_token + h * j.o_head;
@@ -355,13 +367,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
             bool ok = mbar_wait_warp(&q_full, 0, err, kWaitNs) && full(0);
             if (ok) {
                 tc_fence_after();
-                scores(0, 0);
-                scores(1, 0);
+                for (int t = 0; t < used; ++t) scores(t, 0);
                 release(0);
             }
             for (int i = 0; i < nk && ok; ++i) {
                 const bool more = i + 1 < nk;
-                for (int t = 0; t < 2 && ok; ++t) {
+                for (int t = 0; t < used && ok; ++t) {
                     ok = t || full(place_v(i));
                     for (int half = 0; half < 2 && ok; ++half) {
                         ok = mbar_wait_warp(&p_full[t][half], i & 1, err, kWaitNs);
@@ -388,16 +399,6 @@ __global__ void __launch_bounds__(kCThreads, 1)
             // ------------------------------------------------ copies
             const int w = warp - 9;
             const TileCopy<DP> tile(lane, kv.dim);
-            // Q: token by token, a tile each by the first two
-            if (w < 2) {
-                tile.copy(qbase + w * C::kTileBytes, static_cast<const char *>(j.q), [&](int rr, int64_t &off) {
-                    const int r = w * kCM + rr;
-                    off = (int64_t)(kv.first(it.b) + (it.row0 + r) / a.G) * j.q_token +
-                          (int64_t)(it.hk * a.G + (it.row0 + r) % a.G) * j.q_head;
-                    return r < it.rows;
-                });
-                tile.arrive(&q_full);
-            }
             // tiles of K and V in turn
             int x = w;
             for (; x < places; x += kCLoaders) {
@@ -420,11 +421,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 }
                 bool gap = false;
                 tile.copy(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? kv.V : kv.K, [&](int rr, int64_t &off) {
-                    const int key = key0 + rr;
-                    int page = 0, slot = 0;
-                    const bool is = key < it.len && kv.place(it.b, key, page, slot);
-                    gap |= key < it.len && !is;
-                    off = page * ps + slot * ss + hs;
+                    const bool is = key_place(kv, it.b, it.len, key0 + rr, ps, ss, off);
+                    gap |= key0 + rr < it.len && !is;
+                    off += hs;
                     return is;
                 });
                 gap = __any_sync(kFull, gap);
@@ -454,7 +453,6 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!is || it.parts == 1) return;
     const int r0 = blockIdx.y * kJoinRows, rows = min(kJoinRows, it.rows - r0);
-    const int t0 = a.kv.first(it.b);
     for (int id = threadIdx.x; id < rows * (DP / 4); id += kCThreads) {
         const int r = r0 + id / (DP / 4), d = 4 * (id % (DP / 4));
         float M = -INFINITY, L = 0.0f;
@@ -471,7 +469,7 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
             v.z += x.z * e;
             v.w += x.w * e;
         }
-        const int t = t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
+        const int t = it.t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
         const float inv = inverse(M, L);
         if (d < a.kv.dim)
             *reinterpret_cast<uint2 *>(static_cast<char *>(a.j.out) + t * a.j.o_token + h * a.j.o_head + 2 * d) =

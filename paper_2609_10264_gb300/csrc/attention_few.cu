@@ -5,7 +5,7 @@
 // of them, one after the other, are dealt out evenly to the CTAs, whatever the
 // sequences' lengths: CTA c of C takes tiles [N c / C, N (c + 1) / C).  A sequence
 // that one CTA has whole is finished there; parts go to scratch as (maximum, sum,
-// unnormalised output), and k_few_join puts them together in order.
+// unnormalised output), and k_few_finish puts them together in order.
 //
 // A warp takes 16 of a tile's 64 keys through its own ring of asynchronous copies
 // and keeps its own running maximum and sum, so that nothing but the end of a
@@ -26,6 +26,9 @@ constexpr int kFewThreads = 32 * kFewWarps;
 constexpr int kSub = 16;                  // keys per warp and step
 constexpr int kTile = kFewWarps * kSub;   // keys per tile
 constexpr int kRows = kFewRows;           // rows per item, of one MMA
+// Where no sequence has more keys than this, each goes to one CTA, which needs no
+// parts joined by another kernel.
+constexpr int kWholeKeys = 512;
 
 struct FewArgs {
     AttendJob j;
@@ -34,9 +37,10 @@ struct FewArgs {
     float2 *stat;    // [2 C][kRows] their maximum and sum
     float2 *norm;    // [T][Hq] maximum and 1 / sum, where mass is accumulated
     float *scores;   // [B][heads][max tiles x 64][rows] where mass is accumulated
-    int score_rows, max_tiles;
+    int score_rows, max_tiles;  // (rows a multiple of 4)
     float scale2;    // scale x log2(e)
     int G, C;
+    bool whole;      // a CTA takes all keys of a (sequence, key head)
 };
 
 template <int DP>
@@ -83,21 +87,23 @@ __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &
     lo = pack(x - to_f32(a), y - to_f32(b), T{});
 }
 // ---------------------------------------------------------------- work
-// One sequence's share: `items` key heads of `tiles` tiles from key `first` on.
+// One sequence's share: of each key head `tiles` tiles from key `first` on, dealt out
+// in `units`.
 struct Share {
-    int rows, first, tiles;
-    int64_t work;  // tiles over all key heads
+    int rows, first, tiles, units;
+    int64_t work;  // units over all key heads
 };
 __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     Share s;
     const int n = a.kv.news(b), len = a.kv.len(b);
     s.rows = n * a.G;
-    s.first = s.tiles = 0;
+    s.first = s.tiles = s.units = 0;
     s.work = 0;
     if (s.rows <= 0 || s.rows > kRows) return s;
     if (a.j.window > 0) s.first = max(0, len - n - a.j.window + 1) / kTile * kTile;
     s.tiles = max(1, (len - s.first + kTile - 1) / kTile);
-    s.work = (int64_t)s.tiles * a.kv.heads;
+    s.units = a.whole ? 1 : s.tiles;
+    s.work = (int64_t)s.units * a.kv.heads;
     return s;
 }
 // The CTA that takes position p of N, among C <= N.
@@ -134,8 +140,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             done += sh.work;
             sh = share(a, ++b);
         }
-        const int item = (int)((p - done) / sh.tiles), t0 = (int)((p - done) % sh.tiles);
-        const int nt = (int)min((int64_t)(sh.tiles - t0), p1 - p);
+        const int item = (int)((p - done) / sh.units), t0 = (int)((p - done) % sh.units);
+        const int nt = a.whole ? sh.tiles : (int)min((int64_t)(sh.tiles - t0), p1 - p);
         const int hk = item, len = kv.len(b), n = kv.news(b), row0 = kv.first(b);
         // ---- this warp's step i: keys from key0(i) on
         auto key0 = [&](int i) { return sh.first + (t0 + i) * kTile + warp * kSub; };
@@ -356,73 +362,97 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             }
         }
         __syncthreads();
-        p += nt;
+        p += a.whole ? 1 : nt;
     }
 }
 
-// Sequences that several CTAs had: their parts, in the order of the keys.
+// What is left once every part is there.  The first CTA of a (sequence, key head) puts
+// the parts of several CTAs together, in the order of the keys; the others add to the
+// mass of kMassKeys keys each, a thread a key: sum over the rows of exp2(score -
+// maximum) / sum.
+constexpr int kFinThreads = 256, kMassKeys = 1024;
 template <typename T, int DP>
-__global__ void __launch_bounds__(kFewThreads) k_few_join(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constant__ FewArgs a) {
+    __shared__ float2 s_norm[kRows];
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
-    const int b = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x;
-    const Found f = before<kFewThreads>(kv.B, [&](int i) { return share(a, i).work; }, b);
+    const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
     const Share sh = share(a, b);
+    const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = kv.len(b);  // of the keys
+    const bool idle = !sh.work || (blockIdx.x > 0 && first >= len);
+    const Found f = idle ? Found{} : before<kFinThreads>(kv.B, [&](int i) { return share(a, i).work; }, b);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (!sh.work) return;
-    const int64_t C = min((int64_t)a.C, f.total), i0 = f.before + (int64_t)hk * sh.tiles, i1 = i0 + sh.tiles;
-    const int c0 = owner(i0, f.total, C), c1 = owner(i1 - 1, f.total, C);
-    if (c0 == c1) return;
+    if (idle) return;
+    const int64_t C = min((int64_t)a.C, f.total), i0 = f.before + (int64_t)hk * sh.units, i1 = i0 + sh.units;
+    const int c0 = owner(i0, f.total, C), c1 = owner(i1 - 1, f.total, C);  // the CTAs that had parts
     const int row0 = kv.first(b);
-    for (int id = tid; id < sh.rows * (DP / 4); id += kFewThreads) {
-        const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
-        auto stat = [&](int c) { return a.stat[(int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows + r]; };
-        float M = -INFINITY, L = 0.0f;
-        for (int c = c0; c <= c1; ++c) M = fmaxf(M, stat(c).x);
-        const float ref = M == -INFINITY ? 0.0f : M;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int c = c0; c <= c1; ++c) {
-            const float2 z = stat(c);
-            const float e = exp2_fast(z.x - ref);
-            const float4 x = *reinterpret_cast<const float4 *>(
-                a.part + ((int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows + r) * DP + d);
-            L += z.y * e;
-            v.x += x.x * e;
-            v.y += x.y * e;
-            v.z += x.z * e;
-            v.w += x.w * e;
+    auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows; };
+    if (blockIdx.x == 0) {
+        if (c0 == c1) return;
+        for (int id = tid; id < sh.rows * (DP / 4); id += kFinThreads) {
+            const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
+            float M = -INFINITY, L = 0.0f;
+            for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.stat[slot(c) + r].x);
+            const float ref = M == -INFINITY ? 0.0f : M;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int c = c0; c <= c1; ++c) {
+                const float2 z = a.stat[slot(c) + r];
+                const float e = exp2_fast(z.x - ref);
+                const float4 x = *reinterpret_cast<const float4 *>(a.part + (slot(c) + r) * DP + d);
+                L += z.y * e;
+                v.x += x.x * e;
+                v.y += x.y * e;
+                v.z += x.z * e;
+                v.w += x.w * e;
+            }
+            const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
+            const float inv = inverse(M, L);
+            if (d < kv.dim) {
+                uint2 x;
+                x.x = pack(v.x * inv, v.y * inv, T{});
+                x.y = pack(v.z * inv, v.w * inv, T{});
+                *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
+            }
+            if (d == 0 && j.lse) j.lse[(int64_t)t * j.Hq + h] = kLn2 * (M + log2f(L));
         }
-        const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
-        const float inv = inverse(M, L);
-        if (d < kv.dim) {
-            uint2 x;
-            x.x = pack(v.x * inv, v.y * inv, T{});
-            x.y = pack(v.z * inv, v.w * inv, T{});
-            *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
-        }
-        if (d == 0) {
-            if (j.lse) j.lse[(int64_t)t * j.Hq + h] = kLn2 * (M + log2f(L));
-            if (a.norm) a.norm[(int64_t)t * j.Hq + h] = make_float2(M, inv);
-        }
+        return;
     }
-}
-
-// mass += sum over the rows of exp2(score - maximum) / sum, a thread per key.
-__global__ void __launch_bounds__(256) k_few_mass(const __grid_constant__ FewArgs a) {
-    const KvView &kv = a.kv;
-    const int b = blockIdx.z, hk = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-    const Share sh = share(a, b);
-    const int key = sh.first + i;
-    int page, slot;
-    if (!sh.work || key >= kv.len(b) || !kv.place(b, key, page, slot)) return;
-    const float *sc = a.scores + (((int64_t)b * kv.heads + hk) * a.max_tiles * kTile + i) * a.score_rows;
-    const int row0 = kv.first(b);
-    float sum = 0.0f;
-    for (int r = 0; r < sh.rows; ++r) {
-        const float2 z = a.norm[(int64_t)(row0 + r / a.G) * a.j.Hq + hk * a.G + r % a.G];
-        if (z.x != -INFINITY) sum += exp2_fast(sc[r] - z.x) * z.y;
+    if (tid < kRows) {
+        float2 z = make_float2(0.0f, 0.0f);  // rows that are not there, or see nothing, add nothing
+        if (tid < sh.rows) {
+            if (c0 == c1) {
+                z = a.norm[(int64_t)(row0 + tid / a.G) * j.Hq + hk * a.G + tid % a.G];
+            } else {
+                float M = -INFINITY, L = 0.0f;
+                for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.stat[slot(c) + tid].x);
+                for (int c = c0; c <= c1; ++c) {
+                    const float2 p = a.stat[slot(c) + tid];
+                    L += p.y * exp2_fast(p.x - (M == -INFINITY ? 0.0f : M));
+                }
+                z = make_float2(M, inverse(M, L));
+            }
+            if (z.x == -INFINITY) z = make_float2(0.0f, 0.0f);
+        }
+        s_norm[tid] = z;
     }
-    *kv.mass_at(page, slot, hk) += sum;
+    __syncthreads();
+    const float *scores = a.scores + ((int64_t)b * kv.heads + hk) * a.max_tiles * kTile * a.score_rows;
+#pragma unroll
+    for (int k = 0; k < kMassKeys; k += kFinThreads) {
+        const int key = first + k + tid;
+        int page, at;
+        if (key >= len || !kv.place(b, key, page, at)) continue;
+        float sum = 0.0f;
+        for (int r = 0; r < sh.rows; r += 4) {
+            const float4 s = *reinterpret_cast<const float4 *>(scores + (int64_t)(key - sh.first) * a.score_rows + r);
+            const float2 z0 = s_norm[r], z1 = s_norm[r + 1], z2 = s_norm[r + 2], z3 = s_norm[r + 3];
+            sum += exp2_fast(s.x - z0.x) * z0.y;
+            if (r + 1 < sh.rows) sum += exp2_fast(s.y - z1.x) * z1.y;
+            if (r + 2 < sh.rows) sum += exp2_fast(s.z - z2.x) * z2.y;
+            if (r + 3 < sh.rows) sum += exp2_fast(s.w - z3.x) * z3.y;
+        }
+        *kv.mass_at(page, at, hk) += sum;
+    }
 }
 
 int few_ctas() {
@@ -442,7 +472,8 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     a.scale2 = j.scale * kLog2e;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
     a.max_tiles = (int)((room + kTile - 1) / kTile);
-    a.score_rows = (int)std::min<int64_t>(kRows, (int64_t)j.max_new * a.G);
+    a.score_rows = (int)std::min<int64_t>(kRows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
+    a.whole = room <= kWholeKeys;
     auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
     const size_t norms = j.accumulate ? up((size_t)kv.T * j.Hq * sizeof(float2)) : 0;
@@ -463,13 +494,10 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     k_few<T, DP><<<(unsigned)a.C, kFewThreads, Few<DP>::kSmem, s>>>(a);
     e = counted_launch(cudaGetLastError());
-    if (e == cudaSuccess && a.max_tiles > 1)
-        e = launch_dependent(k_few_join<T, DP>, dim3((unsigned)kv.heads, (unsigned)kv.B), kFewThreads, a, s);
-    if (e == cudaSuccess && j.accumulate) {
-        const dim3 grid((unsigned)((room + 255) / 256), (unsigned)kv.heads, (unsigned)kv.B);
-        k_few_mass<<<grid, 256, 0, s>>>(a);
-        e = counted_launch(cudaGetLastError());
-    }
+    if (e != cudaSuccess || (a.whole && !j.accumulate)) return e;
+    const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
+    e = launch_dependent(k_few_finish<T, DP>, dim3((unsigned)(1 + parts_of_keys), (unsigned)kv.heads, (unsigned)kv.B),
+                         kFinThreads, a, s);
     return e;
 }
 

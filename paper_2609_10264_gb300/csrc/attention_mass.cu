@@ -175,10 +175,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
             const TileCopy<DP> tile(lane, kv.dim);
             if (nt && w < 2) {
                 tile.copy(base + w * C::kTileBytes, kv.K, [&](int rr, int64_t &off) {
-                    const int key = k0 + w * kCM + rr;
-                    int page = 0, slot = 0;
-                    const bool is = key < len && kv.place(b, key, page, slot);
-                    off = page * kv.k_page + slot * kv.k_slot + hk * kv.k_head;
+                    const bool is = key_place(kv, b, len, k0 + w * kCM + rr, kv.k_page, kv.k_slot, off);
+                    off += hk * kv.k_head;
                     return is;
                 });
                 tile.arrive(&k_full);
