@@ -6,16 +6,21 @@
 namespace pv {
 
 // Sequences of at most kFewRows rows per key head, single generated tokens above all,
-// go to the kernel that reads K and V as fast as they come; the others to the tensor
-// cores.  A call may have both; the host knows the largest number of new tokens at
-// most, and which sequence has how many is seen on the device.
+// go to the kernel that reads K and V as fast as they come, and where no sequence has
+// more than kFewWholeKeys keys those of kFewRowsWhole rows (eight tokens of 32 rows over
+// themselves 9.6 us on the tensor cores' path, most of it set-up).  The others go to
+// the tensor cores.  A call may have both; the host knows the largest number of new
+// tokens at most, and which sequence has how many is seen on the device.
 cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_t s) {
     AttendJob j = job;
     const int G = j.Hq / kv.heads;
+    j.few_rows = (int64_t)kv.max_pages * kv.ps.d <= kFewWholeKeys ? kFewRowsWhole : kFewRows;
     const bool one = kv.B == 1;  // which has all the new tokens
-    if (G <= kFewRows && !(one && (int64_t)kv.T * G > kFewRows)) {
+    if (G > j.few_rows)
+        j.few_rows = 0;
+    else if (!(one && (int64_t)kv.T * G > j.few_rows)) {
         const cudaError_t e = launch_attention_few(j, kv, s);
-        if (e != cudaSuccess || one || j.max_new <= kFewRows / G) return e;
+        if (e != cudaSuccess || one || j.max_new <= j.few_rows / G) return e;
     }
     if (j.accumulate) {
         void *p = nullptr;

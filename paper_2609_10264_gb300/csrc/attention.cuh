@@ -68,12 +68,15 @@ __device__ __forceinline__ Found find(int B, Work work, Pos pos) {
     }
     int64_t pre = base + incl - sum;
     const int64_t p = pos(total);
-    if (p >= pre && p < pre + sum)
+    if (p >= pre && p < pre + sum && per == 1) {
+        s_before = pre, s_b = b0;
+    } else if (p >= pre && p < pre + sum) {
         for (int b = b0; b < b1; ++b) {
             const int64_t w = work(b);
             if (p >= pre && p < pre + w) s_before = pre, s_b = b;
             pre += w;
         }
+    }
     __syncthreads();
     return Found{total, s_before, s_b};
 }
@@ -104,20 +107,27 @@ __device__ __forceinline__ Found before(int B, Work work, int at) {
     return f;
 }
 
-// Launched as soon as the kernel before lets it, which it waits for itself.
-template <typename K, typename A>
-cudaError_t launch_dependent(K kern, dim3 grid, int threads, const A &a, cudaStream_t s, int smem = 0) {
+// Launched as soon as the kernel before lets it, which it waits for itself: every
+// kernel here begins with `follow`, so that only its launch goes beside the end of the
+// one before.  (What the dependents of this one read before their own wait is then
+// complete, too.)
+template <typename K, typename... A>
+cudaError_t launch_dependent(K kern, dim3 grid, int threads, size_t smem, cudaStream_t s, const A &...a) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return counted_launch(cudaLaunchKernelEx(&cfg, kern, a));
+    return counted_launch(cudaLaunchKernelEx(&cfg, kern, a...));
+}
+__device__ __forceinline__ void follow() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // ---------------------------------------------------------------- tensor cores
@@ -251,9 +261,9 @@ __device__ __forceinline__ bool key_place(const KvView &kv, int b, int len, int 
 }
 
 // New rows of sequence b per key head, where they are too many for the kernel of few.
-__device__ __forceinline__ int many_rows(const KvView &kv, int G, int b) {
+__device__ __forceinline__ int many_rows(const KvView &kv, int few_rows, int G, int b) {
     const int rows = kv.news(b) * G;
-    return G <= kFewRows && rows <= kFewRows ? 0 : rows;
+    return rows <= few_rows ? 0 : rows;
 }
 
 // 1 / L for a row's sum, 0 for one that sees nothing (M its maximum).

@@ -31,13 +31,15 @@ struct AttendJob {
     float *lse2;                             // scratch: log2 of the rows' sums (see row_sum), may be null
     int64_t q_token, q_head, o_token, o_head;  // bytes
     int Hq, window, type, max_new;           // window 0: none
+    int few_rows;                            // see launch_attention_few
     float scale;
     bool causal, accumulate;
 };
 cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t s);
-// Of the sequences with at most kFewRows new rows per key head (tokens x query
-// heads of it); the others are left alone.
-constexpr int kFewRows = 16;
+// Of the sequences with at most few_rows new rows per key head (tokens x query heads
+// of it); the others are left alone.  Where no sequence has more keys than
+// kFewWholeKeys, a CTA takes all of them, and rows are cheap.
+constexpr int kFewRows = 16, kFewRowsWhole = 64, kFewWholeKeys = 512;
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
 // Of the others.
 cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s);

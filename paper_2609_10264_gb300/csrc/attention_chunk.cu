@@ -101,7 +101,7 @@ __device__ __forceinline__ void row_sum(const AttendJob &j, int64_t row, float l
 
 // ---------------------------------------------------------------- work
 __device__ __forceinline__ int chunk_tiles(const ChunkArgs &a, int b) {
-    const int rows = many_rows(a.kv, a.G, b);
+    const int rows = many_rows(a.kv, a.j.few_rows, a.G, b);
     return (rows + kCRows - 1) / kCRows;
 }
 // Item `idx` (row tile and key head of a sequence; the last tiles, which see most
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(kFull, tid >> 5, 0);
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    follow();
     ChunkItem it;
     if (!chunk_item(a, blockIdx.x, it)) return;
     const int split = blockIdx.y;
@@ -448,10 +448,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
 constexpr int kJoinRows = 32;
 template <typename T, int DP>
 __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant__ ChunkArgs a) {
+    follow();
     ChunkItem it;
-    const bool is = chunk_item(a, blockIdx.x, it);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (!is || it.parts == 1) return;
+    if (!chunk_item(a, blockIdx.x, it) || it.parts == 1) return;
     const int r0 = blockIdx.y * kJoinRows, rows = min(kJoinRows, it.rows - r0);
     for (int id = threadIdx.x; id < rows * (DP / 4); id += kCThreads) {
         const int r = r0 + id / (DP / 4), d = 4 * (id % (DP / 4));
@@ -527,10 +526,10 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     cudaError_t e = func_attr(reinterpret_cast<const void *>(k_chunk<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
                               Chunk<DP>::kSmem);
     if (e != cudaSuccess) return e;
-    k_chunk<T, DP><<<dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s>>>(a, maps[0], maps[1], err);
-    e = counted_launch(cudaGetLastError());
+    e = launch_dependent(k_chunk<T, DP>, dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s, a,
+                         maps[0], maps[1], err);
     if (e == cudaSuccess && a.splits > 1)
-        e = launch_dependent(k_chunk_join<T, DP>, dim3((unsigned)items, kCRows / kJoinRows), kCThreads, a, s);
+        e = launch_dependent(k_chunk_join<T, DP>, dim3((unsigned)items, kCRows / kJoinRows), kCThreads, 0, s, a);
     return e;
 }
 

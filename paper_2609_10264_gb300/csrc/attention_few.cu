@@ -25,10 +25,7 @@ constexpr int kFewWarps = 4;
 constexpr int kFewThreads = 32 * kFewWarps;
 constexpr int kSub = 16;                  // keys per warp and step
 constexpr int kTile = kFewWarps * kSub;   // keys per tile
-constexpr int kRows = kFewRows;           // rows per item, of one MMA
-// Where no sequence has more keys than this, each goes to one CTA, which needs no
-// parts joined by another kernel.
-constexpr int kWholeKeys = 512;
+constexpr int kRows = 16;                 // rows per tile of them, of one MMA
 
 struct FewArgs {
     AttendJob j;
@@ -40,7 +37,7 @@ struct FewArgs {
     int score_rows, max_tiles;  // (rows a multiple of 4)
     float scale2;    // scale x log2(e)
     int G, C;
-    bool whole;      // a CTA takes all keys of a (sequence, key head)
+    bool whole;      // a CTA takes all keys of a row tile
 };
 
 template <int DP>
@@ -87,23 +84,24 @@ __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &
     lo = pack(x - to_f32(a), y - to_f32(b), T{});
 }
 // ---------------------------------------------------------------- work
-// One sequence's share: of each key head `tiles` tiles from key `first` on, dealt out
-// in `units`.
+// One sequence's share: of each key head and tile of kRows rows, `tiles` tiles of keys
+// from key `first` on, dealt out in `units`.
 struct Share {
-    int rows, first, tiles, units;
-    int64_t work;  // units over all key heads
+    int len, n, row0;  // cached and new tokens, the first of these
+    int rows, rts, first, tiles, units;
+    int64_t work;  // units of all
 };
 __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     Share s;
-    const int n = a.kv.news(b), len = a.kv.len(b);
-    s.rows = n * a.G;
-    s.first = s.tiles = s.units = 0;
-    s.work = 0;
-    if (s.rows <= 0 || s.rows > kRows) return s;
-    if (a.j.window > 0) s.first = max(0, len - n - a.j.window + 1) / kTile * kTile;
-    s.tiles = max(1, (len - s.first + kTile - 1) / kTile);
+    s.row0 = a.kv.first(b);
+    s.n = a.kv.news(b);
+    s.len = a.kv.len(b);
+    s.rows = s.n * a.G;
+    s.rts = (s.rows + kRows - 1) / kRows;
+    s.first = a.j.window > 0 ? max(0, s.len - s.n - a.j.window + 1) / kTile * kTile : 0;
+    s.tiles = max(1, (s.len - s.first + kTile - 1) / kTile);
     s.units = a.whole ? 1 : s.tiles;
-    s.work = (int64_t)s.units * a.kv.heads;
+    s.work = s.rows <= 0 || s.rows > a.j.few_rows ? 0 : (int64_t)s.units * a.kv.heads * s.rts;
     return s;
 }
 // The CTA that takes position p of N, among C <= N.
@@ -118,7 +116,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, grp = lane >> 2;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    follow();
     const Found f = find<kFewThreads>(
         kv.B, [&](int b) { return share(a, b).work; },
         [&](int64_t total) {
@@ -142,7 +140,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         }
         const int item = (int)((p - done) / sh.units), t0 = (int)((p - done) % sh.units);
         const int nt = a.whole ? sh.tiles : (int)min((int64_t)(sh.tiles - t0), p1 - p);
-        const int hk = item, len = kv.len(b), n = kv.news(b), row0 = kv.first(b);
+        const int hk = item / sh.rts, r0 = item % sh.rts * kRows, rows = min(kRows, sh.rows - r0);
+        const int len = sh.len, n = sh.n, row0 = sh.row0;
         // ---- this warp's step i: keys from key0(i) on
         auto key0 = [&](int i) { return sh.first + (t0 + i) * kTile + warp * kSub; };
         int page_next = 0;
@@ -160,18 +159,18 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         auto load = [&](int i) {  // step i's copies (its pages have been fetched)
             unsigned there = 0;
             if (i < nt) {
-                const int k0 = key0(i), ch = lane % F::kChunks, r0 = lane / F::kChunks;
+                const int k0 = key0(i), ch = lane % F::kChunks, sub = lane / F::kChunks;
                 const bool mine = (one_page || lane < kSub) && page_next >= 0 && page_next < kv.pages &&
                                   k0 + (lane & 15) < len;
                 there = __ballot_sync(kFull, mine) & 0xffffu;
-                uint32_t d = ring + (i % F::kStages) * F::kStage + r0 * F::kRow, q, o;
-                kv.ps.divmod((uint32_t)(k0 + r0), q, o);
+                uint32_t d = ring + (i % F::kStages) * F::kStage + sub * F::kRow, q, o;
+                kv.ps.divmod((uint32_t)(k0 + sub), q, o);
                 const char *ks = kv.K + page_next * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
                 const char *vs = kv.V + page_next * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
                 // a row's chunks by neighbouring lanes; rows of K, and of V behind them
 #pragma unroll
                 for (int u = 0; u < kSub * F::kChunks / 32; ++u) {
-                    const int r = u * (32 / F::kChunks) + r0;
+                    const int r = u * (32 / F::kChunks) + sub;
                     if (!one_page) {
                         const int pg = __shfl_sync(kFull, page_next, r);
                         kv.ps.divmod((uint32_t)(k0 + r), q, o);
@@ -192,9 +191,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         // rows of Q, zero beyond the real ones
         for (int id = tid; id < kRows * F::kChunks; id += kFewThreads) {
             const int r = id / F::kChunks, ch = id % F::kChunks;
-            const bool real = r < sh.rows && ch < chunks;
+            const bool real = r < rows && ch < chunks;
             const char *src = static_cast<const char *>(j.q);
-            if (real) src += (int64_t)(row0 + r / a.G) * j.q_token + (int64_t)(hk * a.G + r % a.G) * j.q_head + ch * 16;
+            if (real)
+                src += (int64_t)(row0 + (r0 + r) / a.G) * j.q_token + (int64_t)(hk * a.G + (r0 + r) % a.G) * j.q_head + ch * 16;
             copy16(qs + r * F::kRow + ((ch ^ (r & 7)) << 4), src, real);
         }
         copy_commit();
@@ -216,8 +216,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         int lo[2], hi[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int r = grp + 8 * h, at = len - n + r / a.G;
-            hi[h] = r < sh.rows ? (j.causal ? min(len, at + 1) : len) : 0;
+            const int r = grp + 8 * h, at = len - n + (r0 + r) / a.G;
+            hi[h] = r < rows ? (j.causal ? min(len, at + 1) : len) : 0;
             lo[h] = j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
         }
         float o[DP / 8][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
@@ -249,13 +249,14 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                     mx[h] = fmaxf(mx[h], s[t][e]);
                 }
             if (a.scores) {
-                float *sc = a.scores + (((int64_t)b * kv.heads + hk) * a.max_tiles * kTile + k0 - sh.first) * a.score_rows;
+                float *sc =
+                    a.scores + (((int64_t)b * kv.heads + hk) * a.max_tiles * kTile + k0 - sh.first) * a.score_rows + r0;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = 8 * t + 2 * quad + (e & 1), r = grp + 8 * (e >> 1);
-                        if (r < sh.rows) sc[key * a.score_rows + r] = s[t][e];
+                        if (r < rows) sc[key * a.score_rows + r] = s[t][e];
                     }
             }
             float shift[2];
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         __syncthreads();
         const bool whole = nt == sh.tiles;
         const int slot = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-        for (int id = tid; id < sh.rows * (DP / 4); id += kFewThreads) {
+        for (int id = tid; id < rows * (DP / 4); id += kFewThreads) {
             const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
             float M = -INFINITY, L = 0.0f;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                 if (d == 0) a.stat[(int64_t)slot * kRows + r] = make_float2(M, L);
                 continue;
             }
-            const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
+            const int t = row0 + (r0 + r) / a.G, h = hk * a.G + (r0 + r) % a.G;
             const float inv = inverse(M, L);
             if (d < kv.dim) {
                 uint2 x;
@@ -373,19 +374,19 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 constexpr int kFinThreads = 256, kMassKeys = 1024;
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constant__ FewArgs a) {
-    __shared__ float2 s_norm[kRows];
+    __shared__ float2 s_norm[kFewRowsWhole];
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+    follow();
     const Share sh = share(a, b);
-    const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = kv.len(b);  // of the keys
-    const bool idle = !sh.work || (blockIdx.x > 0 && first >= len);
-    const Found f = idle ? Found{} : before<kFinThreads>(kv.B, [&](int i) { return share(a, i).work; }, b);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
+    const bool idle = !sh.work || (blockIdx.x > 0 ? first >= len : a.whole);
     if (idle) return;
+    const Found f = a.whole ? Found{1, 0, b} : before<kFinThreads>(kv.B, [&](int i) { return share(a, i).work; }, b);
     const int64_t C = min((int64_t)a.C, f.total), i0 = f.before + (int64_t)hk * sh.units, i1 = i0 + sh.units;
-    const int c0 = owner(i0, f.total, C), c1 = owner(i1 - 1, f.total, C);  // the CTAs that had parts
-    const int row0 = kv.first(b);
+    const int c0 = owner(i0, f.total, C), c1 = a.whole ? c0 : owner(i1 - 1, f.total, C);  // the CTAs that had parts
+    const int row0 = sh.row0;
     auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows; };
     if (blockIdx.x == 0) {
         if (c0 == c1) return;
@@ -417,7 +418,7 @@ __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constan
         }
         return;
     }
-    if (tid < kRows) {
+    if (tid < kFewRowsWhole) {
         float2 z = make_float2(0.0f, 0.0f);  // rows that are not there, or see nothing, add nothing
         if (tid < sh.rows) {
             if (c0 == c1) {
@@ -472,8 +473,8 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     a.scale2 = j.scale * kLog2e;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
     a.max_tiles = (int)((room + kTile - 1) / kTile);
-    a.score_rows = (int)std::min<int64_t>(kRows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
-    a.whole = room <= kWholeKeys;
+    a.score_rows = (int)std::min<int64_t>(j.few_rows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
+    a.whole = room <= kFewWholeKeys;
     auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
     const size_t norms = j.accumulate ? up((size_t)kv.T * j.Hq * sizeof(float2)) : 0;
@@ -492,12 +493,11 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     e = func_attr(reinterpret_cast<const void *>(k_few<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
                   Few<DP>::kSmem);
     if (e != cudaSuccess) return e;
-    k_few<T, DP><<<(unsigned)a.C, kFewThreads, Few<DP>::kSmem, s>>>(a);
-    e = counted_launch(cudaGetLastError());
+    e = launch_dependent(k_few<T, DP>, dim3((unsigned)a.C), kFewThreads, Few<DP>::kSmem, s, a);
     if (e != cudaSuccess || (a.whole && !j.accumulate)) return e;
     const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
     e = launch_dependent(k_few_finish<T, DP>, dim3((unsigned)(1 + parts_of_keys), (unsigned)kv.heads, (unsigned)kv.B),
-                         kFinThreads, a, s);
+                         kFinThreads, 0, s, a);
     return e;
 }
 

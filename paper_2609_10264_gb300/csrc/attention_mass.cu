@@ -39,7 +39,7 @@ __device__ __forceinline__ int mass_first(const MassArgs &a, int b) {
     return a.j.window > 0 && at >= a.j.window ? (at - a.j.window + 1) / kMKeys * kMKeys : 0;
 }
 __device__ __forceinline__ int mass_shares(const MassArgs &a, int b) {
-    return many_rows(a.kv, a.G, b) ? (a.kv.len(b) - mass_first(a, b) + kMKeys - 1) / kMKeys : 0;
+    return many_rows(a.kv, a.j.few_rows, a.G, b) ? (a.kv.len(b) - mass_first(a, b) + kMKeys - 1) / kMKeys : 0;
 }
 
 template <typename T, int DP>
@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(kFull, tid >> 5, 0);
+    follow();
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t ring = base + 2 * C::kTileBytes;
     if (tid == 0) {
@@ -227,8 +228,8 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     const cudaError_t e = func_attr(reinterpret_cast<const void *>(k_mass<T, DP>),
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, Mass<DP>::kSmem);
     if (e != cudaSuccess) return e;
-    k_mass<T, DP><<<(unsigned)std::min<int64_t>(items, sms), kCThreads, Mass<DP>::kSmem, s>>>(a, err);
-    return counted_launch(cudaGetLastError());
+    return launch_dependent(k_mass<T, DP>, dim3((unsigned)std::min<int64_t>(items, sms)), kCThreads, Mass<DP>::kSmem, s, a,
+                            err);
 }
 
 }  // namespace

@@ -121,7 +121,7 @@ __device__ __forceinline__ uint32_t select(Each each, int want, int &equal) {
 __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_constant__ EvictArgs a) {
     const KvView &kv = a.kv;
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    follow();
     const int len = kv.len(b), n = min(len, a.j.budget), fixed = min(a.j.recent, n);
     const int cand = len - fixed, want = n - fixed;
     const int64_t at = (int64_t)b * kv.heads + h;
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
     uint32_t q, o;
     kv.ps.divmod((uint32_t)(r0 + tid), q, o);
     const int ds = (int)o;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    follow();
     const int n = a.kept[b];
     const int from = tid < a.rows && r0 + tid < a.j.budget ? a.list[at * a.j.budget + r0 + tid] : 0;
     if (chunk == 0 && h == 0 && tid == 0) a.j.new_lens[b] = n;
@@ -299,11 +299,11 @@ cudaError_t launch_evict(const EvictJob &j, const KvView &kv, cudaStream_t s) {
     a.list = static_cast<int32_t *>(p);
     a.kept = a.list + lists;
     a.loaded = reinterpret_cast<uint32_t *>(a.kept + kv.B);
-    k_evict_select<<<dim3((unsigned)kv.heads, (unsigned)kv.B), kSelThreads, 0, s>>>(a);
-    const cudaError_t e1 = counted_launch(cudaGetLastError());
+    const cudaError_t e1 =
+        launch_dependent(k_evict_select, dim3((unsigned)kv.heads, (unsigned)kv.B), kSelThreads, 0, s, a);
     if (e1 != cudaSuccess) return e1;
-    return launch_dependent(k_evict_move, dim3((unsigned)a.chunks, (unsigned)kv.heads, (unsigned)kv.B), kMoveThreads, a, s,
-                            kMoveBytes);
+    return launch_dependent(k_evict_move, dim3((unsigned)a.chunks, (unsigned)kv.heads, (unsigned)kv.B), kMoveThreads,
+                            kMoveBytes, s, a);
 }
 
 }  // namespace pv

@@ -9,8 +9,7 @@
 // position 30000.)
 #include <algorithm>
 
-#include "attention.h"
-#include "kv.cuh"
+#include "attention.cuh"
 
 namespace pv {
 namespace {
@@ -58,6 +57,7 @@ __device__ __forceinline__ void head_rows(const RopeArgs &a, int t, int h, int p
 // One thread per (token, head, value pair or copied value): any strides.
 template <typename In, typename Out>
 __global__ void __launch_bounds__(kRopeThreads) k_rope_any(const __grid_constant__ RopeArgs a) {
+    follow();
     const RopeJob &j = a.j;
     const int half = j.rot / 2, units = half + j.dim - j.rot;
     const int64_t id = (int64_t)blockIdx.x * kRopeThreads + threadIdx.x;
@@ -143,6 +143,7 @@ struct RowPlan {
 template <typename In, typename Out, bool kHalves>
 __global__ void __launch_bounds__(kRowThreads, 8) k_rope_rows(const __grid_constant__ RopeArgs a,
                                                           const __grid_constant__ RowPlan plan) {
+    follow();
     const RopeJob &j = a.j;
     __shared__ __align__(16) float s_cos[kMostSines], s_sin[kMostSines];
     __shared__ int s_page[kMostTokens], s_slot[kMostTokens];  // page -1: nowhere
@@ -236,15 +237,12 @@ cudaError_t rope_launch(const RopeArgs &a, cudaStream_t s) {
         plan.per = FastDiv((uint32_t)plan.heads);
         const dim3 grid((unsigned)((j.T + plan.tokens - 1) / plan.tokens),
                         (unsigned)((a.heads + plan.heads - 1) / plan.heads));
-        if (j.interleaved)
-            k_rope_rows<In, Out, false><<<grid, kRowThreads, 0, s>>>(a, plan);
-        else
-            k_rope_rows<In, Out, true><<<grid, kRowThreads, 0, s>>>(a, plan);
-        return counted_launch(cudaGetLastError());
+        return launch_dependent(j.interleaved ? k_rope_rows<In, Out, false> : k_rope_rows<In, Out, true>, grid, kRowThreads,
+                                0, s, a, plan);
     }
     const int64_t n = (int64_t)j.T * a.heads * (j.rot / 2 + j.dim - j.rot);
-    k_rope_any<In, Out><<<(unsigned)((n + kRopeThreads - 1) / kRopeThreads), kRopeThreads, 0, s>>>(a);
-    return counted_launch(cudaGetLastError());
+    return launch_dependent(k_rope_any<In, Out>, dim3((unsigned)((n + kRopeThreads - 1) / kRopeThreads)), kRopeThreads, 0,
+                            s, a);
 }
 template <typename In>
 cudaError_t rope_out(const RopeArgs &a, cudaStream_t s) {
