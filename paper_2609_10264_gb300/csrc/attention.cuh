@@ -18,6 +18,17 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void *src, bool real) 
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// An arrival of this thread's on bar once its copies so far are there (bar counts it).
+__device__ __forceinline__ void copy_arrive(uint64_t *bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
+            "r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
+        : "memory");
+}
 template <int N>
 __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -234,6 +245,17 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *r) {
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 
+// Keys per box: the largest power of two, up to a tile, that divides the page size;
+// of less than 8 (a swizzle's rows) none, and none where a stride is not one that a
+// tensor map can have (64 bits wide, but not negative, nor zero where it is used).
+inline int page_box(const KvView &kv) {
+    int box = 1;
+    while (box < kCN && kv.ps.d % (2 * box) == 0) box *= 2;
+    const int64_t most = (int64_t)1 << 40;
+    for (int64_t st : {kv.k_slot, kv.k_head, kv.k_page, kv.v_slot, kv.v_head, kv.v_page})
+        if (st <= 0 || st >= most) return 0;
+    return box >= 8 ? box : 0;
+}
 // Keys or values as a tensor of (values, slots, heads, pages), for boxes of 64 values
 // x `box` slots.
 inline cudaError_t page_map(CUtensorMap *map, const KvView &kv, bool values, int type, int box) {

@@ -477,18 +477,6 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
     }
 }
 
-// Keys per box: the largest power of two, up to a tile, that divides the page size;
-// of less than 8 (a swizzle's rows) none, and none where a stride is not one that a
-// tensor map can have (64 bits wide, but not negative, nor zero where it is used).
-int page_box(const KvView &kv) {
-    int box = 1;
-    while (box < kCN && kv.ps.d % (2 * box) == 0) box *= 2;
-    const int64_t most = (int64_t)1 << 40;
-    for (int64_t st : {kv.k_slot, kv.k_head, kv.k_page, kv.v_slot, kv.v_head, kv.v_page})
-        if (st <= 0 || st >= most) return 0;
-    return box >= 8 ? box : 0;
-}
-
 template <typename T, int DP>
 cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     ChunkArgs a{};

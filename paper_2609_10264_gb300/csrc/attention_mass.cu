@@ -24,6 +24,9 @@ struct MassArgs {
     KvView kv;
     float scale2;
     int G, negative;
+    FastDiv group;  // G
+    int box;        // keys per TMA box on a page, 0: none (see page_box)
+    bool q_box;     // a tile of rows is a TMA box
 };
 
 template <int DP>
@@ -44,11 +47,13 @@ __device__ __forceinline__ int mass_shares(const MassArgs &a, int b) {
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kCThreads, 1)
-    k_mass(const __grid_constant__ MassArgs a, uint32_t *__restrict__ err) {
+    k_mass(const __grid_constant__ MassArgs a, const __grid_constant__ CUtensorMap k_map,
+           const __grid_constant__ CUtensorMap q_map, uint32_t *__restrict__ err) {
     using C = Mass<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full, mma_done;
+    __shared__ __align__(8) uint64_t shift_full[kShifts];
     __shared__ __align__(16) float s_shift[kShifts][kCM];
     __shared__ uint32_t s_tmem;
     const AttendJob &j = a.j;
@@ -68,6 +73,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
             mbar_init(&s_empty[t >> 1][t & 1], 4);
         }
         mbar_init(&k_full, 2);
+        for (int s = 0; s < kShifts; ++s) mbar_init(&shift_full[s], 32);
         mbar_init(&mma_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -113,30 +119,39 @@ __global__ void __launch_bounds__(kCThreads, 1)
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int i = 0; i < nt && ok; ++i) {
                 const uint32_t x = g + i;
-                ok = mbar_wait_warp(&s_full[tile][x & 1], (x >> 1) & 1, err, kWaitNs);
+                ok = mbar_wait_warp(&shift_full[x % kShifts], (x / kShifts) & 1, err, kWaitNs) &&
+                     mbar_wait_warp(&s_full[tile][x & 1], (x >> 1) & 1, err, kWaitNs);
                 if (!ok) break;
                 tc_fence_after();
-                float s[kCN];
-#pragma unroll
-                for (int c = 0; c < kCN / 32; ++c) tmem_ld32_async(ts + (x & 1) * kCN + 32 * c, s + 32 * c);
-                tmem_ld_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s_empty[tile][x & 1]);
                 const int q0 = r0 + i * kCM;
-                const float4 *sh = reinterpret_cast<const float4 *>(s_shift[x % kShifts]);
-                if (__any_sync(kFull, q0 < lo || hi - kCM < q0)) {
+                const bool masked = __any_sync(kFull, q0 < lo || hi - kCM < q0);
+                // half the scores at a time, which leaves registers for all else
 #pragma unroll
-                    for (int e = 0; e < kCN; ++e)
-                        if (q0 + e < lo || q0 + e >= hi) s[e] = -INFINITY;
-                }
+                for (int c = 0; c < 2; ++c) {
+                    constexpr int kHalf = kCN / 2;
+                    float s[kHalf];
+                    tmem_ld32_async(ts + (x & 1) * kCN + kHalf * c, s);
+                    tmem_ld32_async(ts + (x & 1) * kCN + kHalf * c + 32, s + 32);
+                    tmem_ld_wait();
+                    if (c == 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&s_empty[tile][x & 1]);
+                    }
+                    if (masked) {
 #pragma unroll
-                for (int e = 0; e < kCN; e += 4) {
-                    const float4 z = sh[e / 4];
-                    sum[0] += exp2_fast(fmaf(s[e], a.scale2, -z.x));
-                    sum[1] += exp2_fast(fmaf(s[e + 1], a.scale2, -z.y));
-                    sum[2] += exp2_fast(fmaf(s[e + 2], a.scale2, -z.z));
-                    sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, -z.w));
+                        for (int e = 0; e < kHalf; ++e)
+                            if (q0 + kHalf * c + e < lo || q0 + kHalf * c + e >= hi) s[e] = -INFINITY;
+                    }
+                    const float4 *sh = reinterpret_cast<const float4 *>(s_shift[x % kShifts] + kHalf * c);
+#pragma unroll
+                    for (int e = 0; e < kHalf; e += 4) {
+                        const float4 z = sh[e / 4];
+                        sum[0] += exp2_fast(fmaf(s[e], a.scale2, -z.x));
+                        sum[1] += exp2_fast(fmaf(s[e + 1], a.scale2, -z.y));
+                        sum[2] += exp2_fast(fmaf(s[e + 2], a.scale2, -z.z));
+                        sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, -z.w));
+                    }
                 }
             }
             if (ok && real && nt) *kv.mass_at(page, slot, hk) += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -171,36 +186,69 @@ __global__ void __launch_bounds__(kCThreads, 1)
             __syncwarp();
             mbar_wait_warp(&mma_done, items & 1, err, kWaitNs);
         } else {
-            // ------------------------------------------------ copies: the keys, then tiles of rows in turn
+            // ------------------------------------------------ copies: the keys, then tiles of rows and their lse2
             const int w = warp - 9;
             const TileCopy<DP> tile(lane, kv.dim);
-            if (nt && w < 2) {
-                tile.copy(base + w * C::kTileBytes, kv.K, [&](int rr, int64_t &off) {
-                    const bool is = key_place(kv, b, len, k0 + w * kCM + rr, kv.k_page, kv.k_slot, off);
-                    off += hk * kv.k_head;
-                    return is;
-                });
-                tile.arrive(&k_full);
-            }
             const int t0 = kv.first(b);
-            for (int i = w; i < nt; i += kCLoaders) {
+            if (w < 2 && nt) {
+                const uint32_t dst = base + w * C::kTileBytes;
+                const int key0 = k0 + w * kCM;
+                int page = -1, slot = 0;
+                if (a.box && key0 + kCM <= len && lane * a.box < kCM)
+                    if (!kv.place(b, key0 + lane * a.box, page, slot)) page = -1;
+                if (__all_sync(kFull, page >= 0 || (a.box && lane * a.box >= kCM)) && key0 + kCM <= len) {
+                    tile.fetch(dst, &k_map, a.box, slot, hk, page, &k_full);
+                } else {
+                    tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
+                        const bool is = key_place(kv, b, len, key0 + rr, kv.k_page, kv.k_slot, off);
+                        off += hk * kv.k_head;
+                        return is;
+                    });
+                    tile.arrive(&k_full);
+                }
+            }
+            // the first two take tiles of rows in turn, the third the lse2 of all (rows past
+            // the end are masked)
+            for (int i = w == 1 ? 1 : 0; i < nt; i += w < 2 ? 2 : 1) {
                 const uint32_t x = g + i;
                 if (x >= kSt && !mbar_wait_warp(&empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
                     ok = false;
                     break;
                 }
                 const int q0 = r0 + i * kCM;
-                // the rows' lse2 with them (rows past the end are masked)
-                const float *lse2 = j.lse2 + (int64_t)t0 * j.Hq + hk * a.G;
-                const uint32_t sh = smem_addr(s_shift[x % kShifts]);
-                tile.copy(ring + (x % kSt) * C::kTileBytes, static_cast<const char *>(j.q), [&](int rr, int64_t &off) {
-                    const int r = q0 + rr, t = r / a.G, h = r % a.G;
-                    off = (int64_t)(t0 + t) * j.q_token + (int64_t)(hk * a.G + h) * j.q_head;
-                    copy4(sh + 4 * rr, r < rows ? lse2 + (int64_t)t * j.Hq + h : lse2, r < rows);
-                    return r < rows;
-                });
-                tile.arrive(&full[x % kSt]);
+                if (w == 2) {
+                    const float *lse2 = j.lse2 + (int64_t)t0 * j.Hq + hk * a.G;
+                    const uint32_t sh = smem_addr(s_shift[x % kShifts]);
+#pragma unroll
+                    for (int y = 0; y < kCM / 32; ++y) {
+                        const int rr = 32 * y + lane, r = min(q0 + rr, rows - 1);
+                        uint32_t t, h;
+                        a.group.divmod((uint32_t)r, t, h);
+                        copy4(sh + 4 * rr, lse2 + (int64_t)t * j.Hq + h, true);
+                    }
+                    copy_arrive(&shift_full[x % kShifts]);
+                    continue;
+                }
+                const uint32_t dst = ring + (x % kSt) * C::kTileBytes;
+                if (a.q_box) {
+                    if (lane == 0) {
+                        mbar_arrive_tx(&full[x % kSt], C::kTileBytes);
+#pragma unroll
+                        for (int s = 0; s < C::kSlabs; ++s)
+                            tma_load_3d(dst + s * C::kSlab, &q_map, 64 * s, hk * a.G, t0 + q0 / a.G, &full[x % kSt]);
+                    }
+                    __syncwarp();
+                } else {
+                    tile.copy(dst, static_cast<const char *>(j.q), [&](int rr, int64_t &off) {
+                        uint32_t t, h;
+                        a.group.divmod((uint32_t)(q0 + rr), t, h);
+                        off = (int64_t)(t0 + (int)t) * j.q_token + (int64_t)(hk * a.G + (int)h) * j.q_head;
+                        return q0 + rr < rows;
+                    });
+                    tile.arrive(&full[x % kSt]);
+                }
             }
+            copy_wait<0>();
         }
         g += (uint32_t)nt;
         loaded += nt > 0;
@@ -215,9 +263,36 @@ __global__ void __launch_bounds__(kCThreads, 1)
     }
 }
 
+// New rows as a tensor of (values, heads, tokens), for boxes of a key head's heads and
+// as many tokens as make a tile.
+cudaError_t rows_map(CUtensorMap *map, const AttendJob &j, const KvView &kv, int G) {
+    PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dim[3] = {(cuuint64_t)kv.dim, (cuuint64_t)j.Hq, (cuuint64_t)kv.T};
+    const cuuint64_t stride[2] = {(cuuint64_t)j.q_head, (cuuint64_t)j.q_token};
+    const cuuint32_t part[3] = {64, (cuuint32_t)G, (cuuint32_t)(kCM / G)}, one[3] = {1, 1, 1};
+    const CUresult r = encode(map, j.type == PVMVMD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              3, const_cast<void *>(j.q), dim, stride, part, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <typename T, int DP>
 cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
-    MassArgs a{j, kv, std::max(std::fabs(j.scale) * kLog2e, 1e-37f), j.Hq / kv.heads, j.scale < 0.0f};
+    MassArgs a{};
+    a.j = j;
+    a.kv = kv;
+    a.scale2 = std::max(std::fabs(j.scale) * kLog2e, 1e-37f);
+    a.G = j.Hq / kv.heads;
+    a.negative = j.scale < 0.0f;
+    a.group = FastDiv((uint32_t)a.G);
+    CUtensorMap maps[2] = {};
+    a.box = page_box(kv);
+    if (a.box && page_map(&maps[0], kv, false, j.type, a.box) != cudaSuccess) a.box = 0;
+    // whole tokens in a tile, and strides that a tensor map can have
+    a.q_box = kCM % a.G == 0 && j.q_token > 0 && j.q_head > 0 &&
+              rows_map(&maps[1], j, kv, a.G) == cudaSuccess;
     uint32_t *err = library_error_word();
     if (!err) return cudaErrorUnknown;
     int dev = 0, sms = 0;
@@ -229,7 +304,7 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, Mass<DP>::kSmem);
     if (e != cudaSuccess) return e;
     return launch_dependent(k_mass<T, DP>, dim3((unsigned)std::min<int64_t>(items, sms)), kCThreads, Mass<DP>::kSmem, s, a,
-                            err);
+                            maps[0], maps[1], err);
 }
 
 }  // namespace
