@@ -54,8 +54,9 @@ struct Found {
     int b;
 };
 // The sequence that holds position pos(total) of all the work (a negative one: none).
+// The work before each sequence, and behind them all of it, goes to `list`, if there.
 template <int kThreads, typename Work, typename Pos>
-__device__ __forceinline__ Found find(int B, Work work, Pos pos) {
+__device__ __forceinline__ Found find(int B, Work work, Pos pos, int64_t *list = nullptr) {
     __shared__ int64_t s_warp[kThreads / 32], s_before;
     __shared__ int s_b;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -78,6 +79,14 @@ __device__ __forceinline__ Found find(int B, Work work, Pos pos) {
         total += s_warp[w];
     }
     int64_t pre = base + incl - sum;
+    if (list) {
+        int64_t at = pre;
+        for (int b = b0; b < b1; ++b) {
+            list[b] = at;
+            at += per == 1 ? sum : work(b);
+        }
+        if (tid == 0) list[B] = total;
+    }
     const int64_t p = pos(total);
     if (p >= pre && p < pre + sum && per == 1) {
         s_before = pre, s_b = b0;
@@ -90,32 +99,6 @@ __device__ __forceinline__ Found find(int B, Work work, Pos pos) {
     }
     __syncthreads();
     return Found{total, s_before, s_b};
-}
-// The work before sequence at, which holds any, and all of it.
-template <int kThreads, typename Work>
-__device__ __forceinline__ Found before(int B, Work work, int at) {
-    __shared__ int64_t s_sum[2][kThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int64_t sum = 0, pre = 0;
-    for (int b = tid; b < B; b += kThreads) {
-        const int64_t w = work(b);
-        sum += w;
-        if (b < at) pre += w;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        sum += __shfl_xor_sync(kFull, sum, o);
-        pre += __shfl_xor_sync(kFull, pre, o);
-    }
-    if (lane == 0) s_sum[0][warp] = sum, s_sum[1][warp] = pre;
-    __syncthreads();
-    Found f{0, 0, at};
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        f.total += s_sum[0][w];
-        f.before += s_sum[1][w];
-    }
-    return f;
 }
 
 // Launched as soon as the kernel before lets it, which it waits for itself: every

@@ -32,6 +32,7 @@ struct FewArgs {
     KvView kv;
     float *part;     // [2 C][kRows][DP] unnormalised partial outputs
     float2 *stat;    // [2 C][kRows] their maximum and sum
+    int64_t *before; // [B + 1] work before each sequence, and all of it
     float2 *norm;    // [T][Hq] maximum and 1 / sum, where mass is accumulated
     float *scores;   // [B][heads][max tiles x 64][rows] where mass is accumulated
     int score_rows, max_tiles;  // (rows a multiple of 4)
@@ -66,12 +67,12 @@ __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
 template <typename T>
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (sizeof(T) == 2 && __is_same(T, __half))
-        asm volatile(
+        asm(
             "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile(
+        asm(
             "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -107,6 +108,15 @@ __device__ __forceinline__ Share share(const FewArgs &a, int b) {
 // The CTA that takes position p of N, among C <= N.
 __device__ __forceinline__ int owner(int64_t p, int64_t N, int64_t C) { return (int)(((p + 1) * C - 1) / N); }
 
+// Four values of row r of a sequence and key head, from value d on.
+template <typename T>
+__device__ __forceinline__ void put_row(const FewArgs &a, int row0, int hk, int r, int d, float4 v, float inv) {
+    if (d >= a.kv.dim) return;
+    const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
+    *reinterpret_cast<uint2 *>(static_cast<char *>(a.j.out) + t * a.j.o_token + h * a.j.o_head + 2 * d) =
+        make_uint2(pack(v.x * inv, v.y * inv, T{}), pack(v.z * inv, v.w * inv, T{}));
+}
+
 // ---------------------------------------------------------------- main kernel
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ FewArgs a) {
@@ -122,7 +132,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         [&](int64_t total) {
             const int64_t C = min((int64_t)a.C, total);
             return (int64_t)blockIdx.x < C ? total * blockIdx.x / C : -1;
-        });
+        },
+        blockIdx.x == 0 ? a.before : nullptr);
     const int64_t C = min((int64_t)a.C, f.total);
     if ((int64_t)blockIdx.x >= C) return;
     const int64_t p1 = f.total * (blockIdx.x + 1) / C;
@@ -230,15 +241,27 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             const int k0 = key0(i);
             if (k0 >= len) continue;  // the same for the whole warp
             const unsigned there = (unsigned)(seen >> 16 * (F::kStages - 1)) & 0xffffu;
-            float s[2][4] = {};
+            // two sums a tile of 8 keys, so that the MMAs wait less for one another
+            float s[2][4] = {}, s1[2][4] = {};
 #pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-                uint32_t kf[4];
-                const int r = (lane & 7) + ((lane >> 4) << 3), ch = 2 * k + ((lane >> 3) & 1);
-                ldsm4(st + r * F::kRow + ((ch ^ (r & 7)) << 4), kf);
-                mma<T>(s[0], qf[k], kf[0], kf[1]);
-                mma<T>(s[1], qf[k], kf[2], kf[3]);
+            for (int k = 0; k < DP / 16; k += 4) {
+                uint32_t kf[4][4];
+                const int r = (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int ch = 2 * (k + u) + ((lane >> 3) & 1);
+                    ldsm4(st + r * F::kRow + ((ch ^ (r & 7)) << 4), kf[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    mma<T>(u & 1 ? s1[0] : s[0], qf[k + u], kf[u][0], kf[u][1]);
+                    mma<T>(u & 1 ? s1[1] : s[1], qf[k + u], kf[u][2], kf[u][3]);
+                }
             }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][e] += s1[t][e];
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -296,14 +319,18 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                 split<T>(s[t][2], s[t][3], ph[2 * t + 1], pl[2 * t + 1]);
             }
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) {
-                uint32_t vf[4];
-                const int r = lane & 15, ch = 2 * d + (lane >> 4);
-                ldsm4_t(st + F::kHalf + r * F::kRow + ((ch ^ (r & 7)) << 4), vf);
-                mma<T>(o[2 * d], ph, vf[0], vf[1]);
-                mma<T>(o[2 * d + 1], ph, vf[2], vf[3]);
-                mma<T>(o[2 * d], pl, vf[0], vf[1]);
-                mma<T>(o[2 * d + 1], pl, vf[2], vf[3]);
+            for (int d = 0; d < DP / 16; d += 2) {
+                uint32_t vf[2][4];
+                const int r = lane & 15;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int ch = 2 * (d + u) + (lane >> 4);
+                    ldsm4_t(st + F::kHalf + r * F::kRow + ((ch ^ (r & 7)) << 4), vf[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) mma<T>(o[2 * d + u], ph, vf[u / 2][2 * (u & 1)], vf[u / 2][2 * (u & 1) + 1]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) mma<T>(o[2 * d + u], pl, vf[u / 2][2 * (u & 1)], vf[u / 2][2 * (u & 1) + 1]);
             }
         }
         copy_wait<0>();
@@ -349,14 +376,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                 if (d == 0) a.stat[(int64_t)slot * kRows + r] = make_float2(M, L);
                 continue;
             }
-            const int t = row0 + (r0 + r) / a.G, h = hk * a.G + (r0 + r) % a.G;
             const float inv = inverse(M, L);
-            if (d < kv.dim) {
-                uint2 x;
-                x.x = pack(v.x * inv, v.y * inv, T{});
-                x.y = pack(v.z * inv, v.w * inv, T{});
-                *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
-            }
+            put_row<T>(a, row0, hk, r0 + r, d, v, inv);
+            const int t = row0 + (r0 + r) / a.G, h = hk * a.G + (r0 + r) % a.G;
             if (d == 0) {
                 if (j.lse) j.lse[(int64_t)t * j.Hq + h] = kLn2 * (M + log2f(L));
                 if (a.norm) a.norm[(int64_t)t * j.Hq + h] = make_float2(M, inv);
@@ -371,10 +393,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 // the parts of several CTAs together, in the order of the keys; the others add to the
 // mass of kMassKeys keys each, a thread a key: sum over the rows of exp2(score -
 // maximum) / sum.
-constexpr int kFinThreads = 256, kMassKeys = 1024;
-template <typename T, int DP>
+// (Joining alone takes more threads: of 38 parts a key head 89.8 us a call with 512
+// where 93.5 with 256; the mass wants more CTAs.)
+constexpr int kMassKeys = 1024;
+template <typename T, int DP, int kFinThreads>
 __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constant__ FewArgs a) {
     __shared__ float2 s_norm[kFewRowsWhole];
+    extern __shared__ __align__(16) float s_weight[];  // [rows][parts], then the groups' sums
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
@@ -383,38 +408,69 @@ __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constan
     const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
     const bool idle = !sh.work || (blockIdx.x > 0 ? first >= len : a.whole);
     if (idle) return;
-    const Found f = a.whole ? Found{1, 0, b} : before<kFinThreads>(kv.B, [&](int i) { return share(a, i).work; }, b);
-    const int64_t C = min((int64_t)a.C, f.total), i0 = f.before + (int64_t)hk * sh.units, i1 = i0 + sh.units;
-    const int c0 = owner(i0, f.total, C), c1 = a.whole ? c0 : owner(i1 - 1, f.total, C);  // the CTAs that had parts
+    const int64_t total = a.before[kv.B], C = min((int64_t)a.C, total);
+    const int64_t i0 = a.before[b] + (int64_t)hk * sh.units, i1 = i0 + sh.units;
+    const int c0 = owner(i0, total, C), c1 = a.whole ? c0 : owner(i1 - 1, total, C);  // the CTAs that had parts
     const int row0 = sh.row0;
     auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows; };
     if (blockIdx.x == 0) {
         if (c0 == c1) return;
-        for (int id = tid; id < sh.rows * (DP / 4); id += kFinThreads) {
-            const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
+        // the parts' weights, a warp a row; then their sum, with threads enough for
+        // several parts at a time
+        const int ns = c1 - c0 + 1, lane = tid & 31;
+        for (int r = tid >> 5; r < sh.rows; r += kFinThreads / 32) {
             float M = -INFINITY, L = 0.0f;
-            for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.stat[slot(c) + r].x);
+            for (int i = lane; i < ns; i += 32) M = fmaxf(M, a.stat[slot(c0 + i) + r].x);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
             const float ref = M == -INFINITY ? 0.0f : M;
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int c = c0; c <= c1; ++c) {
-                const float2 z = a.stat[slot(c) + r];
+            for (int i = lane; i < ns; i += 32) {
+                const float2 z = a.stat[slot(c0 + i) + r];
                 const float e = exp2_fast(z.x - ref);
-                const float4 x = *reinterpret_cast<const float4 *>(a.part + (slot(c) + r) * DP + d);
                 L += z.y * e;
+                s_weight[r * ns + i] = e;
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(kFull, L, o);
+            if (lane == 0) {
+                s_norm[r] = make_float2(M, inverse(M, L));
+                if (j.lse) j.lse[(int64_t)(row0 + r / a.G) * j.Hq + hk * a.G + r % a.G] = kLn2 * (M + log2f(L));
+            }
+        }
+        __syncthreads();
+        const int cols = sh.rows * (DP / 4), groups = max(1, kFinThreads / cols);
+        float4 *s_sum = reinterpret_cast<float4 *>(s_weight + (sh.rows * ns + 3) / 4 * 4);
+        for (int id = tid; id < cols * groups; id += kFinThreads) {
+            const int g = id / cols, col = id - g * cols, r = col / (DP / 4), d = 4 * (col % (DP / 4));
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+            for (int i = g; i < ns; i += groups) {
+                const float e = s_weight[r * ns + i];
+                const float4 x = *reinterpret_cast<const float4 *>(a.part + (slot(c0 + i) + r) * DP + d);
                 v.x += x.x * e;
                 v.y += x.y * e;
                 v.z += x.z * e;
                 v.w += x.w * e;
             }
-            const int t = row0 + r / a.G, h = hk * a.G + r % a.G;
-            const float inv = inverse(M, L);
-            if (d < kv.dim) {
-                uint2 x;
-                x.x = pack(v.x * inv, v.y * inv, T{});
-                x.y = pack(v.z * inv, v.w * inv, T{});
-                *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + t * j.o_token + h * j.o_head + 2 * d) = x;
+            if (groups > 1) {
+                s_sum[id] = v;
+                continue;
             }
-            if (d == 0 && j.lse) j.lse[(int64_t)t * j.Hq + h] = kLn2 * (M + log2f(L));
+            put_row<T>(a, row0, hk, r, d, v, s_norm[r].y);
+        }
+        if (groups == 1) return;
+        __syncthreads();
+        if (tid < cols) {
+            float4 v = s_sum[tid];
+            for (int g = 1; g < groups; ++g) {
+                const float4 x = s_sum[g * cols + tid];
+                v.x += x.x;
+                v.y += x.y;
+                v.z += x.z;
+                v.w += x.w;
+            }
+            const int r = tid / (DP / 4);
+            put_row<T>(a, row0, hk, r, 4 * (tid % (DP / 4)), v, s_norm[r].y);
         }
         return;
     }
@@ -477,18 +533,20 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     a.whole = room <= kFewWholeKeys;
     auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
+    const size_t befores = up((size_t)(kv.B + 1) * sizeof(int64_t));
     const size_t norms = j.accumulate ? up((size_t)kv.T * j.Hq * sizeof(float2)) : 0;
     const size_t scores =
         j.accumulate ? (size_t)kv.B * kv.heads * a.max_tiles * kTile * a.score_rows * sizeof(float) : 0;
     void *buf = nullptr;
-    cudaError_t e = stream_scratch(kScratchAttention, parts + stats + norms + scores, s, &buf);
+    cudaError_t e = stream_scratch(kScratchAttention, parts + stats + befores + norms + scores, s, &buf);
     if (e != cudaSuccess) return e;
     char *at = static_cast<char *>(buf);
     a.part = reinterpret_cast<float *>(at);
     a.stat = reinterpret_cast<float2 *>(at + parts);
+    a.before = reinterpret_cast<int64_t *>(at + parts + stats);
     if (j.accumulate) {
-        a.norm = reinterpret_cast<float2 *>(at + parts + stats);
-        a.scores = reinterpret_cast<float *>(at + parts + stats + norms);
+        a.norm = reinterpret_cast<float2 *>(at + parts + stats + befores);
+        a.scores = reinterpret_cast<float *>(at + parts + stats + befores + norms);
     }
     e = func_attr(reinterpret_cast<const void *>(k_few<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
                   Few<DP>::kSmem);
@@ -496,8 +554,12 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     e = launch_dependent(k_few<T, DP>, dim3((unsigned)a.C), kFewThreads, Few<DP>::kSmem, s, a);
     if (e != cudaSuccess || (a.whole && !j.accumulate)) return e;
     const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
-    e = launch_dependent(k_few_finish<T, DP>, dim3((unsigned)(1 + parts_of_keys), (unsigned)kv.heads, (unsigned)kv.B),
-                         kFinThreads, 0, s, a);
+    const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)kv.heads, (unsigned)kv.B);
+    auto finish = [&](auto kern, int threads) {
+        return launch_dependent(kern, grid, threads, (size_t)(kRows * a.C + 4) * sizeof(float) + threads * sizeof(float4), s,
+                                a);
+    };
+    e = j.accumulate ? finish(k_few_finish<T, DP, 256>, 256) : finish(k_few_finish<T, DP, 512>, 512);
     return e;
 }
 
