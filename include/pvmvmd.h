@@ -435,7 +435,8 @@ typedef struct {
  * table_dev[b table_stride + i / page_size].  Entries behind its last page are not
  * read.  Its new tokens are rows cu_dev[b] .. cu_dev[b+1] - 1 of the T token
  * tensors (cu_dev[0] = 0, cu_dev[B] = T, ascending; null: one each, T = B).
- * max_new: at least as many as any sequence has new ones, 0 if not known (then T).
+ * max_new: at least as many as any sequence has new ones, 0 if not known (then T);
+ * tokens beyond it, and rows that cu_dev puts outside the T, are left out.
  * max_pages * page_size is at most 2^30, B and the pool's heads at most 65535.
  * Lengths beyond max_pages pages are taken as max_pages pages; keys on pages
  * outside the pool are not seen, and nothing is written there. */

@@ -60,6 +60,21 @@ __device__ __forceinline__ Found find(int B, Work work, Pos pos, int64_t *list =
     __shared__ int64_t s_warp[kThreads / 32], s_before;
     __shared__ int s_b;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (B <= 32) {  // every warp by itself, a lane a sequence
+        const int64_t w = lane < B ? work(lane) : 0;
+        int64_t incl = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t v = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += v;
+        }
+        const int64_t total = __shfl_sync(kFull, incl, 31), pre = incl - w, p = pos(total);
+        if (list && warp == 0 && lane < B) list[lane] = pre;
+        if (list && tid == 0) list[B] = total;
+        const unsigned at = __ballot_sync(kFull, p >= pre && p < incl);
+        const int b = at ? __ffs(at) - 1 : 0;
+        return Found{total, __shfl_sync(kFull, pre, b), at ? b : -1};
+    }
     const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
     int64_t sum = 0;
     for (int b = b0; b < b1; ++b) sum += work(b);

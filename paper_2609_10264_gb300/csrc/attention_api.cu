@@ -1,7 +1,8 @@
 // C ABI of the client's attention (include/pvmvmd.h): checks of arguments and the
 // launches.
-#include <cmath>
+#include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "attention.h"
 #include "kv.cuh"
@@ -59,6 +60,7 @@ int view(const pvmvmd_kv_pool *p, const pvmvmd_kv_batch *b, KvView &v) {
     v.B = b->B;
     v.T = b->T;
     v.max_pages = b->max_pages;
+    v.max_new = !b->cu_dev ? 1 : b->max_new ? std::min(b->max_new, b->T) : b->T;
     return PVMVMD_OK;
 }
 // the batch of a call that has new tokens
@@ -191,7 +193,7 @@ int pvmvmd_paged_attention(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *ba
     j.Hq = Hq;
     j.window = window;
     j.type = pool->type;
-    j.max_new = !batch->cu_dev ? 1 : batch->max_new ? batch->max_new : kv.T;
+    j.max_new = kv.max_new;
     j.scale = scale;
     j.causal = causal != 0;
     j.accumulate = accumulate != 0;

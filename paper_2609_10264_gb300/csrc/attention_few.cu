@@ -155,35 +155,37 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         const int len = sh.len, n = sh.n, row0 = sh.row0;
         // ---- this warp's step i: keys from key0(i) on
         auto key0 = [&](int i) { return sh.first + (t0 + i) * kTile + warp * kSub; };
-        int page_next = 0;
-        auto fetch_page = [&](int i) {  // of the step's keys, a lane each
+        int pages[F::kStages];  // of the steps to be loaded next, a lane a key
+        auto fetch_page = [&](int i) {
             const int k = key0(i) + (one_page ? 0 : lane & 15);
+#pragma unroll
+            for (int s = 0; s + 1 < F::kStages; ++s) pages[s] = pages[s + 1];
+            pages[F::kStages - 1] = -1;
             if (i < nt && k < len) {
                 uint32_t q, r;
                 kv.ps.divmod((uint32_t)k, q, r);
-                page_next = kv.table[b * kv.table_stride + q];
-            } else {
-                page_next = -1;
+                pages[F::kStages - 1] = kv.table[b * kv.table_stride + q];
             }
         };
         uint64_t seen = 0;  // of the steps loaded last, 16 bits each: the keys that are there
         auto load = [&](int i) {  // step i's copies (its pages have been fetched)
             unsigned there = 0;
+            const int page = pages[0];
             if (i < nt) {
                 const int k0 = key0(i), ch = lane % F::kChunks, sub = lane / F::kChunks;
-                const bool mine = (one_page || lane < kSub) && page_next >= 0 && page_next < kv.pages &&
+                const bool mine = (one_page || lane < kSub) && page >= 0 && page < kv.pages &&
                                   k0 + (lane & 15) < len;
                 there = __ballot_sync(kFull, mine) & 0xffffu;
                 uint32_t d = ring + (i % F::kStages) * F::kStage + sub * F::kRow, q, o;
                 kv.ps.divmod((uint32_t)(k0 + sub), q, o);
-                const char *ks = kv.K + page_next * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
-                const char *vs = kv.V + page_next * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
+                const char *ks = kv.K + page * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
+                const char *vs = kv.V + page * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
                 // a row's chunks by neighbouring lanes; rows of K, and of V behind them
 #pragma unroll
                 for (int u = 0; u < kSub * F::kChunks / 32; ++u) {
                     const int r = u * (32 / F::kChunks) + sub;
                     if (!one_page) {
-                        const int pg = __shfl_sync(kFull, page_next, r);
+                        const int pg = __shfl_sync(kFull, page, r);
                         kv.ps.divmod((uint32_t)(k0 + r), q, o);
                         ks = kv.K + pg * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
                         vs = kv.V + pg * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
@@ -199,6 +201,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             seen = seen << 16 | there;
             copy_commit();
         };
+#pragma unroll
+        for (int i = 0; i < F::kStages; ++i) fetch_page(i);
         // rows of Q, zero beyond the real ones
         for (int id = tid; id < kRows * F::kChunks; id += kFewThreads) {
             const int r = id / F::kChunks, ch = id % F::kChunks;
@@ -209,11 +213,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             copy16(qs + r * F::kRow + ((ch ^ (r & 7)) << 4), src, real);
         }
         copy_commit();
-        fetch_page(0);
 #pragma unroll
         for (int i = 0; i < F::kStages - 1; ++i) {
             load(i);
-            fetch_page(i + 1);
+            fetch_page(i + F::kStages);
         }
         copy_wait<F::kStages - 1>();
         __syncthreads();
@@ -236,7 +239,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             copy_wait<F::kStages - 2>();
             __syncwarp();
             load(i + F::kStages - 1);
-            fetch_page(i + F::kStages);
+            fetch_page(i + 2 * F::kStages - 1);
             const uint32_t st = ring + (i % F::kStages) * F::kStage;
             const int k0 = key0(i);
             if (k0 >= len) continue;  // the same for the whole warp

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <climits>
 #include <cstdint>
 
 #include "common.cuh"
@@ -35,7 +36,7 @@ struct KvView {
     FastDiv ps;  // page size
     const int32_t *table, *lens, *cu;
     int64_t table_stride;
-    int B, T, max_pages;
+    int B, T, max_pages, max_new;
 
     // cached tokens of sequence b, no more than its table has room for
     __device__ __forceinline__ int len(int b) const {
@@ -43,9 +44,12 @@ struct KvView {
         const int l = max(lens[b], 0);
         return room < l ? (int)room : l;
     }
-    // first row and number of the new tokens of sequence b
-    __device__ __forceinline__ int first(int b) const { return cu ? cu[b] : b; }
-    __device__ __forceinline__ int news(int b) const { return cu ? cu[b + 1] - cu[b] : 1; }
+    // first row and number of the new tokens of sequence b: rows of the T there are, and
+    // no more than scratch is made for, whatever cu holds
+    __device__ __forceinline__ int first(int b) const { return cu ? min(max(cu[b], 0), T) : b; }
+    __device__ __forceinline__ int news(int b) const {
+        return cu ? min(max(min(cu[b + 1], T) - first(b), 0), max_new) : 1;
+    }
     // the sequence of row t
     __device__ __forceinline__ int seq(int t) const {
         if (!cu) return t;
@@ -58,6 +62,12 @@ struct KvView {
                 hi = mid;
         }
         return lo;
+    }
+    // the cache index of new token t of sequence b = seq(t); negative in front of the
+    // sequence's start, and the least one of a row that is no token of it
+    __device__ __forceinline__ int index(int b, int t) const {
+        const int n = news(b), i = t - first(b);
+        return i >= 0 && i < n ? len(b) - n + i : INT_MIN;
     }
     // page and slot of cache index i of sequence b; false where there is none
     __device__ __forceinline__ bool place(int b, int i, int &page, int &slot) const {

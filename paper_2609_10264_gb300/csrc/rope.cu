@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope_any(const __grid_constant
     int b = 0, page = -1, slot = 0, idx = 0;
     if (j.cached) {
         b = a.kv.seq(t);
-        idx = a.kv.len(b) - a.kv.news(b) + t - a.kv.first(b);
+        idx = a.kv.index(b, t);
         if (idx < 0 || !a.kv.place(b, idx, page, slot)) page = -1;
     }
     const In *src;
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) k_rope_rows(const __grid_const
     const int turned = j.part[0].heads + j.part[1].heads;  // heads that are rotated
     auto index_of = [&](int t, int &b) {  // the token's cache index
         b = a.kv.seq(t);
-        return a.kv.len(b) - a.kv.news(b) + t - a.kv.first(b);
+        return a.kv.index(b, t);
     };
     if (j.cached && tid < nt) {
         int b, page, slot;

@@ -459,7 +459,10 @@ CHUNKS = [  # lens, news, Hq, H, D, page, kind, layout
     ([130, 40, 300], [129, 1, 77], 4, 4, 64, 24, "f16", "hnd"), ([500, 260], [257, 260], 8, 1, 128, 64, "bf16", "nhd"),
     ([70, 0, 5], [70, 0, 9], 6, 2, 80, 1, "bf16", "fused"), ([400], [130], 5, 1, 96, 100, "f16", "nhd"),
     ([1100], [64], 8, 2, 128, 128, "bf16", "hnd"), ([3, 700, 64, 1], [3, 4, 2, 1], 8, 2, 128, 16, "bf16", "nhd"),
-    ([385], [300], 1, 1, 128, 16, "f16", "nhd"), ([90], [33], 24, 8, 40, 12, "bf16", "nhd")]
+    ([385], [300], 1, 1, 128, 16, "f16", "nhd"), ([90], [33], 24, 8, 40, 12, "bf16", "nhd"),
+    ([700, 333], [200, 300], 4, 2, 128, 16, "bf16", "fused"), ([600], [200], 16, 16, 8, 32, "f16", "nhd"),
+    ([900, 10], [64, 10], 6, 2, 24, 256, "bf16", "hnd"), ([1300, 800, 20], [3, 100, 1], 32, 8, 128, 48, "bf16", "nhd"),
+    ([260] * 3, [1, 257, 2], 64, 1, 64, 8, "f16", "nhd"), ([2500], [400], 12, 4, 128, 64, "bf16", "nhd")]
 
 
 @pytest.mark.gpu
@@ -485,6 +488,44 @@ def test_score_ranges(pv, news, gain):
     """From equal weights to one key that takes them all, with the largest one late or early."""
     check_attention(pv, [1500], news, 4, 1, 128, 16, "bf16", 14, gain=gain, accumulate=True)
     check_attention(pv, [1500], news, 4, 1, 128, 16, "f16", 15, gain=gain, scale=-0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, -0.25, 3.0])
+@pytest.mark.parametrize("lens,news", [([900, 70], [1, 1]), ([900, 70], [100, 60]), ([300], [12])])
+def test_scales(pv, lens, news, scale):
+    check_attention(pv, lens, news, 4, 1, 64, 16, "bf16", 24, scale=scale, accumulate=True)
+
+
+@pytest.mark.gpu
+def test_rows_and_lengths_beyond_what_there_is(pv):
+    """cu that names rows outside the token tensors, more new tokens than max_new, lengths beyond the table: nothing
+    outside is read or written, and what is inside comes out as it should."""
+    import torch
+    c = Cache(pv, [300, 200], [40, 24], 2, 64, 16, "bf16", 25, garbage=False)
+    q = torch.randn(64, 8, 64, device="cuda").to(torch.bfloat16)
+    ref = pv.pvmvmd_paged_attention(c.pool, c.batch, q)
+    guard = torch.full((64 + 64, 8, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    wild = torch.tensor([0, 40, 1 << 30], dtype=torch.int32, device="cuda")
+    pv.pvmvmd_paged_attention(c.pool, pv.KvBatch(c.table, c.dlens, wild), q, out=guard[:64])
+    assert torch.equal(guard[:64], ref) and (guard[64:] == 5).all()
+    guard.fill_(5.0)
+    pv.pvmvmd_paged_attention(c.pool, pv.KvBatch(c.table, c.dlens, c.cu, max_new=24), q, out=guard[:64])
+    assert torch.equal(guard[40:64], ref[40:]) and (guard[64:] == 5).all()
+    wild = torch.tensor([-70, 40, 64], dtype=torch.int32, device="cuda")
+    pv.pvmvmd_paged_attention(c.pool, pv.KvBatch(c.table, c.dlens, wild), q, out=guard[:64], accumulate=True)
+    assert torch.equal(guard[:64], ref) and (guard[64:] == 5).all()
+    K0 = c.K.clone()
+    x = torch.ones(64, 2, 64, dtype=torch.bfloat16, device="cuda")
+    pv.pvmvmd_kv_append(c.pool, pv.KvBatch(c.table, c.dlens, wild), x, x)
+    c.dlens.fill_(1 << 30)
+    pv.pvmvmd_paged_attention(c.pool, c.batch, q, accumulate=True)
+    used = torch.zeros(K0.shape[:2], dtype=torch.bool, device="cuda")
+    for b, (L, n) in enumerate(((300, 40), (200, 24))):
+        p, o = c.at(b)
+        used[torch.from_numpy(p[L - n:]).long().cuda(), torch.from_numpy(o[L - n:]).long().cuda()] = True
+    assert torch.equal(c.K[~used], K0[~used]) and (c.K[used] == 1).all()
+    assert pv.pvmvmd_device_status() == 0
 
 
 @pytest.mark.gpu
