@@ -6,7 +6,10 @@
 // needs no other thread, and no atomics: S^T = K Q^T.  A CTA keeps two tiles of 128
 // keys and walks the rows that see them in tiles of 128 through a ring; each of the
 // two has two accumulators in TMEM, so that the tensor cores work on the next tile
-// while one is summed.  One exp2 a score bounds it.
+// while one is summed.  Few rows over many keys make many short items, so a CTA stays
+// and its rows' copies and sums run on from one item to the next (with a barrier at
+// each, five chunks of 35 tokens over 13000 keys took 130 us).  One exp2 a score bounds
+// it where there are many rows.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -17,7 +20,7 @@ namespace pv {
 namespace {
 
 constexpr int kMKeys = 2 * kCM;  // keys per CTA
-constexpr int kShifts = 8;       // ring of the rows' lse2, which are read after their tiles are let go
+constexpr int kShifts = 4;       // ring of the rows' lse2
 
 struct MassArgs {
     AttendJob j;
@@ -45,6 +48,51 @@ __device__ __forceinline__ int mass_shares(const MassArgs &a, int b) {
     return many_rows(a.kv, a.j.few_rows, a.G, b) ? (a.kv.len(b) - mass_first(a, b) + kMKeys - 1) / kMKeys : 0;
 }
 
+// Keys [k0, k0 + kMKeys) of a sequence and key head, and the tiles of rows that see any
+// of them: nt from row r0 on.
+struct MassItem {
+    int b, hk, k0, len, old, n, rows, t0, r0, nt;
+    // the rows that see a key: [first, last)
+    __device__ __forceinline__ int first_row(const MassArgs &a, int key) const {
+        return a.j.causal && key > old ? (int)min((int64_t)rows, (int64_t)(key - old) * a.G) : 0;
+    }
+    __device__ __forceinline__ int last_row(const MassArgs &a, int key) const {
+        const int64_t t = a.j.window > 0 ? (int64_t)key + a.j.window - old : n;
+        return t >= n ? rows : t <= 0 ? 0 : (int)t * a.G;
+    }
+};
+// A CTA's items in order: every gridDim.x-th of all (shares of keys and their heads).
+struct MassWalk {
+    int64_t idx, before;  // the next item, and the shares before sequence b
+    int b;
+    __device__ __forceinline__ bool next(const MassArgs &a, MassItem &it) {
+        const KvView &kv = a.kv;
+        for (;; idx += gridDim.x) {
+            const int64_t share = idx / kv.heads;
+            for (; b < kv.B; ++b) {
+                const int n = mass_shares(a, b);
+                if (share < before + n) break;
+                before += n;
+            }
+            if (b >= kv.B) return false;
+            it.b = b;
+            it.hk = (int)(idx - share * kv.heads);
+            it.len = kv.len(b);
+            it.n = kv.news(b);
+            it.t0 = kv.first(b);
+            it.rows = it.n * a.G;
+            it.old = it.len - it.n;
+            it.k0 = mass_first(a, b) + (int)(share - before) * kMKeys;
+            it.r0 = it.first_row(a, it.k0) / kCM * kCM;
+            const int r1 = it.last_row(a, min(it.k0 + kMKeys, it.len) - 1);
+            it.nt = r1 > it.r0 ? (r1 - it.r0 + kCM - 1) / kCM : 0;
+            if (it.nt == 0) continue;
+            idx += gridDim.x;
+            return true;
+        }
+    }
+};
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(kCThreads, 1)
     k_mass(const __grid_constant__ MassArgs a, const __grid_constant__ CUtensorMap k_map,
@@ -52,8 +100,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
     using C = Mass<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full, mma_done;
-    __shared__ __align__(8) uint64_t shift_full[kShifts];
+    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full, k_empty, mma_done;
+    __shared__ __align__(8) uint64_t shift_full[kShifts], shift_empty[kShifts];
     __shared__ __align__(16) float s_shift[kShifts][kCM];
     __shared__ uint32_t s_tmem;
     const AttendJob &j = a.j;
@@ -73,7 +121,11 @@ __global__ void __launch_bounds__(kCThreads, 1)
             mbar_init(&s_empty[t >> 1][t & 1], 4);
         }
         mbar_init(&k_full, 2);
-        for (int s = 0; s < kShifts; ++s) mbar_init(&shift_full[s], 32);
+        mbar_init(&k_empty, 1);
+        for (int s = 0; s < kShifts; ++s) {
+            mbar_init(&shift_full[s], 32);
+            mbar_init(&shift_empty[s], 8);
+        }
         mbar_init(&mma_done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -85,45 +137,36 @@ __global__ void __launch_bounds__(kCThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
+    const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
+                                    [&](int64_t) { return (int64_t)blockIdx.x / kv.heads; });
+    MassWalk walk{(int64_t)blockIdx.x, f.before, f.b < 0 ? kv.B : f.b};
     if (warp < 8)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCSoftRegs));
     else
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCOtherRegs));
 
-    uint32_t g = 0;  // tiles of rows of the items before, the same in every warp
-    uint32_t items = 0, loaded = 0;  // of them, those with rows
+    // Every role walks the CTA's items by itself, as far ahead as the barriers let it: a
+    // tile of rows is number g + i of all the CTA's, an item of keys number n.
+    MassItem it;
+    uint32_t g = 0, n = 0;
     bool ok = true;
-    for (int64_t idx = blockIdx.x;; idx += gridDim.x, ++items) {
-        const int hk = (int)(idx % kv.heads);
-        __syncthreads();  // the item before is through
-        const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
-                                        [&](int64_t) { return idx / kv.heads; });
-        if (f.b < 0) break;
-        const int b = f.b, len = kv.len(b), n = kv.news(b), rows = n * a.G, old = len - n;
-        const int k0 = mass_first(a, b) + (int)(idx / kv.heads - f.before) * kMKeys;
-        // rows that see any of the keys: [from, to)
-        auto first_row = [&](int key) { return j.causal && key > old ? (int)min((int64_t)rows, (int64_t)(key - old) * a.G) : 0; };
-        auto last_row = [&](int key) {
-            const int64_t t = j.window > 0 ? (int64_t)key + j.window - old : n;
-            return t >= n ? rows : t <= 0 ? 0 : (int)t * a.G;
-        };
-        const int r0 = first_row(k0) / kCM * kCM, r1 = last_row(min(k0 + kMKeys, len) - 1);
-        const int nt = r1 > r0 ? (r1 - r0 + kCM - 1) / kCM : 0;
-        if (warp < 8) {
-            // ------------------------------------------------ sums
-            const int tile = warp >> 2, key = k0 + tile * kCM + (warp & 3) * 32 + lane;
+    if (warp < 8) {
+        // ------------------------------------------------ sums
+        const int tile = warp >> 2;
+        const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
+        for (; ok && walk.next(a, it); g += (uint32_t)it.nt) {
+            const int key = it.k0 + tile * kCM + (warp & 3) * 32 + lane;
             int page, slot;
-            const bool real = key < len && kv.place(b, key, page, slot);
-            const int lo = real ? first_row(key) : 0, hi = real ? last_row(key) : INT_MAX;
-            const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
+            const bool real = key < it.len && kv.place(it.b, key, page, slot);
+            const int lo = real ? it.first_row(a, key) : 0, hi = real ? it.last_row(a, key) : INT_MAX;
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int i = 0; i < nt && ok; ++i) {
+            for (int i = 0; i < it.nt; ++i) {
                 const uint32_t x = g + i;
                 ok = mbar_wait_warp(&shift_full[x % kShifts], (x / kShifts) & 1, err, kWaitNs) &&
                      mbar_wait_warp(&s_full[tile][x & 1], (x >> 1) & 1, err, kWaitNs);
                 if (!ok) break;
                 tc_fence_after();
-                const int q0 = r0 + i * kCM;
+                const int q0 = it.r0 + i * kCM;
                 const bool masked = __any_sync(kFull, q0 < lo || hi - kCM < q0);
                 // half the scores at a time, which leaves registers for all else
 #pragma unroll
@@ -153,13 +196,17 @@ __global__ void __launch_bounds__(kCThreads, 1)
                         sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, -z.w));
                     }
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&shift_empty[x % kShifts]);
             }
-            if (ok && real && nt) *kv.mass_at(page, slot, hk) += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        } else if (warp == 8) {
-            // ------------------------------------------------ MMA issuer
-            const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
-            if (nt) ok = mbar_wait_warp(&k_full, loaded & 1, err, kWaitNs);
-            for (int i = 0; i < nt && ok; ++i) {
+            if (ok && real) *kv.mass_at(page, slot, it.hk) += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        }
+    } else if (warp == 8) {
+        // ------------------------------------------------ MMA issuer
+        const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
+        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
+            ok = mbar_wait_warp(&k_full, n & 1, err, kWaitNs);
+            for (int i = 0; i < it.nt && ok; ++i) {
                 const uint32_t x = g + i;
                 ok = mbar_wait_warp(&full[x % kSt], (x / kSt) & 1, err, kWaitNs);
                 const uint64_t bd = sw128_desc(ring + (x % kSt) * C::kTileBytes);
@@ -181,47 +228,59 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 if (elect_one()) commit(&empty[x % kSt]);
                 __syncwarp();
             }
-            // the next item's keys go where these are
-            if (elect_one()) commit(&mma_done);
+            if (elect_one()) commit(&k_empty);
             __syncwarp();
-            mbar_wait_warp(&mma_done, items & 1, err, kWaitNs);
-        } else {
-            // ------------------------------------------------ copies: the keys, then tiles of rows and their lse2
-            const int w = warp - 9;
-            const TileCopy<DP> tile(lane, kv.dim);
-            const int t0 = kv.first(b);
-            if (w < 2 && nt) {
-                const uint32_t dst = base + w * C::kTileBytes;
-                const int key0 = k0 + w * kCM;
-                int page = -1, slot = 0;
-                if (a.box && key0 + kCM <= len && lane * a.box < kCM)
-                    if (!kv.place(b, key0 + lane * a.box, page, slot)) page = -1;
-                if (__all_sync(kFull, page >= 0 || (a.box && lane * a.box >= kCM)) && key0 + kCM <= len) {
-                    tile.fetch(dst, &k_map, a.box, slot, hk, page, &k_full);
-                } else {
-                    tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
-                        const bool is = key_place(kv, b, len, key0 + rr, kv.k_page, kv.k_slot, off);
-                        off += hk * kv.k_head;
-                        return is;
-                    });
-                    tile.arrive(&k_full);
+        }
+        // every MMA is through before the memory that it reads goes
+        if (elect_one()) commit(&mma_done);
+        __syncwarp();
+        mbar_wait_warp(&mma_done, 0, err, kWaitNs);
+    } else {
+        // ------------------------------------------------ copies
+        const int w = warp - 9;
+        int64_t last = -1;
+        const TileCopy<DP> tile(lane, kv.dim);
+        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
+            // the third takes the keys, and the lse2 of all rows (those past the end are masked)
+            if (w == 2) {
+                if (n > 0 && !mbar_wait_warp(&k_empty, (n - 1) & 1, err, kWaitNs)) break;
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t dst = base + t * C::kTileBytes;
+                    const int key0 = it.k0 + t * kCM;
+                    const bool whole = a.box && key0 + kCM <= it.len, mine = whole && lane * a.box < kCM;
+                    int page = 0, slot = 0;
+                    const bool there = !mine || kv.place(it.b, key0 + lane * a.box, page, slot);
+                    if (whole && __all_sync(kFull, there)) {
+                        tile.fetch(dst, &k_map, a.box, slot, it.hk, page, &k_full);
+                    } else {
+                        tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
+                            const bool is = key_place(kv, it.b, it.len, key0 + rr, kv.k_page, kv.k_slot, off);
+                            off += it.hk * kv.k_head;
+                            return is;
+                        });
+                        tile.arrive(&k_full);
+                    }
                 }
             }
-            // the first two take tiles of rows in turn, the third the lse2 of all (rows past
-            // the end are masked)
-            for (int i = w == 1 ? 1 : 0; i < nt; i += w < 2 ? 2 : 1) {
+            // the others tiles of rows in turn
+            for (int i = 0; i < it.nt; ++i) {
                 const uint32_t x = g + i;
-                if (x >= kSt && !mbar_wait_warp(&empty[x % kSt], ((x / kSt) & 1) ^ 1, err, kWaitNs)) {
+                if (w < 2 && (int)(x & 1) != w) continue;
+                // (each barrier has one warp that waits for it, which it then is never two phases
+                // ahead of)
+                uint64_t *const place = w == 2 ? &shift_empty[x % kShifts] : &empty[x % kSt];
+                const uint32_t round = w == 2 ? x / kShifts : x / kSt;
+                if (round > 0 && !mbar_wait_warp(place, (round & 1) ^ 1, err, kWaitNs)) {
                     ok = false;
                     break;
                 }
-                const int q0 = r0 + i * kCM;
+                const int q0 = it.r0 + i * kCM;
                 if (w == 2) {
-                    const float *lse2 = j.lse2 + (int64_t)t0 * j.Hq + hk * a.G;
+                    const float *lse2 = j.lse2 + (int64_t)it.t0 * j.Hq + it.hk * a.G;
                     const uint32_t sh = smem_addr(s_shift[x % kShifts]);
 #pragma unroll
                     for (int y = 0; y < kCM / 32; ++y) {
-                        const int rr = 32 * y + lane, r = min(q0 + rr, rows - 1);
+                        const int rr = 32 * y + lane, r = min(q0 + rr, it.rows - 1);
                         uint32_t t, h;
                         a.group.divmod((uint32_t)r, t, h);
                         copy4(sh + 4 * rr, lse2 + (int64_t)t * j.Hq + h, true);
@@ -230,30 +289,33 @@ __global__ void __launch_bounds__(kCThreads, 1)
                     continue;
                 }
                 const uint32_t dst = ring + (x % kSt) * C::kTileBytes;
+                last = x;
                 if (a.q_box) {
                     if (lane == 0) {
                         mbar_arrive_tx(&full[x % kSt], C::kTileBytes);
 #pragma unroll
                         for (int s = 0; s < C::kSlabs; ++s)
-                            tma_load_3d(dst + s * C::kSlab, &q_map, 64 * s, hk * a.G, t0 + q0 / a.G, &full[x % kSt]);
+                            tma_load_3d(dst + s * C::kSlab, &q_map, 64 * s, it.hk * a.G, it.t0 + q0 / a.G, &full[x % kSt]);
                     }
                     __syncwarp();
                 } else {
                     tile.copy(dst, static_cast<const char *>(j.q), [&](int rr, int64_t &off) {
                         uint32_t t, h;
                         a.group.divmod((uint32_t)(q0 + rr), t, h);
-                        off = (int64_t)(t0 + (int)t) * j.q_token + (int64_t)(hk * a.G + (int)h) * j.q_head;
-                        return q0 + rr < rows;
+                        off = (int64_t)(it.t0 + (int)t) * j.q_token + (int64_t)(it.hk * a.G + (int)h) * j.q_head;
+                        return q0 + rr < it.rows;
                     });
                     tile.arrive(&full[x % kSt]);
                 }
             }
-            copy_wait<0>();
         }
-        g += (uint32_t)nt;
-        loaded += nt > 0;
-        ok = __syncthreads_and(ok);
-        if (!ok) break;
+        copy_wait<0>();
+        // copies in flight complete before the CTA may exit: of this warp's tiles the last
+        // two, whose places nothing has filled since
+        static_assert(kSt == 4, "every second tile, two of a round");
+        for (int64_t y = last; w < 2 && y >= 0 && y > last - 4; y -= 2)
+            mbar_wait_warp(&full[y % kSt], (uint32_t)(y / kSt) & 1, err, kWaitNs);
+        if (w == 2 && n > 0) mbar_wait_warp(&k_full, (n - 1) & 1, err, kWaitNs);
     }
     tc_fence_before();
     __syncthreads();
