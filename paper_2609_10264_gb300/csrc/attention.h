@@ -28,7 +28,7 @@ struct AttendJob {
     const void *q;
     void *out;
     float *lse;                              // may be null
-    float *lse2;                             // scratch: log2 of the rows' sums (see row_sum), may be null
+    float *lse2;                             // scratch: -log2 of the rows' sums (see row_sum), may be null
     int64_t q_token, q_head, o_token, o_head;  // bytes
     int Hq, window, type, max_new;           // window 0: none
     int few_rows;                            // see launch_attention_few

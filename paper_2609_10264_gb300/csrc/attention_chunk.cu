@@ -66,37 +66,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(idesc), "r"(acc)
         : "memory");
 }
-// ---------------------------------------------------------------- pairs of 32-bit values
-// (half the instructions of the softmax's multiply-adds and sums)
-__device__ __forceinline__ uint64_t pair(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void unpair(uint64_t v, float &x, float &y) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-
-// A row's log2 of its sum.  The scratch copy, which scores are compared with, has
-// +infinity for a row that sees nothing.
+// A row's log2 of its sum.  The scratch copy is negative, to be added to scores, and
+// -infinity also for a row that sees nothing.
 __device__ __forceinline__ void row_sum(const AttendJob &j, int64_t row, float lse2) {
     if (j.lse) j.lse[row] = kLn2 * lse2;
-    if (j.lse2) j.lse2[row] = lse2 == -INFINITY ? INFINITY : lse2;
+    if (j.lse2) j.lse2[row] = lse2 == -INFINITY ? lse2 : -lse2;
 }
 
 // ---------------------------------------------------------------- work

@@ -153,13 +153,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
     if (warp < 8) {
         // ------------------------------------------------ sums
         const int tile = warp >> 2;
+        const uint64_t scale_2 = pair(a.scale2, a.scale2);
         const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
         for (; ok && walk.next(a, it); g += (uint32_t)it.nt) {
             const int key = it.k0 + tile * kCM + (warp & 3) * 32 + lane;
             int page, slot;
             const bool real = key < it.len && kv.place(it.b, key, page, slot);
             const int lo = real ? it.first_row(a, key) : 0, hi = real ? it.last_row(a, key) : INT_MAX;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            uint64_t sum[2] = {0u, 0u};
             for (int i = 0; i < it.nt; ++i) {
                 const uint32_t x = g + i;
                 ok = mbar_wait_warp(&shift_full[x % kShifts], (x / kShifts) & 1, err, kWaitNs) &&
@@ -168,38 +169,42 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 tc_fence_after();
                 const int q0 = it.r0 + i * kCM;
                 const bool masked = __any_sync(kFull, q0 < lo || hi - kCM < q0);
-                // half the scores at a time, which leaves registers for all else
+                // a quarter of the scores at a time, the next one on its way
+                float s[2][32];
+                tmem_ld32_async(ts + (x & 1) * kCN, s[0]);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    constexpr int kHalf = kCN / 2;
-                    float s[kHalf];
-                    tmem_ld32_async(ts + (x & 1) * kCN + kHalf * c, s);
-                    tmem_ld32_async(ts + (x & 1) * kCN + kHalf * c + 32, s + 32);
+                for (int c = 0; c < kCN / 32; ++c) {
+                    float *v = s[c & 1];
                     tmem_ld_wait();
-                    if (c == 1) {
+                    if (c + 1 < kCN / 32) {
+                        tmem_ld32_async(ts + (x & 1) * kCN + 32 * (c + 1), s[(c + 1) & 1]);
+                    } else {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&s_empty[tile][x & 1]);
                     }
                     if (masked) {
 #pragma unroll
-                        for (int e = 0; e < kHalf; ++e)
-                            if (q0 + kHalf * c + e < lo || q0 + kHalf * c + e >= hi) s[e] = -INFINITY;
+                        for (int e = 0; e < 32; ++e)
+                            if (q0 + 32 * c + e < lo || q0 + 32 * c + e >= hi) v[e] = -INFINITY;
                     }
-                    const float4 *sh = reinterpret_cast<const float4 *>(s_shift[x % kShifts] + kHalf * c);
+                    const ulonglong2 *sh = reinterpret_cast<const ulonglong2 *>(s_shift[x % kShifts] + 32 * c);
 #pragma unroll
-                    for (int e = 0; e < kHalf; e += 4) {
-                        const float4 z = sh[e / 4];
-                        sum[0] += exp2_fast(fmaf(s[e], a.scale2, -z.x));
-                        sum[1] += exp2_fast(fmaf(s[e + 1], a.scale2, -z.y));
-                        sum[2] += exp2_fast(fmaf(s[e + 2], a.scale2, -z.z));
-                        sum[3] += exp2_fast(fmaf(s[e + 3], a.scale2, -z.w));
+                    for (int e = 0; e < 32; e += 4) {
+                        const ulonglong2 z = sh[e / 4];
+                        float p, q;
+                        unpair(fma2(pair(v[e], v[e + 1]), scale_2, z.x), p, q);
+                        sum[0] = add2(sum[0], pair(exp2_fast(p), exp2_fast(q)));
+                        unpair(fma2(pair(v[e + 2], v[e + 3]), scale_2, z.y), p, q);
+                        sum[1] = add2(sum[1], pair(exp2_fast(p), exp2_fast(q)));
                     }
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&shift_empty[x % kShifts]);
             }
-            if (ok && real) *kv.mass_at(page, slot, it.hk) += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            float p, q;
+            unpair(add2(sum[0], sum[1]), p, q);
+            if (ok && real) *kv.mass_at(page, slot, it.hk) += p + q;
         }
     } else if (warp == 8) {
         // ------------------------------------------------ MMA issuer
