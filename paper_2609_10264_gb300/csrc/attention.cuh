@@ -215,21 +215,38 @@ struct TileCopy {
         }
         copy_commit();
     }
-    // The same from pages, by the tensor memory accelerator: boxes of `box` keys that
-    // lie on one page, a lane each; map: (values, slots, heads, pages).  page: of the
-    // lane's box.
-    __device__ __forceinline__ void fetch(uint32_t dst, const CUtensorMap *map, int box, int slot, int hk, int page,
-                                          uint64_t *bar) const {
+    // The 128 keys from key0 on, all within the sequence, from their pages by the tensor
+    // memory accelerator: boxes of `box` keys that lie on one page, dealt out to the
+    // lanes; map: (values, slots, heads, pages).  False, and nothing done, where a page
+    // is not there.  (The swizzle goes by the address, so boxes of fewer than its eight
+    // rows fit too.)
+    __device__ __forceinline__ bool fetch(uint32_t dst, const CUtensorMap *map, int box, const KvView &kv, int b, int hk,
+                                          int key0, uint64_t *bar) const {
+        int page[kCM / 32], slot[kCM / 32];
+        bool there = true;
+#pragma unroll
+        for (int x = 0; x < kCM / 32; ++x) {
+            page[x] = slot[x] = 0;
+            const int r = (32 * x + lane) * box;
+            if (r < kCM) there &= kv.place(b, key0 + r, page[x], slot[x]);
+        }
+        if (!__all_sync(kFull, there)) return false;
         if (lane == 0) mbar_arrive_tx(bar, DP / 64 * kCM * 128);
         __syncwarp();
-        if (lane * box < kCM)
 #pragma unroll
-            for (int s = 0; s < DP / 64; ++s)
-                asm volatile(
-                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
-                    "%4, %5}], [%6];" ::"r"(dst + s * (kCM * 128) + lane * box * 128),
-                    "l"(reinterpret_cast<uint64_t>(map)), "r"(64 * s), "r"(slot), "r"(hk), "r"(page), "r"(smem_addr(bar))
-                    : "memory");
+        for (int x = 0; x < kCM / 32; ++x) {
+            const int r = (32 * x + lane) * box;
+            if (r < kCM)
+#pragma unroll
+                for (int s = 0; s < DP / 64; ++s)
+                    asm volatile(
+                        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+                        "%4, %5}], [%6];" ::"r"(dst + s * (kCM * 128) + r * 128),
+                        "l"(reinterpret_cast<uint64_t>(map)), "r"(64 * s), "r"(slot[x]), "r"(hk), "r"(page[x]),
+                        "r"(smem_addr(bar))
+                        : "memory");
+        }
+        return true;
     }
     // Once it is all there, for the MMAs.
     __device__ __forceinline__ void arrive(uint64_t *bar) const {
@@ -269,16 +286,19 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *r) {
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 
-// Keys per box: the largest power of two, up to a tile, that divides the page size;
-// of less than 8 (a swizzle's rows) none, and none where a stride is not one that a
-// tensor map can have (64 bits wide, but not negative, nor zero where it is used).
+// Keys per TMA box: the largest power of two, up to a tile, that divides the page size;
+// none where that is less than 4, and none where a stride is not one that a tensor map
+// can have.  (2048 tokens over 8192 keys, 32 heads of 128, us: boxes of 1 key 612, of 2
+// 341, of 4 220, of 8 169, of 64 165; gathered row by row by the loaders, at any page
+// size, 240.)
+constexpr int kLeastBox = 4;
 inline int page_box(const KvView &kv) {
     int box = 1;
     while (box < kCN && kv.ps.d % (2 * box) == 0) box *= 2;
     const int64_t most = (int64_t)1 << 40;
     for (int64_t st : {kv.k_slot, kv.k_head, kv.k_page, kv.v_slot, kv.v_head, kv.v_page})
         if (st <= 0 || st >= most) return 0;
-    return box >= 8 ? box : 0;
+    return box >= kLeastBox ? box : 0;
 }
 // Keys or values as a tensor of (values, slots, heads, pages), for boxes of 64 values
 // x `box` slots.

@@ -383,15 +383,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
                               hs = it.hk * (values ? kv.v_head : kv.k_head);
                 const int key0 = (kt0 + i) * kCN;
                 if (a.box && key0 + kCN <= it.len) {
-                    int page = 0, slot = 0;
-                    const bool is = lane * a.box >= kCN || kv.place(it.b, key0 + lane * a.box, page, slot);
-                    if (__all_sync(kFull, is)) {
-                        if (!values && lane == 0) s_gap[i & 3] = false;
-                        __syncwarp();
-                        tile.fetch(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? &v_map : &k_map, a.box, slot, it.hk,
-                                   page, &kv_full[x % kSt]);
+                    // (before the barrier that the copy itself completes)
+                    if (!values && lane == 0) s_gap[i & 3] = false;
+                    __syncwarp();
+                    if (tile.fetch(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? &v_map : &k_map, a.box, kv, it.b,
+                                   it.hk, key0, &kv_full[x % kSt]))
                         continue;
-                    }
                 }
                 bool gap = false;
                 tile.copy(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? kv.V : kv.K, [&](int rr, int64_t &off) {

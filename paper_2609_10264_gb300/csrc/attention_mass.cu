@@ -252,12 +252,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 for (int t = 0; t < 2; ++t) {
                     const uint32_t dst = base + t * C::kTileBytes;
                     const int key0 = it.k0 + t * kCM;
-                    const bool whole = a.box && key0 + kCM <= it.len, mine = whole && lane * a.box < kCM;
-                    int page = 0, slot = 0;
-                    const bool there = !mine || kv.place(it.b, key0 + lane * a.box, page, slot);
-                    if (whole && __all_sync(kFull, there)) {
-                        tile.fetch(dst, &k_map, a.box, slot, it.hk, page, &k_full);
-                    } else {
+                    if (!a.box || key0 + kCM > it.len ||
+                        !tile.fetch(dst, &k_map, a.box, kv, it.b, it.hk, key0, &k_full)) {
                         tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
                             const bool is = key_place(kv, it.b, it.len, key0 + rr, kv.k_page, kv.k_slot, off);
                             off += it.hk * kv.k_head;
