@@ -36,7 +36,7 @@ constexpr float kCHeadroom = 8.0f;   // log2 of the largest P
 struct ChunkArgs {
     AttendJob j;
     KvView kv;
-    float *part;    // [items][splits][256][DP] normalised partial outputs
+    float4 *part;   // [items][splits][DP / 4][256] normalised partial outputs
     float *stat;    // [items][splits][256] log2 of their sums
     float scale2;   // |scale| log2(e)
     int G, splits, negative;
@@ -200,19 +200,21 @@ __global__ void __launch_bounds__(kCThreads, 1)
             const int k0 = (kt0 + i) * kCN;
             const bool gap = s_gap[i & 3];
             tmem_ld_wait();
-            if (__any_sync(kFull, k0 < lo || k0 + kCN > hi) || gap) {
+            if (__any_sync(kFull, k0 < lo || hi - kCN < k0) || gap) {
 #pragma unroll
                 for (int c = 0; c < kCN / 32; ++c) {
-                    uint32_t there = kFull;
+                    // bits of the keys that this row sees
+                    const int from = lo - k0 - 32 * c, to = hi - k0 - 32 * c;
+                    uint32_t see = to >= 32 ? kFull : to <= 0 ? 0u : (1u << to) - 1u;
+                    if (from > 0) see = from >= 32 ? 0u : see & ~((1u << from) - 1u);
                     if (gap) {
                         const int key = k0 + 32 * c + lane;
                         int page, slot;
-                        there = __ballot_sync(kFull, key < it.len && kv.place(it.b, key, page, slot));
+                        see &= __ballot_sync(kFull, key < it.len && kv.place(it.b, key, page, slot));
                     }
+                    if (__any_sync(kFull, see != kFull)) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int key = k0 + 32 * c + e;
-                        if (key < lo || key >= hi || !(there >> e & 1)) s[32 * c + e] = -INFINITY;
+                        for (int e = 0; e < 32; ++e) s[32 * c + e] = see >> e & 1 ? s[32 * c + e] : -INFINITY;
                     }
                 }
             }
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
             tc_fence_after();
             const int t = it.t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
             const float inv = inverse(m, l), lse2 = m == -INFINITY ? (l != l ? l : m) : m * a.scale2 + log2f(l);
-            const int64_t prow = (it.slot + split) * kCRows + r;
+            const int64_t part = it.slot + split;
             char *orow = static_cast<char *>(j.out) + t * j.o_token + h * j.o_head;
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
@@ -283,7 +285,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 if (it.parts > 1) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4 *>(a.part + prow * DP + 32 * c + e) =
+                        a.part[(part * (DP / 4) + 8 * c + e / 4) * kCRows + r] =
                             make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
                 } else {
 #pragma unroll
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
             }
             if (real) {
                 if (it.parts > 1)
-                    a.stat[prow] = lse2;
+                    a.stat[part * kCRows + r] = lse2;
                 else
                     row_sum(j, (int64_t)t * j.Hq + h, lse2);
             }
@@ -415,24 +417,28 @@ __global__ void __launch_bounds__(kCThreads, 1)
     }
 }
 
-// Items of several splits: their parts, in the order of the keys.  32 rows a CTA.
-constexpr int kJoinRows = 32;
-template <typename T, int DP>
+// Items of several splits: their parts, in the order of the keys.  kJoinRows rows a CTA
+// (8 of many parts, else 32; 19 parts of eight items: 58 us a call, with 32 rows 76; 3
+// parts of eighty 148 and 141); a thread 4 values of a row, eight rows of four such side
+// by side.
+template <typename T, int DP, int kJoinRows>
 __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant__ ChunkArgs a) {
     follow();
     ChunkItem it;
     if (!chunk_item(a, blockIdx.x, it) || it.parts == 1) return;
-    const int r0 = blockIdx.y * kJoinRows, rows = min(kJoinRows, it.rows - r0);
-    for (int id = threadIdx.x; id < rows * (DP / 4); id += kCThreads) {
-        const int r = r0 + id / (DP / 4), d = 4 * (id % (DP / 4));
+    const int r0 = blockIdx.y * kJoinRows;
+    for (int id = threadIdx.x; id < kJoinRows * (DP / 4); id += kCThreads) {
+        const int c4 = (id & 3) | (id / (4 * kJoinRows)) << 2, r = r0 + (id / 4) % kJoinRows;
+        if (r >= it.rows) continue;
         float M = -INFINITY, L = 0.0f;
+#pragma unroll 4
         for (int p = 0; p < it.parts; ++p) M = fmaxf(M, a.stat[(it.slot + p) * kCRows + r]);
         const float ref = M == -INFINITY ? 0.0f : M;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
         for (int p = 0; p < it.parts; ++p) {
-            const int64_t row = (it.slot + p) * kCRows + r;
-            const float e = exp2_fast(a.stat[row] - ref);
-            const float4 x = *reinterpret_cast<const float4 *>(a.part + row * DP + d);
+            const float e = exp2_fast(a.stat[(it.slot + p) * kCRows + r] - ref);
+            const float4 x = a.part[((it.slot + p) * (DP / 4) + c4) * kCRows + r];
             L += e;
             v.x += x.x * e;
             v.y += x.y * e;
@@ -441,10 +447,10 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
         }
         const int t = it.t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
         const float inv = inverse(M, L);
-        if (d < a.kv.dim)
-            *reinterpret_cast<uint2 *>(static_cast<char *>(a.j.out) + t * a.j.o_token + h * a.j.o_head + 2 * d) =
+        if (4 * c4 < a.kv.dim)
+            *reinterpret_cast<uint2 *>(static_cast<char *>(a.j.out) + t * a.j.o_token + h * a.j.o_head + 8 * c4) =
                 make_uint2(pack(v.x * inv, v.y * inv, T{}), pack(v.z * inv, v.w * inv, T{}));
-        if (d == 0) row_sum(a.j, (int64_t)t * a.j.Hq + h, M + log2f(L));
+        if (c4 == 0) row_sum(a.j, (int64_t)t * a.j.Hq + h, M + log2f(L));
     }
 }
 
@@ -466,8 +472,17 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     const int64_t rows = (int64_t)kv.T * a.G;
     const int64_t tiles = rows / kCRows + std::min<int64_t>(kv.B, kv.T), items = tiles * kv.heads;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d, keys = (room + kCN - 1) / kCN;
-    // keys are split where the items alone would leave SMs without work
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(sms / items, keys / 4));
+    // Splits of an item's keys: the number with which all of them would be through first,
+    // in turns of one CTA an SM of as many tiles each and as long as kSetUp tiles beside
+    // them.  (80 items of up to 120 tiles: 171 us whole, with as many splits as SMs
+    // without an item, none; 32 items of 470 tiles want 19.)
+    constexpr int kSetUp = 4, kLeast = 8, kMost = 64;
+    a.splits = 1;
+    int64_t best = INT64_MAX;
+    for (int64_t n = 1; n <= kMost && (n == 1 || n * kLeast <= keys); ++n) {
+        const int64_t cost = (items * n + sms - 1) / sms * ((keys + n - 1) / n + (n > 1 ? kSetUp + 2 : kSetUp));
+        if (cost < best) best = cost, a.splits = (int)n;
+    }
     if (items > INT_MAX) return cudaErrorInvalidValue;
     if (a.splits > 1) {
         auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
@@ -475,7 +490,7 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
         void *buf = nullptr;
         const cudaError_t e = stream_scratch(kScratchAttention, parts + n * sizeof(float), s, &buf);
         if (e != cudaSuccess) return e;
-        a.part = static_cast<float *>(buf);
+        a.part = static_cast<float4 *>(buf);
         a.stat = reinterpret_cast<float *>(static_cast<char *>(buf) + parts);
     }
     CUtensorMap maps[2] = {};
@@ -488,7 +503,9 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     e = launch_dependent(k_chunk<T, DP>, dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s, a,
                          maps[0], maps[1], err);
     if (e == cudaSuccess && a.splits > 1)
-        e = launch_dependent(k_chunk_join<T, DP>, dim3((unsigned)items, kCRows / kJoinRows), kCThreads, 0, s, a);
+        e = a.splits > 8
+                ? launch_dependent(k_chunk_join<T, DP, 8>, dim3((unsigned)items, kCRows / 8), kCThreads, 0, s, a)
+                : launch_dependent(k_chunk_join<T, DP, 32>, dim3((unsigned)items, kCRows / 32), kCThreads, 0, s, a);
     return e;
 }
 
