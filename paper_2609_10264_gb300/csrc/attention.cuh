@@ -147,18 +147,25 @@ __device__ __forceinline__ Found find(int B, Work work, Pos pos, int64_t *list =
 // one before.  (What the dependents of this one read before their own wait is then
 // complete, too.)
 template <typename K, typename... A>
-cudaError_t launch_dependent(K kern, dim3 grid, int threads, size_t smem, cudaStream_t s, const A &...a) {
+cudaError_t launch_cluster(K kern, dim3 grid, int cluster, int threads, size_t smem, cudaStream_t s, const A &...a) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return counted_launch(cudaLaunchKernelEx(&cfg, kern, a...));
+}
+template <typename K, typename... A>
+cudaError_t launch_dependent(K kern, dim3 grid, int threads, size_t smem, cudaStream_t s, const A &...a) {
+    return launch_cluster(kern, grid, 1, threads, smem, s, a...);
 }
 __device__ __forceinline__ void follow() {
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -21,6 +21,8 @@ namespace {
 
 constexpr int kMKeys = 2 * kCM;  // keys per CTA
 constexpr int kShifts = 4;       // ring of the rows' lse2
+constexpr int kMostShare = 8;    // CTAs of a cluster
+constexpr int kSumRegs = 176, kCopyRegs = 144;  // of 168 a thread at launch
 
 struct MassArgs {
     AttendJob j;
@@ -31,6 +33,49 @@ struct MassArgs {
     int box;        // keys per TMA box on a page, 0: none (see page_box)
     bool q_box;     // a tile of rows is a TMA box
 };
+
+// ---------------------------------------------------------------- between the CTAs of a cluster
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t peer_addr(const void *p, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void peer_store(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void peer_arrive(uint32_t addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// A bounded wait that makes what the peers wrote before their arrivals visible.
+__device__ __forceinline__ bool peer_wait(uint64_t *bar, uint32_t parity, uint32_t *err) {
+    const uint64_t t0 = global_ns();
+    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(smem_addr(bar)), "r"(parity)
+            : "memory");
+        if (__all_sync(kFull, ok != 0)) return true;
+        if (__any_sync(kFull, global_ns() - t0 > kWaitNs)) break;
+    }
+    record_error(err, kErrMmaTimeout);
+    return false;
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 template <int DP>
 struct Mass {
@@ -48,8 +93,8 @@ __device__ __forceinline__ int mass_shares(const MassArgs &a, int b) {
     return many_rows(a.kv, a.j.few_rows, a.G, b) ? (a.kv.len(b) - mass_first(a, b) + kMKeys - 1) / kMKeys : 0;
 }
 
-// Keys [k0, k0 + kMKeys) of a sequence and key head, and the tiles of rows that see any
-// of them: nt from row r0 on.
+// Keys [k0, k0 + kMKeys) of a sequence and key head, and this CTA's share of the tiles of
+// rows that see any of them: nt from row r0 on, which may be none.
 struct MassItem {
     int b, hk, k0, len, old, n, rows, t0, r0, nt;
     // the rows that see a key: [first, last)
@@ -61,13 +106,13 @@ struct MassItem {
         return t >= n ? rows : t <= 0 ? 0 : (int)t * a.G;
     }
 };
-// A CTA's items in order: every gridDim.x-th of all (shares of keys and their heads).
+// A cluster's items in order: every stride-th of all (shares of keys and their heads).
 struct MassWalk {
     int64_t idx, before;  // the next item, and the shares before sequence b
-    int b;
+    int b, stride, rank, size;
     __device__ __forceinline__ bool next(const MassArgs &a, MassItem &it) {
         const KvView &kv = a.kv;
-        for (;; idx += gridDim.x) {
+        for (;; idx += stride) {
             const int64_t share = idx / kv.heads;
             for (; b < kv.B; ++b) {
                 const int n = mass_shares(a, b);
@@ -85,9 +130,12 @@ struct MassWalk {
             it.k0 = mass_first(a, b) + (int)(share - before) * kMKeys;
             it.r0 = it.first_row(a, it.k0) / kCM * kCM;
             const int r1 = it.last_row(a, min(it.k0 + kMKeys, it.len) - 1);
-            it.nt = r1 > it.r0 ? (r1 - it.r0 + kCM - 1) / kCM : 0;
-            if (it.nt == 0) continue;
-            idx += gridDim.x;
+            const int all = r1 > it.r0 ? (r1 - it.r0 + kCM - 1) / kCM : 0;
+            if (all == 0) continue;
+            const int per = (all + size - 1) / size, from = min(all, rank * per);
+            it.r0 += from * kCM;
+            it.nt = min(all, from + per) - from;
+            idx += stride;
             return true;
         }
     }
@@ -103,6 +151,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
     __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full, k_empty, mma_done;
     __shared__ __align__(8) uint64_t shift_full[kShifts], shift_empty[kShifts];
     __shared__ __align__(16) float s_shift[kShifts][kCM];
+    // the sums of the cluster's other CTAs, in the first one's memory
+    __shared__ float s_sums[kMostShare - 1][kMKeys];
+    __shared__ __align__(8) uint64_t sums_full, sums_empty;
     __shared__ uint32_t s_tmem;
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
@@ -127,6 +178,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
             mbar_init(&shift_empty[s], 8);
         }
         mbar_init(&mma_done, 1);
+        mbar_init(&sums_full, 8 * max(1, (int)cluster_size() - 1));
+        mbar_init(&sums_empty, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8) {
@@ -135,15 +188,17 @@ __global__ void __launch_bounds__(kCThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
+    cluster_meet();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
+    const int size = (int)cluster_size(), rank = (int)cluster_rank(), mine = (int)blockIdx.x / size;
     const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
-                                    [&](int64_t) { return (int64_t)blockIdx.x / kv.heads; });
-    MassWalk walk{(int64_t)blockIdx.x, f.before, f.b < 0 ? kv.B : f.b};
+                                    [&](int64_t) { return (int64_t)mine / kv.heads; });
+    MassWalk walk{(int64_t)mine, f.before, f.b < 0 ? kv.B : f.b, (int)gridDim.x / size, rank, size};
     if (warp < 8)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCSoftRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
     else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCOtherRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
 
     // Every role walks the CTA's items by itself, as far ahead as the barriers let it: a
     // tile of rows is number g + i of all the CTA's, an item of keys number n.
@@ -155,7 +210,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         const int tile = warp >> 2;
         const uint64_t scale_2 = pair(a.scale2, a.scale2);
         const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
-        for (; ok && walk.next(a, it); g += (uint32_t)it.nt) {
+        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
             const int key = it.k0 + tile * kCM + (warp & 3) * 32 + lane;
             int page, slot;
             const bool real = key < it.len && kv.place(it.b, key, page, slot);
@@ -204,12 +259,28 @@ __global__ void __launch_bounds__(kCThreads, 1)
             }
             float p, q;
             unpair(add2(sum[0], sum[1]), p, q);
-            if (ok && real) *kv.mass_at(page, slot, it.hk) += p + q;
+            p += q;
+            if (!ok) break;
+            if (rank > 0) {  // to the first, once it has taken the item before
+                if (n > 0 && !peer_wait(&sums_empty, (n - 1) & 1, err)) break;
+                peer_store(peer_addr(&s_sums[rank - 1][tid], 0), p);
+                __syncwarp();
+                if (lane == 0) peer_arrive(peer_addr(&sums_full, 0));
+                continue;
+            }
+            if (size > 1) {
+                if (!peer_wait(&sums_full, n & 1, err)) break;
+                for (int r = 1; r < size; ++r) p += s_sums[r - 1][tid];
+                __syncwarp();
+                if (lane < size - 1) peer_arrive(peer_addr(&sums_empty, (uint32_t)lane + 1));
+            }
+            if (real) *kv.mass_at(page, slot, it.hk) += p;
         }
     } else if (warp == 8) {
         // ------------------------------------------------ MMA issuer
         const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
-        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
+        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, n += it.nt > 0) {
+            if (it.nt == 0) continue;
             ok = mbar_wait_warp(&k_full, n & 1, err, kWaitNs);
             for (int i = 0; i < it.nt && ok; ++i) {
                 const uint32_t x = g + i;
@@ -245,7 +316,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
         const int w = warp - 9;
         int64_t last = -1;
         const TileCopy<DP> tile(lane, kv.dim);
-        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
+        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, n += it.nt > 0) {
+            if (it.nt == 0) continue;
             // the third takes the keys, and the lse2 of all rows (those past the end are masked)
             if (w == 2) {
                 if (n > 0 && !mbar_wait_warp(&k_empty, (n - 1) & 1, err, kWaitNs)) break;
@@ -320,6 +392,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
+    cluster_meet();  // no peer's store or arrival is on its way here
     if (warp == 8) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -363,11 +436,20 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
     const int64_t items = (int64_t)kv.B * kv.heads * ((room + kMKeys - 1) / kMKeys);
+    const int64_t tiles = ((int64_t)kv.max_new * a.G + kCM - 1) / kCM;
+    // CTAs of a cluster: as many as let all be through first, in turns of items with as
+    // many tiles of rows each, and as long as three beside them (four with peers)
+    int share = 1;
+    int64_t best = INT64_MAX;
+    for (int n = 1; n <= kMostShare; n *= 2) {
+        const int64_t at = std::max(1, sms / n), cost = (items + at - 1) / at * ((tiles + n - 1) / n + (n > 1 ? 4 : 3));
+        if (cost < best) best = cost, share = n;
+    }
     const cudaError_t e = func_attr(reinterpret_cast<const void *>(k_mass<T, DP>),
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, Mass<DP>::kSmem);
     if (e != cudaSuccess) return e;
-    return launch_dependent(k_mass<T, DP>, dim3((unsigned)std::min<int64_t>(items, sms)), kCThreads, Mass<DP>::kSmem, s, a,
-                            maps[0], maps[1], err);
+    const unsigned grid = (unsigned)(std::min<int64_t>(items, std::max(1, sms / share)) * share);
+    return launch_cluster(k_mass<T, DP>, dim3(grid), share, kCThreads, Mass<DP>::kSmem, s, a, maps[0], maps[1], err);
 }
 
 }  // namespace
