@@ -468,9 +468,10 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     int dev = 0, sms = 0;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    // at most as many row tiles as full ones and one more for each sequence of any
+    // at most as many row tiles as full ones and one more for each sequence that can have
+    // more rows than the kernel of few takes
     const int64_t rows = (int64_t)kv.T * a.G;
-    const int64_t tiles = rows / kCRows + std::min<int64_t>(kv.B, kv.T), items = tiles * kv.heads;
+    const int64_t tiles = rows / kCRows + std::min<int64_t>(kv.B, rows / (j.few_rows + 1)), items = tiles * kv.heads;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d, keys = (room + kCN - 1) / kCN;
     // Splits of an item's keys: the number with which all of them would be through first,
     // in turns of one CTA an SM of as many tiles each and as long as kSetUp tiles beside

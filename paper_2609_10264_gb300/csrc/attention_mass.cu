@@ -107,6 +107,7 @@ struct MassItem {
     }
 };
 // A cluster's items in order: every stride-th of all (shares of keys and their heads).
+// By whole warps.
 struct MassWalk {
     int64_t idx, before;  // the next item, and the shares before sequence b
     int b, stride, rank, size;
@@ -114,10 +115,20 @@ struct MassWalk {
         const KvView &kv = a.kv;
         for (;; idx += stride) {
             const int64_t share = idx / kv.heads;
-            for (; b < kv.B; ++b) {
-                const int n = mass_shares(a, b);
-                if (share < before + n) break;
-                before += n;
+            // the sequence that holds it, 32 at a time
+            while (b < kv.B && share >= before + mass_shares(a, b)) {
+                const int lane = threadIdx.x & 31;
+                const int64_t n = b + lane < kv.B ? mass_shares(a, b + lane) : 0;
+                int64_t incl = n;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t v = __shfl_up_sync(kFull, incl, o);
+                    if (lane >= o) incl += v;
+                }
+                const unsigned at = __ballot_sync(kFull, share < before + incl);
+                const int to = at ? __ffs(at) - 1 : 32;
+                before += at ? __shfl_sync(kFull, incl - n, to) : __shfl_sync(kFull, incl, 31);
+                b += to;
             }
             if (b >= kv.B) return false;
             it.b = b;
