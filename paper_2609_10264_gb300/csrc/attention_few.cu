@@ -1,13 +1,13 @@
 // Attention of sequences with few new rows (new tokens x query heads of a key head):
 // single generated tokens above all.  Bound by the reading of K and V.
 //
-// Work.  The keys of a (sequence, key head) come in tiles of 64.  All tiles of all
+// Work.  The keys of a (sequence, key head) come in tiles of 64 or 128.  All tiles of all
 // of them, one after the other, are dealt out evenly to the CTAs, whatever the
 // sequences' lengths: CTA c of C takes tiles [N c / C, N (c + 1) / C).  A sequence
 // that one CTA has whole is finished there; parts go to scratch as (maximum, sum,
 // unnormalised output), and k_few_finish puts them together in order.
 //
-// A warp takes 16 of a tile's 64 keys through its own ring of asynchronous copies
+// A warp takes a quarter of a tile's keys through its own ring of asynchronous copies
 // and keeps its own running maximum and sum, so that nothing but the end of a
 // sequence waits for another warp.  Both products are m16n8k16 MMAs with the rows
 // padded to 16 (tcgen05 would pad them to 128, and its operands would all pass
@@ -23,8 +23,6 @@ namespace {
 
 constexpr int kFewWarps = 4;
 constexpr int kFewThreads = 32 * kFewWarps;
-constexpr int kSub = 16;                  // keys per warp and step
-constexpr int kTile = kFewWarps * kSub;   // keys per tile
 constexpr int kRows = 16;                 // rows per tile of them, of one MMA
 
 struct FewArgs {
@@ -34,22 +32,34 @@ struct FewArgs {
     float2 *stat;    // [2 C][kRows] their maximum and sum
     int64_t *before; // [B + 1] work before each sequence, and all of it
     float2 *norm;    // [T][Hq] maximum and 1 / sum, where mass is accumulated
-    float *scores;   // [B][heads][max tiles x 64][rows] where mass is accumulated
+    float *scores;   // [B][heads][max tiles x tile][rows] where mass is accumulated
     int score_rows, max_tiles;  // (rows a multiple of 4)
     float scale2;    // scale x log2(e)
     int G, C;
     bool whole;      // a CTA takes all keys of a row tile
 };
 
+// DP: the head's values in whole MMAs of the columns that are built (64, 96, 128).
 template <int DP>
 struct Few {
-    static constexpr int kStages = DP == 128 ? 3 : 4;
-    static constexpr int kRow = 2 * DP;  // bytes
+    // Keys per warp and step, and steps of the ring: what two CTAs of an SM have room for.
+    // 32 keys take less than two steps of 16 (57 ragged sequences of up to 3481 keys, 8 heads
+    // of 64 in pages of 16, 64, 100 and 1: 47, 45, 49 and 50 us a call where 16 keys in a
+    // ring of six steps took 50, 47, 54 and 59; heads of 96: 68 to 72 where 69 to 78).
+    static constexpr int kSub = DP == 128 ? 16 : 32;
+    static constexpr int kStages = DP == 96 ? 2 : 3;
+    static constexpr int kTile = kFewWarps * kSub;  // keys per tile
+    // bytes of a row; chunks of 16 are swizzled, or rows of 13 chunks where 12 are used:
+    // either way 8 rows' chunks lie in different banks
+    static constexpr int kRow = DP == 96 ? 208 : 2 * DP;
+    static __device__ __forceinline__ int at(int r, int ch) { return r * kRow + ((DP == 96 ? ch : ch ^ (r & 7)) << 4); }
     static constexpr int kHalf = kSub * kRow;
     static constexpr int kStage = 2 * kHalf;
     static constexpr int kRing = kFewWarps * kStages * kStage;
     static constexpr int kSmem = kRing + kRows * kRow;
     static constexpr int kChunks = DP / 8;
+    static constexpr int kWave = 32 / kChunks;  // rows that a warp copies at a time
+    static constexpr int kDeep = DP == 96 ? 3 : 4;  // MMAs' operands that are read ahead
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -86,12 +96,16 @@ __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &
 }
 // ---------------------------------------------------------------- work
 // One sequence's share: of each key head and tile of kRows rows, `tiles` tiles of keys
-// from key `first` on, dealt out in `units`.
+// from key `first` on, dealt out in `units`: the tiles, behind kSetUp empty units for
+// what a CTA does before and after them (57 sequences of 70 to 3481 keys, 8 heads of 64:
+// 45 us a call where 58 without, when one CTA had several short ones).
+constexpr int kSetUp = 3;
 struct Share {
     int len, n, row0;  // cached and new tokens, the first of these
     int rows, rts, first, tiles, units;
     int64_t work;  // units of all
 };
+template <int kTile>
 __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     Share s;
     s.row0 = a.kv.first(b);
@@ -101,7 +115,7 @@ __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     s.rts = (s.rows + kRows - 1) / kRows;
     s.first = a.j.window > 0 ? max(0, s.len - s.n - a.j.window + 1) / kTile * kTile : 0;
     s.tiles = max(1, (s.len - s.first + kTile - 1) / kTile);
-    s.units = a.whole ? 1 : s.tiles;
+    s.units = a.whole ? 1 : kSetUp + s.tiles;
     s.work = s.rows <= 0 || s.rows > a.j.few_rows ? 0 : (int64_t)s.units * a.kv.heads * s.rts;
     return s;
 }
@@ -121,6 +135,7 @@ __device__ __forceinline__ void put_row(const FewArgs &a, int row0, int hk, int 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ FewArgs a) {
     using F = Few<DP>;
+    constexpr int kSub = F::kSub, kTile = F::kTile;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float2 s_stat[kFewWarps][kRows];
     const AttendJob &j = a.j;
@@ -128,7 +143,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, grp = lane >> 2;
     follow();
     const Found f = find<kFewThreads>(
-        kv.B, [&](int b) { return share(a, b).work; },
+        kv.B, [&](int b) { return share<F::kTile>(a, b).work; },
         [&](int64_t total) {
             const int64_t C = min((int64_t)a.C, total);
             return (int64_t)blockIdx.x < C ? total * blockIdx.x / C : -1;
@@ -139,25 +154,28 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
     const int64_t p1 = f.total * (blockIdx.x + 1) / C;
     int64_t p = f.total * blockIdx.x / C, done = f.before;
     int b = f.b;
-    Share sh = share(a, b);
+    Share sh = share<F::kTile>(a, b);
     const uint32_t ring = smem_addr(smem) + warp * F::kStages * F::kStage, qs = smem_addr(smem) + F::kRing;
-    const bool one_page = kv.ps.d % kSub == 0;
+    const bool one_page = kv.ps.d % 16 == 0;  // for 16 keys
     const int chunks = kv.dim / 8;
 
     while (p < p1) {
         while (p >= done + sh.work) {
             done += sh.work;
-            sh = share(a, ++b);
+            sh = share<F::kTile>(a, ++b);
         }
-        const int item = (int)((p - done) / sh.units), t0 = (int)((p - done) % sh.units);
-        const int nt = a.whole ? sh.tiles : (int)min((int64_t)(sh.tiles - t0), p1 - p);
+        const int item = (int)((p - done) / sh.units), u0 = (int)((p - done) % sh.units);
+        const int units = a.whole ? 1 : (int)min((int64_t)(sh.units - u0), p1 - p);
+        p += units;
+        const int t0 = a.whole ? 0 : max(0, u0 - kSetUp), nt = a.whole ? sh.tiles : u0 + units - kSetUp - t0;
+        if (nt <= 0) continue;
         const int hk = item / sh.rts, r0 = item % sh.rts * kRows, rows = min(kRows, sh.rows - r0);
         const int len = sh.len, n = sh.n, row0 = sh.row0;
         // ---- this warp's step i: keys from key0(i) on
         auto key0 = [&](int i) { return sh.first + (t0 + i) * kTile + warp * kSub; };
         int pages[F::kStages];  // of the steps to be loaded next, a lane a key
         auto fetch_page = [&](int i) {
-            const int k = key0(i) + (one_page ? 0 : lane & 15);
+            const int k = key0(i) + (lane & (kSub - 1));
 #pragma unroll
             for (int s = 0; s + 1 < F::kStages; ++s) pages[s] = pages[s + 1];
             pages[F::kStages - 1] = -1;
@@ -167,38 +185,39 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                 pages[F::kStages - 1] = kv.table[b * kv.table_stride + q];
             }
         };
-        uint64_t seen = 0;  // of the steps loaded last, 16 bits each: the keys that are there
+        unsigned seen[F::kStages] = {};  // of the steps loaded last: the keys that are there
         auto load = [&](int i) {  // step i's copies (its pages have been fetched)
             unsigned there = 0;
             const int page = pages[0];
             if (i < nt) {
                 const int k0 = key0(i), ch = lane % F::kChunks, sub = lane / F::kChunks;
-                const bool mine = (one_page || lane < kSub) && page >= 0 && page < kv.pages &&
-                                  k0 + (lane & 15) < len;
-                there = __ballot_sync(kFull, mine) & 0xffffu;
-                uint32_t d = ring + (i % F::kStages) * F::kStage + sub * F::kRow, q, o;
-                kv.ps.divmod((uint32_t)(k0 + sub), q, o);
-                const char *ks = kv.K + page * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
-                const char *vs = kv.V + page * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
+                const bool mine = page >= 0 && page < kv.pages && k0 + (lane & (kSub - 1)) < len;
+                there = __ballot_sync(kFull, mine);
+                const uint32_t st = ring + (i % F::kStages) * F::kStage;
+                const char *ks = nullptr, *vs = nullptr;
                 // a row's chunks by neighbouring lanes; rows of K, and of V behind them
 #pragma unroll
-                for (int u = 0; u < kSub * F::kChunks / 32; ++u) {
-                    const int r = u * (32 / F::kChunks) + sub;
-                    if (!one_page) {
+                for (int u = 0; u < kSub / F::kWave; ++u) {
+                    const int r = u * F::kWave + sub;
+                    if (!one_page || u % (16 / F::kWave) == 0) {
                         const int pg = __shfl_sync(kFull, page, r);
+                        uint32_t q, o;
                         kv.ps.divmod((uint32_t)(k0 + r), q, o);
                         ks = kv.K + pg * kv.k_page + o * kv.k_slot + hk * kv.k_head + ch * 16;
                         vs = kv.V + pg * kv.v_page + o * kv.v_slot + hk * kv.v_head + ch * 16;
                     }
                     const bool real = (there >> r & 1) && ch < chunks;
-                    copy16(d + ((ch ^ (r & 7)) << 4), real ? ks : kv.K, real);
-                    copy16(d + F::kHalf + ((ch ^ (r & 7)) << 4), real ? vs : kv.V, real);
-                    ks += (32 / F::kChunks) * kv.k_slot;
-                    vs += (32 / F::kChunks) * kv.v_slot;
-                    d += (32 / F::kChunks) * F::kRow;
+                    if (sub < F::kWave) {
+                        copy16(st + F::at(r, ch), real ? ks : kv.K, real);
+                        copy16(st + F::kHalf + F::at(r, ch), real ? vs : kv.V, real);
+                    }
+                    ks += F::kWave * kv.k_slot;
+                    vs += F::kWave * kv.v_slot;
                 }
             }
-            seen = seen << 16 | there;
+#pragma unroll
+            for (int s = 0; s + 1 < F::kStages; ++s) seen[s] = seen[s + 1];
+            seen[F::kStages - 1] = there;
             copy_commit();
         };
 #pragma unroll
@@ -210,7 +229,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             const char *src = static_cast<const char *>(j.q);
             if (real)
                 src += (int64_t)(row0 + (r0 + r) / a.G) * j.q_token + (int64_t)(hk * a.G + (r0 + r) % a.G) * j.q_head + ch * 16;
-            copy16(qs + r * F::kRow + ((ch ^ (r & 7)) << 4), src, real);
+            copy16(qs + F::at(r, ch), src, real);
         }
         copy_commit();
 #pragma unroll
@@ -224,16 +243,19 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
             const int r = lane & 15, ch = 2 * k + (lane >> 4);
-            ldsm4(qs + r * F::kRow + ((ch ^ (r & 7)) << 4), qf[k]);
+            ldsm4(qs + F::at(r, ch), qf[k]);
         }
         // keys that rows grp and grp + 8 see
         int lo[2], hi[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = grp + 8 * h, at = len - n + (r0 + r) / a.G;
-            hi[h] = r < rows ? (j.causal ? min(len, at + 1) : len) : 0;
-            lo[h] = j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
+            hi[h] = r < rows && j.causal ? min(len, at + 1) : len;
+            lo[h] = r < rows && j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
         }
+        // keys that all of them see
+        const int all_lo = __reduce_max_sync(kFull, max(lo[0], lo[1]));
+        const int all_hi = __reduce_min_sync(kFull, min(hi[0], hi[1]));
         float o[DP / 8][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
         for (int i = 0; i < nt; ++i) {
             copy_wait<F::kStages - 2>();
@@ -243,42 +265,50 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             const uint32_t st = ring + (i % F::kStages) * F::kStage;
             const int k0 = key0(i);
             if (k0 >= len) continue;  // the same for the whole warp
-            const unsigned there = (unsigned)(seen >> 16 * (F::kStages - 1)) & 0xffffu;
-            // two sums a tile of 8 keys, so that the MMAs wait less for one another
-            float s[2][4] = {}, s1[2][4] = {};
+            const unsigned there = seen[0];
+            constexpr int kEights = kSub / 8;
+            // two sums of 8 keys where these are few, so that the MMAs wait less for one another
+            constexpr int kSums = kEights == 2 ? 2 : 1;
+            float s[kEights][4], sums[kSums][kEights][4] = {};
 #pragma unroll
-            for (int k = 0; k < DP / 16; k += 4) {
-                uint32_t kf[4][4];
-                const int r = (lane & 7) + ((lane >> 4) << 3);
+            for (int k = 0; k < DP / 16; k += F::kDeep) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int ch = 2 * (k + u) + ((lane >> 3) & 1);
-                    ldsm4(st + r * F::kRow + ((ch ^ (r & 7)) << 4), kf[u]);
-                }
+                for (int t = 0; t < kEights; t += 2) {
+                    uint32_t kf[F::kDeep][4];
+                    const int r = 8 * t + (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    mma<T>(u & 1 ? s1[0] : s[0], qf[k + u], kf[u][0], kf[u][1]);
-                    mma<T>(u & 1 ? s1[1] : s[1], qf[k + u], kf[u][2], kf[u][3]);
+                    for (int u = 0; u < F::kDeep; ++u) ldsm4(st + F::at(r, 2 * (k + u) + ((lane >> 3) & 1)), kf[u]);
+#pragma unroll
+                    for (int u = 0; u < F::kDeep; ++u) {
+                        mma<T>(sums[u % kSums][t], qf[k + u], kf[u][0], kf[u][1]);
+                        mma<T>(sums[u % kSums][t + 1], qf[k + u], kf[u][2], kf[u][3]);
+                    }
                 }
             }
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kEights; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] += s1[t][e];
+                for (int e = 0; e < 4; ++e)
+                    s[t][e] = (kSums == 2 ? sums[0][t][e] + sums[kSums - 1][t][e] : sums[0][t][e]) * a.scale2;
+            if (there != (unsigned)((1ull << kSub) - 1) || k0 < all_lo || k0 + kSub > all_hi) {
+#pragma unroll
+                for (int t = 0; t < kEights; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at = 8 * t + 2 * quad + (e & 1), key = k0 + at, h = e >> 1;
+                        if (!(key >= lo[h] && key < hi[h] && (there >> at & 1))) s[t][e] = -INFINITY;
+                    }
+            }
             float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kEights; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i16 = 8 * t + 2 * quad + (e & 1), key = k0 + i16, h = e >> 1;
-                    s[t][e] = key >= lo[h] && key < hi[h] && (there >> i16 & 1) ? s[t][e] * a.scale2 : -INFINITY;
-                    mx[h] = fmaxf(mx[h], s[t][e]);
-                }
+                for (int e = 0; e < 4; ++e) mx[e >> 1] = fmaxf(mx[e >> 1], s[t][e]);
             if (a.scores) {
                 float *sc =
                     a.scores + (((int64_t)b * kv.heads + hk) * a.max_tiles * kTile + k0 - sh.first) * a.score_rows + r0;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < kEights; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = 8 * t + 2 * quad + (e & 1), r = grp + 8 * (e >> 1);
@@ -309,31 +339,31 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
                     for (int e = 0; e < 4; ++e) o[d][e] *= w[e >> 1];
             }
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kEights; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[t][e] = exp2_fast(s[t][e] - shift[e >> 1]);
                     l[e >> 1] += s[t][e];
                 }
-            uint32_t ph[4], pl[4];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                split<T>(s[t][0], s[t][1], ph[2 * t], pl[2 * t]);
-                split<T>(s[t][2], s[t][3], ph[2 * t + 1], pl[2 * t + 1]);
-            }
+            for (int g = 0; g < kSub / 16; ++g) {
+                uint32_t ph[4], pl[4];
 #pragma unroll
-            for (int d = 0; d < DP / 16; d += 2) {
-                uint32_t vf[2][4];
-                const int r = lane & 15;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int ch = 2 * (d + u) + (lane >> 4);
-                    ldsm4_t(st + F::kHalf + r * F::kRow + ((ch ^ (r & 7)) << 4), vf[u]);
+                for (int t = 0; t < 2; ++t) {
+                    split<T>(s[2 * g + t][0], s[2 * g + t][1], ph[2 * t], pl[2 * t]);
+                    split<T>(s[2 * g + t][2], s[2 * g + t][3], ph[2 * t + 1], pl[2 * t + 1]);
                 }
 #pragma unroll
-                for (int u = 0; u < 4; ++u) mma<T>(o[2 * d + u], ph, vf[u / 2][2 * (u & 1)], vf[u / 2][2 * (u & 1) + 1]);
+                for (int d = 0; d < DP / 16; d += 2) {
+                    uint32_t vf[2][4];
+                    const int r = 16 * g + (lane & 15);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) mma<T>(o[2 * d + u], pl, vf[u / 2][2 * (u & 1)], vf[u / 2][2 * (u & 1) + 1]);
+                    for (int u = 0; u < 2; ++u) ldsm4_t(st + F::kHalf + F::at(r, 2 * (d + u) + (lane >> 4)), vf[u]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) mma<T>(o[2 * d + u], ph, vf[u / 2][2 * (u & 1)], vf[u / 2][2 * (u & 1) + 1]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) mma<T>(o[2 * d + u], pl, vf[u / 2][2 * (u & 1)], vf[u / 2][2 * (u & 1) + 1]);
+                }
             }
         }
         copy_wait<0>();
@@ -388,7 +418,6 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
             }
         }
         __syncthreads();
-        p += a.whole ? 1 : nt;
     }
 }
 
@@ -401,19 +430,20 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 constexpr int kMassKeys = 1024;
 template <typename T, int DP, int kFinThreads>
 __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constant__ FewArgs a) {
+    constexpr int kTile = Few<DP>::kTile;
     __shared__ float2 s_norm[kFewRowsWhole];
     extern __shared__ __align__(16) float s_weight[];  // [rows][parts], then the groups' sums
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
     follow();
-    const Share sh = share(a, b);
+    const Share sh = share<kTile>(a, b);
     const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
     const bool idle = !sh.work || (blockIdx.x > 0 ? first >= len : a.whole);
     if (idle) return;
     const int64_t total = a.before[kv.B], C = min((int64_t)a.C, total);
     const int64_t i0 = a.before[b] + (int64_t)hk * sh.units, i1 = i0 + sh.units;
-    const int c0 = owner(i0, total, C), c1 = a.whole ? c0 : owner(i1 - 1, total, C);  // the CTAs that had parts
+    const int c0 = owner(a.whole ? i0 : i0 + kSetUp, total, C), c1 = a.whole ? c0 : owner(i1 - 1, total, C);  // the CTAs that had parts
     const int row0 = sh.row0;
     auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows; };
     if (blockIdx.x == 0) {
@@ -531,6 +561,7 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     a.C = few_ctas();
     a.scale2 = j.scale * kLog2e;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
+    constexpr int kTile = Few<DP>::kTile;
     a.max_tiles = (int)((room + kTile - 1) / kTile);
     a.score_rows = (int)std::min<int64_t>(j.few_rows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
     a.whole = room <= kFewWholeKeys;
@@ -569,8 +600,10 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
-    if (j.type == PVMVMD_BF16) return kv.dim <= 64 ? few<__nv_bfloat16, 64>(j, kv, s) : few<__nv_bfloat16, 128>(j, kv, s);
-    return kv.dim <= 64 ? few<__half, 64>(j, kv, s) : few<__half, 128>(j, kv, s);
+    const bool bf = j.type == PVMVMD_BF16;
+    if (kv.dim <= 64) return bf ? few<__nv_bfloat16, 64>(j, kv, s) : few<__half, 64>(j, kv, s);
+    if (kv.dim <= 96) return bf ? few<__nv_bfloat16, 96>(j, kv, s) : few<__half, 96>(j, kv, s);
+    return bf ? few<__nv_bfloat16, 128>(j, kv, s) : few<__half, 128>(j, kv, s);
 }
 
 }  // namespace pv
