@@ -466,7 +466,8 @@ int pvmvmd_kv_append(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, c
  * A row that sees nothing gives out = 0 and lse = -infinity (a sequence may be
  * shorter than its new tokens: those in front of its start see nothing).  With
  * accumulate, exp(s_j - lse) of all rows is added to the mass of the keys they see;
- * the sums are formed in an order that does not change from call to call.
+ * the sums are formed in an order that does not change from call to call, and
+ * sequences must then not share pages (as they may without).
  * Hq a multiple of pool->heads; q and out of the pool's type, on 16-byte boundaries,
  * strides multiples of 8; lse_dev float [T][Hq] or null.  What lies behind a
  * sequence's end and on pages of others is not used, whatever it holds.  A key that

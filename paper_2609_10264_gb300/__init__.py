@@ -824,8 +824,8 @@ def pvmvmd_kv_append(pool: KvPool, batch: KvBatch, k, v, positions=None, rope: R
 def pvmvmd_paged_attention(pool: KvPool, batch: KvBatch, q, out=None, lse=None, scale: float | None = None,
                            causal: bool = True, window: int = 0, accumulate: bool = False, stream=None):
     """Attention of the new tokens' q (T x Hq x dim, the pool's type) over the cache -> out (T x Hq x dim).  lse: a
-    float32 T x Hq tensor to fill; accumulate: add the attention weights to the pool's mass; scale: default
-    dim^-1/2."""
+    float32 T x Hq tensor to fill; accumulate: add the attention weights to the pool's mass (sequences must then not
+    share pages); scale: default dim^-1/2."""
     if q.dim() != 3:
         raise ValueError("q must be T x Hq x dim")
     T, Hq, D = q.shape[0], q.shape[1], pool.dim

@@ -16,11 +16,14 @@ cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_
     const int G = j.Hq / kv.heads;
     j.few_rows = (int64_t)kv.max_pages * kv.ps.d <= kFewWholeKeys ? kFewRowsWhole : kFewRows;
     const bool one = kv.B == 1;  // which has all the new tokens
+    bool few = false, joined = false;
     if (G > j.few_rows)
         j.few_rows = 0;
     else if (!(one && (int64_t)kv.T * G > j.few_rows)) {
         const cudaError_t e = launch_attention_few(j, kv, s);
-        if (e != cudaSuccess || one || j.max_new <= j.few_rows / G) return e;
+        if (e != cudaSuccess) return e;
+        if (one || j.max_new <= j.few_rows / G) return launch_attention_few_finish(j, kv, s);
+        few = true;
     }
     if (j.accumulate) {
         void *p = nullptr;
@@ -28,8 +31,17 @@ cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_
         if (e != cudaSuccess) return e;
         j.lse2 = static_cast<float *>(p);
     }
-    const cudaError_t e = launch_attention_chunk(j, kv, s);
-    return e != cudaSuccess || !j.accumulate ? e : launch_attention_mass(j, kv, s);
+    // Where there are both, they run beside one another: the chunks beside the few rows,
+    // the few rows' join beside the chunks', and else beside the mass.  (104 sequences of
+    // 1 to 8 new tokens with mass: XX us a call where XX one after the other.)
+    j.beside = few;
+    cudaError_t e = launch_attention_chunk(j, kv, s, joined);
+    if (e != cudaSuccess) return e;
+    j.beside = joined;
+    if (few) e = launch_attention_few_finish(j, kv, s);
+    if (e != cudaSuccess || !j.accumulate) return e;
+    j.beside = few && !joined;
+    return launch_attention_mass(j, kv, s);
 }
 
 }  // namespace pv

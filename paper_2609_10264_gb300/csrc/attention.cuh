@@ -167,9 +167,16 @@ template <typename K, typename... A>
 cudaError_t launch_dependent(K kern, dim3 grid, int threads, size_t smem, cudaStream_t s, const A &...a) {
     return launch_cluster(kern, grid, 1, threads, smem, s, a...);
 }
-__device__ __forceinline__ void follow() {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+__device__ __forceinline__ void follow(bool beside = false) {
+    if (!beside) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+// A kernel that uses nothing of the one before may run beside it: that one is past its
+// own wait when this one starts, so what came before it is complete.  This one then ends
+// after it, for those that follow (by the first CTA).
+__device__ __forceinline__ void end_after(bool beside) {
+    if (beside && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)
+        asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // ---------------------------------------------------------------- tensor cores

@@ -34,6 +34,7 @@ struct AttendJob {
     int few_rows;                            // see launch_attention_few
     float scale;
     bool causal, accumulate;
+    bool beside;  // the kernel before is of the same call, and of other sequences
 };
 cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t s);
 // Of the sequences with at most few_rows new rows per key head (tokens x query heads
@@ -41,8 +42,10 @@ cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t 
 // kFewWholeKeys, a CTA takes all of them, and rows are cheap.
 constexpr int kFewRows = 16, kFewRowsWhole = 64, kFewWholeKeys = 512;
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
-// Of the others.
-cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s);
+// What joins their parts, once those are there.
+cudaError_t launch_attention_few_finish(const AttendJob &j, const KvView &kv, cudaStream_t s);
+// Of the others; whether that took a kernel that joins parts.
+cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s, bool &joined);
 // Their keys' mass, from lse2.
 cudaError_t launch_attention_mass(const AttendJob &j, const KvView &kv, cudaStream_t s);
 

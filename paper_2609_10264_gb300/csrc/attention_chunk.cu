@@ -115,9 +115,8 @@ __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int idx, ChunkIte
 
 // ---------------------------------------------------------------- main kernel
 template <typename T, int DP>
-__global__ void __launch_bounds__(kCThreads, 1)
-    k_chunk(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap k_map,
-            const __grid_constant__ CUtensorMap v_map, uint32_t *__restrict__ err) {
+__device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMap &k_map, const CUtensorMap &v_map,
+                                            uint32_t *err) {
     using C = Chunk<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
@@ -128,7 +127,6 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(kFull, tid >> 5, 0);
-    follow();
     ChunkItem it;
     if (!chunk_item(a, blockIdx.x, it)) return;
     const int split = blockIdx.y;
@@ -416,6 +414,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
 }
+template <typename T, int DP>
+__global__ void __launch_bounds__(kCThreads, 1)
+    k_chunk(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap k_map,
+            const __grid_constant__ CUtensorMap v_map, uint32_t *__restrict__ err) {
+    follow(a.j.beside);
+    chunk_split<T, DP>(a, k_map, v_map, err);
+    end_after(a.j.beside);
+}
 
 // Items of several splits: their parts, in the order of the keys.  kJoinRows rows a CTA
 // (8 of many parts, else 32; 19 parts of eight items: 58 us a call, with 32 rows 76; 3
@@ -455,7 +461,7 @@ __global__ void __launch_bounds__(kCThreads) k_chunk_join(const __grid_constant_
 }
 
 template <typename T, int DP>
-cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s, bool &joined) {
     ChunkArgs a{};
     a.j = j;
     a.kv = kv;
@@ -489,7 +495,7 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
         auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
         const size_t n = (size_t)items * a.splits * kCRows, parts = up(n * DP * sizeof(float));
         void *buf = nullptr;
-        const cudaError_t e = stream_scratch(kScratchAttention, parts + n * sizeof(float), s, &buf);
+        const cudaError_t e = stream_scratch(kScratchChunk, parts + n * sizeof(float), s, &buf);
         if (e != cudaSuccess) return e;
         a.part = static_cast<float4 *>(buf);
         a.stat = reinterpret_cast<float *>(static_cast<char *>(buf) + parts);
@@ -503,7 +509,8 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     e = launch_dependent(k_chunk<T, DP>, dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s, a,
                          maps[0], maps[1], err);
-    if (e == cudaSuccess && a.splits > 1)
+    joined = a.splits > 1;
+    if (e == cudaSuccess && joined)
         e = a.splits > 8
                 ? launch_dependent(k_chunk_join<T, DP, 8>, dim3((unsigned)items, kCRows / 8), kCThreads, 0, s, a)
                 : launch_dependent(k_chunk_join<T, DP, 32>, dim3((unsigned)items, kCRows / 32), kCThreads, 0, s, a);
@@ -512,9 +519,10 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s) {
-    if (j.type == PVMVMD_BF16) return kv.dim <= 64 ? chunk<__nv_bfloat16, 64>(j, kv, s) : chunk<__nv_bfloat16, 128>(j, kv, s);
-    return kv.dim <= 64 ? chunk<__half, 64>(j, kv, s) : chunk<__half, 128>(j, kv, s);
+cudaError_t launch_attention_chunk(const AttendJob &j, const KvView &kv, cudaStream_t s, bool &joined) {
+    const bool bf = j.type == PVMVMD_BF16;
+    if (kv.dim <= 64) return bf ? chunk<__nv_bfloat16, 64>(j, kv, s, joined) : chunk<__half, 64>(j, kv, s, joined);
+    return bf ? chunk<__nv_bfloat16, 128>(j, kv, s, joined) : chunk<__half, 128>(j, kv, s, joined);
 }
 
 }  // namespace pv

@@ -429,14 +429,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 // where 93.5 with 256; the mass wants more CTAs.)
 constexpr int kMassKeys = 1024;
 template <typename T, int DP, int kFinThreads>
-__global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constant__ FewArgs a) {
+__device__ __forceinline__ void few_finish(const FewArgs &a) {
     constexpr int kTile = Few<DP>::kTile;
     __shared__ float2 s_norm[kFewRowsWhole];
     extern __shared__ __align__(16) float s_weight[];  // [rows][parts], then the groups' sums
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
-    follow();
     const Share sh = share<kTile>(a, b);
     const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
     const bool idle = !sh.work || (blockIdx.x > 0 ? first >= len : a.whole);
@@ -544,6 +543,12 @@ __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constan
         *kv.mass_at(page, at, hk) += sum;
     }
 }
+template <typename T, int DP, int kFinThreads>
+__global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constant__ FewArgs a) {
+    follow(a.j.beside);
+    few_finish<T, DP, kFinThreads>(a);
+    end_after(a.j.beside);
+}
 
 int few_ctas() {
     int dev = 0, sms = 0;
@@ -552,8 +557,11 @@ int few_ctas() {
     return 2 * sms;
 }
 
+bool few_whole(const KvView &kv) { return (int64_t)kv.max_pages * kv.ps.d <= kFewWholeKeys; }
+
 template <typename T, int DP>
-cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finish) {
+    if (finish && !j.accumulate && few_whole(kv)) return cudaSuccess;  // nothing is in parts
     FewArgs a{};
     a.j = j;
     a.kv = kv;
@@ -564,7 +572,7 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     constexpr int kTile = Few<DP>::kTile;
     a.max_tiles = (int)((room + kTile - 1) / kTile);
     a.score_rows = (int)std::min<int64_t>(j.few_rows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
-    a.whole = room <= kFewWholeKeys;
+    a.whole = few_whole(kv);
     auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
     const size_t befores = up((size_t)(kv.B + 1) * sizeof(int64_t));
@@ -582,28 +590,35 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
         a.norm = reinterpret_cast<float2 *>(at + parts + stats + befores);
         a.scores = reinterpret_cast<float *>(at + parts + stats + befores + norms);
     }
-    e = func_attr(reinterpret_cast<const void *>(k_few<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                  Few<DP>::kSmem);
-    if (e != cudaSuccess) return e;
-    e = launch_dependent(k_few<T, DP>, dim3((unsigned)a.C), kFewThreads, Few<DP>::kSmem, s, a);
-    if (e != cudaSuccess || (a.whole && !j.accumulate)) return e;
+    if (!finish) {
+        e = func_attr(reinterpret_cast<const void *>(k_few<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                      Few<DP>::kSmem);
+        return e != cudaSuccess ? e : launch_dependent(k_few<T, DP>, dim3((unsigned)a.C), kFewThreads, Few<DP>::kSmem, s, a);
+    }
     const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
     const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)kv.heads, (unsigned)kv.B);
-    auto finish = [&](auto kern, int threads) {
+    auto launch = [&](auto kern, int threads) {
         return launch_dependent(kern, grid, threads, (size_t)(kRows * a.C + 4) * sizeof(float) + threads * sizeof(float4), s,
                                 a);
     };
-    e = j.accumulate ? finish(k_few_finish<T, DP, 256>, 256) : finish(k_few_finish<T, DP, 512>, 512);
-    return e;
+    return j.accumulate ? launch(k_few_finish<T, DP, 256>, 256) : launch(k_few_finish<T, DP, 512>, 512);
+}
+
+// The kernel of the rows, or the one that finishes them.
+cudaError_t few_by_type(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finish) {
+    const bool bf = j.type == PVMVMD_BF16;
+    if (kv.dim <= 64) return bf ? few<__nv_bfloat16, 64>(j, kv, s, finish) : few<__half, 64>(j, kv, s, finish);
+    if (kv.dim <= 96) return bf ? few<__nv_bfloat16, 96>(j, kv, s, finish) : few<__half, 96>(j, kv, s, finish);
+    return bf ? few<__nv_bfloat16, 128>(j, kv, s, finish) : few<__half, 128>(j, kv, s, finish);
 }
 
 }  // namespace
 
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s) {
-    const bool bf = j.type == PVMVMD_BF16;
-    if (kv.dim <= 64) return bf ? few<__nv_bfloat16, 64>(j, kv, s) : few<__half, 64>(j, kv, s);
-    if (kv.dim <= 96) return bf ? few<__nv_bfloat16, 96>(j, kv, s) : few<__half, 96>(j, kv, s);
-    return bf ? few<__nv_bfloat16, 128>(j, kv, s) : few<__half, 128>(j, kv, s);
+    return few_by_type(j, kv, s, false);
+}
+cudaError_t launch_attention_few_finish(const AttendJob &j, const KvView &kv, cudaStream_t s) {
+    return few_by_type(j, kv, s, true);
 }
 
 }  // namespace pv

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(kFull, tid >> 5, 0);
-    follow();
+    follow(a.j.beside);
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t ring = base + 2 * C::kTileBytes;
     if (tid == 0) {
@@ -408,6 +408,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
+    end_after(a.j.beside);
 }
 
 // New rows as a tensor of (values, heads, tokens), for boxes of a key head's heads and

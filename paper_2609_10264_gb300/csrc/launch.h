@@ -191,8 +191,9 @@ cudaError_t launch_batched_grouped(const BatchJob *jobs, int count, uint32_t *er
 // device, one buffer per stream (see scratch.cu).
 enum ScratchPurpose {
     kScratchDigits = 0,     // digit tiles or planes of the batched products
-    kScratchAttention = 1,  // partial results of attention, lists of eviction
+    kScratchAttention = 1,  // partial results of attention's few rows, lists of eviction
     kScratchLse = 2,        // rows' log sums, for the accumulation of mass
+    kScratchChunk = 3,      // partial results of attention's chunks
 };
 cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out);
 // Whether stream_scratch would return a buffer here: one that is large enough
