@@ -1,20 +1,35 @@
 // Attention of new tokens over a paged cache (pvmvmd_paged_attention): which kernel
 // takes which sequences.
+#include <algorithm>
+
 #include "attention.h"
 #include "kv.cuh"
 
 namespace pv {
 
-// Sequences of at most kFewRows rows per key head, single generated tokens above all,
-// go to the kernel that reads K and V as fast as they come, and where no sequence has
-// more than kFewWholeKeys keys those of kFewRowsWhole rows (eight tokens of 32 rows over
-// themselves 9.6 us on the tensor cores' path, most of it set-up).  The others go to
-// the tensor cores.  A call may have both; the host knows the largest number of new
-// tokens at most, and which sequence has how many is seen on the device.
+// Rows per key head (new tokens x query heads of it) up to which a sequence, single
+// generated tokens above all, goes to the kernel that reads K and V as fast as they
+// come; the others go to the tensor cores' path.
+//   64 where no sequence can have more than kFewWholeKeys keys (eight tokens of 32 rows
+//   over themselves 9.6 us on the tensor cores' path, most of it set-up);
+//   32, two passes over the keys, where that path's set-up or its kernel for the mass
+//   costs more: K and V of no more than kFewBytes (24 rows over 6000 keys 25 -> 22 us, 16
+//   such over 2000 41 -> 32) or mass (43 -> 33 and 57 -> 44; 64 over 4000 224 -> 214);
+//   16 beyond (32 rows over 60000 keys 55 us, in two passes 68; 24 rows of 64 sequences
+//   over 4000 121 and 135).
+int few_rows(const AttendJob &j, const KvView &kv) {
+    const int64_t room = (int64_t)kv.max_pages * kv.ps.d, seen = j.window > 0 ? (int64_t)j.window + j.max_new : room;
+    if (room <= kFewWholeKeys) return kFewRowsWhole;
+    const int64_t bytes = 4 * kv.dim * std::min(room, seen) * kv.heads * kv.B;
+    return j.accumulate || bytes <= kFewBytes ? 2 * kFewRows : kFewRows;
+}
+
+// A call may have sequences for both; the host knows the largest number of new tokens at
+// most, and which sequence has how many is seen on the device.
 cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_t s) {
     AttendJob j = job;
     const int G = j.Hq / kv.heads;
-    j.few_rows = (int64_t)kv.max_pages * kv.ps.d <= kFewWholeKeys ? kFewRowsWhole : kFewRows;
+    j.few_rows = few_rows(j, kv);
     const bool one = kv.B == 1;  // which has all the new tokens
     bool few = false, joined = false;
     if (G > j.few_rows)
@@ -33,7 +48,7 @@ cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_
     }
     // Where there are both, they run beside one another: the chunks beside the few rows,
     // the few rows' join beside the chunks', and else beside the mass.  (104 sequences of
-    // 1 to 8 new tokens with mass: XX us a call where XX one after the other.)
+    // 1 to 8 new tokens with mass: 44 us a call where 65 one after the other.)
     j.beside = few;
     cudaError_t e = launch_attention_chunk(j, kv, s, joined);
     if (e != cudaSuccess) return e;

@@ -41,6 +41,7 @@ cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t 
 // of it); the others are left alone.  Where no sequence has more keys than
 // kFewWholeKeys, a CTA takes all of them, and rows are cheap.
 constexpr int kFewRows = 16, kFewRowsWhole = 64, kFewWholeKeys = 512;
+constexpr int64_t kFewBytes = 192 << 20;
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
 // What joins their parts, once those are there.
 cudaError_t launch_attention_few_finish(const AttendJob &j, const KvView &kv, cudaStream_t s);

@@ -435,22 +435,29 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
     extern __shared__ __align__(16) float s_weight[];  // [rows][parts], then the groups' sums
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
-    const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x;
+    const int b = blockIdx.z, hk = blockIdx.y % kv.heads, rt = blockIdx.y / kv.heads, tid = threadIdx.x;
     const Share sh = share<kTile>(a, b);
     const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
-    const bool idle = !sh.work || (blockIdx.x > 0 ? first >= len : a.whole);
+    const bool idle = !sh.work || (blockIdx.x > 0 ? rt > 0 || first >= len : rt >= sh.rts || a.whole);
     if (idle) return;
     const int64_t total = a.before[kv.B], C = min((int64_t)a.C, total);
-    const int64_t i0 = a.before[b] + (int64_t)hk * sh.units, i1 = i0 + sh.units;
-    const int c0 = owner(a.whole ? i0 : i0 + kSetUp, total, C), c1 = a.whole ? c0 : owner(i1 - 1, total, C);  // the CTAs that had parts
     const int row0 = sh.row0;
-    auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows; };
+    // the CTAs that had parts of row tile t
+    auto owners = [&](int t, int &c0, int &c1) {
+        const int64_t i0 = a.before[b] + ((int64_t)hk * sh.rts + t) * sh.units, i1 = i0 + sh.units;
+        c0 = owner(a.whole ? i0 : i0 + kSetUp, total, C);
+        c1 = a.whole ? c0 : owner(i1 - 1, total, C);
+    };
     if (blockIdx.x == 0) {
+        int c0, c1;
+        owners(rt, c0, c1);
         if (c0 == c1) return;
+        const int r0 = rt * kRows, rows = min(kRows, sh.rows - r0);
+        auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows; };
         // the parts' weights, a warp a row; then their sum, with threads enough for
         // several parts at a time
         const int ns = c1 - c0 + 1, lane = tid & 31;
-        for (int r = tid >> 5; r < sh.rows; r += kFinThreads / 32) {
+        for (int r = tid >> 5; r < rows; r += kFinThreads / 32) {
             float M = -INFINITY, L = 0.0f;
             for (int i = lane; i < ns; i += 32) M = fmaxf(M, a.stat[slot(c0 + i) + r].x);
 #pragma unroll
@@ -466,12 +473,13 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
             for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(kFull, L, o);
             if (lane == 0) {
                 s_norm[r] = make_float2(M, inverse(M, L));
-                if (j.lse) j.lse[(int64_t)(row0 + r / a.G) * j.Hq + hk * a.G + r % a.G] = kLn2 * (M + log2f(L));
+                if (j.lse)
+                    j.lse[(int64_t)(row0 + (r0 + r) / a.G) * j.Hq + hk * a.G + (r0 + r) % a.G] = kLn2 * (M + log2f(L));
             }
         }
         __syncthreads();
-        const int cols = sh.rows * (DP / 4), groups = max(1, kFinThreads / cols);
-        float4 *s_sum = reinterpret_cast<float4 *>(s_weight + (sh.rows * ns + 3) / 4 * 4);
+        const int cols = rows * (DP / 4), groups = max(1, kFinThreads / cols);
+        float4 *s_sum = reinterpret_cast<float4 *>(s_weight + (rows * ns + 3) / 4 * 4);
         for (int id = tid; id < cols * groups; id += kFinThreads) {
             const int g = id / cols, col = id - g * cols, r = col / (DP / 4), d = 4 * (col % (DP / 4));
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -488,7 +496,7 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
                 s_sum[id] = v;
                 continue;
             }
-            put_row<T>(a, row0, hk, r, d, v, s_norm[r].y);
+            put_row<T>(a, row0, hk, r0 + r, d, v, s_norm[r].y);
         }
         if (groups == 1) return;
         __syncthreads();
@@ -502,20 +510,23 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
                 v.w += x.w;
             }
             const int r = tid / (DP / 4);
-            put_row<T>(a, row0, hk, r, 4 * (tid % (DP / 4)), v, s_norm[r].y);
+            put_row<T>(a, row0, hk, r0 + r, 4 * (tid % (DP / 4)), v, s_norm[r].y);
         }
         return;
     }
     if (tid < kFewRowsWhole) {
         float2 z = make_float2(0.0f, 0.0f);  // rows that are not there, or see nothing, add nothing
         if (tid < sh.rows) {
+            int c0, c1;
+            owners(tid / kRows, c0, c1);
             if (c0 == c1) {
                 z = a.norm[(int64_t)(row0 + tid / a.G) * j.Hq + hk * a.G + tid % a.G];
             } else {
+                auto at = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kRows + tid % kRows; };
                 float M = -INFINITY, L = 0.0f;
-                for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.stat[slot(c) + tid].x);
+                for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.stat[at(c)].x);
                 for (int c = c0; c <= c1; ++c) {
-                    const float2 p = a.stat[slot(c) + tid];
+                    const float2 p = a.stat[at(c)];
                     L += p.y * exp2_fast(p.x - (M == -INFINITY ? 0.0f : M));
                 }
                 z = make_float2(M, inverse(M, L));
@@ -596,7 +607,8 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finis
         return e != cudaSuccess ? e : launch_dependent(k_few<T, DP>, dim3((unsigned)a.C), kFewThreads, Few<DP>::kSmem, s, a);
     }
     const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
-    const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)kv.heads, (unsigned)kv.B);
+    const int row_tiles = a.whole ? 1 : (int)((std::min<int64_t>(j.few_rows, (int64_t)j.max_new * a.G) + kRows - 1) / kRows);
+    const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)(kv.heads * row_tiles), (unsigned)kv.B);
     auto launch = [&](auto kern, int threads) {
         return launch_dependent(kern, grid, threads, (size_t)(kRows * a.C + 4) * sizeof(float) + threads * sizeof(float4), s,
                                 a);
