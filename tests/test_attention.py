@@ -473,6 +473,22 @@ def test_chunks(pv, lens, news, Hq, H, D, page, kind, layout, causal, window, ac
                     strided=len(lens) == 1, unknown=window == 37)
 
 
+TOGETHER = [  # lens, news, Hq, H, D, page, kind, layout
+    ([3000, 700, 1200, 0], [3, 1, 200, 0], 16, 2, 128, 16, "bf16", "nhd"),    # 24, 8 and 1600 rows a head
+    ([6044], [5], 8, 2, 80, 24, "f16", "nhd"), ([2000, 900], [4, 2], 32, 4, 96, 100, "bf16", "hnd"),
+    ([9000, 9000], [2, 130], 4, 1, 64, 64, "bf16", "nhd"),                    # the chunk's keys in parts
+    ([40 + 7 * (i % 90) for i in range(150)], [1 + 5 * i % 7 for i in range(150)], 8, 1, 64, 16, "f16", "nhd"),
+    ([5000, 33, 5000], [1, 30, 4], 8, 1, 40, 1, "bf16", "fused")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,news,Hq,H,D,page,kind,layout", TOGETHER)
+@pytest.mark.parametrize("window,accumulate", [(0, False), (0, True), (300, True)])
+def test_few_and_many_rows_together(pv, lens, news, Hq, H, D, page, kind, layout, window, accumulate):
+    """Sequences of one tile of rows, of two, and of many, in one call."""
+    check_attention(pv, lens, news, Hq, H, D, page, kind, 31, layout, window=window, accumulate=accumulate)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("window", [1, 2, 64, 10**9, 2**31 - 1])
 def test_windows(pv, window):
