@@ -676,37 +676,37 @@ def pvmvmd_bv_check(ctx: BvCtx, X, Y, chal, u, key2, accept=None, stream=None):
 
 
 # ---------------------------------------------------------------- the client's attention
-# (argument checks of the tensors here, those of values in the library)
+# (argument checks of the tensors in csrc/calls.c, those of values in the library)
 
 _float_codes = None
+_native = None
 
 
-def _type_code(t, name: str, field: bool = False) -> int:
-    """PVMVMD_BF16, _F16, _F32, or, where field elements are taken, _FIELD."""
+def _type_code(t, name: str) -> int:
+    """PVMVMD_BF16, _F16 or _F32."""
     global _float_codes
     if _float_codes is None:
         torch = _torch or _lazy_torch()
         _float_codes = {torch.bfloat16: PVMVMD_BF16, torch.float16: PVMVMD_F16, torch.float32: PVMVMD_F32}
     code = _float_codes.get(t.dtype)
-    if code is None and field and t.dtype in _u32_types():
-        code = PVMVMD_FIELD
     if code is None:
-        raise TypeError(f"{name} must be a floating{' or field' if field else ''} tensor, got {t.dtype}")
+        raise TypeError(f"{name} must be a floating tensor, got {t.dtype}")
     return code
 
 
-def _token_rows(t, name: str, T: int, H: int, D: int, dtype=None):
-    """(address, token stride, head stride) of a T x H x D tensor, heads contiguous."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if t.shape != (T, H, D):
-        raise ValueError(f"{name} must be {T} x {H} x {D}, got {tuple(t.shape)}")
-    st, sh, sd = t.stride()
-    if sd != 1 and D > 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    return t.data_ptr(), st, sh
+def _open_calls():
+    """The native module that checks the tensors and calls the library (csrc/calls.c)."""
+    global _native
+    torch = _torch or _lazy_torch()
+    lib = load_library()
+    from . import _calls
+    get, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if not (get and dev):
+        get, dev = _current_stream, None
+    _calls.open(lib._handle, torch.bfloat16, torch.float16, torch.float32, torch.int32, getattr(torch, "uint32", None),
+                get, dev)
+    _native = _calls
+    return _calls
 
 
 class RopeTable:
@@ -715,7 +715,7 @@ class RopeTable:
     def __init__(self, turns, rot: int, magnitude: float):
         self.turns, self.rot, self.magnitude = turns, rot, magnitude
         self.views = [pvmvmd_rope_view(turns.data_ptr(), rot, i, magnitude) for i in (0, 1)]
-        self.refs = [ctypes.byref(v) for v in self.views]
+        self.addresses = [ctypes.addressof(v) for v in self.views]
 
 
 def pvmvmd_rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -742,17 +742,9 @@ def pvmvmd_rope_table(rot: int, base: float = 10000.0, scaling: str = "none", fa
 def pvmvmd_rope(x, positions, rope: RopeTable, out=None, interleaved: bool = False, scale: float = 1.0, stream=None):
     """x (T x H x D; floating, or field elements) times scale, rotated at int32 positions (T).
     out: a floating tensor of that shape (may be x); default: x's type, bf16 for field elements."""
-    if x.dim() != 3:
-        raise ValueError("x must be T x H x D")
-    T, H, D = x.shape
-    xp, xt, xh = _token_rows(x, "x", T, H, D)
-    code = _type_code(x, "x", True)
     if out is None:
-        import torch
-        out = torch.empty((T, H, D), dtype=torch.bfloat16 if code == PVMVMD_FIELD else x.dtype, device=x.device)
-    op, ot, oh = _token_rows(out, "out", T, H, D)
-    _check(_lib.pvmvmd_rope(rope.refs[bool(interleaved)], _dev_ptr(positions, "positions", _i32_types(), T), T, H, D,
-                            xp, code, xt, xh, scale, op, _type_code(out, "out"), ot, oh, _stream_ptr(stream)),
+        out = x.new_empty(x.shape, dtype=x.dtype if x.dtype.is_floating_point else (_torch or _lazy_torch()).bfloat16)
+    _check((_native or _open_calls()).rope(rope.addresses[bool(interleaved)], positions, x, out, scale, stream),
            "pvmvmd_rope")
     return out
 
@@ -777,7 +769,7 @@ class KvPool:
             mp = _dev_ptr(mass, "mass", ((_torch or _lazy_torch()).float32,), pages * heads * page)
         self.view = pvmvmd_kv_pool(K.data_ptr(), V.data_ptr(), mp, *K.stride()[:3], *V.stride()[:3], pages, page, heads,
                                    dim, _type_code(K, "K"))
-        self.ref = ctypes.byref(self.view)
+        self.address = ctypes.addressof(self.view)
 
 
 class KvBatch:
@@ -795,29 +787,18 @@ class KvBatch:
         cp = _dev_ptr(cu, "cu", _i32_types(), B + 1) if cu is not None else None
         self.table, self.lens, self.cu, self.B = table, lens, cu, B
         self.view = pvmvmd_kv_batch(table.data_ptr(), lp, cp, table.stride(0), B, B, table.shape[1], max_new)
-        self.ref = ctypes.byref(self.view)
+        self.address = ctypes.addressof(self.view)
 
 
 def pvmvmd_kv_append(pool: KvPool, batch: KvBatch, k, v, positions=None, rope: RopeTable | None = None, q=None,
                      q_out=None, interleaved: bool = False, scale: float = 1.0, stream=None):
     """k and v of the new tokens (T x heads x dim, one floating or field type) into the cache, k rotated at positions
     (default: the cache indexes).  q (T x Hq x dim) is rotated into q_out (the pool's type), which is returned."""
-    T, H, D = k.shape[0], pool.heads, pool.dim
-    kr = _token_rows(k, "k", T, H, D)
-    vr = _token_rows(v, "v", T, H, D, k.dtype)
-    code = _type_code(k, "k", True)
-    Hq, qr, outr = 0, (None, 0, 0), (None, 0, 0)
-    if q is not None:
-        Hq = q.shape[1]
-        qr = _token_rows(q, "q", T, Hq, D, k.dtype)
-        if q_out is None:
-            import torch
-            q_out = torch.empty((T, Hq, D), dtype=pool.K.dtype, device=q.device)
-        outr = _token_rows(q_out, "q_out", T, Hq, D, pool.K.dtype)
-    pp = None if positions is None else _dev_ptr(positions, "positions", _i32_types(), T)
-    batch.view.T = T
-    _check(_lib.pvmvmd_kv_append(pool.ref, batch.ref, rope.refs[bool(interleaved)] if rope is not None else None, pp,
-                                 code, scale, *kr, *vr, Hq, *qr, *outr, _stream_ptr(stream)), "pvmvmd_kv_append")
+    if q is not None and q_out is None:
+        q_out = q.new_empty(q.shape, dtype=pool.K.dtype)
+    _check((_native or _open_calls()).append(pool.address, batch.address,
+                                             rope.addresses[bool(interleaved)] if rope is not None else 0, positions,
+                                             scale, k, v, q, q_out, stream), "pvmvmd_kv_append")
     return q_out
 
 
@@ -826,18 +807,10 @@ def pvmvmd_paged_attention(pool: KvPool, batch: KvBatch, q, out=None, lse=None, 
     """Attention of the new tokens' q (T x Hq x dim, the pool's type) over the cache -> out (T x Hq x dim).  lse: a
     float32 T x Hq tensor to fill; accumulate: add the attention weights to the pool's mass (sequences must then not
     share pages); scale: default dim^-1/2."""
-    if q.dim() != 3:
-        raise ValueError("q must be T x Hq x dim")
-    T, Hq, D = q.shape[0], q.shape[1], pool.dim
-    qr = _token_rows(q, "q", T, Hq, D, pool.K.dtype)
     if out is None:
-        import torch
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
-    outr = _token_rows(out, "out", T, Hq, D, pool.K.dtype)
-    lp = None if lse is None else _dev_ptr(lse, "lse", (_torch.float32,), T * Hq)
-    batch.view.T = T
-    _check(_lib.pvmvmd_paged_attention(pool.ref, batch.ref, Hq, *qr, D**-0.5 if scale is None else scale, causal,
-                                       window, accumulate, *outr, lp, _stream_ptr(stream)), "pvmvmd_paged_attention")
+        out = q.new_empty(q.shape)
+    _check((_native or _open_calls()).attend(pool.address, batch.address, q, out, lse, scale, causal, window, accumulate,
+                                             stream), "pvmvmd_paged_attention")
     return out
 
 
@@ -850,12 +823,8 @@ def pvmvmd_kv_evict(pool: KvPool, batch: KvBatch, budget: int, recent: int = 0, 
         new_lens = batch.lens
     if new_table is None:
         new_table = batch.table
-    if new_table.dim() != 2 or new_table.shape[0] != batch.B or (new_table.shape[1] > 1 and new_table.stride(1) != 1) \
-            or new_table.dtype not in _i32_types() or not new_table.is_cuda:
-        raise ValueError("new_table must be an int32 CUDA tensor B x pages with contiguous rows")
-    _check(_lib.pvmvmd_kv_evict(pool.ref, batch.ref, budget, recent, new_table.data_ptr(), new_table.stride(0),
-                                new_table.shape[1], _dev_ptr(new_lens, "new_lens", _i32_types(), batch.B),
-                                _stream_ptr(stream)), "pvmvmd_kv_evict")
+    _check((_native or _open_calls()).evict(pool.address, batch.address, budget, recent, new_table, new_lens, stream),
+           "pvmvmd_kv_evict")
     return new_lens
 
 

@@ -1,8 +1,8 @@
 """Build libpvmvmd.so in-tree for sm_103a (GB300) with nvcc.
 
 Each translation unit under csrc/ is compiled in parallel into _build/, then
-linked into paper_2609_10264_gb300/libpvmvmd.so.  Rebuilds only when a source
-or header is newer than the library.
+linked into paper_2609_10264_gb300/libpvmvmd.so; csrc/calls.c becomes the Python
+module _calls.so beside it.  Rebuilds only when a source or header is newer.
 """
 from __future__ import annotations
 
@@ -11,6 +11,7 @@ import glob
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,6 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpvmvmd.so")
+CALLS_C = os.path.join(CSRC, "calls.c")
+CALLS = os.path.join(PKG, "_calls.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC", "-diag-suppress", "550", "-I", INCLUDE,
               *ARCH]
@@ -36,13 +39,13 @@ def _sources():
 
 def _inputs():
     return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + \
-        glob.glob(os.path.join(INCLUDE, "*.h")) + [os.path.abspath(__file__)]
+        glob.glob(os.path.join(INCLUDE, "*.h")) + [CALLS_C, os.path.abspath(__file__)]
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     return any(os.path.getmtime(p) > t for p in _inputs())
 
 
@@ -62,9 +65,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
             print(r.stdout, r.stderr)
         return obj
 
+    def compile_calls():
+        tmp = CALLS + f".tmp{os.getpid()}"
+        cmd = [os.environ.get("CC") or shutil.which("gcc") or "cc", "-O2", "-Wall", "-shared", "-fPIC", "-I", INCLUDE,
+               "-I", sysconfig.get_paths()["include"], "-o", tmp, CALLS_C, "-lm", "-ldl"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"the C compiler failed for {CALLS_C}:\n{r.stdout}\n{r.stderr}")
+        if verbose and r.stderr:
+            print(r.stderr)
+        os.replace(tmp, CALLS)
+
     srcs = _sources()
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+        calls = ex.submit(compile_calls)
         objs = list(ex.map(compile_one, srcs))
+        calls.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, "-shared", *ARCH, "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -296,6 +296,78 @@ def test_refusals_before_any_device_use(pv):
 
 # ---------------------------------------------------------------- rotary positions
 
+class Fake:
+    """What the binding looks at of a tensor."""
+
+    def __init__(self, shape, dtype, strides=None, address=0, cuda=True):
+        import torch
+        self.shape, self.dtype, self.is_cuda, self.address = torch.Size(shape), dtype, cuda, address
+        self.strides = strides or torch.empty(shape, device="meta").stride()
+
+    def stride(self):
+        return self.strides
+
+    def data_ptr(self):
+        return self.address
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.shape.numel()
+
+
+def test_binding_refuses_tensors(pv):
+    """What the native binding checks, before the library sees anything (which refuses null pointers)."""
+    import torch
+    bf, f16, f32, i32 = torch.bfloat16, torch.float16, torch.float32, torch.int32
+    pool, batch = object.__new__(pv.KvPool), object.__new__(pv.KvBatch)
+    pool.view = pv.pvmvmd_kv_pool(16, 16, None, 1024, 128, 64, 1024, 128, 64, 4, 8, 2, 64, pv.PVMVMD_BF16)
+    batch.view = pv.pvmvmd_kv_batch(16, 16, None, 4, 3, 3, 4, 0)
+    batch.B, batch.table, batch.lens = 3, Fake((3, 4), i32), Fake((3,), i32)
+    for v in (pool, batch):
+        v.address = ctypes.addressof(v.view)
+    q = Fake((3, 4, 64), bf)
+
+    def refused(kind, match, f, *args, **kw):
+        with pytest.raises(kind, match=match):
+            f(*args, **{"stream": 0, **kw})
+
+    attend = pv.pvmvmd_paged_attention
+    refused(pv.PvmvmdError, None, attend, pool, batch, q, out=q)  # null pointers
+    assert batch.view.T == 3
+    refused(TypeError, "q must be a CUDA tensor", attend, pool, batch, Fake((3, 4, 64), bf, cuda=False), out=q)
+    refused(TypeError, "q must be a CUDA tensor", attend, pool, batch, np.zeros((3, 4, 64)), out=q)
+    refused(TypeError, "q must have dtype torch.bfloat16", attend, pool, batch, Fake((3, 4, 64), f16), out=q)
+    refused(ValueError, "q must have 3 dimensions", attend, pool, batch, Fake((3, 256), bf), out=q)
+    refused(ValueError, "out must be 3 x 4 x 64", attend, pool, batch, q, out=Fake((3, 2, 64), bf))
+    refused(ValueError, "the last dimension of q", attend, pool, batch, Fake((3, 4, 64), bf, (512, 128, 2)), out=q)
+    refused(ValueError, "lse has 9 elements, expected 12", attend, pool, batch, q, out=q, lse=Fake((3, 3), f32))
+    refused(TypeError, "lse must have dtype", attend, pool, batch, q, out=q, lse=Fake((3, 4), f16))
+    refused(OverflowError, "window", attend, pool, batch, q, out=q, window=2**31)
+    refused(TypeError, None, attend, pool, batch, q, out=q, window=1.5)
+    refused(TypeError, None, attend, pool, batch, q, out=q, scale="1")
+    append, k = pv.pvmvmd_kv_append, Fake((3, 2, 64), f16)
+    refused(pv.PvmvmdError, None, append, pool, batch, k, k)
+    refused(TypeError, "k must be a floating or field tensor", append, pool, batch, Fake((3, 2, 64), torch.int64), k)
+    refused(TypeError, "v must have dtype", append, pool, batch, k, Fake((3, 2, 64), bf))
+    refused(ValueError, "v must be 3 x 2 x 64", append, pool, batch, k, Fake((2, 2, 64), f16))
+    refused(TypeError, "q_out must have dtype torch.bfloat16", append, pool, batch, k, k, q=Fake((3, 4, 64), f16),
+            q_out=Fake((3, 4, 64), f16))
+    refused(TypeError, "positions must have dtype", append, pool, batch, k, k, Fake((3,), torch.int64))
+    rope = pv.RopeTable(Fake((32,), torch.int64), 64, 1.0)
+    refused(pv.PvmvmdError, None, pv.pvmvmd_rope, q, Fake((3,), i32), rope, out=q)
+    refused(ValueError, "positions has 2 elements", pv.pvmvmd_rope, q, Fake((2,), i32), rope, out=q)
+    refused(TypeError, "out must be a floating tensor", pv.pvmvmd_rope, q, Fake((3,), i32), rope, out=Fake((3, 4, 64), i32))
+    evict = pv.pvmvmd_kv_evict
+    refused(pv.PvmvmdError, None, evict, pool, batch, 5)  # no mass
+    refused(ValueError, "new_table must be", evict, pool, batch, 5, new_table=Fake((2, 4), i32))
+    refused(ValueError, "new_table must be", evict, pool, batch, 5, new_table=Fake((3, 4), i32, (1, 3)))
+    refused(ValueError, "new_table must be", evict, pool, batch, 5, new_table=Fake((3, 4), torch.int64))
+    refused(ValueError, "new_lens has 4 elements", evict, pool, batch, 5, new_lens=Fake((4,), i32))
+    refused(AttributeError, "cuda_stream", attend, pool, batch, q, out=q, stream="s")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,H,D,rot,kind,out,inter,strided", [
     (1, 1, 2, 2, "f32", "f32", False, False), (1, 40, 128, 128, "bf16", "bf16", False, False),
