@@ -86,6 +86,11 @@ __device__ __forceinline__ Found find(int B, Work work, Pos pos, int64_t *list =
     __shared__ int64_t s_warp[kThreads / 32], s_before;
     __shared__ int s_b;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (B == 1) {
+        const int64_t w = work(0), p = pos(w);
+        if (list && tid == 0) list[0] = 0, list[1] = w;
+        return Found{w, 0, p >= 0 && p < w ? 0 : -1};
+    }
     if (B <= 32) {  // every warp by itself, a lane a sequence
         const int64_t w = lane < B ? work(lane) : 0;
         int64_t incl = w;

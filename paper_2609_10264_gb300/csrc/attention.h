@@ -39,7 +39,7 @@ struct AttendJob {
 cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t s);
 // Of the sequences with at most few_rows new rows per key head (tokens x query heads
 // of it); the others are left alone.  Where no sequence has more keys than
-// kFewWholeKeys, a CTA takes all of them, and rows are cheap.
+// kFewWholeKeys rows are cheap.
 constexpr int kFewRows = 16, kFewRowsWhole = 64, kFewWholeKeys = 512;
 constexpr int64_t kFewBytes = 192 << 20;
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);

@@ -21,8 +21,6 @@
 namespace pv {
 namespace {
 
-constexpr int kFewWarps = 4;
-constexpr int kFewThreads = 32 * kFewWarps;
 constexpr int kRows = 16;                 // rows per tile of them, of one MMA
 
 struct FewArgs {
@@ -36,26 +34,31 @@ struct FewArgs {
     int score_rows, max_tiles;  // (rows a multiple of 4)
     float scale2;    // scale x log2(e)
     int G, C;
+    int tile_log;    // keys per tile
     bool whole;      // a CTA takes all keys of a row tile
 };
 
 // DP: the head's values in whole MMAs of the columns that are built (64, 96, 128).
-template <int DP>
+// W: warps, four of each of two CTAs of an SM; eight of one where a CTA takes all keys of
+// a row tile and there are no more of these than SMs (8 heads, 200 keys: 5.5 us a call,
+// with four 6.7; 20 such sequences 9.8 and 7.1).
+template <int DP, int W>
 struct Few {
+    static constexpr int kThreads = 32 * W;
     // Keys per warp and step, and steps of the ring: what two CTAs of an SM have room for.
     // 32 keys take less than two steps of 16 (57 ragged sequences of up to 3481 keys, 8 heads
     // of 64 in pages of 16, 64, 100 and 1: 47, 45, 49 and 50 us a call where 16 keys in a
     // ring of six steps took 50, 47, 54 and 59; heads of 96: 68 to 72 where 69 to 78).
     static constexpr int kSub = DP == 128 ? 16 : 32;
     static constexpr int kStages = DP == 96 ? 2 : 3;
-    static constexpr int kTile = kFewWarps * kSub;  // keys per tile
+    static constexpr int kTile = W * kSub;  // keys per tile
     // bytes of a row; chunks of 16 are swizzled, or rows of 13 chunks where 12 are used:
     // either way 8 rows' chunks lie in different banks
     static constexpr int kRow = DP == 96 ? 208 : 2 * DP;
     static __device__ __forceinline__ int at(int r, int ch) { return r * kRow + ((DP == 96 ? ch : ch ^ (r & 7)) << 4); }
     static constexpr int kHalf = kSub * kRow;
     static constexpr int kStage = 2 * kHalf;
-    static constexpr int kRing = kFewWarps * kStages * kStage;
+    static constexpr int kRing = W * kStages * kStage;
     static constexpr int kSmem = kRing + kRows * kRow;
     static constexpr int kChunks = DP / 8;
     static constexpr int kWave = 32 / kChunks;  // rows that a warp copies at a time
@@ -105,7 +108,6 @@ struct Share {
     int rows, rts, first, tiles, units;
     int64_t work;  // units of all
 };
-template <int kTile>
 __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     Share s;
     s.row0 = a.kv.first(b);
@@ -113,12 +115,14 @@ __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     s.len = a.kv.len(b);
     s.rows = s.n * a.G;
     s.rts = (s.rows + kRows - 1) / kRows;
-    s.first = a.j.window > 0 ? max(0, s.len - s.n - a.j.window + 1) / kTile * kTile : 0;
-    s.tiles = max(1, (s.len - s.first + kTile - 1) / kTile);
+    s.first = a.j.window > 0 ? max(0, s.len - s.n - a.j.window + 1) >> a.tile_log << a.tile_log : 0;
+    s.tiles = max(1, (s.len - s.first + (1 << a.tile_log) - 1) >> a.tile_log);
     s.units = a.whole ? 1 : kSetUp + s.tiles;
     s.work = s.rows <= 0 || s.rows > a.j.few_rows ? 0 : (int64_t)s.units * a.kv.heads * s.rts;
     return s;
 }
+// The first position of CTA c of C <= N.
+__device__ __forceinline__ int64_t cut(int64_t N, int c, int64_t C) { return N == C ? c : N * c / C; }
 // The CTA that takes position p of N, among C <= N.
 __device__ __forceinline__ int owner(int64_t p, int64_t N, int64_t C) { return (int)(((p + 1) * C - 1) / N); }
 
@@ -132,29 +136,29 @@ __device__ __forceinline__ void put_row(const FewArgs &a, int row0, int hk, int 
 }
 
 // ---------------------------------------------------------------- main kernel
-template <typename T, int DP>
-__global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ FewArgs a) {
-    using F = Few<DP>;
+template <typename T, int DP, int W>
+__global__ void __launch_bounds__(Few<DP, W>::kThreads, 8 / W) k_few(const __grid_constant__ FewArgs a) {
+    using F = Few<DP, W>;
     constexpr int kSub = F::kSub, kTile = F::kTile;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float2 s_stat[kFewWarps][kRows];
+    __shared__ float2 s_stat[W][kRows];
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, grp = lane >> 2;
     follow();
-    const Found f = find<kFewThreads>(
-        kv.B, [&](int b) { return share<F::kTile>(a, b).work; },
+    const Found f = find<F::kThreads>(
+        kv.B, [&](int b) { return share(a, b).work; },
         [&](int64_t total) {
             const int64_t C = min((int64_t)a.C, total);
-            return (int64_t)blockIdx.x < C ? total * blockIdx.x / C : -1;
+            return (int64_t)blockIdx.x < C ? cut(total, blockIdx.x, C) : -1;
         },
         blockIdx.x == 0 ? a.before : nullptr);
     const int64_t C = min((int64_t)a.C, f.total);
     if ((int64_t)blockIdx.x >= C) return;
-    const int64_t p1 = f.total * (blockIdx.x + 1) / C;
-    int64_t p = f.total * blockIdx.x / C, done = f.before;
+    const int64_t p1 = cut(f.total, blockIdx.x + 1, C);
+    int64_t p = cut(f.total, blockIdx.x, C), done = f.before;
     int b = f.b;
-    Share sh = share<F::kTile>(a, b);
+    Share sh = share(a, b);
     const uint32_t ring = smem_addr(smem) + warp * F::kStages * F::kStage, qs = smem_addr(smem) + F::kRing;
     const bool one_page = kv.ps.d % 16 == 0;  // for 16 keys
     const int chunks = kv.dim / 8;
@@ -162,9 +166,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
     while (p < p1) {
         while (p >= done + sh.work) {
             done += sh.work;
-            sh = share<F::kTile>(a, ++b);
+            sh = share(a, ++b);
         }
-        const int item = (int)((p - done) / sh.units), u0 = (int)((p - done) % sh.units);
+        const int64_t in = p - done;
+        const int item = a.whole             ? (int)in
+                         : sh.work >> 32 == 0 ? (int)((uint32_t)in / (uint32_t)sh.units)
+                                              : (int)(in / sh.units);
+        const int u0 = (int)(in - (int64_t)item * sh.units);
         const int units = a.whole ? 1 : (int)min((int64_t)(sh.units - u0), p1 - p);
         p += units;
         const int t0 = a.whole ? 0 : max(0, u0 - kSetUp), nt = a.whole ? sh.tiles : u0 + units - kSetUp - t0;
@@ -223,7 +231,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 #pragma unroll
         for (int i = 0; i < F::kStages; ++i) fetch_page(i);
         // rows of Q, zero beyond the real ones
-        for (int id = tid; id < kRows * F::kChunks; id += kFewThreads) {
+        for (int id = tid; id < kRows * F::kChunks; id += F::kThreads) {
             const int r = id / F::kChunks, ch = id % F::kChunks;
             const bool real = r < rows && ch < chunks;
             const char *src = static_cast<const char *>(j.q);
@@ -386,15 +394,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
         __syncthreads();
         const bool whole = nt == sh.tiles;
         const int slot = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-        for (int id = tid; id < rows * (DP / 4); id += kFewThreads) {
+        for (int id = tid; id < rows * (DP / 4); id += F::kThreads) {
             const int r = id / (DP / 4), d = 4 * (id % (DP / 4));
             float M = -INFINITY, L = 0.0f;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, s_stat[w][r].x);
+            for (int w = 0; w < W; ++w) M = fmaxf(M, s_stat[w][r].x);
             const float ref = M == -INFINITY ? 0.0f : M;
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) {
+            for (int w = 0; w < W; ++w) {
                 const float2 z = s_stat[w][r];
                 const float e = exp2_fast(z.x - ref);
                 const float4 x = *reinterpret_cast<const float4 *>(all + (w * kRows + r) * kPitch + d);
@@ -430,13 +438,12 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_few(const __grid_constant__ 
 constexpr int kMassKeys = 1024;
 template <typename T, int DP, int kFinThreads>
 __device__ __forceinline__ void few_finish(const FewArgs &a) {
-    constexpr int kTile = Few<DP>::kTile;
     __shared__ float2 s_norm[kFewRowsWhole];
     extern __shared__ __align__(16) float s_weight[];  // [rows][parts], then the groups' sums
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int b = blockIdx.z, hk = blockIdx.y % kv.heads, rt = blockIdx.y / kv.heads, tid = threadIdx.x;
-    const Share sh = share<kTile>(a, b);
+    const Share sh = share(a, b);
     const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
     const bool idle = !sh.work || (blockIdx.x > 0 ? rt > 0 || first >= len : rt >= sh.rts || a.whole);
     if (idle) return;
@@ -536,7 +543,7 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
         s_norm[tid] = z;
     }
     __syncthreads();
-    const float *scores = a.scores + ((int64_t)b * kv.heads + hk) * a.max_tiles * kTile * a.score_rows;
+    const float *scores = a.scores + ((int64_t)b * kv.heads + hk) * (a.max_tiles << a.tile_log) * a.score_rows;
 #pragma unroll
     for (int k = 0; k < kMassKeys; k += kFinThreads) {
         const int key = first + k + tid;
@@ -561,14 +568,14 @@ __global__ void __launch_bounds__(kFinThreads) k_few_finish(const __grid_constan
     end_after(a.j.beside);
 }
 
-int few_ctas() {
-    int dev = 0, sms = 0;
-    cudaGetDevice(&dev);
-    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    return 2 * sms;
-}
 
-bool few_whole(const KvView &kv) { return (int64_t)kv.max_pages * kv.ps.d <= kFewWholeKeys; }
+// Whether a CTA takes all keys of a row tile, which saves the finishing kernel: of up to
+// 512 keys, or 1024 of narrow heads, whose steps are of 32 (8 heads of 64 and of 128 over
+// 1000 keys, 8 sequences: 8.0 and 12.3 us a call, in parts 10.2 and 12.9; 64 sequences
+// 22 and 41, in parts 22 and 34).
+bool few_whole(const KvView &kv) {
+    return (int64_t)kv.max_pages * kv.ps.d <= (kv.dim <= 96 ? 2 * kFewWholeKeys : kFewWholeKeys);
+}
 
 template <typename T, int DP>
 cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finish) {
@@ -577,19 +584,25 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finis
     a.j = j;
     a.kv = kv;
     a.G = j.Hq / kv.heads;
-    a.C = few_ctas();
+    a.whole = few_whole(kv);
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const int row_tiles = (int)((std::min<int64_t>(j.few_rows, (int64_t)j.max_new * a.G) + kRows - 1) / kRows);
+    const bool wide = a.whole && (int64_t)kv.B * kv.heads * row_tiles <= sms;
+    a.C = wide ? sms : 2 * sms;
     a.scale2 = j.scale * kLog2e;
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
-    constexpr int kTile = Few<DP>::kTile;
-    a.max_tiles = (int)((room + kTile - 1) / kTile);
+    const int tile = wide ? Few<DP, 8>::kTile : Few<DP, 4>::kTile;
+    while (1 << a.tile_log < tile) ++a.tile_log;
+    a.max_tiles = (int)((room + tile - 1) / tile);
     a.score_rows = (int)std::min<int64_t>(j.few_rows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
-    a.whole = few_whole(kv);
     auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
     const size_t befores = up((size_t)(kv.B + 1) * sizeof(int64_t));
     const size_t norms = j.accumulate ? up((size_t)kv.T * j.Hq * sizeof(float2)) : 0;
     const size_t scores =
-        j.accumulate ? (size_t)kv.B * kv.heads * a.max_tiles * kTile * a.score_rows * sizeof(float) : 0;
+        j.accumulate ? (size_t)kv.B * kv.heads * a.max_tiles * tile * a.score_rows * sizeof(float) : 0;
     void *buf = nullptr;
     cudaError_t e = stream_scratch(kScratchAttention, parts + stats + befores + norms + scores, s, &buf);
     if (e != cudaSuccess) return e;
@@ -601,14 +614,16 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finis
         a.norm = reinterpret_cast<float2 *>(at + parts + stats + befores);
         a.scores = reinterpret_cast<float *>(at + parts + stats + befores + norms);
     }
-    if (!finish) {
-        e = func_attr(reinterpret_cast<const void *>(k_few<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                      Few<DP>::kSmem);
-        return e != cudaSuccess ? e : launch_dependent(k_few<T, DP>, dim3((unsigned)a.C), kFewThreads, Few<DP>::kSmem, s, a);
-    }
+    auto launch_rows = [&](auto kern, int threads, int smem) {
+        const cudaError_t e =
+            func_attr(reinterpret_cast<const void *>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        return e != cudaSuccess ? e : launch_dependent(kern, dim3((unsigned)a.C), threads, smem, s, a);
+    };
+    if (!finish)
+        return wide ? launch_rows(k_few<T, DP, 8>, Few<DP, 8>::kThreads, Few<DP, 8>::kSmem)
+                    : launch_rows(k_few<T, DP, 4>, Few<DP, 4>::kThreads, Few<DP, 4>::kSmem);
     const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
-    const int row_tiles = a.whole ? 1 : (int)((std::min<int64_t>(j.few_rows, (int64_t)j.max_new * a.G) + kRows - 1) / kRows);
-    const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)(kv.heads * row_tiles), (unsigned)kv.B);
+    const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)(kv.heads * (a.whole ? 1 : row_tiles)), (unsigned)kv.B);
     auto launch = [&](auto kern, int threads) {
         return launch_dependent(kern, grid, threads, (size_t)(kRows * a.C + 4) * sizeof(float) + threads * sizeof(float4), s,
                                 a);
