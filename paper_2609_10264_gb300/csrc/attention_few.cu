@@ -1,5 +1,7 @@
 // Attention of sequences with few new rows (new tokens x query heads of a key head):
-// single generated tokens above all.  Bound by the reading of K and V.
+// single generated tokens above all.  Bound by the reading of K and V: 131071 keys of 8
+// heads of 128 89-91 us a call (6.0 TB/s); 64 sequences of up to 8192 with their weights
+// 172 us (6.7 TB/s with the scores written), and 28 to finish.
 //
 // Work.  The keys of a (sequence, key head) come in tiles of 64 or 128.  All tiles of all
 // of them, one after the other, are dealt out evenly to the CTAs, whatever the

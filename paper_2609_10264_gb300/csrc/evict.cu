@@ -11,9 +11,10 @@
 // never moves to a higher index, so in place the rows that lie where a CTA writes are
 // its own or those of CTAs before it: every CTA reports its rows read, and one that
 // writes to a page that the sequence has in that very place waits for the reports
-// before its own first (64 CTAs a list: 170 us with that wait where 105 do without).
+// before its own first (64 CTAs a list: 173 us with that wait where 112 do without).
 // Blocks start in the order of their index (as the other kernels that chain blocks
-// rest on); the wait is bounded.
+// rest on); the wait is bounded.  16 sequences of up to 16384 keys to 4096: 110 us a call,
+// 4.6 TB/s of rows read and written; one of 700 keys 9.6 us, latency of both kernels.
 #include <algorithm>
 
 #include "attention.cuh"

@@ -7,6 +7,9 @@
 // any position; its upper 32 bits, read as signed, go to sincospi with an error of
 // 2^-24 of the angle.  (In 32-bit floating point the angle alone is 2^-9 off at
 // position 30000.)
+//
+// Bound by memory: 4097 tokens of 32 heads of 96 in 32 bits 23 us (4.4 TB/s), 6001
+// tokens of 64 + 8 + 8 heads of 128 into a cache 46 us (5.3 TB/s).
 #include <algorithm>
 
 #include "attention.cuh"
