@@ -16,12 +16,15 @@ namespace pv {
 //   costs more: K and V of no more than kFewBytes (24 rows over 6000 keys 25 -> 22 us, 16
 //   such over 2000 41 -> 32) or mass (43 -> 33 and 57 -> 44; 64 over 4000 224 -> 214);
 //   16 beyond (32 rows over 60000 keys 55 us, in two passes 68; 24 rows of 64 sequences
-//   over 4000 121 and 135).
+//   over 4000 121 and 135), and where others have more rows, so that the tensor cores'
+//   path runs anyway (five of 19 to 56 rows over 16000 keys 57 us, some of them in two
+//   passes 65, with mass 107 and 125).
 int few_rows(const AttendJob &j, const KvView &kv) {
     const int64_t room = (int64_t)kv.max_pages * kv.ps.d, seen = j.window > 0 ? (int64_t)j.window + j.max_new : room;
     if (room <= kFewWholeKeys) return kFewRowsWhole;
     const int64_t bytes = 4 * kv.dim * std::min(room, seen) * kv.heads * kv.B;
-    return j.accumulate || bytes <= kFewBytes ? 2 * kFewRows : kFewRows;
+    const bool all = (int64_t)j.max_new * (j.Hq / kv.heads) <= 2 * kFewRows;
+    return all && (j.accumulate || bytes <= kFewBytes) ? 2 * kFewRows : kFewRows;
 }
 
 // A call may have sequences for both; the host knows the largest number of new tokens at

@@ -14,6 +14,14 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void shared_store16(uint32_t dst, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 shared_load16(uint32_t src) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+    return v;
+}
 __device__ __forceinline__ void copy4(uint32_t dst, const void *src, bool real) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
 }
@@ -333,6 +341,21 @@ inline cudaError_t page_map(CUtensorMap *map, const KvView &kv, bool values, int
                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// New rows as a tensor of (values, heads, tokens), for boxes of a key head's heads and
+// as many tokens as make a tile; false where a tile is not whole tokens, or the strides
+// are such that a tensor map cannot have them.
+inline bool rows_map(CUtensorMap *map, const AttendJob &j, const KvView &kv, int G) {
+    PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
+    if (!encode || kCM % G || j.q_token <= 0 || j.q_head <= 0) return false;
+    const cuuint64_t dim[3] = {(cuuint64_t)kv.dim, (cuuint64_t)j.Hq, (cuuint64_t)kv.T};
+    const cuuint64_t stride[2] = {(cuuint64_t)j.q_head, (cuuint64_t)j.q_token};
+    const cuuint32_t part[3] = {64, (cuuint32_t)G, (cuuint32_t)(kCM / G)}, one[3] = {1, 1, 1};
+    return encode(map, j.type == PVMVMD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                  const_cast<void *>(j.q), dim, stride, part, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Cache index i of sequence b, of length len: whether it is there, and its place in

@@ -43,6 +43,7 @@ struct ChunkArgs {
     float scale2;   // |scale| log2(e)
     int G, splits, negative;
     int box;        // keys per TMA box, 0: the pages are not such that boxes fit them
+    bool q_box;     // a tile of rows is a TMA box (see rows_map)
 };
 
 template <int DP>
@@ -117,8 +118,8 @@ __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int idx, ChunkIte
 
 // ---------------------------------------------------------------- main kernel
 template <typename T, int DP>
-__device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMap &k_map, const CUtensorMap &v_map,
-                                            uint32_t *err) {
+__device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMap &q_map, const CUtensorMap &k_map,
+                                            const CUtensorMap &v_map, uint32_t *err) {
     using C = Chunk<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
@@ -139,7 +140,7 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t qbase = base, ring = base + 2 * C::kTileBytes;
     if (tid == 0) {
-        mbar_init(&q_full, 8);
+        mbar_init(&q_full, a.q_box ? 1 : 8);
         mbar_init(&mma_done, 1);
         for (int s = 0; s < kSt; ++s) {
             mbar_init(&kv_full[s], 1);
@@ -175,8 +176,7 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
         const int hi = !real ? INT_MAX : j.causal ? min(it.len, at + 1) : it.len;
         const int lo = real && j.window > 0 && at >= j.window ? at - j.window + 1 : 0;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        // the warp's rows of Q
-        {
+        if (!a.q_box) {  // the warp's rows of Q
             const TileCopy<DP> q(lane, kv.dim);
             q.template copy<1>(qbase + tile * C::kTileBytes, static_cast<const char *>(j.q), [&](int, int64_t &off) {
                 off = (int64_t)(it.t0 + (it.row0 + r) / a.G) * j.q_token +
@@ -275,14 +275,19 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
             const int t = it.t0 + (it.row0 + r) / a.G, h = it.hk * a.G + (it.row0 + r) % a.G;
             const float inv = inverse(m, l), lse2 = m == -INFINITY ? (l != l ? l : m) : m * a.scale2 + log2f(l);
             const int64_t part = it.slot + split;
-            char *orow = static_cast<char *>(j.out) + t * j.o_token + h * j.o_head;
+            // Rows go through the memory of the warp's rows of Q, which no MMA reads any more, so
+            // that a row's 16-byte pieces leave from neighbouring lanes (a lane a row, 2048
+            // tokens over 8192 keys: 164 us a call, so 160).
+            constexpr int kPieces = DP / 8;
+            const uint32_t rows = qbase + tile * C::kTileBytes + (warp & 3) * 32 * 2 * DP;
+            auto piece = [&](int row, int p) { return rows + (uint32_t)(row * kPieces + (p ^ (row & 7))) * 16; };
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 float o[32];
                 tmem_ld32_async(to + 32 * c, o);
                 tmem_ld_wait();
-                if (!real) continue;
                 if (it.parts > 1) {
+                    if (!real) continue;
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
                         a.part[(part * (DP / 4) + 8 * c + e / 4) * kCRows + r] =
@@ -290,11 +295,22 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
-                        if (32 * c + e < kv.dim)
-                            *reinterpret_cast<uint4 *>(orow + 2 * (32 * c + e)) =
-                                make_uint4(pack(o[e] * inv, o[e + 1] * inv, T{}), pack(o[e + 2] * inv, o[e + 3] * inv, T{}),
-                                           pack(o[e + 4] * inv, o[e + 5] * inv, T{}),
-                                           pack(o[e + 6] * inv, o[e + 7] * inv, T{}));
+                        shared_store16(piece(lane, 4 * c + e / 8), pack(o[e] * inv, o[e + 1] * inv, T{}),
+                                       pack(o[e + 2] * inv, o[e + 3] * inv, T{}), pack(o[e + 4] * inv, o[e + 5] * inv, T{}),
+                                       pack(o[e + 6] * inv, o[e + 7] * inv, T{}));
+                }
+            }
+            if (it.parts == 1) {
+                __syncwarp();
+                const int64_t orow = t * j.o_token + h * j.o_head;
+                const int ch = lane % kPieces;
+                char *out = static_cast<char *>(j.out) + 16 * ch;
+#pragma unroll 4
+                for (int u = 0; u < kPieces; ++u) {
+                    const int row = u * (32 / kPieces) + lane / kPieces;
+                    const int64_t at = __shfl_sync(kFull, orow, row);
+                    if (r - lane + row < it.rows && 8 * ch < kv.dim)
+                        *reinterpret_cast<uint4 *>(out + at) = shared_load16(piece(row, ch));
                 }
             }
             if (real) {
@@ -375,6 +391,17 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
             // ------------------------------------------------ copies
             const int w = warp - 9;
             const TileCopy<DP> tile(lane, kv.dim);
+            if (a.q_box && w == 0) {
+                if (lane == 0) {
+                    mbar_arrive_tx(&q_full, (uint32_t)(used * C::kTileBytes));
+                    for (int t = 0; t < used; ++t)
+#pragma unroll
+                        for (int s = 0; s < C::kSlabs; ++s)
+                            tma_load_3d(qbase + t * C::kTileBytes + s * C::kSlab, &q_map, 64 * s, it.hk * a.G,
+                                        it.t0 + (it.row0 + t * kCM) / a.G, &q_full);
+                }
+                __syncwarp();
+            }
             // tiles of K and V in turn
             int x = w;
             for (; x < places; x += kCLoaders) {
@@ -407,6 +434,7 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
             // been filled again was read, and its barrier is a phase ahead)
             for (int y = x - kCLoaders; y >= 0 && y + kSt >= min(places, x); y -= kCLoaders)
                 mbar_wait_warp(&kv_full[y % kSt], (y / kSt) & 1, err, kWaitNs);
+            if (w == 0) mbar_wait_warp(&q_full, 0, err, kWaitNs);
         }
     }
     tc_fence_before();
@@ -418,10 +446,11 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
 }
 template <typename T, int DP>
 __global__ void __launch_bounds__(kCThreads, 1)
-    k_chunk(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap k_map,
-            const __grid_constant__ CUtensorMap v_map, uint32_t *__restrict__ err) {
+    k_chunk(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap q_map,
+            const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+            uint32_t *__restrict__ err) {
     follow(a.j.beside);
-    chunk_split<T, DP>(a, k_map, v_map, err);
+    chunk_split<T, DP>(a, q_map, k_map, v_map, err);
     end_after(a.j.beside);
 }
 
@@ -502,15 +531,16 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s, bool &jo
         a.part = static_cast<float4 *>(buf);
         a.stat = reinterpret_cast<float *>(static_cast<char *>(buf) + parts);
     }
-    CUtensorMap maps[2] = {};
+    CUtensorMap maps[3] = {};
+    a.q_box = rows_map(&maps[0], j, kv, a.G);
     a.box = page_box(kv);
     for (int v = 0; a.box && v < 2; ++v)
-        if (page_map(&maps[v], kv, v, j.type, a.box) != cudaSuccess) a.box = 0;
+        if (page_map(&maps[1 + v], kv, v, j.type, a.box) != cudaSuccess) a.box = 0;
     cudaError_t e = func_attr(reinterpret_cast<const void *>(k_chunk<T, DP>), cudaFuncAttributeMaxDynamicSharedMemorySize,
                               Chunk<DP>::kSmem);
     if (e != cudaSuccess) return e;
     e = launch_dependent(k_chunk<T, DP>, dim3((unsigned)items, (unsigned)a.splits), kCThreads, Chunk<DP>::kSmem, s, a,
-                         maps[0], maps[1], err);
+                         maps[0], maps[1], maps[2], err);
     joined = a.splits > 1;
     if (e == cudaSuccess && joined)
         e = a.splits > 8

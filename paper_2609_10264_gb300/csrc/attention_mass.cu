@@ -32,7 +32,7 @@ struct MassArgs {
     int G, negative;
     FastDiv group;  // G
     int box;        // keys per TMA box on a page, 0: none (see page_box)
-    bool q_box;     // a tile of rows is a TMA box
+    bool q_box;     // a tile of rows is a TMA box (see rows_map)
 };
 
 // ---------------------------------------------------------------- between the CTAs of a cluster
@@ -412,21 +412,6 @@ __global__ void __launch_bounds__(kCThreads, 1)
     end_after(a.j.beside);
 }
 
-// New rows as a tensor of (values, heads, tokens), for boxes of a key head's heads and
-// as many tokens as make a tile.
-cudaError_t rows_map(CUtensorMap *map, const AttendJob &j, const KvView &kv, int G) {
-    PFN_cuTensorMapEncodeTiled_v12000 encode = tensor_map_encoder();
-    if (!encode) return cudaErrorNotSupported;
-    const cuuint64_t dim[3] = {(cuuint64_t)kv.dim, (cuuint64_t)j.Hq, (cuuint64_t)kv.T};
-    const cuuint64_t stride[2] = {(cuuint64_t)j.q_head, (cuuint64_t)j.q_token};
-    const cuuint32_t part[3] = {64, (cuuint32_t)G, (cuuint32_t)(kCM / G)}, one[3] = {1, 1, 1};
-    const CUresult r = encode(map, j.type == PVMVMD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                              3, const_cast<void *>(j.q), dim, stride, part, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
 template <typename T, int DP>
 cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     MassArgs a{};
@@ -439,9 +424,7 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     CUtensorMap maps[2] = {};
     a.box = page_box(kv);
     if (a.box && page_map(&maps[0], kv, false, j.type, a.box) != cudaSuccess) a.box = 0;
-    // whole tokens in a tile, and strides that a tensor map can have
-    a.q_box = kCM % a.G == 0 && j.q_token > 0 && j.q_head > 0 &&
-              rows_map(&maps[1], j, kv, a.G) == cudaSuccess;
+    a.q_box = rows_map(&maps[1], j, kv, a.G);
     uint32_t *err = library_error_word();
     if (!err) return cudaErrorUnknown;
     int dev = 0, sms = 0;
