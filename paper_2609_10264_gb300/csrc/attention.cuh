@@ -276,11 +276,11 @@ struct TileCopy {
         return true;
     }
     // Once it is all there, for the MMAs.
-    __device__ __forceinline__ void arrive(uint64_t *bar) const {
+    __device__ __forceinline__ void arrive(uint64_t *bar, int tiles = 1) const {
         copy_wait<0>();
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar);
+        for (int t = 0; lane == 0 && t < tiles; ++t) mbar_arrive(bar);
     }
 };
 

@@ -92,6 +92,8 @@ struct ChunkItem {
 };
 __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int idx, ChunkItem &it) {
     const KvView &kv = a.kv;
+    // lengths, which are wanted once the sequence is found
+    asm volatile("prefetch.global.L1 [%0];" ::"l"(kv.lens + min((int)threadIdx.x, kv.B - 1)));
     const int hk = idx % kv.heads;
     const int64_t rank = idx / kv.heads;
     const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)chunk_tiles(a, b); },

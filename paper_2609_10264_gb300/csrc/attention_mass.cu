@@ -30,7 +30,7 @@ struct MassArgs {
     KvView kv;
     float scale2;
     int G, negative;
-    FastDiv group;  // G
+    FastDiv group, heads;  // G, key heads
     int box;        // keys per TMA box on a page, 0: none (see page_box)
     bool q_box;     // a tile of rows is a TMA box (see rows_map)
 };
@@ -82,7 +82,8 @@ template <int DP>
 struct Mass {
     static constexpr int kSlabs = DP / 64, kSlab = kCM * 128, kTileBytes = kSlabs * kSlab;
     static constexpr int kStages = 4;
-    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
+    static constexpr int kItems = DP == 64 ? 2 : 1;  // whose keys are there at a time
+    static constexpr int kSmem = (2 * kItems + kStages) * kTileBytes + 1024;
 };
 
 // Keys [first, len) of a sequence that some new row may see, in CTAs' shares.
@@ -107,17 +108,37 @@ struct MassItem {
         return t >= n ? rows : t <= 0 ? 0 : (int)t * a.G;
     }
 };
-// A cluster's items in order: every stride-th of all (shares of keys and their heads).
-// By whole warps.
+// A cluster's items in order: one of every `stride` of all (shares of keys and their
+// heads), in turns that go forth and back, as later shares have fewer rows.  By whole
+// warps.
 struct MassWalk {
-    int64_t idx, before;  // the next item, and the shares before sequence b
-    int b, stride, rank, size;
+    int64_t before;  // the shares before sequence b
+    int b, mine, stride, rank, size;
+    int turn = 0, at = -1;              // sequence that the following are of
+    int len = 0, n = 0, t0 = 0, first = 0, shares = 0;
+    __device__ __forceinline__ void enter(const MassArgs &a) {
+        if (b >= a.kv.B || at == b) return;
+        at = b;
+        len = a.kv.len(b);
+        n = a.kv.news(b);
+        t0 = a.kv.first(b);
+        first = mass_first(a, b);
+        shares = mass_shares(a, b);
+    }
     __device__ __forceinline__ bool next(const MassArgs &a, MassItem &it) {
         const KvView &kv = a.kv;
-        for (;; idx += stride) {
-            const int64_t share = idx / kv.heads;
+        for (enter(a);;) {
+            const int64_t idx = (int64_t)turn * stride + (turn & 1 ? stride - 1 - mine : mine);
+            int64_t share;
+            if (idx <= INT_MAX) {
+                uint32_t q, r;
+                a.heads.divmod((uint32_t)idx, q, r);
+                share = q;
+            } else {
+                share = idx / kv.heads;
+            }
             // the sequence that holds it, 32 at a time
-            while (b < kv.B && share >= before + mass_shares(a, b)) {
+            while (b < kv.B && share >= before + shares) {
                 const int lane = threadIdx.x & 31;
                 const int64_t n = b + lane < kv.B ? mass_shares(a, b + lane) : 0;
                 int64_t incl = n;
@@ -130,16 +151,18 @@ struct MassWalk {
                 const int to = at ? __ffs(at) - 1 : 32;
                 before += at ? __shfl_sync(kFull, incl - n, to) : __shfl_sync(kFull, incl, 31);
                 b += to;
+                enter(a);
             }
             if (b >= kv.B) return false;
+            ++turn;
             it.b = b;
             it.hk = (int)(idx - share * kv.heads);
-            it.len = kv.len(b);
-            it.n = kv.news(b);
-            it.t0 = kv.first(b);
-            it.rows = it.n * a.G;
-            it.old = it.len - it.n;
-            it.k0 = mass_first(a, b) + (int)(share - before) * kMKeys;
+            it.len = len;
+            it.n = n;
+            it.t0 = t0;
+            it.rows = n * a.G;
+            it.old = len - n;
+            it.k0 = first + (int)(share - before) * kMKeys;
             it.r0 = it.first_row(a, it.k0) / kCM * kCM;
             const int r1 = it.last_row(a, min(it.k0 + kMKeys, it.len) - 1);
             const int all = r1 > it.r0 ? (r1 - it.r0 + kCM - 1) / kCM : 0;
@@ -147,7 +170,6 @@ struct MassWalk {
             const int per = (all + size - 1) / size, from = min(all, rank * per);
             it.r0 += from * kCM;
             it.nt = min(all, from + per) - from;
-            idx += stride;
             return true;
         }
     }
@@ -160,7 +182,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
     using C = Mass<DP>;
     constexpr int kSt = C::kStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full, k_empty, mma_done;
+    __shared__ __align__(8) uint64_t full[kSt], empty[kSt], s_full[2][2], s_empty[2][2], k_full[C::kItems],
+        k_empty[C::kItems], mma_done;
     __shared__ __align__(8) uint64_t shift_full[kShifts], shift_empty[kShifts];
     __shared__ __align__(16) float s_shift[kShifts][kCM];
     // the sums of the cluster's other CTAs, in the first one's memory
@@ -173,7 +196,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const int warp = __shfl_sync(kFull, tid >> 5, 0);
     follow(a.j.beside);
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t ring = base + 2 * C::kTileBytes;
+    constexpr int kItems = C::kItems;
+    const uint32_t ring = base + 2 * kItems * C::kTileBytes;
     if (tid == 0) {
         for (int s = 0; s < kSt; ++s) {
             mbar_init(&full[s], 1);
@@ -183,8 +207,10 @@ __global__ void __launch_bounds__(kCThreads, 1)
             mbar_init(&s_full[t >> 1][t & 1], 1);
             mbar_init(&s_empty[t >> 1][t & 1], 4);
         }
-        mbar_init(&k_full, 2);
-        mbar_init(&k_empty, 1);
+        for (int s = 0; s < kItems; ++s) {
+            mbar_init(&k_full[s], 2);
+            mbar_init(&k_empty[s], 1);
+        }
         for (int s = 0; s < kShifts; ++s) {
             mbar_init(&shift_full[s], 32);
             mbar_init(&shift_empty[s], 8);
@@ -206,7 +232,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const int size = (int)cluster_size(), rank = (int)cluster_rank(), mine = (int)blockIdx.x / size;
     const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
                                     [&](int64_t) { return (int64_t)mine / kv.heads; });
-    MassWalk walk{(int64_t)mine, f.before, f.b < 0 ? kv.B : f.b, (int)gridDim.x / size, rank, size};
+    MassWalk walk{f.before, f.b < 0 ? kv.B : f.b, mine, (int)gridDim.x / size, rank, size};
     if (warp < 8)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
     else
@@ -224,9 +250,13 @@ __global__ void __launch_bounds__(kCThreads, 1)
         const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
         for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
             const int key = it.k0 + tile * kCM + (warp & 3) * 32 + lane;
-            int page, slot;
-            const bool real = key < it.len && kv.place(it.b, key, page, slot);
+            const bool real = key < it.len;
             const int lo = real ? it.first_row(a, key) : 0, hi = real ? it.last_row(a, key) : INT_MAX;
+            // (looked up while the first tile is on its way, and read while it is summed)
+            uint32_t slot, nth;
+            kv.ps.divmod((uint32_t)key, nth, slot);
+            const int page = real && rank == 0 ? kv.table[it.b * kv.table_stride + nth] : -1;
+            float *mass = nullptr, was = 0.0f;
             uint64_t sum[2] = {0u, 0u};
             for (int i = 0; i < it.nt; ++i) {
                 const uint32_t x = g + i;
@@ -234,6 +264,10 @@ __global__ void __launch_bounds__(kCThreads, 1)
                      mbar_wait_warp(&s_full[tile][x & 1], (x >> 1) & 1, err, kWaitNs);
                 if (!ok) break;
                 tc_fence_after();
+                if (i == 0 && page >= 0 && page < kv.pages) {
+                    mass = kv.mass_at(page, (int)slot, it.hk);
+                    was = *mass;
+                }
                 const int q0 = it.r0 + i * kCM;
                 const bool masked = __any_sync(kFull, q0 < lo || hi - kCM < q0);
                 // a quarter of the scores at a time, the next one on its way
@@ -251,9 +285,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
                         if (lane == 0) mbar_arrive(&s_empty[tile][x & 1]);
                     }
                     if (masked) {
+                        // bits of the rows that see this key
+                        const int from = lo - q0 - 32 * c, to = hi - q0 - 32 * c;
+                        uint32_t see = to >= 32 ? kFull : to <= 0 ? 0u : (1u << to) - 1u;
+                        if (from > 0) see = from >= 32 ? 0u : see & ~((1u << from) - 1u);
+                        if (__any_sync(kFull, see != kFull)) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (q0 + 32 * c + e < lo || q0 + 32 * c + e >= hi) v[e] = -INFINITY;
+                            for (int e = 0; e < 32; ++e) v[e] = see >> e & 1 ? v[e] : -INFINITY;
+                        }
                     }
                     const ulonglong2 *sh = reinterpret_cast<const ulonglong2 *>(s_shift[x % kShifts] + 32 * c);
 #pragma unroll
@@ -286,14 +325,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 __syncwarp();
                 if (lane < size - 1) peer_arrive(peer_addr(&sums_empty, (uint32_t)lane + 1));
             }
-            if (real) *kv.mass_at(page, slot, it.hk) += p;
+            if (mass) *mass = was + p;
         }
     } else if (warp == 8) {
         // ------------------------------------------------ MMA issuer
         const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
         for (; ok && walk.next(a, it); g += (uint32_t)it.nt, n += it.nt > 0) {
             if (it.nt == 0) continue;
-            ok = mbar_wait_warp(&k_full, n & 1, err, kWaitNs);
+            ok = mbar_wait_warp(&k_full[n % kItems], (n / kItems) & 1, err, kWaitNs);
             for (int i = 0; i < it.nt && ok; ++i) {
                 const uint32_t x = g + i;
                 ok = mbar_wait_warp(&full[x % kSt], (x / kSt) & 1, err, kWaitNs);
@@ -302,7 +341,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
                     ok = mbar_wait_warp(&s_empty[t][x & 1], ((x >> 1) & 1) ^ 1, err, kWaitNs);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t ad = sw128_desc(base + t * C::kTileBytes);
+                    const uint64_t ad = sw128_desc(base + (2 * (n % kItems) + t) * C::kTileBytes);
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < DP / 16; ++k) {
@@ -316,7 +355,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 if (elect_one()) commit(&empty[x % kSt]);
                 __syncwarp();
             }
-            if (elect_one()) commit(&k_empty);
+            if (elect_one()) commit(&k_empty[n % kItems]);
             __syncwarp();
         }
         // every MMA is through before the memory that it reads goes
@@ -330,49 +369,36 @@ __global__ void __launch_bounds__(kCThreads, 1)
         const TileCopy<DP> tile(lane, kv.dim);
         for (; ok && walk.next(a, it); g += (uint32_t)it.nt, n += it.nt > 0) {
             if (it.nt == 0) continue;
-            // the third takes the keys, and the lse2 of all rows (those past the end are masked)
-            if (w == 2) {
-                if (n > 0 && !mbar_wait_warp(&k_empty, (n - 1) & 1, err, kWaitNs)) break;
+            if (w == 2) {  // the third takes the keys
+                const uint32_t item = n % kItems;
+                if (n >= kItems && !mbar_wait_warp(&k_empty[item], ((n / kItems) & 1) ^ 1, err, kWaitNs)) break;
+                int copied = 0;
                 for (int t = 0; t < 2; ++t) {
-                    const uint32_t dst = base + t * C::kTileBytes;
+                    const uint32_t dst = base + (2 * item + t) * C::kTileBytes;
                     const int key0 = it.k0 + t * kCM;
-                    if (!a.box || key0 + kCM > it.len ||
-                        !tile.fetch(dst, &k_map, a.box, kv, it.b, it.hk, key0, &k_full)) {
-                        tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
-                            const bool is = key_place(kv, it.b, it.len, key0 + rr, kv.k_page, kv.k_slot, off);
-                            off += it.hk * kv.k_head;
-                            return is;
-                        });
-                        tile.arrive(&k_full);
-                    }
+                    if (a.box && key0 + kCM <= it.len &&
+                        tile.fetch(dst, &k_map, a.box, kv, it.b, it.hk, key0, &k_full[item]))
+                        continue;
+                    tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
+                        const bool is = key_place(kv, it.b, it.len, key0 + rr, kv.k_page, kv.k_slot, off);
+                        off += it.hk * kv.k_head;
+                        return is;
+                    });
+                    ++copied;
                 }
+                if (copied) tile.arrive(&k_full[item], copied);
+                continue;
             }
-            // the others tiles of rows in turn
+            // the others tiles of rows in turn, with their lse2 (rows past the end are masked)
             for (int i = 0; i < it.nt; ++i) {
-                const uint32_t x = g + i;
-                if (w < 2 && (int)(x & 1) != w) continue;
+                const uint32_t x = g + i, round = x / kSt;
+                if ((int)(x & 1) != w) continue;
+                static_assert(kSt == kShifts && kSt % 2 == 0);
                 // (each barrier has one warp that waits for it, which it then is never two phases
                 // ahead of)
-                uint64_t *const place = w == 2 ? &shift_empty[x % kShifts] : &empty[x % kSt];
-                const uint32_t round = w == 2 ? x / kShifts : x / kSt;
-                if (round > 0 && !mbar_wait_warp(place, (round & 1) ^ 1, err, kWaitNs)) {
-                    ok = false;
-                    break;
-                }
+                ok = round == 0 || mbar_wait_warp(&empty[x % kSt], (round & 1) ^ 1, err, kWaitNs);
+                if (!ok) break;
                 const int q0 = it.r0 + i * kCM;
-                if (w == 2) {
-                    const float *lse2 = j.lse2 + (int64_t)it.t0 * j.Hq + it.hk * a.G;
-                    const uint32_t sh = smem_addr(s_shift[x % kShifts]);
-#pragma unroll
-                    for (int y = 0; y < kCM / 32; ++y) {
-                        const int rr = 32 * y + lane, r = min(q0 + rr, it.rows - 1);
-                        uint32_t t, h;
-                        a.group.divmod((uint32_t)r, t, h);
-                        copy4(sh + 4 * rr, lse2 + (int64_t)t * j.Hq + h, true);
-                    }
-                    copy_arrive(&shift_full[x % kShifts]);
-                    continue;
-                }
                 const uint32_t dst = ring + (x % kSt) * C::kTileBytes;
                 last = x;
                 if (a.q_box) {
@@ -392,15 +418,29 @@ __global__ void __launch_bounds__(kCThreads, 1)
                     });
                     tile.arrive(&full[x % kSt]);
                 }
+                ok = round == 0 || mbar_wait_warp(&shift_empty[x % kShifts], (round & 1) ^ 1, err, kWaitNs);
+                if (!ok) break;
+                const float *lse2 = j.lse2 + (int64_t)it.t0 * j.Hq + it.hk * a.G;
+                const uint32_t sh = smem_addr(s_shift[x % kShifts]);
+#pragma unroll
+                for (int y = 0; y < kCM / 32; ++y) {
+                    const int rr = 32 * y + lane, r = min(q0 + rr, it.rows - 1);
+                    uint32_t t, h;
+                    a.group.divmod((uint32_t)r, t, h);
+                    copy4(sh + 4 * rr, lse2 + (int64_t)t * j.Hq + h, true);
+                }
+                copy_arrive(&shift_full[x % kShifts]);
             }
         }
+        copy_commit();
         copy_wait<0>();
         // copies in flight complete before the CTA may exit: of this warp's tiles the last
         // two, whose places nothing has filled since
         static_assert(kSt == 4, "every second tile, two of a round");
         for (int64_t y = last; w < 2 && y >= 0 && y > last - 4; y -= 2)
             mbar_wait_warp(&full[y % kSt], (uint32_t)(y / kSt) & 1, err, kWaitNs);
-        if (w == 2 && n > 0) mbar_wait_warp(&k_full, (n - 1) & 1, err, kWaitNs);
+        for (uint32_t y = n > kItems ? n - kItems : 0; w == 2 && y < n; ++y)
+            mbar_wait_warp(&k_full[y % kItems], (y / kItems) & 1, err, kWaitNs);
     }
     tc_fence_before();
     __syncthreads();
@@ -421,6 +461,7 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     a.G = j.Hq / kv.heads;
     a.negative = j.scale < 0.0f;
     a.group = FastDiv((uint32_t)a.G);
+    a.heads = FastDiv((uint32_t)kv.heads);
     CUtensorMap maps[2] = {};
     a.box = page_box(kv);
     if (a.box && page_map(&maps[0], kv, false, j.type, a.box) != cudaSuccess) a.box = 0;
