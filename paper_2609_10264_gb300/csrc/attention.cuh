@@ -242,28 +242,29 @@ struct TileCopy {
         }
         copy_commit();
     }
-    // The 128 keys from key0 on, all within the sequence, from their pages by the tensor
-    // memory accelerator: boxes of `box` keys that lie on one page, dealt out to the
-    // lanes; map: (values, slots, heads, pages).  False, and nothing done, where a page
-    // is not there.  (The swizzle goes by the address, so boxes of fewer than its eight
-    // rows fit too.)
+    // The 128 keys from key0 on from their pages by the tensor memory accelerator: boxes
+    // of `box` keys that lie on one page, dealt out to the lanes; map: (values, slots,
+    // heads, pages).  False, and nothing done, where a page is not there.  Behind the
+    // sequence's end the rows hold anything.  (The swizzle goes by the address, so boxes of
+    // fewer than its eight rows fit too.)
     __device__ __forceinline__ bool fetch(uint32_t dst, const CUtensorMap *map, int box, const KvView &kv, int b, int hk,
-                                          int key0, uint64_t *bar) const {
+                                          int key0, int len, uint64_t *bar) const {
+        const int end = max(0, min(kCM, (len - key0 + box - 1) / box * box));  // of the boxes
         int page[kCM / 32], slot[kCM / 32];
         bool there = true;
 #pragma unroll
         for (int x = 0; x < kCM / 32; ++x) {
             page[x] = slot[x] = 0;
             const int r = (32 * x + lane) * box;
-            if (r < kCM) there &= kv.place(b, key0 + r, page[x], slot[x]);
+            if (r < end) there &= kv.place(b, key0 + r, page[x], slot[x]);
         }
         if (!__all_sync(kFull, there)) return false;
-        if (lane == 0) mbar_arrive_tx(bar, DP / 64 * kCM * 128);
+        if (lane == 0) mbar_arrive_tx(bar, (uint32_t)(DP / 64 * end * 128));
         __syncwarp();
 #pragma unroll
         for (int x = 0; x < kCM / 32; ++x) {
             const int r = (32 * x + lane) * box;
-            if (r < kCM)
+            if (r < end)
 #pragma unroll
                 for (int s = 0; s < DP / 64; ++s)
                     asm volatile(

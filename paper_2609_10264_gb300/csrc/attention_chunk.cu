@@ -226,7 +226,8 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mx[k] = e + 2 * k + 1 < kCN ? max3(mx[k], s[e + 2 * k], s[e + 2 * k + 1]) : mx[k];
             const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
-            if (__any_sync(kFull, (top - m) * a.scale2 > kCHeadroom)) {  // -inf - -inf: not
+            // (-inf - -inf: not; rows that are not of the sequence have no say, as they see anything)
+            if (__any_sync(kFull, real && (top - m) * a.scale2 > kCHeadroom)) {
                 const float mn = fmaxf(m, top), w = m == -INFINITY ? 0.0f : exp2_fast((m - mn) * a.scale2);
                 m = mn;
                 l *= w;
@@ -413,12 +414,13 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
                 const int64_t ps = values ? kv.v_page : kv.k_page, ss = values ? kv.v_slot : kv.k_slot,
                               hs = it.hk * (values ? kv.v_head : kv.k_head);
                 const int key0 = (kt0 + i) * kCN;
-                if (a.box && key0 + kCN <= it.len) {
+                // (what is behind the end must be zero where a P of 0 meets it)
+                if (a.box && (!values || key0 + kCN <= it.len)) {
                     // (before the barrier that the copy itself completes)
                     if (!values && lane == 0) s_gap[i & 3] = false;
                     __syncwarp();
                     if (tile.fetch(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? &v_map : &k_map, a.box, kv, it.b,
-                                   it.hk, key0, &kv_full[x % kSt]))
+                                   it.hk, key0, it.len, &kv_full[x % kSt]))
                         continue;
                 }
                 bool gap = false;

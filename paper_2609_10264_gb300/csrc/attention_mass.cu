@@ -23,7 +23,6 @@ namespace {
 constexpr int kMKeys = 2 * kCM;  // keys per CTA
 constexpr int kShifts = 4;       // ring of the rows' lse2
 constexpr int kMostShare = 8;    // CTAs of a cluster
-constexpr int kSumRegs = 176, kCopyRegs = 144;  // of 168 a thread at launch
 
 struct MassArgs {
     AttendJob j;
@@ -233,22 +232,21 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
                                     [&](int64_t) { return (int64_t)mine / kv.heads; });
     MassWalk walk{f.before, f.b < 0 ? kv.B : f.b, mine, (int)gridDim.x / size, rank, size};
-    if (warp < 8)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
-    else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
-
     // Every role walks the CTA's items by itself, as far ahead as the barriers let it: a
-    // tile of rows is number g + i of all the CTA's, an item of keys number n.
+    // tile of rows is number g + i of all the CTA's, an item of keys number n.  (One loop,
+    // so that the walk's instructions are fetched once.)
     MassItem it;
     uint32_t g = 0, n = 0;
     bool ok = true;
-    if (warp < 8) {
-        // ------------------------------------------------ sums
-        const int tile = warp >> 2;
-        const uint64_t scale_2 = pair(a.scale2, a.scale2);
-        const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
-        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, ++n) {
+    const int w = warp - 9;
+    int64_t last = -1;  // tile of rows that this warp copied
+    const TileCopy<DP> tile(lane, kv.dim);
+    for (; ok && walk.next(a, it); g += (uint32_t)it.nt) {
+        if (warp < 8) {
+            // ------------------------------------------------ sums
+            const int tile = warp >> 2;
+            const uint64_t scale_2 = pair(a.scale2, a.scale2);
+            const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
             const int key = it.k0 + tile * kCM + (warp & 3) * 32 + lane;
             const bool real = key < it.len;
             const int lo = real ? it.first_row(a, key) : 0, hi = real ? it.last_row(a, key) : INT_MAX;
@@ -312,26 +310,28 @@ __global__ void __launch_bounds__(kCThreads, 1)
             unpair(add2(sum[0], sum[1]), p, q);
             p += q;
             if (!ok) break;
+            const uint32_t turn = n++;
             if (rank > 0) {  // to the first, once it has taken the item before
-                if (n > 0 && !peer_wait(&sums_empty, (n - 1) & 1, err)) break;
+                ok = turn == 0 || peer_wait(&sums_empty, (turn - 1) & 1, err);
+                if (!ok) break;
                 peer_store(peer_addr(&s_sums[rank - 1][tid], 0), p);
                 __syncwarp();
                 if (lane == 0) peer_arrive(peer_addr(&sums_full, 0));
                 continue;
             }
             if (size > 1) {
-                if (!peer_wait(&sums_full, n & 1, err)) break;
+                ok = peer_wait(&sums_full, turn & 1, err);
+                if (!ok) break;
                 for (int r = 1; r < size; ++r) p += s_sums[r - 1][tid];
                 __syncwarp();
                 if (lane < size - 1) peer_arrive(peer_addr(&sums_empty, (uint32_t)lane + 1));
             }
             if (mass) *mass = was + p;
-        }
-    } else if (warp == 8) {
-        // ------------------------------------------------ MMA issuer
-        const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
-        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, n += it.nt > 0) {
-            if (it.nt == 0) continue;
+        } else if (it.nt == 0) {
+            continue;
+        } else if (warp == 8) {
+            // ------------------------------------------------ MMA issuer
+            const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
             ok = mbar_wait_warp(&k_full[n % kItems], (n / kItems) & 1, err, kWaitNs);
             for (int i = 0; i < it.nt && ok; ++i) {
                 const uint32_t x = g + i;
@@ -357,18 +357,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
             }
             if (elect_one()) commit(&k_empty[n % kItems]);
             __syncwarp();
-        }
-        // every MMA is through before the memory that it reads goes
-        if (elect_one()) commit(&mma_done);
-        __syncwarp();
-        mbar_wait_warp(&mma_done, 0, err, kWaitNs);
-    } else {
-        // ------------------------------------------------ copies
-        const int w = warp - 9;
-        int64_t last = -1;
-        const TileCopy<DP> tile(lane, kv.dim);
-        for (; ok && walk.next(a, it); g += (uint32_t)it.nt, n += it.nt > 0) {
-            if (it.nt == 0) continue;
+            ++n;
+        } else {
+            // ------------------------------------------------ copies
             if (w == 2) {  // the third takes the keys
                 const uint32_t item = n % kItems;
                 if (n >= kItems && !mbar_wait_warp(&k_empty[item], ((n / kItems) & 1) ^ 1, err, kWaitNs)) break;
@@ -376,9 +367,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 for (int t = 0; t < 2; ++t) {
                     const uint32_t dst = base + (2 * item + t) * C::kTileBytes;
                     const int key0 = it.k0 + t * kCM;
-                    if (a.box && key0 + kCM <= it.len &&
-                        tile.fetch(dst, &k_map, a.box, kv, it.b, it.hk, key0, &k_full[item]))
-                        continue;
+                    if (a.box && tile.fetch(dst, &k_map, a.box, kv, it.b, it.hk, key0, it.len, &k_full[item])) continue;
                     tile.copy(dst, kv.K, [&](int rr, int64_t &off) {
                         const bool is = key_place(kv, it.b, it.len, key0 + rr, kv.k_page, kv.k_slot, off);
                         off += it.hk * kv.k_head;
@@ -387,6 +376,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
                     ++copied;
                 }
                 if (copied) tile.arrive(&k_full[item], copied);
+                ++n;
                 continue;
             }
             // the others tiles of rows in turn, with their lse2 (rows past the end are masked)
@@ -431,7 +421,15 @@ __global__ void __launch_bounds__(kCThreads, 1)
                 }
                 copy_arrive(&shift_full[x % kShifts]);
             }
+            ++n;
         }
+    }
+    if (warp == 8) {
+        // every MMA is through before the memory that it reads goes
+        if (elect_one()) commit(&mma_done);
+        __syncwarp();
+        mbar_wait_warp(&mma_done, 0, err, kWaitNs);
+    } else if (warp > 8) {
         copy_commit();
         copy_wait<0>();
         // copies in flight complete before the CTA may exit: of this warp's tiles the last

@@ -658,6 +658,34 @@ def test_same_bits_from_call_to_call(pv, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("news", [[1, 1, 1], [70, 40, 33], [200, 3, 150], [9, 130, 1]])
+@pytest.mark.parametrize("page", [16, 100, 1])
+@pytest.mark.parametrize("lens", [[300, 190, 517], [2000, 1300, 900]])
+def test_a_sequence_does_not_depend_on_what_is_not_its_own(pv, news, page, lens):
+    """Other numbers behind the ends and in the other sequences leave one's results bit for bit as they were."""
+    import torch
+    c = Cache(pv, lens, news, 2, 80, page, "bf16", 33)
+    q = _dev(3 * np.random.default_rng(5).standard_normal((sum(news), 8, 80)), "bf16")
+    r = slice(c.cu_host[1], c.cu_host[2])
+    p, o = c.at(1)
+    own = torch.zeros(c.K.shape[:2], dtype=torch.bool, device="cuda")
+    own[p, o] = True
+    seen = []
+    for fill in range(3):
+        c.mass.zero_()
+        out, z = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+        pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=out, lse=z, accumulate=True)
+        seen.append((out[r].clone(), z[r].clone(), c.mass[p, :, o].clone()))
+        for x in (c.K, c.V):
+            x[~own] = (torch.randn_like(x) * 10.0**fill)[~own]
+        q[:r.start].mul_(-7.0)
+        q[r.stop:].mul_(30.0)
+    assert pv.pvmvmd_device_status() == 0
+    for s in seen[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(s, seen[0]))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 64])
 def test_keys_that_are_not_numbers(pv, T):
     """A NaN key reaches the rows that see it, and no other row, sequence or head."""
