@@ -24,6 +24,7 @@ namespace pv {
 namespace {
 
 constexpr int kRows = 16;                 // rows per tile of them, of one MMA
+constexpr float kHeadroom = 8.0f;         // log2 of the largest P
 
 struct FewArgs {
     AttendJob j;
@@ -325,21 +326,16 @@ __global__ void __launch_bounds__(Few<DP, W>::kThreads, 8 / W) k_few(const __gri
                         if (r < rows) sc[key * a.score_rows + r] = s[t][e];
                     }
             }
-            float shift[2];
-            bool moved = false;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                mx[h] = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 1));
-                mx[h] = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 2));
-                mx[h] = fmaxf(m[h], mx[h]);
-                moved |= mx[h] != m[h];
-                shift[h] = mx[h] == -INFINITY ? 0.0f : mx[h];
-            }
-            if (__any_sync(kFull, moved)) {
+            // the maximum is raised where a score exceeds it by more than kHeadroom (in steps of
+            // exp2): a P of 2^8 and its sum have the same relative rounding
+            if (__any_sync(kFull, mx[0] - m[0] > kHeadroom || mx[1] - m[1] > kHeadroom)) {  // -inf - -inf: not
                 float w[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    w[h] = exp2_fast(m[h] - shift[h]);
+                    mx[h] = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 1));
+                    mx[h] = fmaxf(mx[h], __shfl_xor_sync(kFull, mx[h], 2));
+                    mx[h] = fmaxf(m[h], mx[h]);
+                    w[h] = exp2_fast(m[h] - (mx[h] == -INFINITY ? 0.0f : mx[h]));
                     l[h] *= w[h];
                     m[h] = mx[h];
                 }
@@ -348,6 +344,7 @@ __global__ void __launch_bounds__(Few<DP, W>::kThreads, 8 / W) k_few(const __gri
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[d][e] *= w[e >> 1];
             }
+            const float shift[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
 #pragma unroll
             for (int t = 0; t < kEights; ++t)
 #pragma unroll
