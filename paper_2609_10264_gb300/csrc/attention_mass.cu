@@ -9,8 +9,8 @@
 // while one is summed.  Few rows over many keys make many short items, so a CTA stays
 // and its rows' copies and sums run on from one item to the next (with a barrier at
 // each, five chunks of 35 tokens over 13000 keys took 130 us).  One exp2 a score bounds
-// it where there are many rows: 2048 tokens of 32 heads of 128 over 8192 keys 161 us
-// beside the attention's 164 (0.75 PFLOP/s, 2.9e12 exp2/s).
+// it where there are many rows: 2048 tokens of 32 heads of 128 over 8192 keys 138 us
+// beside the attention's 160 (0.87 PFLOP/s, 3.4e12 exp2/s).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -23,6 +23,10 @@ namespace {
 constexpr int kMKeys = 2 * kCM;  // keys per CTA
 constexpr int kShifts = 4;       // ring of the rows' lse2
 constexpr int kMostShare = 8;    // CTAs of a cluster
+// Warps: 0-15 sum, four of each tile of keys and of the even and of the odd tiles of rows
+// (four warps a scheduler, as a warp's sums wait for themselves: with two of them 158
+// us); 16 issues the MMAs; 17-19 copy.
+constexpr int kMSums = 16, kMThreads = 32 * (kMSums + 4);
 
 struct MassArgs {
     AttendJob j;
@@ -175,7 +179,7 @@ struct MassWalk {
 };
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kCThreads, 1)
+__global__ void __launch_bounds__(kMThreads, 1)
     k_mass(const __grid_constant__ MassArgs a, const __grid_constant__ CUtensorMap k_map,
            const __grid_constant__ CUtensorMap q_map, uint32_t *__restrict__ err) {
     using C = Mass<DP>;
@@ -188,6 +192,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
     // the sums of the cluster's other CTAs, in the first one's memory
     __shared__ float s_sums[kMostShare - 1][kMKeys];
     __shared__ __align__(8) uint64_t sums_full, sums_empty;
+    // the sums over odd tiles of rows
+    __shared__ float s_half[kMKeys];
+    __shared__ __align__(8) uint64_t half_full, half_empty;
     __shared__ uint32_t s_tmem;
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
@@ -217,9 +224,11 @@ __global__ void __launch_bounds__(kCThreads, 1)
         mbar_init(&mma_done, 1);
         mbar_init(&sums_full, 8 * max(1, (int)cluster_size() - 1));
         mbar_init(&sums_empty, 8);
+        mbar_init(&half_full, 8);
+        mbar_init(&half_empty, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) {
+    if (warp == kMSums) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -229,7 +238,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     const int size = (int)cluster_size(), rank = (int)cluster_rank(), mine = (int)blockIdx.x / size;
-    const Found f = find<kCThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
+    const Found f = find<kMThreads>(kv.B, [&](int b) { return (int64_t)mass_shares(a, b); },
                                     [&](int64_t) { return (int64_t)mine / kv.heads; });
     MassWalk walk{f.before, f.b < 0 ? kv.B : f.b, mine, (int)gridDim.x / size, rank, size};
     // Every role walks the CTA's items by itself, as far ahead as the barriers let it: a
@@ -238,45 +247,48 @@ __global__ void __launch_bounds__(kCThreads, 1)
     MassItem it;
     uint32_t g = 0, n = 0;
     bool ok = true;
-    const int w = warp - 9;
+    const int w = warp - kMSums - 1;
     int64_t last = -1;  // tile of rows that this warp copied
     const TileCopy<DP> tile(lane, kv.dim);
     for (; ok && walk.next(a, it); g += (uint32_t)it.nt) {
-        if (warp < 8) {
+        if (warp < kMSums) {
             // ------------------------------------------------ sums
-            const int tile = warp >> 2;
+            const int tile = (warp >> 2) & 1, odd = warp >> 3, own = tile * kCM + (warp & 3) * 32 + lane;
             const uint64_t scale_2 = pair(a.scale2, a.scale2);
             const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(tile * 2 * kCN);
-            const int key = it.k0 + tile * kCM + (warp & 3) * 32 + lane;
+            const int key = it.k0 + own;
             const bool real = key < it.len;
             const int lo = real ? it.first_row(a, key) : 0, hi = real ? it.last_row(a, key) : INT_MAX;
             // (looked up while the first tile is on its way, and read while it is summed)
             uint32_t slot, nth;
             kv.ps.divmod((uint32_t)key, nth, slot);
-            const int page = real && rank == 0 ? kv.table[it.b * kv.table_stride + nth] : -1;
+            const int page = real && rank == 0 && !odd ? kv.table[it.b * kv.table_stride + nth] : -1;
             float *mass = nullptr, was = 0.0f;
+            auto look = [&] {
+                if (mass || page < 0 || page >= kv.pages) return;
+                mass = kv.mass_at(page, (int)slot, it.hk);
+                was = *mass;
+            };
             uint64_t sum[2] = {0u, 0u};
-            for (int i = 0; i < it.nt; ++i) {
+            for (int i = (int)((g + odd) & 1); i < it.nt; i += 2) {
                 const uint32_t x = g + i;
                 ok = mbar_wait_warp(&shift_full[x % kShifts], (x / kShifts) & 1, err, kWaitNs) &&
                      mbar_wait_warp(&s_full[tile][x & 1], (x >> 1) & 1, err, kWaitNs);
                 if (!ok) break;
                 tc_fence_after();
-                if (i == 0 && page >= 0 && page < kv.pages) {
-                    mass = kv.mass_at(page, (int)slot, it.hk);
-                    was = *mass;
-                }
+                look();
                 const int q0 = it.r0 + i * kCM;
                 const bool masked = __any_sync(kFull, q0 < lo || hi - kCM < q0);
-                // a quarter of the scores at a time, the next one on its way
-                float s[2][32];
-                tmem_ld32_async(ts + (x & 1) * kCN, s[0]);
+                // some of the scores at a time, the next ones on their way
+                constexpr int kPart = 16;
+                float s[2][kPart];
+                tmem_ld16_async(ts + (x & 1) * kCN, s[0]);
 #pragma unroll
-                for (int c = 0; c < kCN / 32; ++c) {
+                for (int c = 0; c < kCN / kPart; ++c) {
                     float *v = s[c & 1];
                     tmem_ld_wait();
-                    if (c + 1 < kCN / 32) {
-                        tmem_ld32_async(ts + (x & 1) * kCN + 32 * (c + 1), s[(c + 1) & 1]);
+                    if (c + 1 < kCN / kPart) {
+                        tmem_ld16_async(ts + (x & 1) * kCN + kPart * (c + 1), s[(c + 1) & 1]);
                     } else {
                         tc_fence_before();
                         __syncwarp();
@@ -284,17 +296,18 @@ __global__ void __launch_bounds__(kCThreads, 1)
                     }
                     if (masked) {
                         // bits of the rows that see this key
-                        const int from = lo - q0 - 32 * c, to = hi - q0 - 32 * c;
-                        uint32_t see = to >= 32 ? kFull : to <= 0 ? 0u : (1u << to) - 1u;
-                        if (from > 0) see = from >= 32 ? 0u : see & ~((1u << from) - 1u);
-                        if (__any_sync(kFull, see != kFull)) {
+                        const int from = lo - q0 - kPart * c, to = hi - q0 - kPart * c;
+                        constexpr uint32_t kAll = (1u << kPart) - 1u;
+                        uint32_t see = to >= kPart ? kAll : to <= 0 ? 0u : (1u << to) - 1u;
+                        if (from > 0) see = from >= kPart ? 0u : see & ~((1u << from) - 1u);
+                        if (__any_sync(kFull, see != kAll)) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = see >> e & 1 ? v[e] : -INFINITY;
+                            for (int e = 0; e < kPart; ++e) v[e] = see >> e & 1 ? v[e] : -INFINITY;
                         }
                     }
-                    const ulonglong2 *sh = reinterpret_cast<const ulonglong2 *>(s_shift[x % kShifts] + 32 * c);
+                    const ulonglong2 *sh = reinterpret_cast<const ulonglong2 *>(s_shift[x % kShifts] + kPart * c);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
+                    for (int e = 0; e < kPart; e += 4) {
                         const ulonglong2 z = sh[e / 4];
                         float p, q;
                         unpair(fma2(pair(v[e], v[e + 1]), scale_2, z.x), p, q);
@@ -311,10 +324,24 @@ __global__ void __launch_bounds__(kCThreads, 1)
             p += q;
             if (!ok) break;
             const uint32_t turn = n++;
+            if (odd) {
+                ok = turn == 0 || mbar_wait_warp(&half_empty, (turn - 1) & 1, err, kWaitNs);
+                if (!ok) break;
+                s_half[own] = p;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&half_full);
+                continue;
+            }
+            look();
+            ok = mbar_wait_warp(&half_full, turn & 1, err, kWaitNs);
+            if (!ok) break;
+            p += s_half[own];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&half_empty);
             if (rank > 0) {  // to the first, once it has taken the item before
                 ok = turn == 0 || peer_wait(&sums_empty, (turn - 1) & 1, err);
                 if (!ok) break;
-                peer_store(peer_addr(&s_sums[rank - 1][tid], 0), p);
+                peer_store(peer_addr(&s_sums[rank - 1][own], 0), p);
                 __syncwarp();
                 if (lane == 0) peer_arrive(peer_addr(&sums_full, 0));
                 continue;
@@ -322,14 +349,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
             if (size > 1) {
                 ok = peer_wait(&sums_full, turn & 1, err);
                 if (!ok) break;
-                for (int r = 1; r < size; ++r) p += s_sums[r - 1][tid];
+                for (int r = 1; r < size; ++r) p += s_sums[r - 1][own];
                 __syncwarp();
                 if (lane < size - 1) peer_arrive(peer_addr(&sums_empty, (uint32_t)lane + 1));
             }
             if (mass) *mass = was + p;
         } else if (it.nt == 0) {
             continue;
-        } else if (warp == 8) {
+        } else if (warp == kMSums) {
             // ------------------------------------------------ MMA issuer
             const uint32_t idesc = chunk_idesc<T>(kCN) | (a.negative ? 1u << 13 : 0u);
             ok = mbar_wait_warp(&k_full[n % kItems], (n / kItems) & 1, err, kWaitNs);
@@ -424,12 +451,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
             ++n;
         }
     }
-    if (warp == 8) {
+    if (warp == kMSums) {
         // every MMA is through before the memory that it reads goes
         if (elect_one()) commit(&mma_done);
         __syncwarp();
         mbar_wait_warp(&mma_done, 0, err, kWaitNs);
-    } else if (warp > 8) {
+    } else if (warp > kMSums) {
         copy_commit();
         copy_wait<0>();
         // copies in flight complete before the CTA may exit: of this warp's tiles the last
@@ -443,7 +470,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     tc_fence_before();
     __syncthreads();
     cluster_meet();  // no peer's store or arrival is on its way here
-    if (warp == 8) {
+    if (warp == kMSums) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
@@ -475,7 +502,7 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
     // CTAs of a cluster: as many as let all be through first, in turns of items with as
     // many tiles of rows each, and as long as three beside them (four with peers).  (2051
     // tokens of 8 heads a key head over themselves: 194 us a call with a CTA an item, 95
-    // with clusters.)
+    // with clusters; 83 now.)
     int share = 1;
     int64_t best = INT64_MAX;
     for (int n = 1; n <= kMostShare; n *= 2) {
@@ -486,7 +513,7 @@ cudaError_t mass(const AttendJob &j, const KvView &kv, cudaStream_t s) {
                                     cudaFuncAttributeMaxDynamicSharedMemorySize, Mass<DP>::kSmem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)(std::min<int64_t>(items, std::max(1, sms / share)) * share);
-    return launch_cluster(k_mass<T, DP>, dim3(grid), share, kCThreads, Mass<DP>::kSmem, s, a, maps[0], maps[1], err);
+    return launch_cluster(k_mass<T, DP>, dim3(grid), share, kMThreads, Mass<DP>::kSmem, s, a, maps[0], maps[1], err);
 }
 
 }  // namespace
