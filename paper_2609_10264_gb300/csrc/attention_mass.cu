@@ -2,8 +2,8 @@
 // rows that see key j of exp2(scale2 q.k_j - lse2), after the attention itself has
 // written lse2, each row's log2 of the sum.
 //
-// Keys are the rows of the product here, so that a thread holds a key and its sum
-// needs no other thread, and no atomics: S^T = K Q^T.  A CTA keeps two tiles of 128
+// Keys are the rows of the product here, so that a thread holds a key, over every second
+// tile of rows, and no atomics are needed: S^T = K Q^T.  A CTA keeps two tiles of 128
 // keys and walks the rows that see them in tiles of 128 through a ring; each of the
 // two has two accumulators in TMEM, so that the tensor cores work on the next tile
 // while one is summed.  Few rows over many keys make many short items, so a CTA stays
