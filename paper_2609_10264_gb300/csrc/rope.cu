@@ -8,7 +8,7 @@
 // 2^-24 of the angle.  (In 32-bit floating point the angle alone is 2^-9 off at
 // position 30000.)
 //
-// Bound by memory: 4097 tokens of 32 heads of 96 in 32 bits 23 us (4.4 TB/s), 6001
+// Bound by memory: 4097 tokens of 32 heads of 96 in 32 bits 18 us (5.5 TB/s), 6001
 // tokens of 64 + 8 + 8 heads of 128 into a cache 46 us (5.3 TB/s).
 #include <algorithm>
 
@@ -230,12 +230,15 @@ cudaError_t rope_launch(const RopeArgs &a, cudaStream_t s) {
     if (rows_ok<In, Out>(a)) {
         const int units = j.interleaved ? j.dim / kGroup : j.rot / (2 * kGroup) + (j.dim - j.rot) / kGroup;
         // Heads a CTA: all, or as many as four turns of its threads take where the
-        // tokens alone would leave SMs without one.  Tokens a CTA: up to eight turns.
+        // tokens alone would leave SMs without one.  Tokens a CTA: up to six turns, but more
+        // than one turn only where twelve CTAs an SM are left (eight run at a time, so that
+        // fewer leave a long tail: 4097 tokens of 32 heads of 96 in 32 bits with 1 token a
+        // CTA 18.9 us, 2 18.2, 3 21.0, 4 22.8, 5 23.5).
         const int turn = std::max(1, kRowThreads / units), sms = 152;
         RowPlan plan;
         plan.heads = j.T >= 4 * sms ? a.heads : std::min(a.heads, j.T >= sms ? 4 * turn : turn);
-        plan.tokens = std::max(1, std::min({kMostTokens, kMostSines / std::max(1, j.rot / 2), 8 * turn / plan.heads,
-                                            j.T / (4 * sms)}));
+        plan.tokens = std::max(1, std::min({kMostTokens, kMostSines / std::max(1, j.rot / 2), 6 * turn / plan.heads,
+                                            j.T / (4 * sms), std::max(j.T / (12 * sms), turn / plan.heads)}));
         plan.units = FastDiv((uint32_t)units);
         plan.per = FastDiv((uint32_t)plan.heads);
         const dim3 grid((unsigned)((j.T + plan.tokens - 1) / plan.tokens),
