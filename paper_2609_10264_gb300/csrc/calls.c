@@ -157,6 +157,10 @@ static int arity(Py_ssize_t n, Py_ssize_t want) {
     if (n != want) PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, n);
     return n == want;
 }
+static int ready(Py_ssize_t n, Py_ssize_t want) {
+    if (!f_rope) PyErr_SetString(PyExc_RuntimeError, "the library has not been opened");
+    return f_rope && arity(n, want);
+}
 #define CALL(status, call)       \
     Py_BEGIN_ALLOW_THREADS       \
     status = call;               \
@@ -169,7 +173,7 @@ static PyObject *rope(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     Rows x, out;
     PyObject *type;
     int in_code, out_code, status;
-    if (!arity(n, 6) || !address(a[0], &view) || !dims(a[2], "x", 3, d) || !rows(a[2], "x", d[0], d[1], d[2], NULL, &x) ||
+    if (!ready(n, 6) || !address(a[0], &view) || !dims(a[2], "x", 3, d) || !rows(a[2], "x", d[0], d[1], d[2], NULL, &x) ||
         !type_code(a[2], "x", 1, &in_code, &type) || !rows(a[3], "out", d[0], d[1], d[2], NULL, &out) ||
         !type_code(a[3], "out", 0, &out_code, &type) || !vector(a[1], "positions", d[0], t_int32, &pos))
         return NULL;
@@ -188,7 +192,7 @@ static PyObject *append(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     Rows k, v, q = {0}, out = {0};
     PyObject *type;
     int code, status;
-    if (!arity(n, 10) || !address(a[0], &pp) || !address(a[1], &bp) || !address(a[2], &view)) return NULL;
+    if (!ready(n, 10) || !address(a[0], &pp) || !address(a[1], &bp) || !address(a[2], &view)) return NULL;
     const pvmvmd_kv_pool *pool = pp;
     pvmvmd_kv_batch *batch = bp;
     if (!dims(a[5], "k", 3, d) || !rows(a[5], "k", d[0], pool->heads, pool->dim, NULL, &k) ||
@@ -214,7 +218,7 @@ static PyObject *attend(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     int64_t d[3];
     Rows q, out;
     int window, status;
-    if (!arity(n, 10) || !address(a[0], &pp) || !address(a[1], &bp)) return NULL;
+    if (!ready(n, 10) || !address(a[0], &pp) || !address(a[1], &bp)) return NULL;
     const pvmvmd_kv_pool *pool = pp;
     pvmvmd_kv_batch *batch = bp;
     if (!dims(a[2], "q", 3, d) || !rows(a[2], "q", d[0], d[1], pool->dim, pool_type(pool), &q) ||
@@ -236,7 +240,7 @@ static PyObject *evict(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     void *pp, *bp, *table, *lens, *stream;
     int64_t d[2], s[2];
     int budget, recent, status;
-    if (!arity(n, 7) || !address(a[0], &pp) || !address(a[1], &bp)) return NULL;
+    if (!ready(n, 7) || !address(a[0], &pp) || !address(a[1], &bp)) return NULL;
     const pvmvmd_kv_batch *batch = bp;
     if (!to_int(a[2], "budget", &budget) || !to_int(a[3], "recent", &recent)) return NULL;
     if (!on_device(a[4], "new_table") || !same_type(a[4], "new_table", t_int32) || !dims(a[4], "new_table", 2, d) ||
