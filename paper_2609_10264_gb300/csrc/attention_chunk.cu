@@ -127,7 +127,13 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t q_full, kv_full[kSt], kv_empty[kSt], s_full[2], p_full[2][2], o_done[2], mma_done;
     __shared__ uint32_t s_tmem;
-    __shared__ bool s_gap[4];  // whether keys of a tile are not there
+    // Whether keys of tile i are not there, at i % kGaps.  K's tiles lie two places apart in
+    // the ring, and the place of tile i is free once the MMAs on it are through, which the
+    // softmax warps' reading of its flag is not.  Tile i + 8 waits for the place of tile
+    // i + 4 or a later one, whose MMAs follow P of tile i + 3, and with it that reading.
+    constexpr int kGaps = 8;
+    static_assert(kSt <= kGaps, "a place is taken again by tile i + kGaps / 2 at the earliest");
+    __shared__ bool s_gap[kGaps];
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 31;
@@ -200,7 +206,7 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
 #pragma unroll
             for (int c = 0; c < kCN / 32; ++c) tmem_ld32_async(ts + 32 * c, s + 32 * c);
             const int k0 = (kt0 + i) * kCN;
-            const bool gap = s_gap[i & 3];
+            const bool gap = s_gap[i % kGaps];
             tmem_ld_wait();
             if (__any_sync(kFull, k0 < lo || hi - kCN < k0) || gap) {
 #pragma unroll
@@ -417,7 +423,7 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
                 // (what is behind the end must be zero where a P of 0 meets it)
                 if (a.box && (!values || key0 + kCN <= it.len)) {
                     // (before the barrier that the copy itself completes)
-                    if (!values && lane == 0) s_gap[i & 3] = false;
+                    if (!values && lane == 0) s_gap[i % kGaps] = false;
                     __syncwarp();
                     if (tile.fetch(ring + (uint32_t)(x % kSt) * C::kTileBytes, values ? &v_map : &k_map, a.box, kv, it.b,
                                    it.hk, key0, it.len, &kv_full[x % kSt]))
@@ -431,7 +437,7 @@ __device__ __forceinline__ void chunk_split(const ChunkArgs &a, const CUtensorMa
                     return is;
                 });
                 gap = __any_sync(kFull, gap);
-                if (!values && lane == 0) s_gap[i & 3] = gap;
+                if (!values && lane == 0) s_gap[i % kGaps] = gap;
                 tile.arrive(&kv_full[x % kSt]);
             }
             // copies in flight complete before the CTA may exit (a tile whose place has

@@ -1,0 +1,77 @@
+"""The client's attention where its ranges end.  Tolerances are those of test_attention.py."""
+import numpy as np
+import pytest
+
+from test_attention import U, Cache, _dev, _host, pv  # noqa: F401
+
+
+def attend_there(q, K, V, there, n, scale, causal=True, window=0):
+    """test_attention.attend over the keys that are there."""
+    L, H, D = K.shape
+    Hq = q.shape[1]
+    out, lse, mass = np.zeros((n, Hq, D)), np.full((n, Hq), -np.inf), np.zeros((H, L))
+    pabs, vabs, e = np.zeros((n, Hq, D)), np.zeros((n, Hq, D)), np.zeros((n, Hq))
+    j = np.arange(L)
+    for t in range(n):
+        at = L - n + t
+        see = there & (j <= at if causal else True) & (at - j < window if window else True)
+        if not see.any():
+            continue
+        for h in range(Hq):
+            hk = h // (Hq // H)
+            k, v = K[see, hk], V[see, hk]
+            s = scale * (k @ q[t, h])
+            z = s.max() + np.log(np.exp(s - s.max()).sum())
+            p = np.exp(s - z)
+            out[t, h], lse[t, h] = p @ v, z
+            pabs[t, h], vabs[t, h] = p @ np.abs(v), np.abs(v).sum(0)
+            e[t, h] = 2.0**-24 * (D + 16) * (abs(scale) * (np.abs(k) @ np.abs(q[t, h]))).max() + 2.0**-20
+            mass[hk, see] += p
+    return out, lse, mass, pabs, vabs, e
+
+
+def check_rows(kind, got, z, ref):
+    """Outputs and log sums within the bounds of test_attention.py."""
+    o, lse, _, pabs, vabs, e = ref
+    u = U[kind]
+    tol = (u * np.abs(o) + (u + 2 * e[..., None]) * pabs + (2.0**-24 * vabs if kind == "f16" else 0) + 1e-30) * (1 + u)
+    assert (np.abs(got - o) <= tol).all(), np.abs(got - o).max()
+    real = np.where(np.isinf(lse), 0, lse)
+    assert np.where(np.isinf(lse), z == lse, np.abs(z - real) <= e + 2.0**-20 * (1 + np.abs(real))).all()
+
+
+# ---------------------------------------------------------------- pages that are not there
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,kind", [(64, "bf16"), (40, "f16"), (128, "f16"), (96, "bf16")])
+@pytest.mark.parametrize("page", [16, 24, 100, 7])  # boxes of 16, 8 and 4 keys, and none
+@pytest.mark.parametrize("T,L", [(150, 1500), (150, 620), (40, 2100), (1, 1500), (5, 900)])
+@pytest.mark.parametrize("holes", ["first", "middle", "last", "all three"])
+def test_missing_pages_in_any_tile(pv, D, kind, page, T, L, holes):
+    """Keys on pages outside the pool, in the first, a middle and the last of five to seventeen tiles of 128 keys:
+    they have no weight, and every other key has its own."""
+    import torch
+    c = Cache(pv, [L, 300], [T, T], 1, D, page, kind, 41)
+    there = np.ones(L, bool)
+    first, middle, last = {0}, {L // 2 // page, L // 2 // page + 1}, {(L - 1) // page}
+    gone = {"first": first, "middle": middle, "last": last, "all three": first | middle | last}[holes]
+    for i, p in enumerate(sorted(gone)):
+        c.table[0, p] = -1 - i if i % 2 else 1 << 30
+        there[p * page:(p + 1) * page] = False
+    G = 4
+    q = _dev(np.random.default_rng(42).standard_normal((2 * T, G, D)), kind)
+    out, z = torch.full_like(q, 7.0), torch.full((2 * T, G), 7.0, device="cuda")
+    pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=out, lse=z, accumulate=True)
+    assert pv.pvmvmd_device_status() == 0
+    qh, oh, zh, mh = _host(q), _host(out), _host(z), _host(c.mass)
+    touched = np.zeros(mh.shape, bool)
+    for b, (n, t) in enumerate(((L, there), (300, np.ones(300, bool)))):
+        r = slice(b * T, (b + 1) * T)
+        ref = attend_there(qh[r], c.rows(b, "K"), c.rows(b, "V"), t, T, D**-0.5)
+        check_rows(kind, oh[r], zh[r], ref)
+        m, e = ref[2], ref[5]
+        got, was = c.masses(b, mh), c.masses(b, c.mass0.astype(np.float64))
+        assert (np.abs(got - was - m) <= m * (2 * e.max() + 2.0**-18) + 2.0**-22 * (was + m)).all()
+        p, o = c.at(b)
+        touched[p[t], :, o[t]] = True
+    assert np.array_equal(mh[~touched], c.mass0.astype(np.float64)[~touched])
