@@ -33,14 +33,15 @@ cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_
     AttendJob j = job;
     const int G = j.Hq / kv.heads;
     j.few_rows = few_rows(j, kv);
-    const bool one = kv.B == 1;  // which has all the new tokens
     bool few = false, joined = false;
-    if (G > j.few_rows)
+    const int64_t most = (int64_t)j.max_new * G;  // rows of a sequence
+    if (G > j.few_rows || (kv.B == 1 && most > j.few_rows)) {
+        // A single sequence goes there whole, however few of `most` rows the device finds.
         j.few_rows = 0;
-    else if (!(one && (int64_t)kv.T * G > j.few_rows)) {
+    } else {
         const cudaError_t e = launch_attention_few(j, kv, s);
         if (e != cudaSuccess) return e;
-        if (one || j.max_new <= j.few_rows / G) return launch_attention_few_finish(j, kv, s);
+        if (most <= j.few_rows) return launch_attention_few_finish(j, kv, s);
         few = true;
     }
     if (j.accumulate) {

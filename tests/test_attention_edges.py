@@ -75,3 +75,34 @@ def test_missing_pages_in_any_tile(pv, D, kind, page, T, L, holes):
         p, o = c.at(b)
         touched[p[t], :, o[t]] = True
     assert np.array_equal(mh[~touched], c.mass0.astype(np.float64)[~touched])
+
+
+# ---------------------------------------------------------------- one sequence with fewer tokens than rows
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("T,n,known", [(40, 2, True), (40, 2, False), (300, 1, True), (300, 1, False), (40, 30, True),
+                                       (40, 30, False), (40, 0, False), (9, 3, True), (9, 3, False)])
+@pytest.mark.parametrize("L", [700, 90])
+def test_one_sequence_of_fewer_tokens_than_rows(pv, T, n, known, L, accumulate):
+    """B = 1 and n of the T rows: bounded by max_new, or by a cu that ends before T.  The n come out as they do in a
+    call of n rows, and the others are left alone."""
+    import torch
+    H, G, D = 2, 8, 64
+    c = Cache(pv, [L], [max(n, 1)], H, D, 16, "bf16", 43)
+    q = _dev(np.random.default_rng(44).standard_normal((T, H * G, D)), "bf16")
+    cu = torch.tensor([0, T if known else n], dtype=torch.int32, device="cuda")
+    batch = pv.KvBatch(c.table, c.dlens, cu, max_new=n if known else 0)
+    out, z = torch.full_like(q, 7.0), torch.full((T, H * G), 7.0, device="cuda")
+    pv.pvmvmd_paged_attention(c.pool, batch, q, out=out, lse=z, accumulate=accumulate)
+    assert pv.pvmvmd_device_status() == 0
+    assert (out[n:] == 7).all() and (z[n:] == 7).all()
+    mh = _host(c.mass)
+    if n == 0:
+        assert np.array_equal(mh, c.mass0.astype(np.float64))
+        return
+    ref = attend_there(_host(q[:n]), c.rows(0, "K"), c.rows(0, "V"), np.ones(L, bool), n, D**-0.5)
+    check_rows("bf16", _host(out[:n]), _host(z[:n]), ref)
+    m = ref[2] if accumulate else 0 * ref[2]
+    got, was = c.masses(0, mh), c.masses(0, c.mass0.astype(np.float64))
+    assert (np.abs(got - was - m) <= m * (2 * ref[5].max() + 2.0**-18) + 2.0**-22 * (was + m)).all()
