@@ -118,7 +118,8 @@ __device__ __forceinline__ Share share(const FewArgs &a, int b) {
     s.len = a.kv.len(b);
     s.rows = s.n * a.G;
     s.rts = (s.rows + kRows - 1) / kRows;
-    s.first = a.j.window > 0 ? max(0, s.len - s.n - a.j.window + 1) >> a.tile_log << a.tile_log : 0;
+    const int at = s.len - s.n;  // of the first new token
+    s.first = a.j.window > 0 && at >= a.j.window ? (at - a.j.window + 1) >> a.tile_log << a.tile_log : 0;
     s.tiles = max(1, (s.len - s.first + (1 << a.tile_log) - 1) >> a.tile_log);
     s.units = a.whole ? 1 : kSetUp + s.tiles;
     s.work = s.rows <= 0 || s.rows > a.j.few_rows ? 0 : (int64_t)s.units * a.kv.heads * s.rts;

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from test_attention import U, Cache, _dev, _host, pv  # noqa: F401
+from test_attention import U, Cache, _dev, _host, check_attention, pv  # noqa: F401
 
 
 def attend_there(q, K, V, there, n, scale, causal=True, window=0):
@@ -106,3 +106,15 @@ def test_one_sequence_of_fewer_tokens_than_rows(pv, T, n, known, L, accumulate):
     m = ref[2] if accumulate else 0 * ref[2]
     got, was = c.masses(0, mh), c.masses(0, c.mass0.astype(np.float64))
     assert (np.abs(got - was - m) <= m * (2 * ref[5].max() + 2.0**-18) + 2.0**-22 * (was + m)).all()
+
+
+# ---------------------------------------------------------------- windows
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 3, 2**30, 40])
+@pytest.mark.parametrize("lens,news", [([5, 700], [9, 1]), ([5, 1700], [20, 2]), ([0, 2100], [16, 1]), ([30], [60])])
+@pytest.mark.parametrize("Hq", [1, 3])
+def test_windows_over_sequences_shorter_than_their_new_tokens(pv, window, lens, news, Hq):
+    """The largest windows, where the first new token lies in front of its sequence's start."""
+    check_attention(pv, lens, news, Hq, 1, 64, 16, "bf16", 45, window=window, accumulate=True)
+    check_attention(pv, lens, news, Hq, 1, 128, 16, "f16", 46, window=window)
