@@ -194,7 +194,7 @@ static PyObject *append(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     int code, status;
     if (!ready(n, 10) || !address(a[0], &pp) || !address(a[1], &bp) || !address(a[2], &view)) return NULL;
     const pvmvmd_kv_pool *pool = pp;
-    pvmvmd_kv_batch *batch = bp;
+    pvmvmd_kv_batch batch = *(const pvmvmd_kv_batch *)bp; /* (other threads' calls may use it with rows of theirs) */
     if (!dims(a[5], "k", 3, d) || !rows(a[5], "k", d[0], pool->heads, pool->dim, NULL, &k) ||
         !type_code(a[5], "k", 1, &code, &type) || !rows(a[6], "v", d[0], pool->heads, pool->dim, type, &v))
         return NULL;
@@ -206,8 +206,8 @@ static PyObject *append(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     const double scale = PyFloat_AsDouble(a[4]);
     if (PyErr_Occurred() || !stream_of(a[9], &stream)) return NULL;
     if (d[0] > INT_MAX || dq[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
-    batch->T = (int)d[0];
-    CALL(status, f_append(pool, batch, view, pos, code, (float)scale, k.p, k.token, k.head, v.p, v.token, v.head,
+    batch.T = (int)d[0];
+    CALL(status, f_append(pool, &batch, view, pos, code, (float)scale, k.p, k.token, k.head, v.p, v.token, v.head,
                           (int)dq[1], q.p, q.token, q.head, out.p, out.token, out.head, stream))
     return PyLong_FromLong(status);
 }
@@ -220,7 +220,7 @@ static PyObject *attend(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     int window, status;
     if (!ready(n, 10) || !address(a[0], &pp) || !address(a[1], &bp)) return NULL;
     const pvmvmd_kv_pool *pool = pp;
-    pvmvmd_kv_batch *batch = bp;
+    pvmvmd_kv_batch batch = *(const pvmvmd_kv_batch *)bp; /* (other threads' calls may use it with rows of theirs) */
     if (!dims(a[2], "q", 3, d) || !rows(a[2], "q", d[0], d[1], pool->dim, pool_type(pool), &q) ||
         !rows(a[3], "out", d[0], d[1], pool->dim, pool_type(pool), &out) ||
         (a[4] != Py_None && !vector(a[4], "lse", d[0] * d[1], t_float[2], &lse)))
@@ -229,8 +229,8 @@ static PyObject *attend(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     const int causal = PyObject_IsTrue(a[6]), accumulate = PyObject_IsTrue(a[8]);
     if (PyErr_Occurred() || !to_int(a[7], "window", &window) || !stream_of(a[9], &stream)) return NULL;
     if (d[0] > INT_MAX || d[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
-    batch->T = (int)d[0];
-    CALL(status, f_attend(pool, batch, (int)d[1], q.p, q.token, q.head, (float)scale, causal, window, accumulate, out.p,
+    batch.T = (int)d[0];
+    CALL(status, f_attend(pool, &batch, (int)d[1], q.p, q.token, q.head, (float)scale, causal, window, accumulate, out.p,
                           out.token, out.head, lse, stream))
     return PyLong_FromLong(status);
 }
