@@ -474,7 +474,9 @@ int pvmvmd_kv_append(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, c
  * is not finite gives rows that see it NaN; a value that is not finite may reach
  * rows of the same call that do not see it (0 times it), among the keys in reach of
  * any of them.  Partial results of long sequences live in library scratch held per
- * stream, as for pvmvmd_server_mvm.  T = 0 does nothing. */
+ * stream, as for pvmvmd_server_mvm; this call and pvmvmd_kv_evict, of several kernels
+ * each, may be made from several threads on one stream, where one is enqueued whole
+ * before the next.  T = 0 does nothing. */
 int pvmvmd_paged_attention(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, int Hq, const void *q_dev,
                            int64_t q_token, int64_t q_head, float scale, int causal, int window, int accumulate,
                            void *out_dev, int64_t out_token, int64_t out_head, float *lse_dev, void *stream);

@@ -197,6 +197,7 @@ int pvmvmd_paged_attention(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *ba
     j.scale = scale;
     j.causal = causal != 0;
     j.accumulate = accumulate != 0;
+    const StreamTurn turn(static_cast<cudaStream_t>(stream));
     PV_CUDA(launch_attention(j, kv, static_cast<cudaStream_t>(stream)));
     return PVMVMD_OK;
 }
@@ -213,6 +214,7 @@ int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, in
     const int64_t room = (int64_t)new_max_pages * pool->page_size;
     if (room < budget && room < (int64_t)kv.max_pages * pool->page_size) return PVMVMD_E_SHAPE;
     const EvictJob j{budget, recent, new_table_dev, new_table_stride, new_lens_dev};
+    const StreamTurn turn(static_cast<cudaStream_t>(stream));
     PV_CUDA(launch_evict(j, kv, static_cast<cudaStream_t>(stream)));
     return PVMVMD_OK;
 }

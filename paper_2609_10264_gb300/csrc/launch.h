@@ -3,6 +3,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <mutex>
 
 #include <cuda_runtime.h>
 
@@ -199,6 +200,20 @@ cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out)
 // Whether stream_scratch would return a buffer here: one that is large enough
 // already, or a stream that is not being captured.
 bool stream_scratch_ready(int purpose, size_t need, cudaStream_t s);
+
+// The calling thread's turn on a stream: held by a call while it enqueues several
+// kernels that share the stream's scratch, so that those of another thread's call on
+// that stream come before or after all of them.
+class StreamTurn {
+  public:
+    explicit StreamTurn(cudaStream_t s);
+    ~StreamTurn();
+    StreamTurn(const StreamTurn &) = delete;
+    StreamTurn &operator=(const StreamTurn &) = delete;
+
+  private:
+    std::mutex *mu_;
+};
 
 // cudaFuncSetAttribute for the current device, done once per (kernel,
 // attribute, device): function attributes belong to each device's instance

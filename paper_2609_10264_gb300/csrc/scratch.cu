@@ -33,7 +33,19 @@ struct Buf {
 constexpr size_t kGrowSlack = 32u << 20;
 std::mutex g_bufs_mu;
 std::map<std::tuple<int, int, cudaStream_t>, Buf> g_bufs;
+std::map<std::pair<int, cudaStream_t>, std::mutex> g_turns;  // under g_bufs_mu, each kept for good
 }  // namespace
+
+StreamTurn::StreamTurn(cudaStream_t s) : mu_(nullptr) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) (void)cudaGetLastError();
+    {
+        std::lock_guard<std::mutex> lock(g_bufs_mu);
+        mu_ = &g_turns[std::make_pair(dev, s)];
+    }
+    mu_->lock();
+}
+StreamTurn::~StreamTurn() { mu_->unlock(); }
 
 bool stream_scratch_ready(int purpose, size_t need, cudaStream_t s) {
     int dev = 0;

@@ -118,3 +118,44 @@ def test_windows_over_sequences_shorter_than_their_new_tokens(pv, window, lens, 
     """The largest windows, where the first new token lies in front of its sequence's start."""
     check_attention(pv, lens, news, Hq, 1, 64, 16, "bf16", 45, window=window, accumulate=True)
     check_attention(pv, lens, news, Hq, 1, 128, 16, "f16", 46, window=window)
+
+
+# ---------------------------------------------------------------- threads
+
+@pytest.mark.gpu
+def test_threads_on_one_stream(pv):
+    """Two threads attend (in parts, with weights) and evict on one stream, over caches of their own, as the scratch
+    that they share grows: the same bits as one after the other."""
+    import threading
+
+    import torch
+    sizes = [([3000, 40], [1, 1]), ([9000, 333, 50], [1, 2, 1]), ([700, 12000], [60, 1]), ([20000], [3])]
+
+    def work(seed, stream):
+        out, kept = [], []  # (what the stream's kernels read stays)
+        for i, (lens, news) in enumerate(sizes):
+            c = Cache(pv, lens, news, 2, 128, 16, "bf16", seed + i, garbage=False)
+            q = _dev(np.random.default_rng(seed + 10 + i).standard_normal((sum(news), 8, 128)), "bf16")
+            kept.append((c, q))
+            torch.cuda.synchronize()
+            for _ in range(6):
+                o, z = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+                pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=o, lse=z, accumulate=True, stream=stream)
+                pv.pvmvmd_kv_evict(c.pool, c.batch, max(lens) - 1 if i % 2 else 10**6, 3, stream=stream)
+                out += [o, z]
+            out += [c.mass, c.K, c.dlens]
+        stream.synchronize()
+        return [x.cpu() for x in out]
+    alone = [work(s, torch.cuda.Stream()) for s in (51, 71)]
+    shared, got = torch.cuda.Stream(), [None, None]
+
+    def go(i, seed):
+        got[i] = work(seed, shared)
+    threads = [threading.Thread(target=go, args=(i, s)) for i, s in enumerate((51, 71))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert pv.pvmvmd_device_status() == 0
+    for a, b in zip(alone, got):
+        assert len(a) == len(b) and all(torch.equal(x, y) for x, y in zip(a, b))
