@@ -198,6 +198,7 @@ int pvmvmd_paged_attention(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *ba
     j.causal = causal != 0;
     j.accumulate = accumulate != 0;
     const StreamTurn turn(static_cast<cudaStream_t>(stream));
+    if (!turn) return PVMVMD_E_NOMEM;
     PV_CUDA(launch_attention(j, kv, static_cast<cudaStream_t>(stream)));
     return PVMVMD_OK;
 }
@@ -215,6 +216,7 @@ int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, in
     if (room < budget && room < (int64_t)kv.max_pages * pool->page_size) return PVMVMD_E_SHAPE;
     const EvictJob j{budget, recent, new_table_dev, new_table_stride, new_lens_dev};
     const StreamTurn turn(static_cast<cudaStream_t>(stream));
+    if (!turn) return PVMVMD_E_NOMEM;
     PV_CUDA(launch_evict(j, kv, static_cast<cudaStream_t>(stream)));
     return PVMVMD_OK;
 }

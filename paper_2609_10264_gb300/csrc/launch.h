@@ -203,11 +203,12 @@ bool stream_scratch_ready(int purpose, size_t need, cudaStream_t s);
 
 // The calling thread's turn on a stream: held by a call while it enqueues several
 // kernels that share the stream's scratch, so that those of another thread's call on
-// that stream come before or after all of them.
+// that stream come before or after all of them.  False: the host has no memory for it.
 class StreamTurn {
   public:
-    explicit StreamTurn(cudaStream_t s);
+    explicit StreamTurn(cudaStream_t s) noexcept;
     ~StreamTurn();
+    explicit operator bool() const { return mu_ != nullptr; }
     StreamTurn(const StreamTurn &) = delete;
     StreamTurn &operator=(const StreamTurn &) = delete;
 

@@ -36,16 +36,23 @@ std::map<std::tuple<int, int, cudaStream_t>, Buf> g_bufs;
 std::map<std::pair<int, cudaStream_t>, std::mutex> g_turns;  // under g_bufs_mu, each kept for good
 }  // namespace
 
-StreamTurn::StreamTurn(cudaStream_t s) : mu_(nullptr) {
+StreamTurn::StreamTurn(cudaStream_t s) noexcept : mu_(nullptr) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) (void)cudaGetLastError();
-    {
-        std::lock_guard<std::mutex> lock(g_bufs_mu);
-        mu_ = &g_turns[std::make_pair(dev, s)];
+    try {
+        std::mutex *mu;
+        {
+            std::lock_guard<std::mutex> lock(g_bufs_mu);
+            mu = &g_turns[std::make_pair(dev, s)];
+        }
+        mu->lock();
+        mu_ = mu;
+    } catch (...) {
     }
-    mu_->lock();
 }
-StreamTurn::~StreamTurn() { mu_->unlock(); }
+StreamTurn::~StreamTurn() {
+    if (mu_) mu_->unlock();
+}
 
 bool stream_scratch_ready(int purpose, size_t need, cudaStream_t s) {
     int dev = 0;
@@ -59,7 +66,8 @@ bool stream_scratch_ready(int purpose, size_t need, cudaStream_t s) {
     return cudaStreamIsCapturing(s, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone;
 }
 
-cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out) {
+// (The map's entries are of the host's memory: nothing is thrown where it is at an end.)
+cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out) try {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -91,9 +99,11 @@ cudaError_t stream_scratch(int purpose, size_t need, cudaStream_t s, void **out)
     }
     *out = b.ptr;
     return cudaSuccess;
+} catch (...) {
+    return cudaErrorMemoryAllocation;
 }
 
-cudaError_t func_attr(const void *fn, cudaFuncAttribute attr, int value) {
+cudaError_t func_attr(const void *fn, cudaFuncAttribute attr, int value) try {
     static std::mutex mu;
     static std::map<std::tuple<const void *, int, int>, std::pair<int, cudaError_t>> done;
     int dev = 0;
@@ -106,6 +116,8 @@ cudaError_t func_attr(const void *fn, cudaFuncAttribute attr, int value) {
     e = cudaFuncSetAttribute(fn, attr, value);
     done[key] = std::make_pair(value, e);
     return e;
+} catch (...) {
+    return cudaErrorMemoryAllocation;
 }
 
 }  // namespace pv

@@ -1,8 +1,10 @@
 // The host side of the client's attention (csrc/attention_api.cu) with launches that
-// only take time: which of them are under way together.  Driven by
-// test_attention_host.py.
+// only take time: which of them are under way together, and what a call does where the
+// host's memory is at an end.  Driven by test_attention_host.py.
 #include <atomic>
 #include <chrono>
+#include <cstdlib>
+#include <new>
 #include <thread>
 
 #include <cuda_runtime.h>
@@ -15,6 +17,15 @@ static inline unsigned __funnelshift_l(unsigned, unsigned, unsigned) { return 0;
 static inline unsigned __funnelshift_r(unsigned, unsigned, unsigned) { return 0; }
 static inline int max(int a, int b) { return a < b ? b : a; }
 static inline int min(int a, int b) { return b < a ? b : a; }
+
+static std::atomic<bool> g_no_memory;
+void *operator new(size_t n) {
+    void *p = g_no_memory ? nullptr : std::malloc(n ? n : 1);
+    if (!p) throw std::bad_alloc();
+    return p;
+}
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, size_t) noexcept { std::free(p); }
 
 #include "attention_api.cu"
 #include "scratch.cu"
@@ -63,4 +74,24 @@ void host_reset(void) {
     for (std::atomic<int> &m : g_most) m = 0;
 }
 int host_most(int stream) { return stream < 0 ? g_most_all : g_most[stream]; }
+
+// What a call returns while the host has no memory; 1000: it threw.
+int host_without_memory(int what, const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch) {
+    void *p = reinterpret_cast<void *>(4096), *s = reinterpret_cast<void *>((size_t)2), *out;
+    int status = 1000;
+    g_no_memory = true;
+    try {
+        status = what == 0   ? pvmvmd_paged_attention(pool, batch, 2, p, 64, 64, 1.0f, 1, 0, 0, p, 64, 64, nullptr, s)
+                 : what == 1 ? pvmvmd_kv_evict(pool, batch, 8, 2, (int32_t *)p, 4, 4, (int32_t *)p, s)
+                 : what == 2 ? (int)pv::stream_scratch(pv::kScratchDigits, 100, (cudaStream_t)s, &out)
+                             : (int)pv::func_attr(p, cudaFuncAttributeMaxDynamicSharedMemorySize, 1000);
+    } catch (...) {
+    }
+    g_no_memory = false;
+    return status;
+}
+void host_forget(void) {
+    pv::g_bufs.clear();
+    pv::g_turns.clear();
+}
 }

@@ -1,7 +1,7 @@
-"""Calls of the client's attention from several threads (csrc/attention_api.cu over
-launches that only take time).  A call is several kernels that share a stream's
-scratch: those of two calls on one stream must not be enqueued among one another;
-calls on different streams need not wait."""
+"""The host side of the client's attention (csrc/attention_api.cu over launches that only
+take time).  A call is several kernels that share a stream's scratch: those of two
+threads' calls on one stream must not be enqueued among one another; calls on different
+streams need not wait.  And nothing throws where the host's memory is at an end."""
 import ctypes
 import os
 import shutil
@@ -49,3 +49,14 @@ def test_calls_on_one_stream_follow_one_another(lib, kinds, streams):
     assert status == [pv.PVMVMD_OK] * 4
     assert all(lib.host_most(s) == 1 for s in streams)
     assert lib.host_most(-1) == len(set(streams))
+
+
+@pytest.mark.parametrize("what", range(4))
+def test_host_memory_at_an_end(lib, what):
+    """A status, not an exception, from the calls and from what they and others take scratch from."""
+    import paper_2609_10264_gb300 as pv
+    pool = pv.pvmvmd_kv_pool(4096, 8192, 4096, 1024, 64, 64, 1024, 64, 64, 4, 16, 1, 64, pv.PVMVMD_BF16)
+    batch = pv.pvmvmd_kv_batch(4096, 4096, None, 4, 2, 2, 4, 0)
+    lib.host_forget()
+    expect = pv.PVMVMD_E_NOMEM if what < 2 else 2  # cudaErrorMemoryAllocation
+    assert lib.host_without_memory(what, ctypes.byref(pool), ctypes.byref(batch)) == expect
