@@ -438,6 +438,11 @@ typedef struct {
  * max_new: at least as many as any sequence has new ones, 0 if not known (then T);
  * tokens beyond it, and rows that cu_dev puts outside the T, are left out.
  * max_pages * page_size is at most 2^30, B and the pool's heads at most 65535.
+ * Lengths are read on the device, so plans and scratch of the calls go by max_pages:
+ * where a table has columns for contexts much longer than the present ones, name the
+ * columns that are in use (table_stride need not be max_pages).  Scratch per stream is
+ * at most 2 GiB for the scores of few rows (with accumulate) and, where a chunk's keys
+ * are split, 1 GiB for the parts, whatever the table.
  * Lengths beyond max_pages pages are taken as max_pages pages; keys on pages
  * outside the pool are not seen, and nothing is written there. */
 typedef struct {

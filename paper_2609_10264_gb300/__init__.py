@@ -775,7 +775,8 @@ class KvPool:
 class KvBatch:
     """Sequences over a KvPool: table (B x max_pages int32, page numbers), lens (B int32, cached tokens with the new
     ones), cu (B + 1 int32, the rows of each one's new tokens; None: one each) and max_new (at least as many as any
-    has new ones, 0 if not known).  Checked once; the tensors' values may change between calls."""
+    has new ones, 0 if not known).  Checked once; the tensors' values may change between calls.  Plans and scratch go
+    by max_pages: of a table for much longer contexts give the columns in use, table[:, :n]."""
 
     def __init__(self, table, lens, cu=None, max_new: int = 0):
         if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) or table.dtype not in _i32_types():

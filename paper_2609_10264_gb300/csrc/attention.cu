@@ -7,6 +7,14 @@
 
 namespace pv {
 
+int64_t seen_keys(const AttendJob &j, const KvView &kv, int align) {
+    const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
+    return j.window > 0 ? std::min(room, (int64_t)j.window + j.max_new + align - 2) : room;
+}
+int score_rows(const AttendJob &j, const KvView &kv) {
+    return (int)std::min<int64_t>(j.few_rows, ((int64_t)j.max_new * (j.Hq / kv.heads) + 3) / 4 * 4);
+}
+
 // Rows per key head (new tokens x query heads of it) up to which a sequence, single
 // generated tokens above all, goes to the kernel that reads K and V as fast as they
 // come; the others go to the tensor cores' path.
@@ -35,7 +43,12 @@ cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_
     j.few_rows = few_rows(j, kv);
     bool few = false, joined = false;
     const int64_t most = (int64_t)j.max_new * G;  // rows of a sequence
-    if (G > j.few_rows || (kv.B == 1 && most > j.few_rows)) {
+    // Scores that k_few would keep for the mass.  Their room goes by the table, as the lengths
+    // are on the device; beyond kMostScores the tensor cores' path takes all sequences,
+    // which forms the scores anew (64 sequences of 8 heads of 8 rows reach that with room for
+    // 131072 keys; eight with room for 2^28 would ask for 550 GB).
+    const double scores = (double)sizeof(float) * kv.B * kv.heads * seen_keys(j, kv, kFewMostTile) * score_rows(j, kv);
+    if (G > j.few_rows || (kv.B == 1 && most > j.few_rows) || (j.accumulate && scores > kMostScores)) {
         // A single sequence goes there whole, however few of `most` rows the device finds.
         j.few_rows = 0;
     } else {

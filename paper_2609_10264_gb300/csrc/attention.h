@@ -42,6 +42,14 @@ cudaError_t launch_attention(const AttendJob &j, const KvView &kv, cudaStream_t 
 // kFewWholeKeys rows are cheap.
 constexpr int kFewRows = 16, kFewRowsWhole = 64, kFewWholeKeys = 512;
 constexpr int64_t kFewBytes = 192 << 20;
+// Bytes of scratch at most for the scores of few rows (see launch_attention) and, as
+// long as an item has several splits, for the parts of chunks.
+constexpr int64_t kMostScores = (int64_t)2 << 30, kMostParts = (int64_t)1 << 30;
+constexpr int kFewMostTile = 256;  // keys per tile of launch_attention_few
+// Keys of a sequence, from a boundary of `align` on, that any of its new rows may see.
+int64_t seen_keys(const AttendJob &j, const KvView &kv, int align);
+// Scores kept per key and key head: a multiple of 4.
+int score_rows(const AttendJob &j, const KvView &kv);
 cudaError_t launch_attention_few(const AttendJob &j, const KvView &kv, cudaStream_t s);
 // What joins their parts, once those are there.
 cudaError_t launch_attention_few_finish(const AttendJob &j, const KvView &kv, cudaStream_t s);

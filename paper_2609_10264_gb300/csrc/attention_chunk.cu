@@ -523,11 +523,14 @@ cudaError_t chunk(const AttendJob &j, const KvView &kv, cudaStream_t s, bool &jo
     // Splits of an item's keys: the number with which all of them would be through first,
     // in turns of one CTA an SM of as many tiles each and as long as kSetUp tiles beside
     // them.  (80 items of up to 120 tiles: 171 us whole, with as many splits as SMs
-    // without an item, none; 32 items of 470 tiles want 19.)
+    // without an item, none; 32 items of 470 tiles want 19.)  No more than kMostParts
+    // has room for: the tiles are those of the table, which may be far wider than what is
+    // cached, and more items than that have little to gain.
     constexpr int kSetUp = 4, kLeast = 8, kMost = 64;
     a.splits = 1;
     int64_t best = INT64_MAX;
-    for (int64_t n = 1; n <= kMost && (n == 1 || n * kLeast <= keys); ++n) {
+    const int64_t part = (int64_t)kCRows * (DP + 1) * sizeof(float);
+    for (int64_t n = 1; n <= kMost && (n == 1 || (n * kLeast <= keys && items * n * part <= kMostParts)); ++n) {
         const int64_t cost = (items * n + sms - 1) / sms * ((keys + n - 1) / n + (n > 1 ? kSetUp + 2 : kSetUp));
         if (cost < best) best = cost, a.splits = (int)n;
     }

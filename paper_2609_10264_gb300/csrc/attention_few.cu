@@ -33,7 +33,7 @@ struct FewArgs {
     float2 *stat;    // [2 C][kRows] their maximum and sum
     int64_t *before; // [B + 1] work before each sequence, and all of it
     float2 *norm;    // [T][Hq] maximum and 1 / sum, where mass is accumulated
-    float *scores;   // [B][heads][max tiles x tile][rows] where mass is accumulated
+    float *scores;   // [B][heads][max tiles x tile][rows] where mass is accumulated (see seen_keys)
     int score_rows, max_tiles;  // (rows a multiple of 4)
     float scale2;    // scale x log2(e)
     int G, C;
@@ -55,6 +55,7 @@ struct Few {
     static constexpr int kSub = DP == 128 ? 16 : 32;
     static constexpr int kStages = DP == 96 ? 2 : 3;
     static constexpr int kTile = W * kSub;  // keys per tile
+    static_assert(kTile <= kFewMostTile);
     // bytes of a row; chunks of 16 are swizzled, or rows of 13 chunks where 12 are used:
     // either way 8 rows' chunks lie in different banks
     static constexpr int kRow = DP == 96 ? 208 : 2 * DP;
@@ -592,11 +593,11 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finis
     const bool wide = a.whole && (int64_t)kv.B * kv.heads * row_tiles <= sms;
     a.C = wide ? sms : 2 * sms;
     a.scale2 = j.scale * kLog2e;
-    const int64_t room = (int64_t)kv.max_pages * kv.ps.d;
     const int tile = wide ? Few<DP, 8>::kTile : Few<DP, 4>::kTile;
     while (1 << a.tile_log < tile) ++a.tile_log;
-    a.max_tiles = (int)((room + tile - 1) / tile);
-    a.score_rows = (int)std::min<int64_t>(j.few_rows, ((int64_t)j.max_new * a.G + 3) / 4 * 4);
+    const int64_t seen = seen_keys(j, kv, tile);
+    a.max_tiles = (int)((seen + tile - 1) / tile);
+    a.score_rows = score_rows(j, kv);
     auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t parts = up((size_t)2 * a.C * kRows * DP * sizeof(float)), stats = up((size_t)2 * a.C * kRows * sizeof(float2));
     const size_t befores = up((size_t)(kv.B + 1) * sizeof(int64_t));
@@ -622,7 +623,7 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finis
     if (!finish)
         return wide ? launch_rows(k_few<T, DP, 8>, Few<DP, 8>::kThreads, Few<DP, 8>::kSmem)
                     : launch_rows(k_few<T, DP, 4>, Few<DP, 4>::kThreads, Few<DP, 4>::kSmem);
-    const int64_t parts_of_keys = j.accumulate ? (room + kMassKeys - 1) / kMassKeys : 0;
+    const int64_t parts_of_keys = j.accumulate ? (seen + kMassKeys - 1) / kMassKeys : 0;
     const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)(kv.heads * (a.whole ? 1 : row_tiles)), (unsigned)kv.B);
     auto launch = [&](auto kern, int threads) {
         return launch_dependent(kern, grid, threads, (size_t)(kRows * a.C + 4) * sizeof(float) + threads * sizeof(float4), s,

@@ -159,3 +159,58 @@ def test_threads_on_one_stream(pv):
     assert pv.pvmvmd_device_status() == 0
     for a, b in zip(alone, got):
         assert len(a) == len(b) and all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# ---------------------------------------------------------------- wide tables
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("places", [1 << 14, 1 << 28])
+@pytest.mark.parametrize("news", [[1] * 8, [1, 3, 2, 1, 40, 1, 2, 1]])
+def test_tables_far_wider_than_what_is_cached(pv, places, news):
+    """Room for up to 2^28 keys a sequence, some hundreds of them there: the call has the workspace it needs."""
+    import torch
+    lens = [200, 17, 333, 90, 400, 1, 64, 129]
+    H, G, D, page = 8, 8, 64, 1024
+    c = Cache(pv, lens, news, H, D, page, "bf16", 47)
+    wide = torch.full((8, places // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c.table.shape[1]] = c.table
+    batch = pv.KvBatch(wide, c.dlens, c.cu, max_new=max(news))
+    q = _dev(np.random.default_rng(48).standard_normal((sum(news), H * G, D)), "bf16")
+    out, z = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    pv.pvmvmd_paged_attention(c.pool, batch, q, out=out, lse=z, accumulate=True)
+    assert pv.pvmvmd_device_status() == 0
+    mh = _host(c.mass)
+    for b, (L, n) in enumerate(zip(lens, news)):
+        r = slice(c.cu_host[b], c.cu_host[b + 1])
+        ref = attend_there(_host(q[r]), c.rows(b, "K"), c.rows(b, "V"), np.ones(L, bool), n, D**-0.5)
+        check_rows("bf16", _host(out[r]), _host(z[r]), ref)
+        got, was = c.masses(b, mh), c.masses(b, c.mass0.astype(np.float64))
+        assert (np.abs(got - was - ref[2]) <= ref[2] * (2 * ref[5].max() + 2.0**-18) + 2.0**-22 * (was + ref[2])).all()
+
+
+@pytest.mark.gpu
+def test_a_window_bounds_the_workspace(pv):
+    """Few rows with their weights under a window, over a table of 2^20 places: scores of what the window shows."""
+    import torch
+    L, T, W = 9000, 2, 700
+    c = Cache(pv, [L, L - 5], [T, T], 2, 64, 16, "f16", 49)
+    wide = torch.full((2, (1 << 20) // 16), -1, dtype=torch.int32, device="cuda")
+    wide[:, :c.table.shape[1]] = c.table
+    q = _dev(np.random.default_rng(50).standard_normal((2 * T, 8, 64)), "f16")
+    res = []
+    for table in (c.table, wide):
+        c.mass.copy_(torch.from_numpy(c.mass0))
+        out, z = torch.empty_like(q), torch.empty(2 * T, 8, device="cuda")
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        free = torch.cuda.mem_get_info()[0]
+        pv.pvmvmd_paged_attention(c.pool, pv.KvBatch(table, c.dlens, c.cu, max_new=T), q, out=out, lse=z, window=W,
+                                  accumulate=True, stream=s)
+        s.synchronize()
+        assert free - torch.cuda.mem_get_info()[0] < 64 << 20
+        res.append((out, z, c.mass.clone()))
+    assert all(torch.equal(x, y) for x, y in zip(*res))
+    for b, n in enumerate((L, L - 5)):
+        r = slice(b * T, (b + 1) * T)
+        check_rows("f16", _host(out[r]), _host(z[r]),
+                   attend_there(_host(q[r]), c.rows(b, "K"), c.rows(b, "V"), np.ones(n, bool), T, 64**-0.5, window=W))
