@@ -38,6 +38,7 @@ struct FewArgs {
     float scale2;    // scale x log2(e)
     int G, C;
     int tile_log;    // keys per tile
+    unsigned finishers;  // CTAs of k_few_finish for a key head and tile of rows
     bool whole;      // a CTA takes all keys of a row tile
 };
 
@@ -443,10 +444,12 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
     extern __shared__ __align__(16) float s_weight[];  // [rows][parts], then the groups' sums
     const AttendJob &j = a.j;
     const KvView &kv = a.kv;
-    const int b = blockIdx.z, hk = blockIdx.y % kv.heads, rt = blockIdx.y / kv.heads, tid = threadIdx.x;
+    // (one long dimension: the others end at 65535)
+    const int nth = (int)(blockIdx.x % a.finishers), item = (int)(blockIdx.x / a.finishers);
+    const int b = blockIdx.z, hk = item % kv.heads, rt = item / kv.heads, tid = threadIdx.x;
     const Share sh = share(a, b);
-    const int first = sh.first + ((int)blockIdx.x - 1) * kMassKeys, len = sh.len;  // of the keys
-    const bool idle = !sh.work || (blockIdx.x > 0 ? rt > 0 || first >= len : rt >= sh.rts || a.whole);
+    const int first = sh.first + (nth - 1) * kMassKeys, len = sh.len;  // of the keys
+    const bool idle = !sh.work || (nth > 0 ? rt > 0 || first >= len : rt >= sh.rts || a.whole);
     if (idle) return;
     const int64_t total = a.before[kv.B], C = min((int64_t)a.C, total);
     const int row0 = sh.row0;
@@ -456,7 +459,7 @@ __device__ __forceinline__ void few_finish(const FewArgs &a) {
         c0 = owner(a.whole ? i0 : i0 + kSetUp, total, C);
         c1 = a.whole ? c0 : owner(i1 - 1, total, C);
     };
-    if (blockIdx.x == 0) {
+    if (nth == 0) {
         int c0, c1;
         owners(rt, c0, c1);
         if (c0 == c1) return;
@@ -623,8 +626,9 @@ cudaError_t few(const AttendJob &j, const KvView &kv, cudaStream_t s, bool finis
     if (!finish)
         return wide ? launch_rows(k_few<T, DP, 8>, Few<DP, 8>::kThreads, Few<DP, 8>::kSmem)
                     : launch_rows(k_few<T, DP, 4>, Few<DP, 4>::kThreads, Few<DP, 4>::kSmem);
-    const int64_t parts_of_keys = j.accumulate ? (seen + kMassKeys - 1) / kMassKeys : 0;
-    const dim3 grid((unsigned)(1 + parts_of_keys), (unsigned)(kv.heads * (a.whole ? 1 : row_tiles)), (unsigned)kv.B);
+    // (with accumulate fewer than 2^20 in all, as kMostScores bounds them)
+    a.finishers = 1 + (j.accumulate ? (unsigned)((seen + kMassKeys - 1) / kMassKeys) : 0u);
+    const dim3 grid(a.finishers * (unsigned)(kv.heads * (a.whole ? 1 : row_tiles)), 1, (unsigned)kv.B);
     auto launch = [&](auto kern, int threads) {
         return launch_dependent(kern, grid, threads, (size_t)(kRows * a.C + 4) * sizeof(float) + threads * sizeof(float4), s,
                                 a);

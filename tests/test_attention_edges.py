@@ -214,3 +214,29 @@ def test_a_window_bounds_the_workspace(pv):
         r = slice(b * T, (b + 1) * T)
         check_rows("f16", _host(out[r]), _host(z[r]),
                    attend_there(_host(q[r]), c.rows(b, "K"), c.rows(b, "V"), np.ones(n, bool), T, 64**-0.5, window=W))
+
+
+# ---------------------------------------------------------------- many heads
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,T", [(33000, 20), (65535, 1)])
+def test_as_many_heads_as_the_header_admits(pv, H, T):
+    """A window of one key: every row's output is the value of its own key, and its log sum that key's score."""
+    import torch
+    D, page, L = 8, 64, 1100
+    pages = -(-L // page)
+    K = torch.randn(pages, page, H, D, device="cuda").to(torch.bfloat16)
+    V = torch.randn(pages, page, H, D, device="cuda").to(torch.bfloat16)
+    pool = pv.KvPool(K, V)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous()
+    lens = torch.tensor([L], dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    q = torch.randn(T, H, D, device="cuda").to(torch.bfloat16)
+    out, z = torch.full_like(q, 7.0), torch.full((T, H), 7.0, device="cuda")
+    pv.pvmvmd_paged_attention(pool, pv.KvBatch(table, lens, cu, max_new=T), q, out=out, lse=z, window=1)
+    k, v = (x.view(-1, H, D)[L - T:L] for x in (K, V))
+    # one key: p = 1, a value of the cache's type comes back as it is
+    assert torch.equal(out, v)
+    s = (q.double() * k.double()).sum(-1) * D**-0.5
+    e = 2.0**-24 * (D + 16) * (q.double() * k.double()).abs().sum(-1) * D**-0.5 + 2.0**-20
+    assert ((z.double() - s).abs() <= e + 2.0**-20 * (1 + s.abs())).all()
