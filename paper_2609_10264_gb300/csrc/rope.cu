@@ -237,6 +237,7 @@ cudaError_t rope_launch(const RopeArgs &a, cudaStream_t s) {
         const int turn = std::max(1, kRowThreads / units), sms = 152;
         RowPlan plan;
         plan.heads = j.T >= 4 * sms ? a.heads : std::min(a.heads, j.T >= sms ? 4 * turn : turn);
+        plan.heads = std::max(plan.heads, a.heads / 65535 + 1);  // a grid's second dimension ends there
         plan.tokens = std::max(1, std::min({kMostTokens, kMostSines / std::max(1, j.rot / 2), 6 * turn / plan.heads,
                                             j.T / (4 * sms), std::max(j.T / (12 * sms), turn / plan.heads)}));
         plan.units = FastDiv((uint32_t)units);

@@ -240,3 +240,20 @@ def test_as_many_heads_as_the_header_admits(pv, H, T):
     s = (q.double() * k.double()).sum(-1) * D**-0.5
     e = 2.0**-24 * (D + 16) * (q.double() * k.double()).abs().sum(-1) * D**-0.5 + 2.0**-20
     assert ((z.double() - s).abs() <= e + 2.0**-20 * (1 + s.abs())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,H,D,inter", [(1, 70000, 2048, False), (1, 66000, 2056, True), (2, 65600, 2048, True)])
+def test_rope_of_many_wide_heads(pv, T, H, D, inter):
+    import torch
+    table = pv.pvmvmd_rope_table(64)
+    x = torch.randn(T, H, D, device="cuda").to(torch.bfloat16)
+    pos = torch.arange(5, 5 + T, dtype=torch.int32, device="cuda")
+    y = pv.pvmvmd_rope(x, pos, table, interleaved=inter)
+    assert torch.equal(y[..., 64:], x[..., 64:])
+    few = torch.tensor([0, 1, H // 2, H - 2, H - 1], device="cuda")
+    assert torch.equal(y[:, few], pv.pvmvmd_rope(x[:, few].contiguous(), pos, table, interleaved=inter))
+    a = x[..., :64].float().view(T, H, 32, 2) if inter else x[..., :64].float().view(T, H, 2, 32).transpose(2, 3)
+    b = y[..., :64].float().view(T, H, 32, 2) if inter else y[..., :64].float().view(T, H, 2, 32).transpose(2, 3)
+    # a rotation keeps a pair's length, but for two roundings to bf16
+    assert ((a.norm(dim=-1) - b.norm(dim=-1)).abs() <= 2.0**-8 * b.norm(dim=-1) + 1e-5).all()
