@@ -699,7 +699,11 @@ def _open_calls():
     global _native
     torch = _torch or _lazy_torch()
     lib = load_library()
-    from . import _calls
+    try:
+        from . import _calls
+    except ImportError as e:
+        raise ImportError("the client's attention goes through the native module _calls, which the build makes where "
+                          "Python's headers are installed") from e
     get, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
     if not (get and dev):
         get, dev = _current_stream, None

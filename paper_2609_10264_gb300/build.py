@@ -2,7 +2,8 @@
 
 Each translation unit under csrc/ is compiled in parallel into _build/, then
 linked into paper_2609_10264_gb300/libpvmvmd.so; csrc/calls.c becomes the Python
-module _calls.so beside it.  Rebuilds only when a source or header is newer.
+module _calls beside it, which the client's attention goes through, where Python's
+headers are installed.  Rebuilds only when a source or header is newer.
 """
 from __future__ import annotations
 
@@ -20,7 +21,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpvmvmd.so")
 CALLS_C = os.path.join(CSRC, "calls.c")
-CALLS = os.path.join(PKG, "_calls.so")
+CALLS = os.path.join(PKG, "_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-Xcompiler", "-fPIC", "-diag-suppress", "550", "-I", INCLUDE,
               *ARCH]
@@ -42,10 +43,17 @@ def _inputs():
         glob.glob(os.path.join(INCLUDE, "*.h")) + [CALLS_C, os.path.abspath(__file__)]
 
 
+def _python_headers():
+    """Their directory, or None where they are not installed."""
+    d = sysconfig.get_paths()["include"]
+    return d if os.path.exists(os.path.join(d, "Python.h")) else None
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+    made = [LIB, CALLS] if _python_headers() else [LIB]
+    if not all(os.path.exists(p) for p in made):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    t = min(os.path.getmtime(p) for p in made)
     return any(os.path.getmtime(p) > t for p in _inputs())
 
 
@@ -66,9 +74,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return obj
 
     def compile_calls():
+        headers = _python_headers()
+        if headers is None:
+            print(f"{CALLS_C} is not built: no Python.h in {sysconfig.get_paths()['include']}")
+            return
         tmp = CALLS + f".tmp{os.getpid()}"
         cmd = [os.environ.get("CC") or shutil.which("gcc") or "cc", "-O2", "-Wall", "-shared", "-fPIC", "-I", INCLUDE,
-               "-I", sysconfig.get_paths()["include"], "-o", tmp, CALLS_C, "-lm", "-ldl"]
+               "-I", headers, "-o", tmp, CALLS_C, "-lm", "-ldl"]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"the C compiler failed for {CALLS_C}:\n{r.stdout}\n{r.stderr}")
