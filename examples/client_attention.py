@@ -52,6 +52,7 @@ class AttentionBlock:
         self.W["o"] = wl.weights_gaussian(hidden, heads * dim, (seed, 3))
         self.mat = {n: Delegated(W, key=100 + i) for i, (n, W) in enumerate(self.W.items())}
         pages = -(-room // page)
+        self.room = pages * page
         self.pool = pv.KvPool(torch.zeros(pages, page, kv_heads, dim, dtype=torch.bfloat16, device="cuda"),
                               torch.zeros(pages, page, kv_heads, dim, dtype=torch.bfloat16, device="cuda"),
                               torch.zeros(pages, kv_heads, page, device="cuda"))
@@ -84,6 +85,8 @@ class AttentionBlock:
     def step(self, x_int):
         """T new tokens' int8 activations (T x hidden) -> (T x hidden field elements of W_o's product, q, attention)."""
         T = x_int.shape[0]
+        if self.length + T > self.room:  # nothing outside the table is written or seen
+            raise ValueError(f"{T} tokens behind {self.length} are more than the cache's {self.room} places")
         q, k, v = self.delegate(("q", "k", "v"), x_int)
         self.lens += T
         self.length += T

@@ -257,3 +257,18 @@ def test_rope_of_many_wide_heads(pv, T, H, D, inter):
     b = y[..., :64].float().view(T, H, 32, 2) if inter else y[..., :64].float().view(T, H, 2, 32).transpose(2, 3)
     # a rotation keeps a pair's length, but for two roundings to bf16
     assert ((a.norm(dim=-1) - b.norm(dim=-1)).abs() <= 2.0**-8 * b.norm(dim=-1) + 1e-5).all()
+
+
+# ---------------------------------------------------------------- the example
+
+@pytest.mark.gpu
+def test_example_refuses_tokens_beyond_its_cache(pv):
+    import torch
+    from test_attention_example import _example
+    block = _example().AttentionBlock(hidden=64, heads=2, kv_heads=1, dim=32, budget=48, room=60, page=16)
+    x = torch.randint(-127, 128, (70, 64), device="cuda")
+    block.step(x[:50])
+    with pytest.raises(ValueError, match="64 places"):
+        block.step(x[:15])
+    block.step(x[:14])
+    assert block.length == int(block.lens) == 48
