@@ -272,3 +272,78 @@ def test_example_refuses_tokens_beyond_its_cache(pv):
         block.step(x[:15])
     block.step(x[:14])
     assert block.length == int(block.lens) == 48
+
+
+# ---------------------------------------------------------------- more candidates than an eviction holds in registers
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,H,D,page,budget,recent", [([40000, 33000], 2, 16, 64, 9000, 100),
+                                                         ([32769], 1, 8, 7, 32768, 0), ([32768, 32770], 1, 8, 16, 1, 0),
+                                                         ([70001, 5], 1, 8, 100, 66000, 40000)])
+@pytest.mark.parametrize("where", ["own", "new"])
+@pytest.mark.parametrize("values", ["any", "ties", "odd"])
+def test_evict_from_long_caches(pv, lens, H, D, page, budget, recent, where, values):
+    import torch
+    from test_attention import kept_indexes
+    need = [-(-min(budget, L) // page) for L in lens]
+    c = Cache(pv, lens, [1] * len(lens), H, D, page, "bf16", 61, extra=2 + len(lens) * max(need), garbage=False)
+    rng = np.random.default_rng(62)
+    m = c.mass0
+    if values == "ties":
+        m = rng.integers(0, 3, m.shape).astype(np.float32)
+    elif values == "odd":
+        m = rng.choice(np.array([0.0, -0.0, 1e-45, 3e38, np.inf, -np.inf, np.nan, -1.0], np.float32), m.shape)
+    c.mass.copy_(torch.from_numpy(m))
+    K0, V0, m0 = _host(c.K), _host(c.V), m.astype(np.float64)
+    new_lens = torch.full((len(lens),), -1, dtype=torch.int32, device="cuda")
+    table, tab = c.table, c.tab
+    if where == "new":
+        used = set(c.tab[c.tab >= 0].tolist())
+        free = [p for p in range(c.K.shape[0]) if p not in used]
+        tab = np.array(free[:len(lens) * max(need)], np.int32).reshape(len(lens), max(need))
+        table = _dev(tab, "field")
+    pv.pvmvmd_kv_evict(c.pool, c.batch, max(min(budget, L) for L in lens), recent, new_lens=new_lens, new_table=table)
+    assert pv.pvmvmd_device_status() == 0
+    assert new_lens.tolist() == [min(L, budget) for L in lens]
+    Kg, Vg, mg = _host(c.K), _host(c.V), _host(c.mass)
+    for b, L in enumerate(lens):
+        p, o = c.at(b)
+        dp, do = c.at(b, min(L, budget), tab)
+        for h in range(H):
+            idx = kept_indexes(m0[p, h, o], L, budget, recent)
+            assert np.array_equal(Kg[dp, do, h], K0[p[idx], o[idx], h]), (b, h)
+            assert np.array_equal(Vg[dp, do, h], V0[p[idx], o[idx], h]), (b, h)
+            assert np.array_equal(mg[dp, h, do], m0[p[idx], h, o[idx]], equal_nan=True), (b, h)
+
+
+# ---------------------------------------------------------------- a captured call with weights
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("news", [[1, 1], [40, 40], [2, 300]])
+def test_captured_accumulation(pv, news):
+    """Rows of few, of chunks and of both with their weights, replayed over new contents and lengths: the same bits as
+    the calls."""
+    import torch
+    c = Cache(pv, [6000, 700], news, 2, 64, 16, "bf16", 63, garbage=False)
+    q = _dev(np.random.default_rng(64).standard_normal((sum(news), 8, 64)), "bf16")
+    out, z = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=out, lse=z, accumulate=True, stream=s)  # its scratch
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=out, lse=z, accumulate=True)
+    for lens in ((6000, 700), (310, 650), (5000, 1), (0, 20)):
+        c.dlens.copy_(torch.tensor(lens, dtype=torch.int32))
+        q.normal_()
+        c.mass.zero_()
+        g.replay()
+        g.replay()
+        got = [out.clone(), z.clone(), c.mass.clone()]
+        c.mass.zero_()
+        for _ in range(2):
+            o2, z2 = torch.empty_like(q), torch.empty_like(z)
+            pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=o2, lse=z2, accumulate=True)
+        assert all(torch.equal(x, y) for x, y in zip(got, (o2, z2, c.mass)))
+    assert pv.pvmvmd_device_status() == 0
