@@ -392,7 +392,8 @@ typedef struct {
 /* turns[i] = theta_i / (2 pi) in units of 2^-64 of a turn, modulo whole turns, for
  * i < rot/2 (host array).  position * turns[i] modulo 2^64 is then the angle at
  * any position without a loss of precision.  Host only; needs no GPU.  Returns
- * PVMVMD_E_PARAM for parameters outside the ranges above. */
+ * PVMVMD_E_PARAM for parameters outside the ranges above, and where a frequency is not
+ * finite. */
 int pvmvmd_rope_turns(const pvmvmd_rope_params *params, uint64_t *turns);
 
 /* How a call rotates: turns_dev the rot/2 values of pvmvmd_rope_turns on the

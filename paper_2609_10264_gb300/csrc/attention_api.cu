@@ -98,6 +98,7 @@ int pvmvmd_rope_turns(const pvmvmd_rope_params *p, uint64_t *turns) {
             th *= g + (1 - g) / s;
         }
         double turn = th / two_pi;
+        if (!std::isfinite(turn)) return PVMVMD_E_PARAM;  // bases next to 0
         turn -= std::floor(turn);  // exact; bases below 1 turn more than once a position
         turn *= 18446744073709551616.0;
         turns[i] = turn >= 18446744073709551615.0 ? 0 : (uint64_t)turn;

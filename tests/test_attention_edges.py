@@ -347,3 +347,13 @@ def test_captured_accumulation(pv, news):
             pv.pvmvmd_paged_attention(c.pool, c.batch, q, out=o2, lse=z2, accumulate=True)
         assert all(torch.equal(x, y) for x, y in zip(got, (o2, z2, c.mass)))
     assert pv.pvmvmd_device_status() == 0
+
+
+# ---------------------------------------------------------------- frequencies that no double holds
+
+def test_turns_refuse_frequencies_that_are_not_finite(pv):
+    assert (pv.pvmvmd_rope_turns(128, base=1e-300) >= 0).all()
+    for kw in ({"base": 5e-324}, {"base": 1e-320, "scaling": "linear", "factor": 1.0}):
+        with pytest.raises(pv.PvmvmdError) as e:
+            pv.pvmvmd_rope_turns(1024, **kw)
+        assert e.value.status == pv.PVMVMD_E_PARAM
