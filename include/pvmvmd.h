@@ -400,7 +400,9 @@ int pvmvmd_rope_turns(const pvmvmd_rope_params *params, uint64_t *turns);
  * device.  A pair (a, b) at position p becomes
  *     magnitude (a cos x - b sin x, a sin x + b cos x),  x = p theta_i;
  * the pairs are values i and i + rot/2 of a head, or 2i and 2i + 1 where
- * interleaved is not 0.  Values from rot on are copied. */
+ * interleaved is not 0.  Values from rot on are copied.
+ * turns_dev may hold any frequencies: those of a scaling that is not among the above,
+ * a ramp over the pairs' indexes for one, are made by the caller. */
 typedef struct {
     const uint64_t *turns_dev;
     int rot, interleaved;
@@ -457,7 +459,9 @@ typedef struct {
  * from them once a cache has been evicted).  With q_dev, q (T x Hq x dim) is
  * rotated likewise into q_out_dev (T x Hq x dim, the pool's type, not overlapping
  * the inputs).  rope null: nothing is rotated.  All inputs have type in_type, and
- * are multiplied by scale.  The new tokens' mass is set to 0.  Sequences must not
+ * are multiplied by one scale: where q, k and v are products of matrices whose
+ * quantisation scales differ, the factors of q and k relative to it belong into the
+ * attention's scale, that of v into what the next product's input is scaled by.  The new tokens' mass is set to 0.  Sequences must not
  * share the pages that their new tokens fall into.  T = 0 does nothing. */
 int pvmvmd_kv_append(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, const pvmvmd_rope_view *rope,
                      const int32_t *pos_dev, int in_type, float scale, const void *k_dev, int64_t k_token,
@@ -476,8 +480,11 @@ int pvmvmd_kv_append(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, c
  * sequences must then not share pages (as they may without).
  * Hq a multiple of pool->heads; q and out of the pool's type, on 16-byte boundaries,
  * strides multiples of 8; lse_dev float [T][Hq] or null.  What lies behind a
- * sequence's end and on pages of others is not used, whatever it holds.  A key that
- * is not finite gives rows that see it NaN; a value that is not finite may reach
+ * sequence's end and on pages of others is not used, whatever it holds.  Scores, sums and
+ * outputs are held in 32 bits; sequences of many new rows hold exp(s_j - lse) in the
+ * pool's 16-bit type for the product with V, those of few rows in two such parts.  A key
+ * that is not finite gives rows that see it NaN (or no weight, where its score is
+ * -infinity and others are not); a value that is not finite may reach
  * rows of the same call that do not see it (0 times it), among the keys in reach of
  * any of them.  Partial results of long sequences live in library scratch held per
  * stream, as for pvmvmd_server_mvm; this call and pvmvmd_kv_evict, of several kernels
@@ -494,7 +501,9 @@ int pvmvmd_paged_attention(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *ba
  * new_table_dev (B x new_max_pages, stride new_table_stride), which may be the
  * batch's own table (eviction in place; no other sequence may use those pages) or
  * name pages that no sequence of the batch uses; new_lens_dev[b] = min(len, budget)
- * (may be lens_dev itself).  Keys keep the rotation of their old positions.
+ * (may be lens_dev itself).  Keys keep the rotation of their old positions.  The tokens
+ * of a sequence must lie on pages of the pool: one that does not counts as of NaN mass,
+ * and where it stays all the same its new place keeps what it holds.
  * budget >= 1, recent >= 0, new_max_pages * page_size >= budget or >= max_pages *
  * page_size.  cu_dev, T and max_new are not used. */
 int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, int budget, int recent,

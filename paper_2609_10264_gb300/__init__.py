@@ -714,7 +714,9 @@ def _open_calls():
 
 
 class RopeTable:
-    """Rotary frequencies on the device: what pvmvmd_rope and pvmvmd_kv_append rotate by."""
+    """Rotary frequencies on the device: what pvmvmd_rope and pvmvmd_kv_append rotate by.  Made by
+    pvmvmd_rope_table, or of any rot/2 frequencies of one's own: turns is a CUDA tensor of 64-bit integers, fractions
+    of a turn per position in units of 2^-64."""
 
     def __init__(self, turns, rot: int, magnitude: float):
         self.turns, self.rot, self.magnitude = turns, rot, magnitude
@@ -797,8 +799,8 @@ class KvBatch:
 
 def pvmvmd_kv_append(pool: KvPool, batch: KvBatch, k, v, positions=None, rope: RopeTable | None = None, q=None,
                      q_out=None, interleaved: bool = False, scale: float = 1.0, stream=None):
-    """k and v of the new tokens (T x heads x dim, one floating or field type) into the cache, k rotated at positions
-    (default: the cache indexes).  q (T x Hq x dim) is rotated into q_out (the pool's type), which is returned."""
+    """k and v of the new tokens (T x heads x dim, one floating or field type, times scale) into the cache, k rotated at
+    positions (default: the cache indexes).  q (T x Hq x dim) is rotated into q_out (the pool's type), which is returned."""
     if q is not None and q_out is None:
         q_out = q.new_empty(q.shape, dtype=pool.K.dtype)
     _check((_native or _open_calls()).append(pool.address, batch.address,

@@ -46,7 +46,8 @@ cudaError_t launch_attention(const AttendJob &job, const KvView &kv, cudaStream_
     // Scores that k_few would keep for the mass.  Their room goes by the table, as the lengths
     // are on the device; beyond kMostScores the tensor cores' path takes all sequences,
     // which forms the scores anew (64 sequences of 8 heads of 8 rows reach that with room for
-    // 131072 keys; eight with room for 2^28 would ask for 550 GB).
+    // 131072 keys, of which up to 8192 are there: 300 us, just beyond it 494; with room for 2^20,
+    // 495, k_few would ask for 17 GB).
     const double scores = (double)sizeof(float) * kv.B * kv.heads * seen_keys(j, kv, kFewMostTile) * score_rows(j, kv);
     if (G > j.few_rows || (kv.B == 1 && most > j.few_rows) || (j.accumulate && scores > kMostScores)) {
         // A single sequence goes there whole, however few of `most` rows the device finds.

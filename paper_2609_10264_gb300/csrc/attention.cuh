@@ -324,8 +324,8 @@ __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.
 // Keys per TMA box: the largest power of two, up to a tile, that divides the page size;
 // none where that is less than 4, and none where a stride is not one that a tensor map
 // can have.  (2048 tokens over 8192 keys, 32 heads of 128, us: boxes of 1 key 612, of 2
-// 341, of 4 220, of 8 169, of 64 165; gathered row by row by the loaders, at any page
-// size, 240.)
+// 341, of 4 220, of 8 169, of 64 165; gathered row by row by the loaders 271 in pages of 2,
+// 277 of 1.)
 constexpr int kLeastBox = 4;
 inline int page_box(const KvView &kv) {
     int box = 1;

@@ -8,9 +8,10 @@
 // two has two accumulators in TMEM, so that the tensor cores work on the next tile
 // while one is summed.  Few rows over many keys make many short items, so a CTA stays
 // and its rows' copies and sums run on from one item to the next (with a barrier at
-// each, five chunks of 35 tokens over 13000 keys took 130 us).  One exp2 a score bounds
-// it where there are many rows: 2048 tokens of 32 heads of 128 over 8192 keys 138 us
-// beside the attention's 160 (0.87 PFLOP/s, 3.4e12 exp2/s).
+// each, five chunks of 35 tokens over 13000 keys took 130 us).  Where there are many rows the
+// chain of a warp's sums bounds it: 2048 tokens of 32 heads of 128 over 8192 keys 138 us
+// beside the attention's 160 (0.87 PFLOP/s, 3.4e12 exp2/s), with the tensor cores, the
+// exp2 pipe and the issue slots each busy for about half of that.
 #include <algorithm>
 #include <climits>
 #include <cmath>

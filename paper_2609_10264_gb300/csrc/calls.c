@@ -1,8 +1,8 @@
 /* The binding's calls of the client's attention, whose kernels for a few tokens take
  * less time than ctypes needs for a call's twenty arguments: a Python module that looks
  * at the tensors and calls libpvmvmd.so.  (One token rotated 3.7 us a call where 6.5
- * through ctypes, 8 appended 4.6 and 8.7, attention of 8 over 8 6.1 and 8.2, which the
- * device takes.)
+ * through ctypes, 8 appended 4.6 and 8.7, attention of 8 over 8 5.1 and 8.2, of which the
+ * device takes the 5.1.)
  * Shapes, types and strides are checked here, everything else by the library. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>

@@ -11,10 +11,13 @@
 // never moves to a higher index, so in place the rows that lie where a CTA writes are
 // its own or those of CTAs before it: every CTA reports its rows read, and one that
 // writes to a page that the sequence has in that very place waits for the reports
-// before its own first (64 CTAs a list: 173 us with that wait where 112 do without).
+// before its own first.
 // Blocks start in the order of their index (as the other kernels that chain blocks
-// rest on); the wait is bounded.  16 sequences of up to 16384 keys to 4096: 110 us a call,
-// 4.6 TB/s of rows read and written; one of 700 keys 9.6 us, latency of both kernels.
+// rest on); the wait is bounded.  16 sequences of up to 16384 keys to 4096: 110 us a call to
+// other pages, 4.6 TB/s of rows read and written, and 152 in place, of which the waits for
+// the CTAs before are the difference; one of 700 keys 9.4 us, latency of both kernels.
+// To a quarter: 8 sequences of 32768 masses, in registers, 140 us, of 33024, read again,
+// 140; one of 131072 389.
 #include <algorithm>
 
 #include "attention.cuh"
