@@ -510,6 +510,142 @@ int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, in
                     const int32_t *new_table_dev, int64_t new_table_stride, int new_max_pages, int32_t *new_lens_dev,
                     void *stream);
 
+/* ---------------------------------------------------------------------
+ * The client's other steps between two delegated products: the norms around a block
+ * with its gate and residual (pvmvmd_block_norm), the gated activation of a
+ * feed-forward block (pvmvmd_glu), and behind the last product the choice of the
+ * next token (pvmvmd_sample).
+ *
+ * Decoded products come in as field elements with the scales that weights and
+ * activations were quantised by, and the next product's input goes out as field
+ * elements.  Those are whole numbers, which the next check compares as they are, so the
+ * steps are defined in IEEE numbers of 32 bits: every product, sum, quotient and
+ * conversion written below is rounded to nearest by itself, in the order written.
+ * Means and mean squares are formed in more bits (of 2^-40 and better) and rounded
+ * once.  Rows' squares must stay below 2^126 in sum; beyond, a norm gives NaN or 0.
+ *
+ * Conventions, besides those at the top of this file and of the client's attention
+ * (types, structs read during the call):
+ *  - Tensors are T rows (tokens) of D values, contiguous in a row; `token` is the
+ *    stride between rows in elements.  Rows have any alignment; those on 16-byte
+ *    boundaries are read and written 16 bytes at a time.
+ *  - An output may be one of the call's inputs of the same address, row stride and
+ *    type size, and must not overlap them otherwise.
+ *  - T = 0 does nothing.  The calls use no scratch, so that any number of them may run at
+ *    once, on one stream or several.
+ */
+
+/* Rows to read.  Value i of row t is
+ *     (x (scale token_scale_dev[t])) channel_scale_dev[i]
+ * with x the value, or the centred integer that a field element stands for, as a 32-bit
+ * number; null scales are left out.  token 0: one row for all. */
+typedef struct {
+    const void *data_dev;
+    const float *token_scale_dev, *channel_scale_dev; /* [T], [D], or null */
+    int64_t token;
+    float scale;
+    int type; /* any */
+} pvmvmd_rows;
+
+/* Rows to write.  A floating type takes the values z, each rounded once.  PVMVMD_FIELD
+ * takes the integers n = round(min(max(z m, -limit), limit)) (halves to even), as field
+ * elements, where
+ *     m = scale if token_scale_dev is null (NaN gives 0), and otherwise
+ *     m = min(limit / a, FLT_MAX) with a = max_i |z_i| of the row, whose step
+ *     token_scale_dev[t] = a / limit is written (a row with a value that is not finite
+ *     gives zeros, and NaN for its step).
+ * 1 <= limit <= 2^23. */
+typedef struct {
+    void *data_dev;
+    float *token_scale_dev; /* [T] or null; null for floating types */
+    int64_t token;
+    float scale;
+    int limit, type;
+} pvmvmd_rows_out;
+
+/* A norm over the D values of a row:
+ *     PVMVMD_NORM_RMS    n_i = x_i inv w_i + b_i,        inv = 1 / sqrt(mean_i x_i^2 + eps);
+ *     PVMVMD_NORM_LAYER  n_i = (x_i - mu) inv w_i + b_i,  mu = mean_i x_i,
+ *                        inv = 1 / sqrt(mean_i (x_i - mu)^2 + eps),
+ * with w_i = weight + weight_add (1 where weights are stored as what they differ from 1
+ * by).  Null: w_i = 1 + weight_add, b_i = 0 (and their product or sum is left out where it
+ * changes nothing).  mu and inv are 32-bit numbers.  eps > 0. */
+enum { PVMVMD_NORM_RMS = 1, PVMVMD_NORM_LAYER = 2 };
+typedef struct {
+    const void *weight_dev, *bias_dev; /* [D] of a floating type, or null */
+    float eps, weight_add;
+    int kind, type;
+} pvmvmd_norm;
+
+/* What lies between two blocks, for T rows of D values:
+ *     u = y, or post(y);   u = u gate (if there is a gate);
+ *     r' = residual_scale residual + branch_scale u;
+ *     z = r', or pre(r');
+ * r' is rounded to residual_out, and z, formed of the 32-bit r', goes to out.  Null: y (no
+ * branch: r' = residual_scale residual), post, gate, residual (r' = branch_scale u),
+ * residual_out, pre, out; y or residual, and residual_out or out, must be there.
+ * residual and residual_out have floating types, no scales, and may be one tensor.
+ * D <= PVMVMD_MAX_K.  Errors: PVMVMD_E_ARG (null pointer, unknown type or norm, a step for a
+ * floating output), PVMVMD_E_SHAPE (T < 0, D outside [1, PVMVMD_MAX_K]), PVMVMD_E_PARAM (eps
+ * not above 0, a limit outside [1, 2^23], a scale that is not finite). */
+int pvmvmd_block_norm(int T, int D, const pvmvmd_rows *y, const pvmvmd_norm *post, const pvmvmd_rows *gate,
+                      float branch_scale, const pvmvmd_rows *residual, float residual_scale,
+                      const pvmvmd_rows_out *residual_out, const pvmvmd_norm *pre, const pvmvmd_rows_out *out,
+                      void *stream);
+
+/* The gated activation z = act(gate) up of T rows of D values, or act(gate) where up is
+ * null, to out:
+ *     PVMVMD_ACT_NONE     act(x) = x;          PVMVMD_ACT_RELU  max(x, 0);
+ *     PVMVMD_ACT_SIGMOID  1 / (1 + E(x l));    PVMVMD_ACT_SILU  x / (1 + E(x l));
+ *     PVMVMD_ACT_GELU     x / (1 + E(x ((x x) c' + c))), the tanh form,
+ * with l = log2 e, c = 2 sqrt(2/pi) l and c' = 0.044715 c as 32-bit numbers, and E(d) = 2^-d as
+ * follows.  d is cut to [-128, 125], n = round(d), f = d - n, and
+ *     P(f) = ((((k5 f + k4) f + k3) f + k2) f + k1) f + 1,  k1 .. k5 = -0.693147004,
+ *     0.240222424, -0.0555073395, 0.00967151299, -0.00132647157 (9 digits name a 32-bit number);
+ * n is taken off the exponent of P(f): 2^-d within 2^-22.3 of itself, infinity at -128.
+ * NaN gives NaN.  D <= PVMVMD_MAX_K.  Errors as for pvmvmd_block_norm. */
+enum { PVMVMD_ACT_NONE = 0, PVMVMD_ACT_RELU = 1, PVMVMD_ACT_SIGMOID = 2, PVMVMD_ACT_SILU = 3, PVMVMD_ACT_GELU = 4 };
+int pvmvmd_glu(int T, int D, const pvmvmd_rows *gate, int act, const pvmvmd_rows *up, const pvmvmd_rows_out *out,
+               void *stream);
+
+/* How the next token is chosen; a device array of T values, or null and one for all rows. */
+typedef struct {
+    const float *temperature_dev;
+    const int32_t *top_k_dev;
+    const float *top_p_dev, *min_p_dev;
+    float temperature; /* not above 0 (or NaN): the token of the largest logit, greedily */
+    int top_k;         /* below 1: no limit                                               */
+    float top_p;       /* 1 and above (or NaN): no limit                                  */
+    float min_p;       /* 0 and below (or NaN): no limit; above 1 as 1                    */
+} pvmvmd_sampling;
+
+/* One token for each of T rows of V logits.  Random numbers are the caller's: random_dev[t]
+ * is a uniform 32-bit word.
+ *   Distances.  x_i = min((l_i m) channel_scale_dev[i], FLT_MAX), where
+ *       m = min((scale token_scale_dev[t]) (log2 e / temperature), FLT_MAX)
+ *     (null scales left out; m = scale token_scale_dev[t] for a greedy row).  Tokens whose x_i is
+ *     not above -infinity (NaN among them), and those whose bit of allowed_dev is 0, are never
+ *     chosen; bit i of a row is bit i % 32 of its word i / 32, rows are allowed_row words
+ *     apart (0: one row for all).  d_i = min(max_j x_j - x_i, 63).
+ *   Weights.  W_i = (R << 18) >> n with n = round(d_i), R = round(2^22 P(d_i - n)) (P as above):
+ *     2^(x_i - max) in units of 2^-40, of 22 bits.  All that follows is of whole numbers, so that
+ *     the token is the same on every implementation.
+ *   Limits, on the tokens in falling order of x, equal ones by their index:
+ *     the first top_k are kept; of those the ones before which less than
+ *     floor(S floor(2^31 top_p) / 2^31) of weight lies, S theirs in all, and the first in any case;
+ *     of those the ones with W_i >= 2^9 floor(2^31 min_p).
+ *   Choice.  Z the kept tokens' weight: the first kept token, in the order of the vocabulary, up to
+ *     which they weigh more than floor(Z random_dev[t] / 2^32).
+ * token_dev[t] is its index, and logprob_dev[t] (or null) = log(W / Z), the log of the
+ * probability that it was drawn with; the token of lowest index among the largest and 0 for a greedy row;
+ * -1 and -infinity where no token can be chosen.  logits->token as for other rows, not
+ * below V unless it is 0 (equal rows).  1 <= V <= 2^24.  Errors: PVMVMD_E_ARG (null pointer,
+ * unknown type), PVMVMD_E_SHAPE (T < 0, V outside its range), PVMVMD_E_PARAM (a logits' scale that
+ * is not finite). */
+#define PVMVMD_MAX_V (1 << 24)
+int pvmvmd_sample(int T, int V, const pvmvmd_rows *logits, const pvmvmd_sampling *sampling, const uint32_t *allowed_dev,
+                  int64_t allowed_row, const uint32_t *random_dev, int32_t *token_dev, float *logprob_dev, void *stream);
+
 /* The number of kernels the library has enqueued in this process since it
  * was loaded, on every device and stream: each launch counts once when it is
  * enqueued, also while a stream is being captured.  Replaying a captured CUDA

@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -111,6 +112,32 @@ class pvmvmd_kv_batch(ctypes.Structure):
                [(f, ctypes.c_int) for f in ("B", "T", "max_pages", "max_new")]
 
 
+PVMVMD_MAX_V = 1 << 24
+PVMVMD_NORM = {"rms": 1, "layer": 2}
+PVMVMD_ACT = {"none": 0, "relu": 1, "sigmoid": 2, "silu": 3, "gelu": 4}
+
+
+class pvmvmd_rows(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("data_dev", "token_scale_dev", "channel_scale_dev")] + \
+               [("token", ctypes.c_int64), ("scale", ctypes.c_float), ("type", ctypes.c_int)]
+
+
+class pvmvmd_rows_out(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("token_scale_dev", ctypes.c_void_p), ("token", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("limit", ctypes.c_int), ("type", ctypes.c_int)]
+
+
+class pvmvmd_norm(ctypes.Structure):
+    _fields_ = [("weight_dev", ctypes.c_void_p), ("bias_dev", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("weight_add", ctypes.c_float), ("kind", ctypes.c_int), ("type", ctypes.c_int)]
+
+
+class pvmvmd_sampling(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("temperature_dev", "top_k_dev", "top_p_dev", "min_p_dev")] + \
+               [("temperature", ctypes.c_float), ("top_k", ctypes.c_int), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float)]
+
+
 # Exported symbols and their ctypes signatures (mirrors include/pvmvmd.h).
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
 _l, _f = ctypes.c_int64, ctypes.c_float
@@ -151,6 +178,14 @@ SIGNATURES = {
                                     _i, _i, *_rows, _vp, _vp]),
     "pvmvmd_kv_evict": (_i, [ctypes.POINTER(pvmvmd_kv_pool), ctypes.POINTER(pvmvmd_kv_batch), _i, _i, _vp, _l, _i, _vp,
                              _vp]),
+    "pvmvmd_block_norm": (_i, [_i, _i, ctypes.POINTER(pvmvmd_rows), ctypes.POINTER(pvmvmd_norm),
+                               ctypes.POINTER(pvmvmd_rows), _f, ctypes.POINTER(pvmvmd_rows), _f,
+                               ctypes.POINTER(pvmvmd_rows_out), ctypes.POINTER(pvmvmd_norm),
+                               ctypes.POINTER(pvmvmd_rows_out), _vp]),
+    "pvmvmd_glu": (_i, [_i, _i, ctypes.POINTER(pvmvmd_rows), _i, ctypes.POINTER(pvmvmd_rows),
+                        ctypes.POINTER(pvmvmd_rows_out), _vp]),
+    "pvmvmd_sample": (_i, [_i, _i, ctypes.POINTER(pvmvmd_rows), ctypes.POINTER(pvmvmd_sampling), _vp, _l, _vp, _vp, _vp,
+                           _vp]),
     "pvmvmd_device_status": (_i, [_vp]),
     "pvmvmd_kernel_launches": (ctypes.c_ulonglong, []),
     "pvmvmd_debug_expire_wait": (_i, [_i, ctypes.c_uint32, ctypes.c_uint64]),
@@ -833,6 +868,120 @@ def pvmvmd_kv_evict(pool: KvPool, batch: KvBatch, budget: int, recent: int = 0, 
     _check((_native or _open_calls()).evict(pool.address, batch.address, budget, recent, new_table, new_lens, stream),
            "pvmvmd_kv_evict")
     return new_lens
+
+
+# ---------------------------------------------------------------- the client's other steps
+
+class Rows(NamedTuple):
+    """Rows to read (T x D, floating or field elements; contiguous in a row) with the scales that take them to numbers:
+    scale, and float32 vectors of one scale a row and one a column.  The calls below take one, or a tensor alone."""
+    data: object
+    scale: float = 1.0
+    token_scale: object = None
+    channel_scale: object = None
+
+
+class _NormView(ctypes.Structure):
+    _fields_ = [("norm", pvmvmd_norm), ("D", ctypes.c_int64)]
+
+
+class _SamplingView(ctypes.Structure):
+    _fields_ = [("how", pvmvmd_sampling), ("T", ctypes.c_int64)]
+
+
+class Norm:
+    """A norm over rows of D values: kind "rms" or "layer", weight and bias D values of one floating type (or None);
+    weight_add is added to the weights (1 where they are stored as what they differ from 1 by).  Checked once, used by
+    every call while the tensors live."""
+
+    def __init__(self, kind: str = "rms", weight=None, bias=None, eps: float = 1e-6, weight_add: float = 0.0):
+        if kind not in PVMVMD_NORM:
+            raise ValueError(f"kind must be one of {sorted(PVMVMD_NORM)}")
+        given = [t for t in (weight, bias) if t is not None]
+        code, D = PVMVMD_F32, 0
+        for t in given:
+            if t.dim() != 1 or t.dtype != given[0].dtype or t.shape != given[0].shape:
+                raise ValueError("weight and bias must be vectors of one length and type")
+            code, D = _type_code(t, "weight"), t.numel()
+        ptrs = [None if t is None else _dev_ptr(t, n, (t.dtype,)) for t, n in ((weight, "weight"), (bias, "bias"))]
+        self.weight, self.bias = weight, bias
+        self.view = _NormView(pvmvmd_norm(*ptrs, eps, weight_add, PVMVMD_NORM[kind], code), D)
+        self.address = ctypes.addressof(self.view)
+
+
+class Sampling:
+    """How tokens are chosen: each parameter a number for all rows or a CUDA vector of one a row (float32, top_k int32).
+    temperature 0: greedy; top_k 0, top_p 1, min_p 0: no limit.  Checked once; the vectors' values may change between
+    calls."""
+
+    def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        torch = _torch or _lazy_torch()
+        self.T, ptrs, numbers = 0, [], []
+        for v, name in ((temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p")):
+            if isinstance(v, torch.Tensor):
+                ptrs.append(_dev_ptr(v, name, (torch.int32 if name == "top_k" else torch.float32,), self.T or None))
+                if v.dim() != 1 or v.numel() == 0:
+                    raise ValueError(f"{name} must be a vector of one value a row")
+                self.T = v.numel()
+                numbers.append(0)
+            else:
+                ptrs.append(None)
+                numbers.append(int(v) if name == "top_k" else float(v))
+        if not -2**31 <= numbers[1] < 2**31:
+            raise OverflowError("top_k does not fit 32 bits")
+        self.kept = (temperature, top_k, top_p, min_p)
+        self.view = _SamplingView(pvmvmd_sampling(*ptrs, *numbers), self.T)
+        self.address = ctypes.addressof(self.view)
+
+
+def pvmvmd_block_norm(y, residual=None, post: Norm | None = None, gate=None, branch_scale: float = 1.0,
+                      residual_scale: float = 1.0, residual_out=None, pre: Norm | None = None, out=None,
+                      out_scale: float = 1.0, limit: int = 127, out_token_scale=None, stream=None):
+    """r' = residual_scale residual + branch_scale gate post(y), out = pre(r') -> (residual_out, out).
+
+    y (T x D): a Rows or tensor, or None (r' = residual_scale residual); gate: the same, or one row of D values for all.
+    residual_out: a floating tensor to take r' (may be residual itself); default: a new one of residual's type, bf16 without
+    one; False: r' is not kept.  out: a floating tensor, or an int32 one for field elements of the integers round(z out_scale) within +-limit; with
+    out_token_scale (float32, T) each row has a step of its own, max |z| / limit, which is written there.  Without out,
+    only r' is formed."""
+    like = residual if y is None else y[0] if type(y) is Rows else y
+    if residual_out is None:
+        torch = _torch or _lazy_torch()
+        residual_out = like.new_empty(like.shape, dtype=torch.bfloat16 if residual is None else residual.dtype)
+    elif residual_out is False:
+        residual_out = None
+    _check((_native or _open_calls()).norm(y, residual, 0 if post is None else post.address, gate, branch_scale,
+                                           residual_scale, residual_out, 0 if pre is None else pre.address, out, out_scale,
+                                           limit, out_token_scale, stream), "pvmvmd_block_norm")
+    return residual_out, out
+
+
+def pvmvmd_glu(gate, up=None, act: str = "silu", out=None, out_scale: float = 1.0, limit: int = 127,
+               out_token_scale=None, stream=None):
+    """act(gate) up -> out, T x D (up None: act(gate)).  gate, up: Rows or tensors; act: "none", "relu", "sigmoid", "silu"
+    or "gelu" (the tanh form); out as for pvmvmd_block_norm, default int32 field elements."""
+    code = PVMVMD_ACT.get(act)
+    if code is None:
+        raise ValueError(f"act must be one of {sorted(PVMVMD_ACT)}")
+    if out is None:
+        x = gate[0] if type(gate) is Rows else gate
+        out = x.new_empty(x.shape, dtype=(_torch or _lazy_torch()).int32)
+    _check((_native or _open_calls()).glu(gate, code, up, out, out_scale, limit, out_token_scale, stream), "pvmvmd_glu")
+    return out
+
+
+def pvmvmd_sample(logits, random, sampling: Sampling, allowed=None, token=None, logprob=None, stream=None):
+    """One token for each row of logits (T x V, a Rows or tensor) -> token (int32, T; -1 where none may be chosen).
+
+    random: T uniform words of 32 bits (int32 or uint32).  allowed: bits of the tokens that may be chosen, 32-bit words
+    (T x ceil(V / 32), or one row for all; bit i % 32 of word i / 32).  logprob: a float32 tensor (T) to fill with the log
+    of the probability that the token was drawn with."""
+    if token is None:
+        x = logits[0] if type(logits) is Rows else logits
+        token = x.new_empty(x.shape[0], dtype=(_torch or _lazy_torch()).int32)
+    _check((_native or _open_calls()).sample(logits, random, sampling.address, allowed, token, logprob, stream),
+           "pvmvmd_sample")
+    return token
 
 
 PVMVMD_DEBUG_WAIT_OFF = 0

@@ -1,5 +1,5 @@
-/* The binding's calls of the client's attention, whose kernels for a few tokens take
- * less time than ctypes needs for a call's twenty arguments: a Python module that looks
+/* The binding's calls of the client's attention and its other steps, whose kernels for a few tokens
+ * take less time than ctypes needs for a call's twenty arguments: a Python module that looks
  * at the tensors and calls libpvmvmd.so.  (One token rotated 3.7 us a call where 6.5
  * through ctypes, 8 appended 4.6 and 8.7, attention of 8 over 8 5.1 and 8.2, of which the
  * device takes the 5.1.)
@@ -10,6 +10,7 @@
 #include <limits.h>
 #include <math.h>
 #include <stdint.h>
+#include <string.h>
 
 #include "pvmvmd.h"
 
@@ -21,6 +22,9 @@ static __typeof__(&pvmvmd_rope) f_rope;
 static __typeof__(&pvmvmd_kv_append) f_append;
 static __typeof__(&pvmvmd_paged_attention) f_attend;
 static __typeof__(&pvmvmd_kv_evict) f_evict;
+static __typeof__(&pvmvmd_block_norm) f_norm;
+static __typeof__(&pvmvmd_glu) f_glu;
+static __typeof__(&pvmvmd_sample) f_sample;
 
 typedef struct {
     void *p;
@@ -255,6 +259,190 @@ static PyObject *evict(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
+/* ---- the client's other steps */
+
+/* What a Norm and a Sampling of the binding hold: the library's struct and the length it is for (0: any). */
+typedef struct {
+    pvmvmd_norm norm;
+    int64_t D;
+} NormView;
+typedef struct {
+    pvmvmd_sampling how;
+    int64_t T;
+} SamplingView;
+
+/* T x D values with contiguous rows, of which `one` says whether a single row (or D values) may stand for all. */
+static int matrix(PyObject *t, const char *name, int64_t T, int64_t D, int one, void **p, int64_t *token) {
+    int64_t d[2], s[2];
+    if (!on_device(t, name)) return 0;
+    PyObject *shape = PyObject_GetAttr(t, s_shape);
+    const int flat = one && shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 1;
+    Py_XDECREF(shape);
+    if (!shape) return 0;
+    if (flat) {
+        if (!dims(t, name, 1, d + 1) || !numbers(PyObject_CallMethodNoArgs(t, s_stride), 1, s + 1)) return 0;
+        d[0] = 1;
+        s[0] = 0;
+    } else if (!dims(t, name, 2, d) || !numbers(PyObject_CallMethodNoArgs(t, s_stride), 2, s)) {
+        return 0;
+    }
+    if (d[1] != D || (d[0] != T && !(one && d[0] == 1))) {
+        PyErr_Format(PyExc_ValueError, "%s must be %lld x %lld, got %lld x %lld", name, (long long)T, (long long)D,
+                     (long long)d[0], (long long)d[1]);
+        return 0;
+    }
+    if (s[1] != 1 && D > 1) {
+        PyErr_Format(PyExc_ValueError, "the last dimension of %s must be contiguous", name);
+        return 0;
+    }
+    *token = d[0] == 1 && T != 1 ? 0 : s[0];
+    return to_ptr(t, p);
+}
+/* The tensor of a Rows (a tuple: data, scale, token_scale, channel_scale), or the tensor itself. */
+static PyObject *data_of(PyObject *o) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4 ? PyTuple_GET_ITEM(o, 0) : o; }
+static int rows_in(PyObject *o, const char *name, int64_t T, int64_t D, int one, pvmvmd_rows *r) {
+    PyObject *data = data_of(o), *type;
+    void *p;
+    memset(r, 0, sizeof(*r));
+    r->scale = 1.0f;
+    if (!matrix(data, name, T, D, one, &p, &r->token) || !type_code(data, name, 1, &r->type, &type)) return 0;
+    r->data_dev = p;
+    if (data == o) return 1;
+    PyObject *scale = PyTuple_GET_ITEM(o, 1), *token = PyTuple_GET_ITEM(o, 2), *channel = PyTuple_GET_ITEM(o, 3);
+    r->scale = (float)PyFloat_AsDouble(scale);
+    if (PyErr_Occurred()) return 0;
+    if (token != Py_None) {
+        if (!vector(token, "token_scale", T, t_float[2], &p)) return 0;
+        r->token_scale_dev = p;
+    }
+    if (channel != Py_None) {
+        if (!vector(channel, "channel_scale", D, t_float[2], &p)) return 0;
+        r->channel_scale_dev = p;
+    }
+    return 1;
+}
+/* out, its scale, limit and token_scale (three arguments from a on) */
+static int rows_out(PyObject *o, const char *name, int64_t T, int64_t D, PyObject *const *a, pvmvmd_rows_out *r) {
+    PyObject *type;
+    memset(r, 0, sizeof(*r));
+    r->scale = 1.0f;
+    r->limit = 1;
+    if (!matrix(o, name, T, D, 0, &r->data_dev, &r->token) || !type_code(o, name, a != NULL, &r->type, &type)) return 0;
+    if (!a) return 1;
+    r->scale = (float)PyFloat_AsDouble(a[0]);
+    if (PyErr_Occurred() || !to_int(a[1], "limit", &r->limit)) return 0;
+    void *p = NULL;
+    if (a[2] != Py_None && !vector(a[2], "out_token_scale", T, t_float[2], &p)) return 0;
+    r->token_scale_dev = p;
+    return 1;
+}
+static int norm_view(PyObject *v, const char *name, int64_t D, const NormView **n) {
+    void *p;
+    if (!address(v, &p)) return 0;
+    *n = p;
+    if (p && (*n)->D && (*n)->D != D) {
+        PyErr_Format(PyExc_ValueError, "%s is of %lld values, the rows are of %lld", name, (long long)(*n)->D, (long long)D);
+        return 0;
+    }
+    return 1;
+}
+static int has(void *f) {
+    if (!f) PyErr_SetString(PyExc_RuntimeError, "the library has not been opened, or does not have this call");
+    return f != NULL;
+}
+
+/* norm(y or None, residual or None, post or 0, gate or None, branch_scale, residual_scale, residual_out or None, pre or 0,
+ *      out or None, out_scale, limit, out_token_scale or None, stream) */
+static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    int64_t d[2];
+    pvmvmd_rows y, gate, residual;
+    pvmvmd_rows_out residual_out, out;
+    const NormView *post, *pre;
+    void *stream;
+    int status;
+    if (!has((void *)f_norm) || !arity(n, 13)) return NULL;
+    if (a[0] == Py_None && a[1] == Py_None) {
+        PyErr_SetString(PyExc_ValueError, "y or residual must be there");
+        return NULL;
+    }
+    if (!dims(a[0] != Py_None ? data_of(a[0]) : a[1], a[0] != Py_None ? "y" : "residual", 2, d) ||
+        (a[0] != Py_None && !rows_in(a[0], "y", d[0], d[1], 0, &y)) ||
+        (a[1] != Py_None && !rows_in(a[1], "residual", d[0], d[1], 0, &residual)) ||
+        !norm_view(a[2], "post", d[1], &post) || (a[3] != Py_None && !rows_in(a[3], "gate", d[0], d[1], 1, &gate)) ||
+        (a[6] != Py_None && !rows_out(a[6], "residual_out", d[0], d[1], NULL, &residual_out)) ||
+        !norm_view(a[7], "pre", d[1], &pre) || (a[8] != Py_None && !rows_out(a[8], "out", d[0], d[1], a + 9, &out)))
+        return NULL;
+    const double branch = PyFloat_AsDouble(a[4]), keep = PyErr_Occurred() ? 0 : PyFloat_AsDouble(a[5]);
+    if (PyErr_Occurred() || !stream_of(a[12], &stream)) return NULL;
+    if (d[0] > INT_MAX || d[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
+    CALL(status, f_norm((int)d[0], (int)d[1], a[0] != Py_None ? &y : NULL, post ? &post->norm : NULL,
+                        a[3] != Py_None ? &gate : NULL, (float)branch, a[1] != Py_None ? &residual : NULL, (float)keep,
+                        a[6] != Py_None ? &residual_out : NULL, pre ? &pre->norm : NULL, a[8] != Py_None ? &out : NULL,
+                        stream))
+    return PyLong_FromLong(status);
+}
+
+/* glu(gate, act, up or None, out, out_scale, limit, out_token_scale or None, stream) */
+static PyObject *glu(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    int64_t d[2];
+    pvmvmd_rows gate, up;
+    pvmvmd_rows_out out;
+    void *stream;
+    int act, status;
+    if (!has((void *)f_glu) || !arity(n, 8) || !dims(data_of(a[0]), "gate", 2, d) ||
+        !rows_in(a[0], "gate", d[0], d[1], 0, &gate) || !to_int(a[1], "act", &act) ||
+        (a[2] != Py_None && !rows_in(a[2], "up", d[0], d[1], 0, &up)) ||
+        !rows_out(a[3], "out", d[0], d[1], a + 4, &out) || !stream_of(a[7], &stream))
+        return NULL;
+    if (d[0] > INT_MAX || d[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
+    CALL(status, f_glu((int)d[0], (int)d[1], &gate, act, a[2] != Py_None ? &up : NULL, &out, stream))
+    return PyLong_FromLong(status);
+}
+
+/* A vector of n words of 32 bits. */
+static int words(PyObject *t, const char *name, int64_t n, void **p) {
+    PyObject *d = PyObject_GetAttr(t, s_dtype);
+    if (!d) {
+        PyErr_Clear();
+        return on_device(t, name);
+    }
+    const int other = d != Py_None && d == t_uint32;
+    Py_DECREF(d);
+    return vector(t, name, n, other ? t_uint32 : t_int32, p);
+}
+/* sample(logits, random, sampling, allowed or None, token, logprob or None, stream) */
+static PyObject *sample(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    int64_t d[2], row = 0;
+    pvmvmd_rows logits;
+    void *v, *random, *allowed = NULL, *token, *logprob = NULL, *stream;
+    PyObject *type;
+    int code, status;
+    if (!has((void *)f_sample) || !arity(n, 7) || !dims(data_of(a[0]), "logits", 2, d) ||
+        !rows_in(a[0], "logits", d[0], d[1], 0, &logits) || !words(a[1], "random", d[0], &random) || !address(a[2], &v))
+        return NULL;
+    const SamplingView *how = v;
+    if (how->T && how->T != d[0]) {
+        PyErr_Format(PyExc_ValueError, "the sampling is of %lld rows, the logits of %lld", (long long)how->T,
+                     (long long)d[0]);
+        return NULL;
+    }
+    if (a[3] != Py_None) {
+        if (!matrix(a[3], "allowed", d[0], (d[1] + 31) / 32, 1, &allowed, &row) ||
+            !type_code(a[3], "allowed", 1, &code, &type))
+            return NULL;
+        if (code != PVMVMD_FIELD) {
+            PyErr_SetString(PyExc_TypeError, "allowed must hold words of 32 bits");
+            return NULL;
+        }
+    }
+    if (!vector(a[4], "token", d[0], t_int32, &token) ||
+        (a[5] != Py_None && !vector(a[5], "logprob", d[0], t_float[2], &logprob)) || !stream_of(a[6], &stream))
+        return NULL;
+    if (d[0] > INT_MAX || d[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
+    CALL(status, f_sample((int)d[0], (int)d[1], &logits, &how->how, allowed, row, random, token, logprob, stream))
+    return PyLong_FromLong(status);
+}
+
 /* open(library handle, bfloat16, float16, float32, int32, uint32 or None, stream, device or None) */
 static PyObject *open_library(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     void *h;
@@ -263,6 +451,9 @@ static PyObject *open_library(PyObject *self, PyObject *const *a, Py_ssize_t n) 
     f_append = (__typeof__(f_append))dlsym(h, "pvmvmd_kv_append");
     f_attend = (__typeof__(f_attend))dlsym(h, "pvmvmd_paged_attention");
     f_evict = (__typeof__(f_evict))dlsym(h, "pvmvmd_kv_evict");
+    f_norm = (__typeof__(f_norm))dlsym(h, "pvmvmd_block_norm");
+    f_glu = (__typeof__(f_glu))dlsym(h, "pvmvmd_glu");
+    f_sample = (__typeof__(f_sample))dlsym(h, "pvmvmd_sample");
     if (!f_rope || !f_append || !f_attend || !f_evict) {
         PyErr_SetString(PyExc_ImportError, "libpvmvmd.so does not have the calls of the client's attention");
         return NULL;
@@ -277,6 +468,9 @@ static PyMethodDef methods[] = {{"open", (PyCFunction)(void (*)(void))open_libra
                                 {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, NULL},
                                 {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, NULL},
                                 {"evict", (PyCFunction)(void (*)(void))evict, METH_FASTCALL, NULL},
+                                {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, NULL},
+                                {"glu", (PyCFunction)(void (*)(void))glu, METH_FASTCALL, NULL},
+                                {"sample", (PyCFunction)(void (*)(void))sample, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
