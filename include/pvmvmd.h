@@ -554,7 +554,7 @@ typedef struct {
  *     m = min(limit / a, FLT_MAX) with a = max_i |z_i| of the row, whose step
  *     token_scale_dev[t] = a / limit is written (a row with a value that is not finite
  *     gives zeros, and NaN for its step).
- * 1 <= limit <= 2^23. */
+ * 1 <= limit <= 2^22. */
 typedef struct {
     void *data_dev;
     float *token_scale_dev; /* [T] or null; null for floating types */
@@ -587,7 +587,7 @@ typedef struct {
  * residual and residual_out have floating types, no scales, and may be one tensor.
  * D <= PVMVMD_MAX_K.  Errors: PVMVMD_E_ARG (null pointer, unknown type or norm, a step for a
  * floating output), PVMVMD_E_SHAPE (T < 0, D outside [1, PVMVMD_MAX_K]), PVMVMD_E_PARAM (eps
- * not above 0, a limit outside [1, 2^23], a scale that is not finite). */
+ * not above 0, a limit outside [1, 2^22], a scale that is not finite). */
 int pvmvmd_block_norm(int T, int D, const pvmvmd_rows *y, const pvmvmd_norm *post, const pvmvmd_rows *gate,
                       float branch_scale, const pvmvmd_rows *residual, float residual_scale,
                       const pvmvmd_rows_out *residual_out, const pvmvmd_norm *pre, const pvmvmd_rows_out *out,

@@ -8,140 +8,161 @@ namespace {
 struct NormArgs {
     NormJob j;
     RowDeal d;
+    Pair inverse;  // 1 / D
 };
 
-// n = norm(x) in place, for all of a thread's chunks.  Values outside the row are 0 and stay out of the
-// sums.
+// n = norm(x) in place, for all of a thread's chunks.  Values outside the row must be 0 at the call (and are
+// anything after it).
 template <bool kVec, int kChunks>
-__device__ __forceinline__ void norm(RowThreads &r, const pvmvmd_norm &n, int threads, int D, float (&x)[kChunks][kWide]) {
+__device__ __forceinline__ void norm(RowThreads &r, const pvmvmd_norm &n, Pair inverse, const Place<kVec> &at,
+                                     Two (&x)[kChunks][kTwos]) {
     if (n.kind == PVMVMD_NORM_LAYER) {
-        Pair s{0.0f, 0.0f};
+        Pairs s{both(0.0f), both(0.0f)};
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) add_term(s, x[c][e], 0.0f);
-        const Pair m = mean_of(row_sum(r, s), (float)D);
-        const float mu = __fadd_rn(m.h, m.l);
+            for (int i = 0; i < kTwos; ++i) add_terms(s, x[c][i]);
+        const Pair m = mean_of(row_sum(r, join(s)), inverse);
+        const Two mu = both(__fadd_rn(m.h, m.l));
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
-            const Place<kVec> p = place_of<kVec>(r, threads, c, kChunks, D);
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) x[c][e] = p.in(e) ? __fsub_rn(x[c][e], mu) : 0.0f;
+            for (int i = 0; i < kTwos; ++i) x[c][i] = sub2(x[c][i], mu);
+            outside_zero<kVec>(at.chunk(c), x[c]);
         }
     }
-    Pair s{0.0f, 0.0f};
+    Pairs s{both(0.0f), both(0.0f)};
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-        for (int e = 0; e < kWide; ++e) add_square(s, x[c][e]);
-    const float inv = inverse_root(mean_of(row_sum(r, s), (float)D), n.eps);
+        for (int i = 0; i < kTwos; ++i) add_squares(s, x[c][i]);
+    // (the weights are on their way meanwhile)
+    Raw w[kChunks];
+    if (n.weight_dev)
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) w[c] = load_raw<kVec>(n.weight_dev, n.type, at.chunk(c));
+    const Two inv = both(inverse_root(mean_of(row_sum(r, join(s)), inverse), n.eps));
+    Two v[kTwos];
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
-        const Place<kVec> p = place_of<kVec>(r, threads, c, kChunks, D);
-        float v[kWide];
 #pragma unroll
-        for (int e = 0; e < kWide; ++e) x[c][e] = __fmul_rn(x[c][e], inv);
+        for (int i = 0; i < kTwos; ++i) x[c][i] = mul2(x[c][i], inv);
         if (n.weight_dev) {
-            unpack(load_raw<kVec>(n.weight_dev, n.type, p), n.type, v);
+            unpack(w[c], n.type, v);
+            if (n.weight_add != 0.0f)
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) x[c][e] = __fmul_rn(x[c][e], __fadd_rn(v[e], n.weight_add));
+                for (int i = 0; i < kTwos; ++i) v[i] = add2(v[i], both(n.weight_add));
+#pragma unroll
+            for (int i = 0; i < kTwos; ++i) x[c][i] = mul2(x[c][i], v[i]);
         } else if (n.weight_add != 0.0f) {
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) x[c][e] = __fmul_rn(x[c][e], __fadd_rn(1.0f, n.weight_add));
+            for (int i = 0; i < kTwos; ++i) x[c][i] = mul2(x[c][i], both(__fadd_rn(1.0f, n.weight_add)));
         }
         if (n.bias_dev) {
-            unpack(load_raw<kVec>(n.bias_dev, n.type, p), n.type, v);
+            unpack(load_raw<kVec>(n.bias_dev, n.type, at.chunk(c)), n.type, v);
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) x[c][e] = p.in(e) ? __fadd_rn(x[c][e], v[e]) : 0.0f;
+            for (int i = 0; i < kTwos; ++i) x[c][i] = add2(x[c][i], v[i]);
         }
     }
 }
 
-template <bool kVec, int kChunks>
+// kY, kR, kO: the kinds of y (and a gate), of the residual and its output, and of out; kGate: there may be a
+// gate.
+template <bool kVec, int kChunks, Kind kY, Kind kR, Kind kO, bool kGate>
 __global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 ? 1 : 2)
     k_block_norm(const __grid_constant__ NormArgs a) {
     follow();
     const NormJob &j = a.j;
     __shared__ RowShared sh;
     RowThreads r = row_threads(&sh, a.d);
-    cluster_begin(r.ctas);
-    const int threads = a.d.threads, D = j.D;
-    const int64_t t = a.d.rows > 1 ? (int64_t)blockIdx.x * a.d.rows + r.warp : blockIdx.x / r.ctas;
+    const int64_t t = r.t;
     if (t >= j.T) return;  // (warps of several rows have no exchanges)
+    const int yt = known<kY>(j.y.type), rt = known<kR>(j.residual.type), qt = known<kR>(j.residual_out.type),
+              ot = known<kO>(j.out.type), gt = j.gate.type;
+    const Place<kVec> at = place_of<kVec, kChunks>(r, j.D);
     Raw y[kChunks], g[kChunks], s[kChunks];
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
-        const Place<kVec> p = place_of<kVec>(r, threads, c, kChunks, D);
-        if (j.has_y) y[c] = load_raw<kVec>(row_of(j.y, t), j.y.type, p);
-        if (j.has_residual) s[c] = load_raw<kVec>(row_of(j.residual, t), j.residual.type, p);
-        if (j.has_gate) g[c] = load_raw<kVec>(row_of(j.gate, t), j.gate.type, p);
+        if (j.has_y) y[c] = load_raw<kVec>(row_of(j.y, yt, t), yt, at.chunk(c));
+        if (j.has_residual) s[c] = load_raw<kVec>(row_of(j.residual, rt, t), rt, at.chunk(c));
+        if (kGate && j.has_gate) g[c] = load_raw<kVec>(row_of(j.gate, gt, t), gt, at.chunk(c));
     }
-    float x[kChunks][kWide];
+    Two x[kChunks][kTwos];
     if (j.has_y) {
         const float c0 = row_scale(j.y, t);
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-            read<kVec>(y[c], j.y, c0, place_of<kVec>(r, threads, c, kChunks, D), x[c]);
-        if (j.post.kind) norm<kVec, kChunks>(r, j.post, threads, D, x);
+        for (int c = 0; c < kChunks; ++c) read<kVec>(y[c], j.y, yt, c0, at.chunk(c), x[c]);
+        if (j.post.kind) norm<kVec, kChunks>(r, j.post, a.inverse, at, x);
     }
-    const float gc = j.has_gate ? row_scale(j.gate, t) : 0.0f;
+    const float gc = kGate && j.has_gate ? row_scale(j.gate, t) : 0.0f;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
-        const Place<kVec> p = place_of<kVec>(r, threads, c, kChunks, D);
+        Two v[kTwos];
         if (j.has_y) {
-            if (j.has_gate) {
-                float v[kWide];
-                read<kVec>(g[c], j.gate, gc, p, v);
+            if (kGate && j.has_gate) {
+                read<kVec>(g[c], j.gate, gt, gc, at.chunk(c), v);
 #pragma unroll
-                for (int e = 0; e < kWide; ++e) x[c][e] = __fmul_rn(x[c][e], v[e]);
+                for (int i = 0; i < kTwos; ++i) x[c][i] = mul2(x[c][i], v[i]);
             }
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) x[c][e] = __fmul_rn(x[c][e], j.branch_scale);
+            for (int i = 0; i < kTwos; ++i) x[c][i] = mul2(x[c][i], both(j.branch_scale));
         }
         if (j.has_residual) {
-            float v[kWide];
-            unpack(s[c], j.residual.type, v);
+            unpack(s[c], rt, v);
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) {
-                const float q = __fmul_rn(v[e], j.residual_scale);
-                x[c][e] = j.has_y ? __fadd_rn(q, x[c][e]) : q;
+            for (int i = 0; i < kTwos; ++i) {
+                v[i] = mul2(v[i], both(j.residual_scale));
+                x[c][i] = j.has_y ? add2(v[i], x[c][i]) : v[i];
             }
         }
-        if (j.residual_out.data_dev) write<kVec>(j.residual_out, t, p, x[c], 1.0f);
-        // what lies outside the row is 0 from here on (a scale that is not finite made it NaN)
-#pragma unroll
-        for (int e = 0; e < kWide; ++e)
-            if (!p.in(e)) x[c][e] = 0.0f;
+        if (j.residual_out.data_dev) write<kVec>(j.residual_out, qt, t, at.chunk(c), x[c], Step{1.0f, false});
+        // what lies outside the row is 0 from here on (a bias, or a scale that is not finite, made it another value)
+        outside_zero<kVec>(at.chunk(c), x[c]);
     }
     if (j.out.data_dev) {
-        if (j.pre.kind) norm<kVec, kChunks>(r, j.pre, threads, D, x);
-        float m = j.out.scale;
+        if (j.pre.kind) norm<kVec, kChunks>(r, j.pre, a.inverse, at, x);
+        Step m{j.out.scale, false};
         if (j.out.token_scale_dev) {
-            uint32_t big = 0;
+            float big = 0.0f;
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c)
+            for (int c = 0; c < kChunks; ++c) {
+                outside_zero<kVec>(at.chunk(c), x[c]);
 #pragma unroll
-                for (int e = 0; e < kWide; ++e) big = max(big, __float_as_uint(x[c][e]) & 0x7fffffffu);
-            float step;
-            m = dynamic_scale(j.out, row_max(r, big), step);
-            if (r.lane == 0 && r.rank == 0 && (r.warps == 1 || r.warp == 0)) j.out.token_scale_dev[t] = step;
+                for (int i = 0; i < kTwos; ++i) big = larger(larger(big, first(x[c][i])), second(x[c][i]));
+            }
+            big = row_max(r, big);
+            m = step_of(j.out, big);
+            if (r.lane == 0 && r.rank == 0 && (r.warps == 1 || r.warp == 0)) write_step(j.out, t, big);
         }
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-            write<kVec>(j.out, t, place_of<kVec>(r, threads, c, kChunks, D), x[c], m);
+        for (int c = 0; c < kChunks; ++c) write<kVec>(j.out, ot, t, at.chunk(c), x[c], m);
     }
-    row_end(r);
+    row_begun(r);
 }
 
-template <bool kVec>
-cudaError_t launch_vec(const NormArgs &a, cudaStream_t s) {
-    const RowDeal &d = a.d;
-    const dim3 grid((unsigned)(((int64_t)a.j.T + d.rows - 1) / d.rows * d.ctas));
-    switch (d.chunks) {
-        case 1: return launch_cluster(k_block_norm<kVec, 1>, grid, d.ctas, d.threads, 0, s, a);
-        case 2: return launch_cluster(k_block_norm<kVec, 2>, grid, d.ctas, d.threads, 0, s, a);
-        default: return launch_cluster(k_block_norm<kVec, 4>, grid, d.ctas, d.threads, 0, s, a);
+template <bool kVec, Kind kY, Kind kR, Kind kO, bool kGate>
+cudaError_t launch_kind(const NormArgs &a, cudaStream_t s) {
+    const dim3 grid = grid_of(a.d, a.j.T);
+    const int ctas = 1 << a.d.log_ctas;
+    switch (a.d.chunks) {
+        case 1: return launch_cluster(k_block_norm<kVec, 1, kY, kR, kO, kGate>, grid, ctas, a.d.threads, 0, s, a);
+        case 2: return launch_cluster(k_block_norm<kVec, 2, kY, kR, kO, kGate>, grid, ctas, a.d.threads, 0, s, a);
+        default: return launch_cluster(k_block_norm<kVec, 4, kY, kR, kO, kGate>, grid, ctas, a.d.threads, 0, s, a);
     }
+}
+// Kernels for the kinds of a model's own types, and of the field, beside the one for any: with the kinds known, 600
+// instructions a thread are left of 1170.
+template <Kind kY, Kind kR, Kind kO>
+cudaError_t launch_gate(const NormArgs &a, cudaStream_t s) {
+    return a.j.has_gate ? launch_kind<true, kY, kR, kO, true>(a, s) : launch_kind<true, kY, kR, kO, false>(a, s);
+}
+template <Kind kY, Kind kR>
+cudaError_t launch_out(const NormArgs &a, cudaStream_t s) {
+    return kind_of(a.j.out.type) == kField ? launch_gate<kY, kR, kField>(a, s) : launch_gate<kY, kR, kHalf>(a, s);
+}
+template <Kind kY>
+cudaError_t launch_residual(const NormArgs &a, cudaStream_t s) {
+    return kind_of(a.j.residual.type) == kF32 ? launch_out<kY, kF32>(a, s) : launch_out<kY, kHalf>(a, s);
 }
 
 bool whole16(const pvmvmd_norm &n) {
@@ -151,11 +172,15 @@ bool whole16(const pvmvmd_norm &n) {
 }  // namespace
 
 cudaError_t launch_block_norm(const NormJob &j, cudaStream_t s) {
-    NormArgs a{j, deal_rows(j.T, j.D)};
+    const NormArgs a{j, deal_rows(j.T, j.D), inverse_of(j.D)};
     const bool vec = j.D % kWide == 0 && (!j.has_y || whole16(j.y)) && (!j.has_gate || whole16(j.gate)) &&
                      (!j.has_residual || whole16(j.residual)) && whole16(j.residual_out) && whole16(j.out) &&
                      whole16(j.post) && whole16(j.pre);
-    return vec ? launch_vec<true>(a, s) : launch_vec<false>(a, s);
+    if (!vec) return launch_kind<false, kAny, kAny, kAny, true>(a, s);
+    if (j.has_y && j.has_residual && j.out.data_dev && kind_of(j.y.type) != kF32 && kind_of(j.out.type) != kF32 &&
+        (!j.residual_out.data_dev || kind_of(j.residual_out.type) == kind_of(j.residual.type)))
+        return kind_of(j.y.type) == kField ? launch_residual<kField>(a, s) : launch_residual<kHalf>(a, s);
+    return launch_kind<true, kAny, kAny, kAny, true>(a, s);
 }
 
 }  // namespace pv

@@ -1,9 +1,9 @@
 // Rows of values as the client's other steps read and write them (pvmvmd_rows and
 // pvmvmd_rows_out of include/pvmvmd.h), and the arithmetic that these steps are defined in.
 //
-// The types are known at run time: what a thread reads first goes into registers as it
-// is (Raw), so that all of its loads are under way before the first value is needed, and a branch
-// that is the same for the whole grid turns it into 32-bit numbers.
+// What a thread reads first goes into registers as it is (Raw), so that all of its loads are under way
+// before the first value is needed, and then becomes 32-bit numbers, by a branch that is the same for
+// the whole grid where the kernel is compiled for any type.
 #pragma once
 
 #include <algorithm>
@@ -15,54 +15,101 @@ namespace pv {
 
 constexpr float kFltMax = 3.402823466e+38f;
 constexpr int kWide = 8;  // values that a thread takes at a time
+constexpr int kTwos = kWide / 2;
 
 __host__ __device__ inline bool two_bytes(int type) { return type == PVMVMD_BF16 || type == PVMVMD_F16; }
 
+// What a kernel is compiled for: a kind of values, or any.
+enum Kind { kAny, kHalf, kF32, kField };
+inline Kind kind_of(int type) { return two_bytes(type) ? kHalf : type == PVMVMD_F32 ? kF32 : kField; }
+// The type of values of a kind, with what the kind says known to the compiler.
+template <Kind k>
+__device__ __forceinline__ int known(int type) {
+    if (k == kHalf) return type == PVMVMD_BF16 ? PVMVMD_BF16 : PVMVMD_F16;
+    return k == kF32 ? PVMVMD_F32 : k == kField ? PVMVMD_FIELD : type;
+}
+
+// ---------------------------------------------------------------- two numbers at a time
+// Products and sums of pairs by one instruction, each rounded by itself as if alone.  They are kept as the
+// 64 bits that the instruction takes: as two of 32 they would be moved together every time.
+struct Two {
+    unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ Two two(uint32_t a, uint32_t b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ Two both(float v) { return two(v, v); }
+__device__ __forceinline__ float first(Two x) { return __uint_as_float((uint32_t)x.v); }
+__device__ __forceinline__ float second(Two x) { return __uint_as_float((uint32_t)(x.v >> 32)); }
+__device__ __forceinline__ Two add2(Two x, Two y) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(x.v), "l"(y.v));
+    return r;
+}
+__device__ __forceinline__ Two sub2(Two x, Two y) {
+    Two r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(x.v), "l"(y.v));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two x, Two y, Two z) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(x.v), "l"(y.v), "l"(z.v));
+    return r;
+}
+__device__ __forceinline__ Two minus2(Two x) { return Two{x.v ^ 0x8000000080000000ull}; }
+// A product alone.  (mul.rn.f32x2 and an add.rn.f32x2 after it are joined by the assembler of CUDA 13.0 to one
+// rounding, also under -fmad=false; so are a product plus a constant -0 and a sum times a constant 1.  With a -0
+// that only the running kernel knows there is nothing to join.)
+static __constant__ float s_minus_zero = -0.0f;
+__device__ __forceinline__ Two mul2(Two x, Two y) { return fma2(x, y, both(s_minus_zero)); }
+
+// ---------------------------------------------------------------- reading
 // Eight values as they lie in memory.
 struct Raw {
     uint4 a, b;  // b: of 32-bit types alone
 };
 
-__device__ __forceinline__ float half_bits(uint32_t v, bool bf) {  // a 16-bit value
-    return bf ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((unsigned short)v));
-}
-__device__ __forceinline__ void unpack2(uint32_t v, bool bf, float &x, float &y) {
-    if (bf) {
-        x = __uint_as_float(v << 16);
-        y = __uint_as_float(v & 0xffff0000u);
-    } else {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
-        x = f.x;
-        y = f.y;
-    }
+__device__ __forceinline__ Two unpack2(uint32_t v, bool bf) {
+    if (bf) return two(v << 16, v & 0xffff0000u);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+    return two(f.x, f.y);
 }
 // The values of a type, times nothing yet.
-__device__ __forceinline__ void unpack(const Raw &r, int type, float (&x)[kWide]) {
+__device__ __forceinline__ void unpack(const Raw &r, int type, Two (&x)[kTwos]) {
     if (two_bytes(type)) {
         const bool bf = type == PVMVMD_BF16;
-        unpack2(r.a.x, bf, x[0], x[1]);
-        unpack2(r.a.y, bf, x[2], x[3]);
-        unpack2(r.a.z, bf, x[4], x[5]);
-        unpack2(r.a.w, bf, x[6], x[7]);
+        x[0] = unpack2(r.a.x, bf);
+        x[1] = unpack2(r.a.y, bf);
+        x[2] = unpack2(r.a.z, bf);
+        x[3] = unpack2(r.a.w, bf);
         return;
     }
     const uint32_t w[kWide] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
-    if (type == PVMVMD_F32) {
 #pragma unroll
-        for (int e = 0; e < kWide; ++e) x[e] = __uint_as_float(w[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < kWide; ++e) x[e] = to_f32<uint32_t>(w[e]);
-    }
+    for (int i = 0; i < kTwos; ++i)
+        x[i] = type == PVMVMD_F32 ? two(w[2 * i], w[2 * i + 1])
+                                  : two(to_f32<uint32_t>(w[2 * i]), to_f32<uint32_t>(w[2 * i + 1]));
 }
 
-// Where a thread's values lie in a row: eight side by side (kVec: rows on 16-byte boundaries,
-// D a multiple of 8), or eight that are `step` apart, so that a warp's are side by side.
+// Where a thread's values lie in a row: a warp takes 256 at a time, a lane eight of them, which are side by
+// side (kVec: rows on 16-byte boundaries, D a multiple of 8, so that all are in the row or none), or 32
+// apart, so that the warp's are side by side.
+constexpr int kTile = 32 * kWide;
 template <bool kVec>
 struct Place {
-    int at, step, D;  // the first, the distance of the others (1 where kVec)
-    __device__ __forceinline__ int index(int e) const { return kVec ? at + e : at + e * step; }
-    __device__ __forceinline__ bool in(int e) const { return index(e) < D; }
+    int at, D;
+    __device__ __forceinline__ bool any() const { return at < D; }
+    __device__ __forceinline__ int index(int e) const { return kVec ? at + e : at + e * 32; }
+    __device__ __forceinline__ bool in(int e) const { return kVec ? at < D : index(e) < D; }
+    // of a thread's chunk c, counted from its first
+    __device__ __forceinline__ Place chunk(int c) const { return Place{at + c * kTile, D}; }
 };
 
 template <bool kVec>
@@ -70,7 +117,7 @@ __device__ __forceinline__ Raw load_raw(const void *row, int type, const Place<k
     Raw r;
     if (kVec) {
         r.a = r.b = make_uint4(0, 0, 0, 0);
-        if (p.at < p.D) {
+        if (p.any()) {
             if (two_bytes(type)) {
                 r.a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + p.at);
             } else {
@@ -99,60 +146,73 @@ __device__ __forceinline__ Raw load_raw(const void *row, int type, const Place<k
 }
 
 // A row's address: rows may be one for all.
-__device__ __forceinline__ const void *row_of(const pvmvmd_rows &r, int64_t t) {
-    return static_cast<const char *>(r.data_dev) + t * r.token * (two_bytes(r.type) ? 2 : 4);
+__device__ __forceinline__ const void *row_of(const pvmvmd_rows &r, int type, int64_t t) {
+    return static_cast<const char *>(r.data_dev) + t * r.token * (two_bytes(type) ? 2 : 4);
 }
 // scale token_scale[t]
 __device__ __forceinline__ float row_scale(const pvmvmd_rows &r, int64_t t) {
     return r.token_scale_dev ? __fmul_rn(r.scale, r.token_scale_dev[t]) : r.scale;
 }
 
-// 32-bit values of one row for all tokens: channel scales, or a norm's weights of any type.
-template <bool kVec>
-__device__ __forceinline__ void load_f32(const float *v, const Place<kVec> &p, float (&x)[kWide]) {
-    unpack(load_raw<kVec>(v, PVMVMD_F32, p), PVMVMD_F32, x);
-}
-
 // Raw values to numbers: (x c) channel_scale
 template <bool kVec>
-__device__ __forceinline__ void read(const Raw &raw, const pvmvmd_rows &r, float c, const Place<kVec> &p, float (&x)[kWide]) {
-    unpack(raw, r.type, x);
+__device__ __forceinline__ void read(const Raw &raw, const pvmvmd_rows &r, int type, float c, const Place<kVec> &p,
+                                     Two (&x)[kTwos]) {
+    unpack(raw, type, x);
 #pragma unroll
-    for (int e = 0; e < kWide; ++e) x[e] = __fmul_rn(x[e], c);
+    for (int i = 0; i < kTwos; ++i) x[i] = mul2(x[i], both(c));
     if (r.channel_scale_dev) {
-        float s[kWide];
-        load_f32<kVec>(r.channel_scale_dev, p, s);
+        Two s[kTwos];
+        unpack(load_raw<kVec>(r.channel_scale_dev, PVMVMD_F32, p), PVMVMD_F32, s);
 #pragma unroll
-        for (int e = 0; e < kWide; ++e) x[e] = __fmul_rn(x[e], s[e]);
+        for (int i = 0; i < kTwos; ++i) x[i] = mul2(x[i], s[i]);
     }
 }
-
-// The integer of a value that has been multiplied, as a field element.
-__device__ __forceinline__ uint32_t field_of(float v, float limit) {
-    v = fminf(fmaxf(v, -limit), limit);
-    const int n = __float2int_rn(v);
-    return n < 0 ? (uint32_t)n + kQ : (uint32_t)n;
+// Zeros in the place of what lies outside the row.
+template <bool kVec>
+__device__ __forceinline__ void outside_zero(const Place<kVec> &p, Two (&x)[kTwos]) {
+    if (kVec && p.any()) return;
+#pragma unroll
+    for (int i = 0; i < kTwos; ++i)
+        x[i] = two(p.in(2 * i) ? first(x[i]) : 0.0f, p.in(2 * i + 1) ? second(x[i]) : 0.0f);
 }
 
-// Eight values to a row: a floating type, or integers by m.
+// ---------------------------------------------------------------- writing
+// A number of up to 2^22 rounded to a whole one, halves to even, as a field element: adding
+// 1.5 2^23 leaves the whole number in the sum's lower bits; of n and n + q, read without signs, the
+// smaller one is canonical.
+__device__ __forceinline__ uint32_t field_of(float v) {
+    const uint32_t b = __float_as_uint(__fadd_rn(v, 12582912.0f));
+    return min(b - 0x4b400000u, b + (kQ - 0x4b400000u));
+}
+constexpr int kMostLimit = 1 << 22;
+
+// What becomes of a row's values: by_row: m is the row's own, so that every |z m| is below limit + 1/2,
+// or 0 where the row is not finite.
+struct Step {
+    float m;
+    bool by_row;
+};
+
+// Eight values to a row: a floating type, or integers.
 template <bool kVec>
-__device__ __forceinline__ void write(const pvmvmd_rows_out &o, int64_t t, const Place<kVec> &p, const float (&z)[kWide],
-                                      float m) {
-    if (o.type == PVMVMD_BF16 || o.type == PVMVMD_F16) {
+__device__ __forceinline__ void write(const pvmvmd_rows_out &o, int type, int64_t t, const Place<kVec> &p,
+                                      const Two (&z)[kTwos], Step s) {
+    if (two_bytes(type)) {
         uint16_t *row = static_cast<uint16_t *>(o.data_dev) + t * o.token;
-        uint32_t w[kWide / 2];
+        uint32_t w[kTwos];
 #pragma unroll
-        for (int e = 0; e < kWide / 2; ++e) {
-            if (o.type == PVMVMD_BF16) {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(z[2 * e], z[2 * e + 1]);
-                w[e] = *reinterpret_cast<const uint32_t *>(&v);
+        for (int i = 0; i < kTwos; ++i) {
+            if (type == PVMVMD_BF16) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(first(z[i]), second(z[i]));
+                w[i] = *reinterpret_cast<const uint32_t *>(&v);
             } else {
-                const __half2 v = __floats2half2_rn(z[2 * e], z[2 * e + 1]);
-                w[e] = *reinterpret_cast<const uint32_t *>(&v);
+                const __half2 v = __floats2half2_rn(first(z[i]), second(z[i]));
+                w[i] = *reinterpret_cast<const uint32_t *>(&v);
             }
         }
         if (kVec) {
-            if (p.at < p.D) *reinterpret_cast<uint4 *>(row + p.at) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (p.any()) *reinterpret_cast<uint4 *>(row + p.at) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
 #pragma unroll
             for (int e = 0; e < kWide; ++e)
@@ -161,20 +221,31 @@ __device__ __forceinline__ void write(const pvmvmd_rows_out &o, int64_t t, const
         return;
     }
     uint32_t w[kWide];
-    if (o.type == PVMVMD_F32) {
+    if (type == PVMVMD_F32) {
 #pragma unroll
-        for (int e = 0; e < kWide; ++e) w[e] = __float_as_uint(z[e]);
+        for (int i = 0; i < kTwos; ++i) {
+            w[2 * i] = __float_as_uint(first(z[i]));
+            w[2 * i + 1] = __float_as_uint(second(z[i]));
+        }
+    } else if (s.by_row && s.m != 0.0f) {
+#pragma unroll
+        for (int i = 0; i < kTwos; ++i) {
+            const Two v = mul2(z[i], both(s.m));
+            w[2 * i] = field_of(first(v));
+            w[2 * i + 1] = field_of(second(v));
+        }
     } else {
         const float limit = (float)o.limit;
 #pragma unroll
-        for (int e = 0; e < kWide; ++e) {
-            const float v = __fmul_rn(z[e], m);
-            w[e] = v == v ? field_of(v, limit) : 0u;
+        for (int i = 0; i < kTwos; ++i) {
+            Two v = mul2(z[i], both(s.m));
+            w[2 * i] = first(v) == first(v) ? field_of(fminf(fmaxf(first(v), -limit), limit)) : 0u;
+            w[2 * i + 1] = second(v) == second(v) ? field_of(fminf(fmaxf(second(v), -limit), limit)) : 0u;
         }
     }
     uint32_t *row = static_cast<uint32_t *>(o.data_dev) + t * o.token;
     if (kVec) {
-        if (p.at < p.D) {
+        if (p.any()) {
             uint4 *q = reinterpret_cast<uint4 *>(row + p.at);
             q[0] = make_uint4(w[0], w[1], w[2], w[3]);
             q[1] = make_uint4(w[4], w[5], w[6], w[7]);
@@ -186,40 +257,46 @@ __device__ __forceinline__ void write(const pvmvmd_rows_out &o, int64_t t, const
     }
 }
 
-// What a row's integers are multiplied by, from the largest |z| (as bits), and its step.  A row that is not finite:
+// The larger of a and |b|; NaN if one is.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+// What a row's integers are multiplied by, from its largest |z|, and its step.  A row that is not finite:
 // m = 0 gives zeros for what is finite, NaN (zeros) for what is not.
-__device__ __forceinline__ float dynamic_scale(const pvmvmd_rows_out &o, uint32_t big, float &step) {
-    if (big >= 0x7f800000u) {
-        step = __uint_as_float(0x7fffffffu);
-        return 0.0f;
-    }
-    const float a = __uint_as_float(big), limit = (float)o.limit;
-    step = __fdiv_rn(a, limit);
-    return fminf(__fdiv_rn(limit, a), kFltMax);
+__device__ __forceinline__ Step step_of(const pvmvmd_rows_out &o, float big) {
+    if (!(big <= kFltMax)) return Step{0.0f, true};
+    return Step{fminf(__fdiv_rn((float)o.limit, big), kFltMax), true};
+}
+__device__ __forceinline__ void write_step(const pvmvmd_rows_out &o, int64_t t, float big) {
+    o.token_scale_dev[t] = big <= kFltMax ? __fdiv_rn(big, (float)o.limit) : __uint_as_float(0x7fffffffu);
 }
 
 // ---------------------------------------------------------------- powers of two
 // 2^-f, |f| <= 1/2: the polynomial of degree 5 that is 1 at 0 and whose largest relative
 // error is least (2^-23.4; found by weighted least squares), products and sums rounded
-// one by one (2^-22.3 in all).
-__device__ __forceinline__ float exp_poly(float f) {
-    float p = __fadd_rn(__fmul_rn(f, -0.00132647157f), 0.00967151299f);
-    p = __fadd_rn(__fmul_rn(p, f), -0.0555073395f);
-    p = __fadd_rn(__fmul_rn(p, f), 0.240222424f);
-    p = __fadd_rn(__fmul_rn(p, f), -0.693147004f);
-    return __fadd_rn(__fmul_rn(p, f), 1.0f);
+// one by one (2^-22.3 in all).  gain: a power of two that the result is multiplied by (which
+// rounds nothing).
+__device__ __forceinline__ Two exp_poly(Two f, float gain = 1.0f) {
+    Two p = add2(mul2(f, both(-0.00132647157f * gain)), both(0.00967151299f * gain));
+    p = add2(mul2(p, f), both(-0.0555073395f * gain));
+    p = add2(mul2(p, f), both(0.240222424f * gain));
+    p = add2(mul2(p, f), both(-0.693147004f * gain));
+    return add2(mul2(p, f), both(gain));
 }
-// d = n + f, n the nearest whole number (adding 1.5 2^23 rounds to it), |d| <= 2^22
-__device__ __forceinline__ float split(float d, int &n) {
-    const float t = __fadd_rn(d, 12582912.0f);
-    n = __float_as_int(t) - 0x4b400000;
-    return __fsub_rn(d, __fsub_rn(t, 12582912.0f));
+// d = n + f, n the nearest whole number (adding 1.5 2^23 rounds to it), |d| <= 2^22.  Returns f; n + 0x4b400000
+// is what the bits of `sum` are.
+__device__ __forceinline__ Two split(Two d, Two &sum) {
+    sum = add2(d, both(12582912.0f));
+    return sub2(d, sub2(sum, both(12582912.0f)));
 }
-// 1 + 2^-d
-__device__ __forceinline__ float one_plus_exp(float d) {
-    int n;
-    const float p = exp_poly(split(fminf(fmaxf(d, -128.0f), 125.0f), n));
-    return __fadd_rn(1.0f, __int_as_float(__float_as_int(p) - (n << 23)));
+// 1 + 2^-d  (23 bits up, nothing is left of 0x4b400000)
+__device__ __forceinline__ Two one_plus_exp(Two d) {
+    Two n;
+    d = two(fminf(fmaxf(first(d), -128.0f), 125.0f), fminf(fmaxf(second(d), -128.0f), 125.0f));
+    const Two p = exp_poly(split(d, n));
+    return add2(both(1.0f), two((uint32_t)p.v - ((uint32_t)n.v << 23), (uint32_t)(p.v >> 32) - ((uint32_t)(n.v >> 32) << 23)));
 }
 
 // ---------------------------------------------------------------- sums in pairs
@@ -228,27 +305,38 @@ __device__ __forceinline__ float one_plus_exp(float d) {
 struct Pair {
     float h, l;
 };
-__device__ __forceinline__ void add_term(Pair &s, float x, float low) {
-    const float t = __fadd_rn(s.h, x), b = __fsub_rn(t, s.h);
-    const float e = __fadd_rn(__fsub_rn(s.h, __fsub_rn(t, b)), __fsub_rn(x, b));
+inline Pair inverse_of(int n) {
+    const float h = (float)(1.0 / n);
+    return Pair{h, (float)(1.0 / n - h)};
+}
+struct Pairs {  // two of them
+    Two h, l;
+};
+__device__ __forceinline__ void add_terms(Pairs &s, Two x) {
+    const Two t = add2(s.h, x), b = sub2(t, s.h);
+    s.l = add2(s.l, add2(sub2(s.h, sub2(t, b)), sub2(x, b)));
     s.h = t;
-    s.l = __fadd_rn(s.l, __fadd_rn(e, low));
 }
-__device__ __forceinline__ void add_square(Pair &s, float x) {
-    const float p = __fmul_rn(x, x);
-    add_term(s, p, __fmaf_rn(x, x, -p));
+__device__ __forceinline__ void add_squares(Pairs &s, Two x) {
+    const Two p = mul2(x, x), low = fma2(x, x, minus2(p)), t = add2(s.h, p), b = sub2(t, s.h);
+    s.l = add2(s.l, add2(add2(sub2(s.h, sub2(t, b)), sub2(p, b)), low));
+    s.h = t;
 }
-// s / n for a whole number n < 2^24
-__device__ __forceinline__ Pair mean_of(Pair s, float n) {
-    const float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l);
-    const float q = __fdiv_rn(h, n);
-    return Pair{q, __fdiv_rn(__fadd_rn(__fmaf_rn(-q, n, h), l), n)};
+__device__ __forceinline__ Pair join(Pair a, Pair b) {  // the same for (b, a)
+    const float t = __fadd_rn(a.h, b.h), bb = __fsub_rn(t, a.h);
+    const float e = __fadd_rn(__fsub_rn(a.h, __fsub_rn(t, bb)), __fsub_rn(b.h, bb));
+    return Pair{t, __fadd_rn(__fadd_rn(a.l, b.l), e)};
+}
+__device__ __forceinline__ Pair join(const Pairs &s) { return join(Pair{first(s.h), first(s.l)}, Pair{second(s.h), second(s.l)}); }
+// s (1 / n), the latter a pair of the host's
+__device__ __forceinline__ Pair mean_of(Pair s, Pair inverse) {
+    const float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l), p = __fmul_rn(h, inverse.h);
+    return Pair{p, __fmaf_rn(l, inverse.h, __fmaf_rn(h, inverse.l, __fmaf_rn(h, inverse.h, -p)))};
 }
 // 1 / sqrt(a + eps), rounded once: the approximation y of a's upper part, corrected by
 // what 1 - a y^2 is in twice the bits.
 __device__ __forceinline__ float inverse_root(Pair a, float eps) {
-    Pair s{a.h, a.l};
-    add_term(s, eps, 0.0f);
+    const Pair s = join(a, Pair{eps, 0.0f});
     const float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l);
     const float y = rsqrtf(h), t = __fmul_rn(y, y), te = __fmaf_rn(y, y, -t);
     const float r = -__fmaf_rn(l, t, __fmaf_rn(h, te, __fmaf_rn(h, t, -1.0f)));
@@ -256,19 +344,30 @@ __device__ __forceinline__ float inverse_root(Pair a, float eps) {
 }
 
 // ---------------------------------------------------------------- across a row's threads
+// How rows are dealt to threads: rows of up to 1024 values to a warp each, others to a CTA
+// or to a cluster of them; a thread takes `chunks` times eight values.
+constexpr int kRowThreadsMost = 512, kWarpRows = 8, kMostCluster = 8, kMostWarps = kRowThreadsMost / 32;
+struct RowDeal {
+    int threads;   // of a CTA
+    int rows;      // of a CTA: one a warp, or one
+    int log_ctas;  // CTAs of a row: 2^log_ctas
+    int chunks;    // 1, 2 or 4
+};
+
 // A row's threads: the lanes of a warp, the warps of a CTA, the CTAs of a cluster.  Every
 // exchange has a place of its own in shared memory, so that none waits for the reads
-// of the one before, and every thread gets the same result.
-constexpr int kMostCluster = 8, kMostWarps = 32, kExchanges = 5;
+// of the one before.
+constexpr int kPlaces = 5;
 struct RowShared {
-    Pair warp[kExchanges][kMostWarps];
-    Pair cta[kExchanges][kMostCluster];
+    Pair warp[kPlaces][kMostWarps];
+    Pair cta[kPlaces][kMostCluster];
 };
 struct RowThreads {
     RowShared *sh;
-    int warps;             // 1: a warp by itself, with others' rows beside it
-    int lane, warp, used;  // used: exchanges so far
+    int warps;              // 1: a warp by itself, with others' rows beside it
+    int lane, warp, place;  // place: of the next exchange
     uint32_t ctas, rank;
+    int64_t t;              // the row
 };
 
 __device__ __forceinline__ uint32_t cta_rank() {
@@ -276,12 +375,7 @@ __device__ __forceinline__ uint32_t cta_rank() {
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ uint32_t cta_count() {
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-// At a kernel's start and before its first store to a peer: all of the cluster's CTAs run.
+// At a kernel's start, and before its first store to a peer: all of the cluster's CTAs run.
 __device__ __forceinline__ void cluster_begin(uint32_t ctas) {
     if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
@@ -298,101 +392,101 @@ __device__ __forceinline__ void store_peer(const void *p, uint32_t rank, Pair v)
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v.h), "f"(v.l) : "memory");
 }
 
-// op(a, b) is the same for (b, a); neutral: op(a, neutral) = a.
-template <typename Op>
-__device__ __forceinline__ Pair reduce_lanes(Pair v, int from, Op op) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (o <= from)
-            v = op(v, Pair{__shfl_xor_sync(kFull, v.h, o), __shfl_xor_sync(kFull, v.l, o)});
-    return v;
+// The sum over a warp's lanes, the same in all: as whole numbers in units of 2^-46 of the power of two
+// above the largest, in two parts that the warp adds in one instruction each.  (Five steps
+// of shuffles and sums of pairs take three times the instructions.)  NaN where a value is not
+// finite.
+__device__ __forceinline__ Pair lanes_sum(Pair v) {
+    const float h = __fadd_rn(v.h, v.l), l = __fadd_rn(__fsub_rn(v.h, h), v.l);
+    const uint32_t most = __reduce_max_sync(kFull, __float_as_uint(h) & 0x7fffffffu);
+    if (most >= 0x7f800000u) return Pair{__uint_as_float(0x7fffffffu), 0.0f};
+    const uint32_t e = max(most >> 23, 24u);
+    const float up = __uint_as_float((275u - e) << 23), down = __uint_as_float((e - 21u) << 23);  // 2^(148-e), its inverse
+    const float a = __fmul_rn(h, up);                      // |a| < 2^22
+    const float whole = __fadd_rn(a, 12582912.0f);         // 1.5 2^23: rounds to whole numbers
+    const float rest = __fmaf_rn(l, up, __fsub_rn(a, __fsub_rn(whole, 12582912.0f)));  // |rest| < 1
+    const int n = __reduce_add_sync(kFull, __float_as_int(whole) - 0x4b400000);
+    const int m = __reduce_add_sync(kFull, __float2int_rn(__fmul_rn(rest, 16777216.0f)));
+    // n + 2^-24 m: n may have more than 24 bits
+    const float nh = __int2float_rn(n), nl = __int2float_rn(n - (int)nh);
+    return Pair{__fmul_rn(nh, down), __fmul_rn(__fmaf_rn(__int2float_rn(m), 5.9604644775390625e-8f, nl), down)};
 }
-template <typename Op>
-__device__ __forceinline__ Pair reduce_row(RowThreads &r, Pair v, Pair neutral, Op op) {
-    v = reduce_lanes(v, 16, op);
-    if (r.warps == 1) return v;
-    Pair *mine = r.sh->warp[r.used];
-    if (r.lane == 0) mine[r.warp] = v;
-    __syncthreads();
-    v = r.lane < r.warps ? mine[r.lane] : neutral;
-    v = reduce_lanes(v, 16, op);
-    if (r.ctas > 1) {
-        Pair *all = r.sh->cta[r.used];
-        if (r.used == 0) cluster_begun(r.ctas);
-        if (r.warp == 0 && r.lane < (int)r.ctas) store_peer(&all[r.rank], (uint32_t)r.lane, v);
-        clusters_meet();
-        v = r.lane < (int)r.ctas ? all[r.lane] : neutral;
-        v = reduce_lanes(v, kMostCluster / 2, op);
-        v = Pair{__shfl_sync(kFull, v.h, 0), __shfl_sync(kFull, v.l, 0)};
-    }
-    ++r.used;
-    return v;
+// Before the first store to a peer, or at the end where there is none.
+__device__ __forceinline__ void row_begun(const RowThreads &r) {
+    if (r.place == 0) cluster_begun(r.ctas);
 }
 __device__ __forceinline__ Pair row_sum(RowThreads &r, Pair v) {
-    return reduce_row(r, v, Pair{0.0f, 0.0f}, [](Pair a, Pair b) {
-        // symmetric, so that all lanes hold the same bits
-        const float t = __fadd_rn(a.h, b.h), bb = __fsub_rn(t, a.h);
-        const float e = __fadd_rn(__fsub_rn(a.h, __fsub_rn(t, bb)), __fsub_rn(b.h, bb));
-        return Pair{t, __fadd_rn(__fadd_rn(a.l, b.l), e)};
-    });
-}
-__device__ __forceinline__ uint32_t row_max(RowThreads &r, uint32_t v) {
-    v = __reduce_max_sync(kFull, v);
+    v = lanes_sum(v);
     if (r.warps == 1) return v;
-    const Pair m = reduce_row(r, Pair{__uint_as_float(v), 0.0f}, Pair{0.0f, 0.0f}, [](Pair a, Pair b) {
-        return Pair{__uint_as_float(max(__float_as_uint(a.h), __float_as_uint(b.h))), 0.0f};
-    });
-    return __float_as_uint(m.h);
+    Pair *mine = r.sh->warp[r.place];
+    if (r.lane == 0) mine[r.warp] = v;
+    __syncthreads();
+    v = lanes_sum(r.lane < r.warps ? mine[r.lane] : Pair{0.0f, 0.0f});
+    if (r.ctas > 1) {
+        Pair *all = r.sh->cta[r.place];
+        row_begun(r);
+        if (r.warp == 0 && r.lane < (int)r.ctas) store_peer(&all[r.rank], (uint32_t)r.lane, v);
+        clusters_meet();
+        v = lanes_sum(r.lane < (int)r.ctas ? all[r.lane] : Pair{0.0f, 0.0f});
+    }
+    ++r.place;
+    return v;
+}
+// The largest of values that are not below 0; NaN if one is (whose bits are above all others').
+__device__ __forceinline__ float row_max(RowThreads &r, float value) {
+    uint32_t v = __reduce_max_sync(kFull, __float_as_uint(value));
+    if (r.warps > 1) {
+        Pair *mine = r.sh->warp[r.place];
+        if (r.lane == 0) mine[r.warp].h = __uint_as_float(v);
+        __syncthreads();
+        v = __reduce_max_sync(kFull, r.lane < r.warps ? __float_as_uint(mine[r.lane].h) : 0u);
+        if (r.ctas > 1) {
+            Pair *all = r.sh->cta[r.place];
+            row_begun(r);
+            if (r.warp == 0 && r.lane < (int)r.ctas) store_peer(&all[r.rank], (uint32_t)r.lane, Pair{__uint_as_float(v), 0.0f});
+            clusters_meet();
+            v = __reduce_max_sync(kFull, r.lane < (int)r.ctas ? __float_as_uint(all[r.lane].h) : 0u);
+        }
+        ++r.place;
+    }
+    return __uint_as_float(v);
 }
 
-// A row's threads never exchanged anything: the wait that goes with cluster_begin.
-__device__ __forceinline__ void row_end(const RowThreads &r) {
-    if (r.used == 0) cluster_begun(r.ctas);
-}
-
-// How rows are dealt to threads: rows of up to 1024 values to a warp each, others to a CTA
-// or to a cluster of them; a thread takes `chunks` times eight values.
-constexpr int kRowThreadsMost = 512, kWarpRows = 8;
-struct RowDeal {
-    int threads;  // of a CTA
-    int rows;     // of a CTA: one a warp, or one
-    int ctas;     // of a row
-    int chunks;   // 1, 2 or 4
-};
 inline RowDeal deal_rows(int T, int D) {
-    const int units = (D + kWide - 1) / kWide;
-    RowDeal d{32, 1, 1, 1};
-    if (units <= 4 * 32) {
-        while (units > 32 * d.chunks) d.chunks *= 2;
-        d.rows = std::max(1, std::min(kWarpRows, T / 152));
+    const int tiles = (D + kTile - 1) / kTile, sms = 152, most = kRowThreadsMost / 32;
+    RowDeal d{32, 1, 0, 1};
+    if (tiles <= 4) {
+        while (tiles > d.chunks) d.chunks *= 2;
+        d.rows = std::max(1, std::min(kWarpRows, T / sms));
         d.threads = 32 * d.rows;
         return d;
     }
-    d.chunks = T >= 152 ? 2 : 1;
-    while (units > kRowThreadsMost * d.chunks * d.ctas && d.ctas < kMostCluster) d.ctas *= 2;
-    while (units > kRowThreadsMost * d.chunks * d.ctas) d.chunks *= 2;
-    const int each = (units + d.ctas * d.chunks - 1) / (d.ctas * d.chunks);
-    d.threads = (each + 31) / 32 * 32;
+    d.chunks = T >= sms ? 2 : 1;
+    while (tiles > most * d.chunks << d.log_ctas && d.log_ctas < 3) ++d.log_ctas;
+    while (tiles > most * d.chunks << d.log_ctas) d.chunks *= 2;
+    d.threads = 32 * ((tiles + (d.chunks << d.log_ctas) - 1) / (d.chunks << d.log_ctas));
     return d;
 }
-// The place of a thread's chunk c among the values of its row.
-template <bool kVec>
-__device__ __forceinline__ Place<kVec> place_of(const RowThreads &r, int threads, int chunk, int chunks, int D) {
-    // of a CTA's part, chunks one after the other, threads side by side
-    const int width = r.warps == 1 ? 32 : threads, tid = r.warps == 1 ? r.lane : r.warp * 32 + r.lane;
-    const int first = ((int)r.rank * chunks + chunk) * width * kWide;
-    return kVec ? Place<kVec>{first + tid * kWide, 1, D} : Place<kVec>{first + tid, width, D};
-}
+inline dim3 grid_of(const RowDeal &d, int T) { return dim3((unsigned)((T + d.rows - 1) / d.rows) << d.log_ctas); }
+
 __device__ __forceinline__ RowThreads row_threads(RowShared *sh, const RowDeal &d) {
     RowThreads r;
     r.sh = sh;
     r.lane = threadIdx.x % 32;
     r.warp = threadIdx.x / 32;
-    r.warps = d.rows > 1 || d.threads == 32 ? 1 : d.threads / 32;
-    r.ctas = (uint32_t)d.ctas;
-    r.rank = d.ctas > 1 ? cta_rank() : 0;
-    r.used = 0;
+    r.warps = d.rows > 1 ? 1 : d.threads / 32;
+    r.ctas = 1u << d.log_ctas;
+    r.rank = d.log_ctas ? cta_rank() : 0;
+    r.place = 0;
+    r.t = d.rows > 1 ? (int)blockIdx.x * d.rows + r.warp : (int)(blockIdx.x >> d.log_ctas);
+    cluster_begin(r.ctas);
     return r;
+}
+// The place of a thread's first chunk among the values of its row: a warp's chunks are side by side.
+template <bool kVec, int kChunks>
+__device__ __forceinline__ Place<kVec> place_of(const RowThreads &r, int D) {
+    const int warp = r.warps == 1 ? 0 : (int)r.rank * r.warps + r.warp;
+    return Place<kVec>{warp * kChunks * kTile + r.lane * (kVec ? kWide : 1), D};
 }
 
 // Whether a row's values can be taken 16 bytes at a time.

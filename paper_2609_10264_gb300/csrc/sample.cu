@@ -9,7 +9,6 @@ namespace pv {
 namespace {
 
 constexpr int kSThreads = 512, kSWarps = kSThreads / 32;
-constexpr int kTile = 32 * kWide;  // tokens that a warp takes at a time
 constexpr int kBins = 2048;
 using u64 = unsigned long long;
 
@@ -45,10 +44,10 @@ constexpr uint32_t kNoKey = 0x007fffffu;  // of -infinity
 
 // W of a token: 2^-(big - x) in units of 2^-40.
 __device__ __forceinline__ u64 weight(float big, float x) {
-    int n;
-    const float f = split(fminf(__fsub_rn(big, x), 63.0f), n);
-    const float r = __fadd_rn(__fmul_rn(exp_poly(f), 4194304.0f), 8388608.0f);  // 2^23 + round(2^22 P)
-    return ((u64)(__float_as_uint(r) & 0x7fffffu) << 18) >> n;
+    Two sum;
+    const Two f = split(both(fminf(__fsub_rn(big, x), 63.0f)), sum);
+    const float r = __fadd_rn(first(exp_poly(f, 4194304.0f)), 8388608.0f);  // 2^23 + round(2^22 P)
+    return ((u64)(__float_as_uint(r) & 0x7fffffu) << 18) >> ((uint32_t)sum.v - 0x4b400000u);
 }
 
 struct SampleArgs {
@@ -64,7 +63,7 @@ struct Row {
     uint32_t rank, ctas;
     const char *base;  // the 16-byte boundary at or before the row
     int off, end;      // the row's tokens are off .. end - 1 from there
-    int first, last;   // tiles of this warp
+    int begin, last;   // tiles of this warp
     float m;
     const uint32_t *allowed;
     float big;         // the largest x
@@ -88,7 +87,10 @@ struct Row {
             if (at < end && at + 4 > off) r.a = *reinterpret_cast<const uint4 *>(base + (int64_t)at * 4);
             if (at + 4 < end && at + 8 > off) r.b = *reinterpret_cast<const uint4 *>(base + (int64_t)at * 4 + 16);
         }
-        unpack(r, l.type, x);
+        Two v2[kTwos];
+        unpack(r, l.type, v2);
+#pragma unroll
+        for (int i = 0; i < kTwos; ++i) x[2 * i] = first(v2[i]), x[2 * i + 1] = second(v2[i]);
         const int i0 = at - off, V = a.j.V;
         uint32_t ok = 0xff;
         if (allowed) {
@@ -111,7 +113,7 @@ struct Row {
     // f(x, index) for every token of this warp's tiles that may be chosen
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        for (int k = first; k < last; ++k) {
+        for (int k = begin; k < last; ++k) {
             float x[kWide];
             const int i0 = tokens(k, x);
 #pragma unroll
@@ -226,14 +228,14 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
     r.ctas = (uint32_t)a.ctas;
     r.rank = a.ctas > 1 ? cta_rank() : 0;
     const int V = j.V;
-    const char *row = static_cast<const char *>(row_of(j.logits, r.t));
+    const char *row = static_cast<const char *>(row_of(j.logits, j.logits.type, r.t));
     const int size = two_bytes(j.logits.type) ? 2 : 4, before16 = (int)(reinterpret_cast<uintptr_t>(row) % 16);
     r.base = row - before16;
     r.off = before16 / size;
     r.end = r.off + V;
     const int tiles = (r.end + kTile - 1) / kTile, per = (tiles + a.ctas * kSWarps - 1) / (a.ctas * kSWarps);
-    r.first = min(tiles, ((int)r.rank * kSWarps + r.warp) * per);
-    r.last = min(tiles, r.first + per);
+    r.begin = min(tiles, ((int)r.rank * kSWarps + r.warp) * per);
+    r.last = min(tiles, r.begin + per);
     r.allowed = j.allowed ? j.allowed + r.t * j.allowed_row : nullptr;
 
     const pvmvmd_sampling &how = j.how;
@@ -352,7 +354,7 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
     }
     const u64 at_random = __umul64hi(Z, (u64)j.random[r.t] << 32);
     if (at_random < front || at_random >= front + sum) return;
-    for (int k = r.first; k < r.last; ++k) {
+    for (int k = r.begin; k < r.last; ++k) {
         float x[kWide];
         const int i0 = r.tokens(k, x);
         u64 w[kWide], all = 0;

@@ -31,7 +31,7 @@ int check(const pvmvmd_rows_out &o, bool field = true) {
     if (!o.data_dev || !(field ? any_type(o.type) : float_type(o.type))) return PVMVMD_E_ARG;
     if (reinterpret_cast<uintptr_t>(o.data_dev) % size_of(o.type)) return PVMVMD_E_ARG;
     if (o.type != PVMVMD_FIELD) return o.token_scale_dev ? PVMVMD_E_ARG : PVMVMD_OK;
-    if (o.limit < 1 || o.limit > 1 << 23) return PVMVMD_E_PARAM;
+    if (o.limit < 1 || o.limit > 1 << 22) return PVMVMD_E_PARAM;
     return o.token_scale_dev || std::isfinite(o.scale) ? PVMVMD_OK : PVMVMD_E_PARAM;
 }
 int check(const pvmvmd_norm &n) {

@@ -122,7 +122,7 @@ NORMS = [
     dict(T=200, D=4096, y=None, out="bf16"),
     dict(T=3, D=5001, y="f16", res="f32", out="field", post="layer", bias=True, pad=5, at=3),
     dict(T=2, D=8200, pre=None, out="f32"),
-    dict(T=160, D=8192, post="rms", scale=1e6, limit=1 << 23),
+    dict(T=160, D=8192, post="rms", scale=1e6, limit=1 << 22),
     dict(T=1, D=16384, post="rms", pre="layer", w=None, add=0.5),
     dict(T=153, D=16392, dynamic=True, limit=1),
     dict(T=2, D=40000, y="bf16", out="f16", gate="row", dynamic=False),
@@ -540,7 +540,7 @@ def test_steps_refuse_bad_arguments_before_device_use(pv):
     assert norm(residual=R(type=pv.PVMVMD_FIELD)) == norm(residual=R(scale=2.0)) == norm(residual=R(token_scale_dev=64)) == ARG
     assert norm(rout=O()) == norm(out=O(type=5)) == norm(out=O(data_dev=None)) == ARG
     assert norm(out=O(token_scale_dev=64, **F32)) == ARG
-    assert norm(out=O(limit=0)) == norm(out=O(limit=(1 << 23) + 1)) == norm(out=O(scale=inf)) == PARAM
+    assert norm(out=O(limit=0)) == norm(out=O(limit=(1 << 22) + 1)) == norm(out=O(scale=inf)) == PARAM
     assert norm(pre=N(kind=3)) == norm(post=N(kind=0)) == norm(pre=N(weight_dev=64, type=4)) == ARG
     assert norm(pre=N(eps=0.0)) == norm(pre=N(eps=float("nan"))) == norm(post=N(weight_add=inf)) == PARAM
     assert norm(branch=inf) == norm(keep=float("nan")) == norm(y=R(scale=inf)) == PARAM
