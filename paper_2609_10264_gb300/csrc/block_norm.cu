@@ -66,10 +66,12 @@ __device__ __forceinline__ void norm(RowThreads &r, const pvmvmd_norm &n, Pair i
     }
 }
 
-// kY, kR, kO: the kinds of y (and a gate), of the residual and its output, and of out; kGate: there may be a
-// gate.
-template <bool kVec, int kChunks, Kind kY, Kind kR, Kind kO, bool kGate>
-__global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 ? 1 : 2)
+// kY, kR, kO, kG: the types of y, of the residual and its output, of out, and of the gate (kNone: there is
+// none).  With a gate of a known type two CTAs of the most threads would spill registers (4096 rows of 2560 37 us
+// instead of 32).
+constexpr int kNone = -1;
+template <bool kVec, int kChunks, int kY, int kR, int kO, int kG>
+__global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 || kG > kAny ? 1 : 2)
     k_block_norm(const __grid_constant__ NormArgs a) {
     follow();
     const NormJob &j = a.j;
@@ -78,14 +80,14 @@ __global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 ? 1 : 2)
     const int64_t t = r.t;
     if (t >= j.T) return;  // (warps of several rows have no exchanges)
     const int yt = known<kY>(j.y.type), rt = known<kR>(j.residual.type), qt = known<kR>(j.residual_out.type),
-              ot = known<kO>(j.out.type), gt = j.gate.type;
+              ot = known<kO>(j.out.type), gt = known<kG>(j.gate.type);
     const Place<kVec> at = place_of<kVec, kChunks>(r, j.D);
     Raw y[kChunks], g[kChunks], s[kChunks];
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
         if (j.has_y) y[c] = load_raw<kVec>(row_of(j.y, yt, t), yt, at.chunk(c));
         if (j.has_residual) s[c] = load_raw<kVec>(row_of(j.residual, rt, t), rt, at.chunk(c));
-        if (kGate && j.has_gate) g[c] = load_raw<kVec>(row_of(j.gate, gt, t), gt, at.chunk(c));
+        if (kG != kNone && j.has_gate) g[c] = load_raw<kVec>(row_of(j.gate, gt, t), gt, at.chunk(c));
     }
     Two x[kChunks][kTwos];
     if (j.has_y) {
@@ -94,12 +96,12 @@ __global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 ? 1 : 2)
         for (int c = 0; c < kChunks; ++c) read<kVec>(y[c], j.y, yt, c0, at.chunk(c), x[c]);
         if (j.post.kind) norm<kVec, kChunks>(r, j.post, a.inverse, at, x);
     }
-    const float gc = kGate && j.has_gate ? row_scale(j.gate, t) : 0.0f;
+    const float gc = kG != kNone && j.has_gate ? row_scale(j.gate, t) : 0.0f;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
         Two v[kTwos];
         if (j.has_y) {
-            if (kGate && j.has_gate) {
+            if (kG != kNone && j.has_gate) {
                 read<kVec>(g[c], j.gate, gt, gc, at.chunk(c), v);
 #pragma unroll
                 for (int i = 0; i < kTwos; ++i) x[c][i] = mul2(x[c][i], v[i]);
@@ -140,29 +142,36 @@ __global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 ? 1 : 2)
     row_begun(r);
 }
 
-template <bool kVec, Kind kY, Kind kR, Kind kO, bool kGate>
-cudaError_t launch_kind(const NormArgs &a, cudaStream_t s) {
+template <bool kVec, int kY, int kR, int kO, int kG>
+cudaError_t launch_types(const NormArgs &a, cudaStream_t s) {
     const dim3 grid = grid_of(a.d, a.j.T);
-    const int ctas = 1 << a.d.log_ctas;
+    const int ctas = cluster_of(a.d);
     switch (a.d.chunks) {
-        case 1: return launch_cluster(k_block_norm<kVec, 1, kY, kR, kO, kGate>, grid, ctas, a.d.threads, 0, s, a);
-        case 2: return launch_cluster(k_block_norm<kVec, 2, kY, kR, kO, kGate>, grid, ctas, a.d.threads, 0, s, a);
-        default: return launch_cluster(k_block_norm<kVec, 4, kY, kR, kO, kGate>, grid, ctas, a.d.threads, 0, s, a);
+        case 1: return launch_cluster(k_block_norm<kVec, 1, kY, kR, kO, kG>, grid, ctas, a.d.threads, 0, s, a);
+        case 2: return launch_cluster(k_block_norm<kVec, 2, kY, kR, kO, kG>, grid, ctas, a.d.threads, 0, s, a);
+        default: return launch_cluster(k_block_norm<kVec, 4, kAny, kAny, kAny, kAny>, grid, ctas, a.d.threads, 0, s, a);
     }
 }
-// Kernels for the kinds of a model's own types, and of the field, beside the one for any: with the kinds known, 600
-// instructions a thread are left of 1170.
-template <Kind kY, Kind kR, Kind kO>
-cudaError_t launch_gate(const NormArgs &a, cudaStream_t s) {
-    return a.j.has_gate ? launch_kind<true, kY, kR, kO, true>(a, s) : launch_kind<true, kY, kR, kO, false>(a, s);
-}
-template <Kind kY, Kind kR>
+// Kernels for the types that a model has together, beside the one for any: with the types known, 600
+// instructions a thread are left of 1170.  kH: the model's own, of 16 bits; y may be a field element, the residual of
+// 32 bits, and out a field element.
+template <int kH, int kY, int kR>
 cudaError_t launch_out(const NormArgs &a, cudaStream_t s) {
-    return kind_of(a.j.out.type) == kField ? launch_gate<kY, kR, kField>(a, s) : launch_gate<kY, kR, kHalf>(a, s);
+    if (a.j.out.type == kField)
+        return a.j.has_gate ? launch_types<true, kY, kR, kField, kH>(a, s) : launch_types<true, kY, kR, kField, kNone>(a, s);
+    return a.j.has_gate ? launch_types<true, kY, kR, kH, kH>(a, s) : launch_types<true, kY, kR, kH, kNone>(a, s);
 }
-template <Kind kY>
-cudaError_t launch_residual(const NormArgs &a, cudaStream_t s) {
-    return kind_of(a.j.residual.type) == kF32 ? launch_out<kY, kF32>(a, s) : launch_out<kY, kHalf>(a, s);
+template <int kH>
+cudaError_t launch_model(const NormArgs &a, cudaStream_t s) {
+    if (a.j.y.type == kField)
+        return a.j.residual.type == kF32 ? launch_out<kH, kField, kF32>(a, s) : launch_out<kH, kField, kH>(a, s);
+    return a.j.residual.type == kF32 ? launch_out<kH, kH, kF32>(a, s) : launch_out<kH, kH, kH>(a, s);
+}
+// Whether a call's types are those of a model of type h.
+bool of_model(const NormJob &j, int h) {
+    return j.has_y && j.has_residual && j.out.data_dev && (j.y.type == h || j.y.type == kField) &&
+           (j.residual.type == h || j.residual.type == kF32) && (j.out.type == h || j.out.type == kField) && (!j.has_gate || j.gate.type == h) &&
+           (!j.residual_out.data_dev || j.residual_out.type == j.residual.type);
 }
 
 bool whole16(const pvmvmd_norm &n) {
@@ -172,15 +181,13 @@ bool whole16(const pvmvmd_norm &n) {
 }  // namespace
 
 cudaError_t launch_block_norm(const NormJob &j, cudaStream_t s) {
-    const NormArgs a{j, deal_rows(j.T, j.D), inverse_of(j.D)};
+    const NormArgs a{j, deal_rows(j.T, j.D, true), inverse_of(j.D)};
     const bool vec = j.D % kWide == 0 && (!j.has_y || whole16(j.y)) && (!j.has_gate || whole16(j.gate)) &&
                      (!j.has_residual || whole16(j.residual)) && whole16(j.residual_out) && whole16(j.out) &&
                      whole16(j.post) && whole16(j.pre);
-    if (!vec) return launch_kind<false, kAny, kAny, kAny, true>(a, s);
-    if (j.has_y && j.has_residual && j.out.data_dev && kind_of(j.y.type) != kF32 && kind_of(j.out.type) != kF32 &&
-        (!j.residual_out.data_dev || kind_of(j.residual_out.type) == kind_of(j.residual.type)))
-        return kind_of(j.y.type) == kField ? launch_residual<kField>(a, s) : launch_residual<kHalf>(a, s);
-    return launch_kind<true, kAny, kAny, kAny, true>(a, s);
+    if (vec && of_model(j, kBf16)) return launch_model<kBf16>(a, s);
+    if (vec && of_model(j, kF16)) return launch_model<kF16>(a, s);
+    return vec ? launch_types<true, kAny, kAny, kAny, kAny>(a, s) : launch_types<false, kAny, kAny, kAny, kAny>(a, s);
 }
 
 }  // namespace pv

@@ -19,14 +19,11 @@ constexpr int kTwos = kWide / 2;
 
 __host__ __device__ inline bool two_bytes(int type) { return type == PVMVMD_BF16 || type == PVMVMD_F16; }
 
-// What a kernel is compiled for: a kind of values, or any.
-enum Kind { kAny, kHalf, kF32, kField };
-inline Kind kind_of(int type) { return two_bytes(type) ? kHalf : type == PVMVMD_F32 ? kF32 : kField; }
-// The type of values of a kind, with what the kind says known to the compiler.
-template <Kind k>
+// What a kernel is compiled for: values of one type, or (0) of any.
+constexpr int kAny = 0, kBf16 = PVMVMD_BF16, kF16 = PVMVMD_F16, kF32 = PVMVMD_F32, kField = PVMVMD_FIELD;
+template <int k>
 __device__ __forceinline__ int known(int type) {
-    if (k == kHalf) return type == PVMVMD_BF16 ? PVMVMD_BF16 : PVMVMD_F16;
-    return k == kF32 ? PVMVMD_F32 : k == kField ? PVMVMD_FIELD : type;
+    return k == kAny ? type : k;
 }
 
 // ---------------------------------------------------------------- two numbers at a time
@@ -76,19 +73,22 @@ struct Raw {
     uint4 a, b;  // b: of 32-bit types alone
 };
 
-__device__ __forceinline__ Two unpack2(uint32_t v, bool bf) {
-    if (bf) return two(v << 16, v & 0xffff0000u);
+__device__ __forceinline__ Two half2_of(uint32_t v) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
     return two(f.x, f.y);
 }
+__device__ __forceinline__ Two bfloat2_of(uint32_t v) { return two(v << 16, v & 0xffff0000u); }
 // The values of a type, times nothing yet.
 __device__ __forceinline__ void unpack(const Raw &r, int type, Two (&x)[kTwos]) {
-    if (two_bytes(type)) {
-        const bool bf = type == PVMVMD_BF16;
-        x[0] = unpack2(r.a.x, bf);
-        x[1] = unpack2(r.a.y, bf);
-        x[2] = unpack2(r.a.z, bf);
-        x[3] = unpack2(r.a.w, bf);
+    const uint32_t h[kTwos] = {r.a.x, r.a.y, r.a.z, r.a.w};
+    if (type == PVMVMD_BF16) {
+#pragma unroll
+        for (int i = 0; i < kTwos; ++i) x[i] = bfloat2_of(h[i]);
+        return;
+    }
+    if (type == PVMVMD_F16) {
+#pragma unroll
+        for (int i = 0; i < kTwos; ++i) x[i] = half2_of(h[i]);
         return;
     }
     const uint32_t w[kWide] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
@@ -201,12 +201,15 @@ __device__ __forceinline__ void write(const pvmvmd_rows_out &o, int type, int64_
     if (two_bytes(type)) {
         uint16_t *row = static_cast<uint16_t *>(o.data_dev) + t * o.token;
         uint32_t w[kTwos];
+        if (type == PVMVMD_BF16) {
 #pragma unroll
-        for (int i = 0; i < kTwos; ++i) {
-            if (type == PVMVMD_BF16) {
+            for (int i = 0; i < kTwos; ++i) {
                 const __nv_bfloat162 v = __floats2bfloat162_rn(first(z[i]), second(z[i]));
                 w[i] = *reinterpret_cast<const uint32_t *>(&v);
-            } else {
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTwos; ++i) {
                 const __half2 v = __floats2half2_rn(first(z[i]), second(z[i]));
                 w[i] = *reinterpret_cast<const uint32_t *>(&v);
             }
@@ -291,12 +294,12 @@ __device__ __forceinline__ Two split(Two d, Two &sum) {
     sum = add2(d, both(12582912.0f));
     return sub2(d, sub2(sum, both(12582912.0f)));
 }
-// 1 + 2^-d  (23 bits up, nothing is left of 0x4b400000)
-__device__ __forceinline__ Two one_plus_exp(Two d) {
+// 2^-d for d cut to [-128, 125], infinity at -128.  (23 bits up, nothing is left of 0x4b400000.)
+__device__ __forceinline__ Two power(Two d) {
     Two n;
     d = two(fminf(fmaxf(first(d), -128.0f), 125.0f), fminf(fmaxf(second(d), -128.0f), 125.0f));
     const Two p = exp_poly(split(d, n));
-    return add2(both(1.0f), two((uint32_t)p.v - ((uint32_t)n.v << 23), (uint32_t)(p.v >> 32) - ((uint32_t)(n.v >> 32) << 23)));
+    return two((uint32_t)p.v - ((uint32_t)n.v << 23), (uint32_t)(p.v >> 32) - ((uint32_t)(n.v >> 32) << 23));
 }
 
 // ---------------------------------------------------------------- sums in pairs
@@ -344,7 +347,7 @@ __device__ __forceinline__ float inverse_root(Pair a, float eps) {
 }
 
 // ---------------------------------------------------------------- across a row's threads
-// How rows are dealt to threads: rows of up to 1024 values to a warp each, others to a CTA
+// How rows are dealt to threads: rows of up to 512 values to a warp each, others to a CTA
 // or to a cluster of them; a thread takes `chunks` times eight values.
 constexpr int kRowThreadsMost = 512, kWarpRows = 8, kMostCluster = 8, kMostWarps = kRowThreadsMost / 32;
 struct RowDeal {
@@ -352,6 +355,7 @@ struct RowDeal {
     int rows;      // of a CTA: one a warp, or one
     int log_ctas;  // CTAs of a row: 2^log_ctas
     int chunks;    // 1, 2 or 4
+    bool joint;    // the CTAs of a row are a cluster
 };
 
 // A row's threads: the lanes of a warp, the warps of a CTA, the CTAs of a cluster.  Every
@@ -370,11 +374,6 @@ struct RowThreads {
     int64_t t;              // the row
 };
 
-__device__ __forceinline__ uint32_t cta_rank() {
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 // At a kernel's start, and before its first store to a peer: all of the cluster's CTAs run.
 __device__ __forceinline__ void cluster_begin(uint32_t ctas) {
     if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
@@ -452,22 +451,25 @@ __device__ __forceinline__ float row_max(RowThreads &r, float value) {
     return __uint_as_float(v);
 }
 
-inline RowDeal deal_rows(int T, int D) {
+// joint: the row's CTAs have something to tell one another.
+inline RowDeal deal_rows(int T, int D, bool joint) {
     const int tiles = (D + kTile - 1) / kTile, sms = 152, most = kRowThreadsMost / 32;
-    RowDeal d{32, 1, 0, 1};
-    if (tiles <= 4) {
-        while (tiles > d.chunks) d.chunks *= 2;
+    RowDeal d{32, 1, 0, 1, joint};
+    if (tiles <= 2) {
+        d.chunks = tiles;
         d.rows = std::max(1, std::min(kWarpRows, T / sms));
         d.threads = 32 * d.rows;
         return d;
     }
     d.chunks = T >= sms ? 2 : 1;
-    while (tiles > most * d.chunks << d.log_ctas && d.log_ctas < 3) ++d.log_ctas;
+    // CTAs of 8 warps where they need not wait for one another, else as few as there can be
+    while (tiles > (joint ? most : 8) * d.chunks << d.log_ctas && (d.log_ctas < 3 || !joint)) ++d.log_ctas;
     while (tiles > most * d.chunks << d.log_ctas) d.chunks *= 2;
     d.threads = 32 * ((tiles + (d.chunks << d.log_ctas) - 1) / (d.chunks << d.log_ctas));
     return d;
 }
 inline dim3 grid_of(const RowDeal &d, int T) { return dim3((unsigned)((T + d.rows - 1) / d.rows) << d.log_ctas); }
+inline int cluster_of(const RowDeal &d) { return d.joint ? 1 << d.log_ctas : 1; }
 
 __device__ __forceinline__ RowThreads row_threads(RowShared *sh, const RowDeal &d) {
     RowThreads r;
@@ -475,8 +477,8 @@ __device__ __forceinline__ RowThreads row_threads(RowShared *sh, const RowDeal &
     r.lane = threadIdx.x % 32;
     r.warp = threadIdx.x / 32;
     r.warps = d.rows > 1 ? 1 : d.threads / 32;
-    r.ctas = 1u << d.log_ctas;
-    r.rank = d.log_ctas ? cta_rank() : 0;
+    r.ctas = d.joint ? 1u << d.log_ctas : 1u;
+    r.rank = blockIdx.x & ((1u << d.log_ctas) - 1);  // in a cluster, too
     r.place = 0;
     r.t = d.rows > 1 ? (int)blockIdx.x * d.rows + r.warp : (int)(blockIdx.x >> d.log_ctas);
     cluster_begin(r.ctas);

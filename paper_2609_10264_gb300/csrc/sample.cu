@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
     r.lane = threadIdx.x % 32;
     r.warp = threadIdx.x / 32;
     r.ctas = (uint32_t)a.ctas;
-    r.rank = a.ctas > 1 ? cta_rank() : 0;
+    r.rank = blockIdx.x % (uint32_t)a.ctas;
     const int V = j.V;
     const char *row = static_cast<const char *>(row_of(j.logits, j.logits.type, r.t));
     const int size = two_bytes(j.logits.type) ? 2 : 4, before16 = (int)(reinterpret_cast<uintptr_t>(row) % 16);
