@@ -639,10 +639,11 @@ typedef struct {
  * token_dev[t] is its index, and logprob_dev[t] (or null) = log(W / Z), the log of the
  * probability that it was drawn with; the token of lowest index among the largest and 0 for a greedy row;
  * -1 and -infinity where no token can be chosen.  logits->token as for other rows, not
- * below V unless it is 0 (equal rows).  1 <= V <= 2^24.  Errors: PVMVMD_E_ARG (null pointer,
+ * below V unless it is 0 (equal rows).  1 <= V <= 2^22 (whose
+ * weights' sums are below 2^62).  Errors: PVMVMD_E_ARG (null pointer,
  * unknown type), PVMVMD_E_SHAPE (T < 0, V outside its range), PVMVMD_E_PARAM (a logits' scale that
  * is not finite). */
-#define PVMVMD_MAX_V (1 << 24)
+#define PVMVMD_MAX_V (1 << 22)
 int pvmvmd_sample(int T, int V, const pvmvmd_rows *logits, const pvmvmd_sampling *sampling, const uint32_t *allowed_dev,
                   int64_t allowed_row, const uint32_t *random_dev, int32_t *token_dev, float *logprob_dev, void *stream);
 

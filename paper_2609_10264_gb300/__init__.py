@@ -112,7 +112,7 @@ class pvmvmd_kv_batch(ctypes.Structure):
                [(f, ctypes.c_int) for f in ("B", "T", "max_pages", "max_new")]
 
 
-PVMVMD_MAX_V = 1 << 24
+PVMVMD_MAX_V = 1 << 22
 PVMVMD_NORM = {"rms": 1, "layer": 2}
 PVMVMD_ACT = {"none": 0, "relu": 1, "sigmoid": 2, "silu": 3, "gelu": 4}
 

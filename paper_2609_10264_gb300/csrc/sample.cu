@@ -9,8 +9,9 @@
 // values above the k-th largest of them); the second reading puts the tokens up to there into a list, of a few
 // times k, and the first CTA finds limits and choice in it: by histograms, whose one bin
 // that a limit falls into is resolved by comparing its members with one another.
-// Where the list does not hold what the limits leave (flat rows, a large k), the limit is looked
-// for digit by digit in all values, each digit another reading.
+// Where the list does not hold what the limits leave (flat rows, a large k), a histogram of all tokens says in
+// which bin a limit falls; that bin's tokens become the list, in which the limit is looked for digit by digit.
+// Where they are too many for it (equal logits), the digits are those of all tokens, each another reading.
 #include "rows.cuh"
 
 namespace pv {
@@ -23,15 +24,16 @@ constexpr int kMostK = 1024;     // a larger k (twice of it with several CTAs) i
 constexpr int kMembers = 1024;   // of a bin at most that are compared with one another
 constexpr int kTopPList = 768;   // tokens that are put in a list for top-p alone, about
 constexpr int kGroups = 4;       // largest values that a thread keeps
+constexpr int kExchanges = 4;    // between the CTAs of a row, at most
 using u64 = unsigned long long;
 
 struct SampleShared {
-    u64 bins[kBins];
+    uint32_t low[kBins], high[kBins];  // bins' sums
     uint32_t counts[kBins];
     float x[kList], bin_x[kList];    // the list; one bin's members
     int index[kList], bin_index[kList];
-    u64 warp[kSWarps], cta, before, weight, kept;
-    uint32_t warp_count[kSWarps], found, key[kSWarps], ctakey, count, members, cut_index, general;
+    u64 warp[kSWarps], cta[kExchanges][kMostCluster], before, weight, kept;
+    uint32_t warp_count[kSWarps], found, count, members, cut_index, general, bin;
     float cut_x;
 };
 
@@ -41,6 +43,11 @@ __device__ __forceinline__ u64 peer_u64(const u64 *p, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
     return v;
+}
+__device__ __forceinline__ void store_peer_u64(const u64 *p, uint32_t rank, u64 v) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 __device__ __forceinline__ uint32_t peer_u32(const uint32_t *p, uint32_t rank) {
     uint32_t a, v;
@@ -89,10 +96,14 @@ __device__ __forceinline__ int bin_of(float d) {
     const int b = (int)(__float_as_uint(d) >> (23 - kFine)) - (117 << kFine);
     return min(max(b, 0), (16 << kFine) - 1);
 }
-// d is in a bin up to b exactly where d < this.
+// What is in bin b.
+struct Range {
+    uint32_t from, to;  // bits of distances, `to` not among them
+};
 template <int kFine>
-__device__ __forceinline__ float bin_end(int b) {
-    return __uint_as_float((uint32_t)(b + 1 + (117 << kFine)) << (23 - kFine));
+__device__ __forceinline__ Range range_of(int b) {
+    const uint32_t from = (uint32_t)(b + (117 << kFine)) << (23 - kFine);
+    return Range{b ? from : 0u, from + (1u << (23 - kFine))};
 }
 
 struct SampleArgs {
@@ -100,14 +111,16 @@ struct SampleArgs {
     int ctas;  // of a row
 };
 
-template <int kType>
-struct Row;
-template <int kType>
-__device__ __noinline__ void limits_by_digits(Row<kType> r, int top_k, float top_p, u64 least);
+// Sums of 64 bits in shared memory, in two words: an addition of 32 bits is one instruction, one of
+// 64 a loop, which equal tokens' bins make long.
+__device__ __forceinline__ void add_to(SampleShared &sh, int bin, u64 w) {
+    const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh.low[bin], lo);
+    const uint32_t hi = (uint32_t)(w >> 32) + (old + lo < old);
+    if (hi) atomicAdd(&sh.high[bin], hi);
+}
+__device__ __forceinline__ u64 sum_of(const SampleShared &sh, int bin) { return (u64)sh.high[bin] << 32 | sh.low[bin]; }
 
-// kType: the logits', all of which are allowed and have no scales of their own; or kAny, and anything.
-template <int kType>
-struct Row {
+struct RowData {
     const SampleArgs &a;
     SampleShared &sh;
     int64_t t;
@@ -115,12 +128,21 @@ struct Row {
     uint32_t rank, ctas;
     const char *base;  // the 16-byte boundary at or before the row
     int off, end;      // the row's tokens are off .. end - 1 from there
+    int tiles, share;  // the row's, and a warp's
     int begin, last;   // tiles of this warp
     float m;
     const uint32_t *allowed;
+    bool wide_scales;  // channel scales can be read four at a time
+    int exchanges;     // so far
     float big;         // the largest x
     uint32_t top;      // its key
+};
+__device__ __noinline__ void limits_in_all(RowData r, int top_k, float top_p, u64 least);
+__device__ __noinline__ bool choose_from_list(RowData r, int n, int top_k, float top_p, u64 least, u64 total);
 
+// kType: the logits', or any.
+template <int kType>
+struct Row : RowData {
     __device__ __forceinline__ void meet() const {
         if (ctas > 1)
             clusters_meet();
@@ -154,7 +176,7 @@ struct Row {
         unpack(r, type, v2);
         const int i0 = at - off, V = a.j.V;
         uint32_t ok = 0xff;
-        if (kType == kAny && allowed) {
+        if (allowed) {
             const int w = i0 >> 5, words = (V + 31) >> 5;
             const uint32_t lo = w >= 0 && w < words ? allowed[w] : 0u;
             const uint32_t hi = (i0 & 31) > 24 && w + 1 < words ? allowed[w + 1] : 0u;
@@ -164,19 +186,46 @@ struct Row {
         for (int e = 0; e < kWide; ++e) {
             float v = __fmul_rn(e & 1 ? second(v2[e / 2]) : first(v2[e / 2]), m);
             const bool in = i0 + e >= 0 && i0 + e < V;
-            if (kType == kAny && l.channel_scale_dev && in) v = __fmul_rn(v, l.channel_scale_dev[i0 + e]);
+            if (l.channel_scale_dev && in) v = __fmul_rn(v, l.channel_scale_dev[i0 + e]);
             v = v > -INFINITY ? fminf(v, kFltMax) : -INFINITY;  // (NaN is not)
             x[e] = in && (ok >> e & 1) ? v : -INFINITY;
         }
         return i0;
     }
-    // The same for a tile inside the row and kType, from what load_inside gave, without the cut at FLT_MAX: NaN and
+    // Bit e: whether the token i0 + e may be chosen, for a tile inside the row.
+    __device__ __forceinline__ uint32_t allowed_bits(int i0) const {
+        const int w = i0 >> 5;
+        return __funnelshift_r(allowed[w], (i0 & 31) > 24 ? allowed[w + 1] : 0u, i0 & 31);
+    }
+    // The same for a tile inside the row, from what load_inside gave, without the cut at FLT_MAX: NaN and
     // infinities as they come.
-    __device__ __forceinline__ void plain_tokens(const Raw &r, Two (&x)[kTwos]) const {
+    __device__ __forceinline__ void plain_tokens(const Raw &r, int i0, Two (&x)[kTwos]) const {
         unpack(r, type, x);
 #pragma unroll
         for (int i = 0; i < kTwos; ++i) x[i] = mul2(x[i], both(m));
+        if (const float *c = a.j.logits.channel_scale_dev) {
+            Raw s;
+            if (wide_scales) {
+                s.a = *reinterpret_cast<const uint4 *>(c + i0);
+                s.b = *reinterpret_cast<const uint4 *>(c + i0 + 4);
+            } else {
+                const uint32_t *p = reinterpret_cast<const uint32_t *>(c + i0);
+                s.a = make_uint4(p[0], p[1], p[2], p[3]);
+                s.b = make_uint4(p[4], p[5], p[6], p[7]);
+            }
+            Two v[kTwos];
+            unpack(s, PVMVMD_F32, v);
+#pragma unroll
+            for (int i = 0; i < kTwos; ++i) x[i] = mul2(x[i], v[i]);
+        }
+        if (allowed) {
+            const uint32_t ok = allowed_bits(i0);
+#pragma unroll
+            for (int i = 0; i < kTwos; ++i)
+                x[i] = two(ok >> 2 * i & 1 ? first(x[i]) : -INFINITY, ok >> (2 * i + 1) & 1 ? second(x[i]) : -INFINITY);
+        }
     }
+    __device__ __forceinline__ int index_of(int tile) const { return tile * kTile + lane * kWide - off; }
 
     // f(x, index) for every token of this warp's tiles that may be chosen
     template <typename F>
@@ -191,18 +240,30 @@ struct Row {
         }
     }
 
-    __device__ __forceinline__ uint32_t max_key(uint32_t k) const {
-        k = __reduce_max_sync(kFull, k);
-        if (lane == 0) sh.key[warp] = k;
-        __syncthreads();
-        k = __reduce_max_sync(kFull, lane < kSWarps ? sh.key[lane] : 0u);
+    __device__ __forceinline__ u64 peer_sum(int bin, uint32_t c) const {
+        return (u64)peer_u32(&sh.high[bin], c) << 32 | peer_u32(&sh.low[bin], c);
+    }
+    // Every CTA's value, in this CTA's memory.
+    __device__ __forceinline__ const u64 *exchange(u64 v) {
+        u64 *all = sh.cta[exchanges++];
         if (ctas > 1) {
-            if (threadIdx.x == 0) sh.ctakey = k;
+            if (threadIdx.x < ctas) store_peer_u64(&all[rank], threadIdx.x, v);
             clusters_meet();
-            k = __reduce_max_sync(kFull, lane < (int)ctas ? peer_u32(&sh.ctakey, (uint32_t)lane) : 0u);
+        } else {
+            if (threadIdx.x == 0) all[0] = v;
+            __syncthreads();
         }
-        meet();
-        return k;
+        return all;
+    }
+    __device__ __forceinline__ uint32_t max_key(uint32_t k) {
+        k = __reduce_max_sync(kFull, k);
+        __syncthreads();  // (an earlier call's have been read)
+        if (lane == 0) sh.warp_count[warp] = k;
+        __syncthreads();
+        k = __reduce_max_sync(kFull, lane < kSWarps ? sh.warp_count[lane] : 0u);
+        if (ctas == 1) return k;
+        const u64 *all = exchange(k);
+        return __reduce_max_sync(kFull, lane < (int)ctas ? (uint32_t)all[lane] : 0u);
     }
 
     // The largest x of a thread's tokens in kGroups parts of them (-infinity: none).
@@ -216,10 +277,10 @@ struct Row {
 #pragma unroll
             for (int e = 0; e < kWide; ++e) g[e % kGroups] = fmaxf(g[e % kGroups], x[e]);
         };
-        if (kType != kAny && m > 0.0f) {
+        const int from = whole_from(), to = whole_to();
+        for (; k < from; ++k) edge(k);
+        if (m > 0.0f && !allowed && !a.j.logits.channel_scale_dev) {
             // rounding keeps the order, so that the largest logit has the largest x
-            const int from = whole_from(), to = whole_to();
-            for (; k < from; ++k) edge(k);
             if (from < to) {
                 uint32_t n[kGroups];
                 float v[kGroups];
@@ -260,15 +321,31 @@ struct Row {
                     if (p > -INFINITY) g[i] = fmaxf(g[i], fminf(p, kFltMax));  // (a part of NaN alone stays as it was)
                 }
             }
+        } else {
+#pragma unroll 2
+            for (; k < to; ++k) {
+                Two x[kTwos];
+                plain_tokens(load_inside(k), index_of(k), x);
+#pragma unroll
+                for (int i = 0; i < kTwos; ++i) {  // (NaN is not taken)
+                    g[i] = fmaxf(g[i], fminf(fmaxf(first(x[i]), -INFINITY), kFltMax));
+                    g[i] = fmaxf(g[i], fminf(fmaxf(second(x[i]), -INFINITY), kFltMax));
+                }
+            }
         }
 #pragma unroll 1
         for (; k < last; ++k) edge(k);
     }
 
-    // One pass over the warp's tiles: sum, where asked for, of the weights that are at least `least`; and collect(x,
-    // index) for the tokens nearer than `near`.
-    template <bool kSum, bool kCollect, typename C>
-    __device__ __forceinline__ u64 pass(u64 least, float near, C collect) const {
+    // One pass over the warp's tiles: the sum, where asked for, of the weights that are at least `least` (and with kCut of
+    // tokens up to a cut); collect(x, index) for the tokens whose distance is below `near`; hist(d, w) for all of some weight.
+    struct Cut {
+        float x;
+        uint32_t index;
+        __device__ __forceinline__ bool keeps(float v, int i) const { return v > x || (v == x && (uint32_t)i <= index); }
+    };
+    template <bool kSum, bool kCollect, bool kHist, bool kCut, typename C, typename H>
+    __device__ __forceinline__ u64 pass(u64 least, float near, Cut cut, C collect, H hist) const {
         u64 sum = 0;
         int k = begin;
         auto edge = [&](int tile) {
@@ -277,56 +354,62 @@ struct Row {
 #pragma unroll
             for (int e = 0; e < kWide; ++e) {
                 if (x[e] > -INFINITY) {
-                    if (kSum) {
+                    if (kSum && (!kCut || cut.keeps(x[e], i0 + e))) {
                         const u64 w = weight(big, x[e]);
                         sum += w >= least ? w : 0ull;
                     }
-                    if (kCollect && __fsub_rn(big, x[e]) < near) collect(x[e], i0 + e);
+                    const float d = __fsub_rn(big, x[e]);
+                    if (kCollect && d < near) collect(x[e], i0 + e);
+                    if (kHist) hist(d, weight(big, x[e]));
                 }
             }
         };
-        if (kType != kAny && big < kFltMax) {  // (no x is cut)
-            const int from = whole_from(), to = whole_to();
-            for (; k < from; ++k) edge(k);
+        const int from = whole_from(), to = big < kFltMax ? whole_to() : from;  // (else x may be cut)
+#pragma unroll 1
+        for (; k < from; ++k) edge(k);
 #pragma unroll 2
-            for (; k < to; ++k) {
-                Two x[kTwos];
-                plain_tokens(load_inside(k), x);
-                uint32_t hits = 0, low = 0;
+        for (; k < to; ++k) {
+            Two x[kTwos];
+            const int i0 = index_of(k);
+            plain_tokens(load_inside(k), i0, x);
+            uint32_t hits = 0, low = 0;
 #pragma unroll
-                for (int i = 0; i < kTwos; ++i) {
-                    Two d = sub2(both(big), x[i]);
-                    if (kCollect) hits |= (first(d) < near ? 1u << 2 * i : 0u) | (second(d) < near ? 2u << 2 * i : 0u);
-                    if (kSum) {
-                        d = two(fminf(first(d), 63.0f), fminf(second(d), 63.0f));  // (NaN: 63)
-                        Two n;
-                        const Two r = add2(exp_poly(split(d, n), 4194304.0f), both(8388608.0f));
+            for (int i = 0; i < kTwos; ++i) {
+                Two d = sub2(both(big), x[i]);
+                if (kCollect) hits |= (first(d) < near ? 1u << 2 * i : 0u) | (second(d) < near ? 2u << 2 * i : 0u);
+                if (kSum || kHist) {
+                    d = two(fminf(first(d), 63.0f), fminf(second(d), 63.0f));  // (NaN: 63)
+                    Two n;
+                    const Two r = add2(exp_poly(split(d, n), 4194304.0f), both(8388608.0f));
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t p = (uint32_t)(h ? r.v >> 32 : r.v) & 0x7fffffu, q = (uint32_t)(h ? n.v >> 32 : n.v);
-                            if (least) {
-                                const u64 w = ((u64)p << 18) >> (q - 0x4b400000u);
-                                sum += w >= least ? w : 0ull;
-                            } else {  // p 2^(18 - n) for n < 18; the others are below 2^23
-                                sum += (u64)p * shift_left(2u, 0x4b400000u + 17u - q);
-                                low += shift_right(p, q - (0x4b400000u + 18u));
-                            }
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t p = (uint32_t)(h ? r.v >> 32 : r.v) & 0x7fffffu;
+                        const uint32_t q = (uint32_t)(h ? n.v >> 32 : n.v);
+                        if (kCut && !cut.keeps(h ? second(x[i]) : first(x[i]), i0 + 2 * i + h)) p = 0;
+                        if (kHist) {
+                            hist(h ? second(d) : first(d), ((u64)p << 18) >> (q - 0x4b400000u));
+                        } else if (least) {
+                            const u64 w = ((u64)p << 18) >> (q - 0x4b400000u);
+                            sum += w >= least ? w : 0ull;
+                        } else {  // p 2^(18 - n) for n < 18; the others are below 2^23
+                            sum += (u64)p * shift_left(2u, 0x4b400000u + 17u - q);
+                            low += shift_right(p, q - (0x4b400000u + 18u));
                         }
                     }
                 }
-                if (kSum) sum += low;
-                if (kCollect && hits) {
-                    const int i0 = k * kTile + lane * kWide - off;
+            }
+            if (kSum) sum += low;
+            if (kCollect && hits) {
 #pragma unroll
-                    for (int e = 0; e < kWide; ++e)
-                        if (hits >> e & 1) collect(e & 1 ? second(x[e / 2]) : first(x[e / 2]), i0 + e);
-                }
+                for (int e = 0; e < kWide; ++e)
+                    if (hits >> e & 1) collect(e & 1 ? second(x[e / 2]) : first(x[e / 2]), i0 + e);
             }
         }
 #pragma unroll 1
         for (; k < last; ++k) edge(k);
         return sum;
     }
+    __device__ __forceinline__ Cut no_cut() const { return Cut{-INFINITY, ~0u}; }
 
     // Bins' sums from the front: of a thread's four (of 2048).  pre: in front of the first of them.
     template <typename T>
@@ -364,7 +447,7 @@ struct Row {
         for (int left = bits; left > 0; left = (int)open) {
             const int digit = min(left, 11);
             open = (uint32_t)(left - digit);
-            for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.bins[i] = 0;
+            for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.low[i] = sh.high[i] = 0;
             if (threadIdx.x == 0) sh.found = ~0u;
             __syncthreads();
             const uint32_t high = v;
@@ -372,7 +455,7 @@ struct Row {
                 uint32_t value;
                 u64 w;
                 if (f(x, i, value, w) && ((u64)value >> left) == ((u64)high >> left) && w)
-                    atomicAdd(&sh.bins[(value >> open) & ((1u << digit) - 1)], w);
+                    add_to(sh, (int)((value >> open) & ((1u << digit) - 1)), w);
             });
             meet();
             constexpr int kMine = kBins / kSThreads;
@@ -381,7 +464,7 @@ struct Row {
             for (int i = 0; i < kMine; ++i) {
                 const int b = (int)threadIdx.x * kMine + i;
                 mine[i] = 0;
-                for (uint32_t c = 0; c < ctas; ++c) mine[i] += ctas > 1 ? peer_u64(&sh.bins[b], c) : sh.bins[b];
+                for (uint32_t c = 0; c < ctas; ++c) mine[i] += ctas > 1 ? peer_sum(b, c) : sum_of(sh, b);
             }
             u64 pre = before + scan(mine, sh.warp, total);
 #pragma unroll
@@ -425,17 +508,10 @@ struct Row {
         u64 mine = 0, front = 0, Z = 0;  // of this CTA; of the CTAs in front; of all
 #pragma unroll
         for (int k = 0; k < kSWarps; ++k) mine += sh.warp[k];
-        if (ctas > 1) {
-            if (threadIdx.x == 0) sh.cta = mine;
-            clusters_meet();
-            for (uint32_t c = 0; c < ctas; ++c) {
-                const u64 v = peer_u64(&sh.cta, c);
-                if (c < rank) front += v;
-                Z += v;
-            }
-            clusters_meet();  // nothing of a CTA's is read once it may have ended
-        } else {
-            Z = mine;
+        const u64 *all = exchange(mine);
+        for (uint32_t c = 0; c < ctas; ++c) {
+            if (c < rank) front += all[c];
+            Z += all[c];
         }
         const u64 at = random_part(Z);
         if (at < front || at >= front + mine) return;  // another CTA's
@@ -498,7 +574,6 @@ struct Row {
             if (at < front) return;
         }
     }
-    int tiles, share;  // the row's, and a warp's
     __device__ __forceinline__ int begin_of(int w) const { return min(tiles, ((int)rank * kSWarps + w) * share); }
     __device__ __forceinline__ int last_of(int w) const { return min(tiles, begin_of(w) + share); }
 
@@ -586,7 +661,7 @@ struct Row {
     // too many fall into one bin.
     __device__ __forceinline__ bool choose_listed(int n, int top_k, float top_p, u64 least, u64 total) {
         constexpr int kMine = kBins / kSThreads;
-        for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.bins[i] = 0, sh.counts[i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.low[i] = sh.high[i] = sh.counts[i] = 0;
         if (threadIdx.x == 0) {
             sh.found = ~0u;
             sh.cut_x = -INFINITY;
@@ -596,7 +671,7 @@ struct Row {
         __syncthreads();
         listed(n, [&](float x, int) {
             const int b = bin_of<7>(__fsub_rn(big, x));
-            atomicAdd(&sh.bins[b], weight(big, x));
+            add_to(sh, b, weight(big, x));
             atomicAdd(&sh.counts[b], 1u);
         });
         __syncthreads();
@@ -604,7 +679,7 @@ struct Row {
         uint32_t count[kMine], number;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            mass[i] = sh.bins[threadIdx.x * kMine + i];
+            mass[i] = sum_of(sh, threadIdx.x * kMine + i);
             count[i] = sh.counts[threadIdx.x * kMine + i];
         }
         const uint32_t pre_count = scan(count, sh.warp_count, number);
@@ -687,15 +762,15 @@ struct Row {
             return w >= least ? w : 0ull;
         };
         const int shift = max(0, 32 - __clz(a.j.V - 1) - 11);
-        for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.bins[i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.low[i] = sh.high[i] = 0;
         __syncthreads();
         listed(n, [&](float x, int i) {
             const u64 w = kept(x, i);
-            if (w) atomicAdd(&sh.bins[i >> shift], w);
+            if (w) add_to(sh, i >> shift, w);
         });
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) mass[i] = sh.bins[threadIdx.x * kMine + i];
+        for (int i = 0; i < kMine; ++i) mass[i] = sum_of(sh, threadIdx.x * kMine + i);
         u64 Z, w = scan(mass, sh.warp, Z);
         const u64 at_random = random_part(Z);
 #pragma unroll
@@ -722,100 +797,319 @@ struct Row {
         return true;
     }
 
-    // With top-k or top-p.
-    __device__ __forceinline__ void limited(int top_k, float top_p, u64 least, const float (&g)[kGroups]) {
-        // The bin up to which so many groups have their largest value.
-        const int most_k = ctas > 1 ? 2 * kMostK : kMostK;  // (the groups are 2048 a CTA)
-        const uint32_t want = top_k ? (uint32_t)min(top_k, most_k) : (uint32_t)kTopPList;
-        for (int i = threadIdx.x; i < kSThreads; i += kSThreads) sh.counts[i] = 0;
-        if (threadIdx.x == 0) {
-            sh.found = kSThreads - 1;
-            sh.count = 0;
-        }
+    // The tokens whose distance's bits are in a range, to this CTA's part of the list; then, in the first CTA, all of them.  Their number, in every CTA; what is above kList is not in the list.
+    // total (of the weights, where asked for).
+    template <bool kSum>
+    __device__ __forceinline__ uint32_t collect_list(Range range, u64 &total) {
+        if (threadIdx.x == 0) sh.count = 0;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            const float d = __fsub_rn(big, g[i]);
-            if (d < 64.0f) atomicAdd(&sh.counts[bin_of<5>(d)], 1u);
-        }
-        meet();
-        static_assert(kSThreads == 16 << 5, "a bin a thread");
-        uint32_t c = 0;
-        for (uint32_t k = 0; k < ctas; ++k) c += ctas > 1 ? peer_u32(&sh.counts[threadIdx.x], k) : sh.counts[threadIdx.x];
-        uint32_t pre = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t u = __shfl_up_sync(kFull, pre, o);
-            if (lane >= o) pre += u;
-        }
-        if (lane == 31) sh.warp_count[warp] = pre;
-        __syncthreads();
-        pre -= c;
-        for (int k = 0; k < warp; ++k) pre += sh.warp_count[k];
-        if (pre < want && pre + c >= want) sh.found = threadIdx.x;
-        __syncthreads();
-        const float near = bin_end<5>((int)sh.found);
         auto collect = [&](float x, int i) {
+            if (range.from && __float_as_uint(__fsub_rn(big, x)) < range.from) return;
             const uint32_t p = atomicAdd(&sh.count, 1u);
             if (p < (uint32_t)kList) {
                 sh.x[p] = x;
                 sh.index[p] = i;
             }
         };
-        u64 total = 0;
-        if (top_k)
-            pass<false, true>(0, near, collect);
-        else
-            total = pass<true, true>(0, near, collect);
-        if (!top_k) {
+        total = pass<kSum, true, false, false>(0, __uint_as_float(range.to), no_cut(), collect, [](float, u64) {});
+        if (kSum) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
             if (lane == 0) sh.warp[warp] = total;
-            __syncthreads();
-            total = 0;
+        }
+        __syncthreads();
+        total = 0;
+        if (kSum)
 #pragma unroll
             for (int k = 0; k < kSWarps; ++k) total += sh.warp[k];
-            if (threadIdx.x == 0) sh.cta = total;
-        }
-        meet();
         uint32_t n = sh.count;
-        bool fits = top_k <= most_k;
-        if (ctas > 1) {
-            n = 0;
+        if (ctas == 1) return n;
+        // (weights' sums are below 2^64 / 2^5; numbers go beside them, up to kList + 1)
+        const uint32_t mine = min(n, (uint32_t)kList + 1);
+        const u64 *all = exchange(mine);
+        n = 0;
+        for (uint32_t c = 0; c < ctas; ++c) n += (uint32_t)all[c];
+        if (kSum) {
+            const u64 *sums = exchange(total);
             total = 0;
-            for (uint32_t k = 0; k < ctas; ++k) {
-                n += peer_u32(&sh.count, k);
-                if (!top_k) total += peer_u64(&sh.cta, k);
-            }
+            for (uint32_t c = 0; c < ctas; ++c) total += sums[c];
         }
-        fits = fits && n <= (uint32_t)kList;
-        if (rank == 0) {
-            bool done = false;
-            if (fits) {
-                uint32_t at = sh.count;
-                for (uint32_t k = 1; k < ctas; ++k) {
-                    const uint32_t theirs = peer_u32(&sh.count, k);
-                    for (uint32_t i = threadIdx.x; i < theirs; i += kSThreads) {
-                        sh.x[at + i] = __uint_as_float(peer_u32(reinterpret_cast<const uint32_t *>(&sh.x[i]), k));
-                        sh.index[at + i] = (int)peer_u32(reinterpret_cast<const uint32_t *>(&sh.index[i]), k);
-                    }
-                    at += theirs;
+        if (rank == 0 && n <= (uint32_t)kList) {
+            uint32_t at = mine;
+            for (uint32_t c = 1; c < ctas; ++c) {
+                const uint32_t theirs = (uint32_t)all[c];
+                for (uint32_t i = threadIdx.x; i < theirs; i += kSThreads) {
+                    sh.x[at + i] = __uint_as_float(peer_u32(reinterpret_cast<const uint32_t *>(&sh.x[i]), c));
+                    sh.index[at + i] = (int)peer_u32(reinterpret_cast<const uint32_t *>(&sh.index[i]), c);
                 }
-                __syncthreads();
-                done = choose_listed((int)n, top_k, top_p, least, total);
+                at += theirs;
             }
-            if (threadIdx.x == 0) sh.general = !done;
         }
+        clusters_meet();  // the lists have been read
+        return n;
+    }
+
+    // The same as reach, for the first n tokens of the list and by one CTA.
+    template <typename F>
+    __device__ __forceinline__ bool reach_listed(int n, int bits, u64 target, F f, uint32_t &v, u64 &before, u64 &at) const {
+        v = 0;
+        before = at = 0;
+        uint32_t open = 0;
+        for (int left = bits; left > 0; left = (int)open) {
+            const int digit = min(left, 11);
+            open = (uint32_t)(left - digit);
+            __syncthreads();
+            for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.low[i] = sh.high[i] = 0;
+            if (threadIdx.x == 0) sh.found = ~0u;
+            __syncthreads();
+            const uint32_t high = v;
+            listed(n, [&](float x, int i) {
+                uint32_t value;
+                u64 w;
+                if (f(x, i, value, w) && ((u64)value >> left) == ((u64)high >> left) && w)
+                    add_to(sh, (int)((value >> open) & ((1u << digit) - 1)), w);
+            });
+            __syncthreads();
+            constexpr int kMine = kBins / kSThreads;
+            u64 mine[kMine], total;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) mine[i] = sum_of(sh, threadIdx.x * kMine + i);
+            u64 pre = before + scan(mine, sh.warp, total);
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                if (pre < target && pre + mine[i] >= target) {
+                    sh.found = threadIdx.x * kMine + i;
+                    sh.before = pre;
+                    sh.weight = mine[i];
+                }
+                pre += mine[i];
+            }
+            __syncthreads();
+            if (sh.found == ~0u) return false;
+            v |= sh.found << open;
+            before = sh.before;
+            at = sh.weight;
+        }
+        return true;
+    }
+    // Of the listed tokens that `within` keeps, in order: those up to which `target` of weight lies (one each where
+    // ones).  The cut after them.
+    __device__ __forceinline__ Cut cut_listed(int n, u64 target, bool ones, Cut within) const {
+        uint32_t v;
+        u64 before, at;
+        reach_listed(n, 32, target, [&](float x, int i, uint32_t &value, u64 &w) {
+            value = top - key_of(x);
+            w = ones ? 1ull : weight(big, x);
+            return within.keeps(x, i);
+        }, v, before, at);
+        const float x0 = of_key(top - v);
+        const u64 each = ones ? 1ull : weight(big, x0), ties = (target - before + each - 1) / each;
+        Cut cut{x0, x0 == within.x ? within.index : ~0u};
+        if (ties < at / each) {
+            u64 b, w1;
+            reach_listed(n, 24, ties, [&](float x, int i, uint32_t &value, u64 &w) {
+                value = (uint32_t)i;
+                w = 1;
+                return x == x0 && within.keeps(x, i);
+            }, cut.index, b, w1);
+        }
+        return cut;
+    }
+
+    // A histogram of the tokens in a range, by bin(bits of the distance): weights, and numbers where asked for.  A
+    // thread's bins of it, for all CTAs, and what lies in front of them.
+    static constexpr int kMine = kBins / kSThreads;
+    template <typename F>
+    __device__ __forceinline__ void histogram(Range range, bool numbers, F bin, u64 (&mass)[kMine], u64 &pre_mass, u64 &all,
+                                              uint32_t (&count)[kMine], uint32_t &pre_count, uint32_t &number) {
+        for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.low[i] = sh.high[i] = sh.counts[i] = 0;
+        __syncthreads();
+        pass<false, false, true, false>(0, 0.0f, no_cut(), [](float, int) {}, [&](float d, u64 w) {
+            const uint32_t bits = __float_as_uint(d);
+            if (w && bits >= range.from && bits < range.to) {
+                const int b = bin(d, bits);
+                add_to(sh, b, w);
+                if (numbers) atomicAdd(&sh.counts[b], 1u);
+            }
+        });
         meet();
-        const bool again = ctas > 1 ? peer_u32(&sh.general, 0) != 0 : sh.general != 0;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int b = threadIdx.x * kMine + i;
+            mass[i] = sum_of(sh, b);
+            count[i] = sh.counts[b];
+            if (ctas > 1) {
+                mass[i] = 0;
+                count[i] = 0;
+                for (uint32_t c = 0; c < ctas; ++c) {
+                    mass[i] += peer_sum(b, c);
+                    count[i] += peer_u32(&sh.counts[b], c);
+                }
+            }
+        }
+        pre_count = scan(count, sh.warp_count, number);
+        pre_mass = scan(mass, sh.warp, all);
+        meet();  // (the bins have been read)
+    }
+    // Where a limit falls: the bin, and what is in front of it.
+    struct Fall {
+        Range range;
+        u64 mass;   // of weight
+        u64 count;  // of tokens
+    };
+    // `target` of weight (by_count: of tokens) reached in a thread's bins: to shared memory.
+    __device__ __forceinline__ int fall(bool by_count, u64 target, const u64 (&mass)[kMine], u64 pre_mass,
+                                        const uint32_t (&count)[kMine], uint32_t pre_count, Fall &f) const {
+        __syncthreads();  // (an earlier one's results have been read)
+        u64 c = f.count + pre_count, w = f.mass + pre_mass;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const u64 v = by_count ? c : w;
+            c += count[i];
+            w += mass[i];
+            if (v < target && (by_count ? c : w) >= target) {
+                sh.bin = threadIdx.x * kMine + i;
+                sh.before = w - mass[i];
+                sh.weight = c - count[i];
+            }
+        }
+        __syncthreads();
+        f.mass = sh.before;
+        f.count = sh.weight;
+        return (int)sh.bin;
+    }
+    // The bin's tokens in the list, from narrower bins where they are too many; their number, or more than kList where
+    // that does not help.
+    __device__ __forceinline__ uint32_t narrow(bool by_count, u64 target, Fall &f) {
+        u64 none;
+        for (;;) {
+            exchanges = 0;
+            meet();  // (what it overwrites has been read)
+            const uint32_t n = collect_list<false>(f.range, none), width = f.range.to - f.range.from;
+            if (n <= (uint32_t)kList || width <= 1) return n;
+            const int shift = max(0, 32 - __clz(width - 1) - 11);
+            u64 mass[kMine], pre_mass, all;
+            uint32_t count[kMine], pre_count, number;
+            const uint32_t from = f.range.from;
+            histogram(f.range, true, [&](float, uint32_t bits) { return (int)((bits - from) >> shift); }, mass, pre_mass, all, count,
+                      pre_count, number);
+            const uint32_t b = (uint32_t)fall(by_count, target, mass, pre_mass, count, pre_count, f);
+            f.range = Range{from + (b << shift), min(f.range.to, from + ((b + 1) << shift))};
+        }
+    }
+
+    // The limits looked for by histograms of all tokens.  False where equal distances have more of them than the list.
+    __device__ __forceinline__ bool by_bins(int top_k, float top_p, u64 least) {
+        u64 mass[kMine], pre_mass, all;
+        uint32_t count[kMine], pre_count, number;
+        histogram(Range{0, range_of<7>(kBins - 1).to}, top_k != 0, [](float d, uint32_t) { return bin_of<7>(d); }, mass, pre_mass,
+                  all, count, pre_count, number);
+        Cut cut = no_cut();
+        u64 S = all;
+        Fall f{Range{0, 0}, ~0ull, 0};  // of top-k: everything is in front of it where there is none
+        uint32_t n = 0;
+        if (top_k && (uint32_t)top_k < number) {
+            f.mass = 0;
+            f.range = range_of<7>(fall(true, (u64)top_k, mass, pre_mass, count, pre_count, f));
+            n = narrow(true, (u64)top_k, f);
+            if (n > (uint32_t)kList) return false;
+            if (rank == 0) {
+                cut = cut_listed((int)n, (u64)top_k - f.count, true, no_cut());
+                if (threadIdx.x == 0) sh.kept = 0;
+                __syncthreads();
+                u64 mine = 0;
+                listed((int)n, [&](float x, int i) { mine += cut.keeps(x, i) ? weight(big, x) : 0ull; });
+                if (mine) atomicAdd(&sh.kept, mine);
+                __syncthreads();
+            }
+            S = f.mass + (ctas > 1 ? (meet(), peer_u64(&sh.kept, 0)) : sh.kept);
+        }
+        if (top_p < 1.0f) {
+            const u64 target = max(part_of(S, part31(top_p)), 1ull);
+            if (target <= f.mass) {  // in front of top-k's bin, or without it
+                f = Fall{Range{0, 0}, 0, 0};
+                f.range = range_of<7>(fall(false, target, mass, pre_mass, count, pre_count, f));
+                cut = no_cut();
+                n = narrow(false, target, f);
+                if (n > (uint32_t)kList) return false;
+            }
+            if (rank == 0) cut = cut_listed((int)n, target - f.mass, false, cut);
+        }
+        if (ctas > 1) {  // the first CTA's cut
+            if (rank == 0 && threadIdx.x == 0) sh.cut_x = cut.x, sh.cut_index = cut.index;
+            meet();
+            cut = Cut{__uint_as_float(peer_u32(reinterpret_cast<const uint32_t *>(&sh.cut_x), 0)), peer_u32(&sh.cut_index, 0)};
+        }
+        exchanges = 0;
         meet();
-        if (again) limits_by_digits(*this, top_k, top_p, least);
+        const u64 sum = pass<true, false, false, true>(least, 0.0f, cut, [](float, int) {}, [](float, u64) {});
+        choose_in_order(sum, [&](float x, int i) {
+            const u64 w = cut.keeps(x, i) ? weight(big, x) : 0ull;
+            return w >= least ? w : 0ull;
+        });
+        return true;
+    }
+
+    // With top-k or top-p.
+    __device__ __forceinline__ void limited(int top_k, float top_p, u64 least, const float (&g)[kGroups]) {
+        // The bin up to which so many groups have their largest value.
+        const int most_k = ctas > 1 ? 2 * kMostK : kMostK;  // (the groups are 2048 a CTA)
+        const uint32_t want = top_k ? (uint32_t)min(top_k, most_k) : (uint32_t)kTopPList;
+        bool again = top_k > most_k;
+        if (!again) {
+            sh.counts[threadIdx.x] = 0;
+            if (threadIdx.x == 0) sh.found = kSThreads - 1;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                const float d = __fsub_rn(big, g[i]);
+                if (d < 64.0f) atomicAdd(&sh.counts[bin_of<5>(d)], 1u);
+            }
+            meet();
+            static_assert(kSThreads == 16 << 5, "a bin a thread");
+            uint32_t c = 0;
+            for (uint32_t k = 0; k < ctas; ++k) c += ctas > 1 ? peer_u32(&sh.counts[threadIdx.x], k) : sh.counts[threadIdx.x];
+            uint32_t pre = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(kFull, pre, o);
+                if (lane >= o) pre += u;
+            }
+            if (lane == 31) sh.warp_count[warp] = pre;
+            __syncthreads();
+            pre -= c;
+            for (int k = 0; k < warp; ++k) pre += sh.warp_count[k];
+            if (pre < want && pre + c >= want) sh.found = threadIdx.x;
+            __syncthreads();
+            const Range near{0, range_of<5>((int)sh.found).to};
+            u64 total = 0;
+            const uint32_t n = top_k ? collect_list<false>(near, total) : collect_list<true>(near, total);
+            again = n > (uint32_t)kList;
+            if (!again) {
+                if (rank == 0) {
+                    const bool done = choose_from_list(*this, (int)n, top_k, top_p, least, total);
+                    if (threadIdx.x == 0) sh.general = !done;
+                }
+                meet();
+                again = ctas > 1 ? peer_u32(&sh.general, 0) != 0 : sh.general != 0;
+                meet();
+            }
+        }
+        if (again) limits_in_all(*this, top_k, top_p, least);
     }
 };
-// (A copy of the row: its values stay in the caller's registers.)
-template <int kType>
-__device__ void limits_by_digits(Row<kType> r, int top_k, float top_p, u64 least) {
-    r.general(top_k, top_p, least);
+// (Copies of the row: its values stay in the caller's registers.)
+__device__ bool choose_from_list(RowData d, int n, int top_k, float top_p, u64 least, u64 total) {
+    return Row<kAny>{d}.choose_listed(n, top_k, top_p, least, total);
+}
+__device__ void limits_in_all(RowData d, int top_k, float top_p, u64 least) {
+    Row<kAny> r{d};
+    r.exchanges = 0;
+    if (!r.by_bins(top_k, top_p, least)) {
+        r.exchanges = 0;
+        r.meet();
+        r.general(top_k, top_p, least);
+    }
 }
 
 template <int kType>
@@ -825,7 +1119,7 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
     SampleShared &sh = *reinterpret_cast<SampleShared *>(s_mem);
     const SampleJob &j = a.j;
     cluster_begin((uint32_t)a.ctas);
-    Row<kType> r{a, sh};
+    Row<kType> r{RowData{a, sh}};
     r.t = blockIdx.x / a.ctas;
     r.lane = threadIdx.x % 32;
     r.warp = threadIdx.x / 32;
@@ -843,6 +1137,8 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
     r.begin = r.begin_of(r.warp);
     r.last = r.last_of(r.warp);
     r.allowed = j.allowed ? j.allowed + r.t * j.allowed_row : nullptr;
+    r.wide_scales = r.off % 4 == 0 && reinterpret_cast<uintptr_t>(j.logits.channel_scale_dev) % 16 == 0;
+    r.exchanges = 0;
 
     const pvmvmd_sampling &how = j.how;
     const float temperature = how.temperature_dev ? how.temperature_dev[r.t] : how.temperature;
@@ -891,7 +1187,7 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
         r.limited(by_k ? top_k : 0, top_p, least, g);
         return;
     }
-    const u64 sum = r.template pass<true, false>(least, 0.0f, [](float, int) {});
+    const u64 sum = r.template pass<true, false, false, false>(least, 0.0f, r.no_cut(), [](float, int) {}, [](float, u64) {});
     r.choose_in_order(sum, [&](float x, int) {
         const u64 w = weight(r.big, x);
         return w >= least ? w : 0ull;
@@ -911,7 +1207,6 @@ cudaError_t launch_type(const SampleArgs &a, cudaStream_t s) {
 cudaError_t launch_sample(const SampleJob &j, cudaStream_t s) {
     SampleArgs a{j, 1};
     while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 304 && j.V / a.ctas >= 8192) a.ctas *= 2;
-    if (j.allowed || j.logits.channel_scale_dev) return launch_type<kAny>(a, s);
     switch (j.logits.type) {
         case kBf16: return launch_type<kBf16>(a, s);
         case kF16: return launch_type<kF16>(a, s);
