@@ -27,13 +27,17 @@ constexpr int kGroups = 4;       // largest values that a thread keeps
 constexpr int kExchanges = 4;    // between the CTAs of a row, at most
 using u64 = unsigned long long;
 
-struct SampleShared {
+struct SampleSmall {  // what a row without top-k and top-p needs
+    u64 warp[kSWarps], cta[kExchanges][kMostCluster];
+    uint32_t warp_count[kSWarps];
+};
+struct SampleShared : SampleSmall {
     uint32_t low[kBins], high[kBins];  // bins' sums
     uint32_t counts[kBins];
-    float x[kList], bin_x[kList];    // the list; one bin's members
+    float x[kList], bin_x[kList];      // the list; one bin's members
     int index[kList], bin_index[kList];
-    u64 warp[kSWarps], cta[kExchanges][kMostCluster], before, weight, kept;
-    uint32_t warp_count[kSWarps], found, count, members, cut_index, general, bin;
+    u64 before, weight, kept;
+    uint32_t found, count, members, cut_index, general, bin;
     float cut_x;
 };
 
@@ -48,6 +52,11 @@ __device__ __forceinline__ void store_peer_u64(const u64 *p, uint32_t rank, u64 
     uint32_t a;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+}
+__device__ __forceinline__ void store_peer_u32(const void *p, uint32_t rank, uint32_t v) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
 __device__ __forceinline__ uint32_t peer_u32(const uint32_t *p, uint32_t rank) {
     uint32_t a, v;
@@ -255,15 +264,19 @@ struct Row : RowData {
         }
         return all;
     }
-    __device__ __forceinline__ uint32_t max_key(uint32_t k) {
+    // The largest key of all CTAs, and the first of them that has it.
+    __device__ __forceinline__ uint32_t max_key(uint32_t k, int &owner) {
         k = __reduce_max_sync(kFull, k);
-        __syncthreads();  // (an earlier call's have been read)
         if (lane == 0) sh.warp_count[warp] = k;
         __syncthreads();
         k = __reduce_max_sync(kFull, lane < kSWarps ? sh.warp_count[lane] : 0u);
+        owner = 0;
         if (ctas == 1) return k;
         const u64 *all = exchange(k);
-        return __reduce_max_sync(kFull, lane < (int)ctas ? (uint32_t)all[lane] : 0u);
+        const uint32_t theirs = lane < (int)ctas ? (uint32_t)all[lane] : 0u;
+        k = __reduce_max_sync(kFull, theirs);
+        owner = __ffs(__ballot_sync(kFull, lane < (int)ctas && theirs == k)) - 1;
+        return k;
     }
 
     // The largest x of a thread's tokens in kGroups parts of them (-infinity: none).
@@ -347,7 +360,7 @@ struct Row : RowData {
     template <bool kSum, bool kCollect, bool kHist, bool kCut, typename C, typename H>
     __device__ __forceinline__ u64 pass(u64 least, float near, Cut cut, C collect, H hist) const {
         u64 sum = 0;
-        int k = begin;
+        int k;
         auto edge = [&](int tile) {
             float x[kWide];
             const int i0 = tokens(tile, x);
@@ -366,12 +379,21 @@ struct Row : RowData {
         };
         const int from = whole_from(), to = big < kFltMax ? whole_to() : from;  // (else x may be cut)
 #pragma unroll 1
-        for (; k < from; ++k) edge(k);
+        for (k = last - 1; k >= to; --k) edge(k);
+        // Backwards: the cache still has what was read last.  The next two tiles are on their way meanwhile.
+        Raw tile0, tile1;
+        if (k >= from) {
+            tile0 = load_inside(k);
+            tile1 = load_inside(max(k - 1, from));
+        }
 #pragma unroll 2
-        for (; k < to; ++k) {
+        for (; k >= from; --k) {
             Two x[kTwos];
             const int i0 = index_of(k);
-            plain_tokens(load_inside(k), i0, x);
+            const Raw now = tile0;
+            tile0 = tile1;
+            tile1 = load_inside(max(k - 2, from));
+            plain_tokens(now, i0, x);
             uint32_t hits = 0, low = 0;
 #pragma unroll
             for (int i = 0; i < kTwos; ++i) {
@@ -406,7 +428,7 @@ struct Row : RowData {
             }
         }
 #pragma unroll 1
-        for (; k < last; ++k) edge(k);
+        for (; k >= begin; --k) edge(k);
         return sum;
     }
     __device__ __forceinline__ Cut no_cut() const { return Cut{-INFINITY, ~0u}; }
@@ -496,6 +518,32 @@ struct Row : RowData {
         if (a.j.logprob) a.j.logprob[t] = -log1pf(__fdiv_rn((float)(Z - w), (float)w));
     }
     __device__ __forceinline__ u64 random_part(u64 Z) const { return __umul64hi(Z, (u64)a.j.random[t] << 32); }
+
+    // The lowest index of the largest x, in the first CTA that has it: all warps look at the tiles of the first warp that
+    // has it.
+    __device__ __forceinline__ void first_largest() const {
+        const int w = __ffs(__ballot_sync(kFull, lane < kSWarps && sh.warp_count[lane % kSWarps] == top)) - 1;
+        const int per = (last_of(w) - begin_of(w) + kSWarps - 1) / kSWarps;
+        const int from = min(last_of(w), begin_of(w) + warp * per), to = min(last_of(w), from + per);
+        uint32_t low = ~0u;
+        for (int k = from; k < to; ++k) {
+            float x[kWide];
+            const int i0 = tokens(k, x);
+#pragma unroll
+            for (int e = 0; e < kWide; ++e)
+                if (x[e] > -INFINITY && key_of(x[e]) == top) low = min(low, (uint32_t)(i0 + e));
+        }
+        low = __reduce_min_sync(kFull, low);
+        if (lane == 0) sh.warp[warp] = low;
+        __syncthreads();
+        if (warp == 0) {
+            low = __reduce_min_sync(kFull, lane < kSWarps ? (uint32_t)sh.warp[lane] : ~0u);
+            if (lane == 0) {
+                a.j.token[t] = (int)low;
+                if (a.j.logprob) a.j.logprob[t] = 0.0f;
+            }
+        }
+    }
 
     // The choice among the tokens that kept(x, index) gives a weight to, `sum` being that of this warp's.
     template <typename F>
@@ -834,18 +882,15 @@ struct Row : RowData {
             total = 0;
             for (uint32_t c = 0; c < ctas; ++c) total += sums[c];
         }
-        if (rank == 0 && n <= (uint32_t)kList) {
-            uint32_t at = mine;
-            for (uint32_t c = 1; c < ctas; ++c) {
-                const uint32_t theirs = (uint32_t)all[c];
-                for (uint32_t i = threadIdx.x; i < theirs; i += kSThreads) {
-                    sh.x[at + i] = __uint_as_float(peer_u32(reinterpret_cast<const uint32_t *>(&sh.x[i]), c));
-                    sh.index[at + i] = (int)peer_u32(reinterpret_cast<const uint32_t *>(&sh.index[i]), c);
-                }
-                at += theirs;
+        if (rank && n <= (uint32_t)kList) {
+            uint32_t at = 0;
+            for (uint32_t c = 0; c < rank; ++c) at += (uint32_t)all[c];
+            for (uint32_t i = threadIdx.x; i < mine; i += kSThreads) {
+                store_peer_u32(&sh.x[at + i], 0, __float_as_uint(sh.x[i]));
+                store_peer_u32(&sh.index[at + i], 0, (uint32_t)sh.index[i]);
             }
         }
-        clusters_meet();  // the lists have been read
+        clusters_meet();
         return n;
     }
 
@@ -1088,11 +1133,15 @@ struct Row : RowData {
             if (!again) {
                 if (rank == 0) {
                     const bool done = choose_from_list(*this, (int)n, top_k, top_p, least, total);
-                    if (threadIdx.x == 0) sh.general = !done;
+                    if (threadIdx.x < ctas) {
+                        if (ctas > 1)
+                            store_peer_u32(&sh.general, threadIdx.x, !done);
+                        else
+                            sh.general = !done;
+                    }
                 }
                 meet();
-                again = ctas > 1 ? peer_u32(&sh.general, 0) != 0 : sh.general != 0;
-                meet();
+                again = sh.general != 0;
             }
         }
         if (again) limits_in_all(*this, top_k, top_p, least);
@@ -1112,8 +1161,9 @@ __device__ void limits_in_all(RowData d, int top_k, float top_p, u64 least) {
     }
 }
 
-template <int kType>
-__global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__ SampleArgs a) {
+// kLimited: rows may have top-k or top-p.  Without them there is room for a third CTA an SM.
+template <int kType, bool kLimited>
+__global__ void __launch_bounds__(kSThreads, kLimited ? 2 : 3) k_sample(const __grid_constant__ SampleArgs a) {
     follow();
     extern __shared__ __align__(16) unsigned char s_mem[];
     SampleShared &sh = *reinterpret_cast<SampleShared *>(s_mem);
@@ -1158,7 +1208,8 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) key = max(key, key_of(g[i]));
     cluster_begun(r.ctas);
-    r.top = r.max_key(key);
+    int owner;
+    r.top = r.max_key(key, owner);
     const bool writes = threadIdx.x == 0 && r.rank == 0;
     if (r.top <= kNoKey) {
         if (writes) {
@@ -1168,22 +1219,13 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
         return;
     }
     r.big = of_key(r.top);
-    if (greedy) {  // the lowest index, as the largest of its complement
-        uint32_t low = 0;
-        if (__any_sync(kFull, key == r.top))
-            r.each([&](float x, int i) {
-                if (key_of(x) == r.top) low = max(low, ~(uint32_t)i);
-            });
-        low = ~r.max_key(low);
-        if (writes) {
-            j.token[r.t] = (int)low;
-            if (j.logprob) j.logprob[r.t] = 0.0f;
-        }
+    if (greedy) {
+        if ((int)r.rank == owner) r.first_largest();
         return;
     }
     const u64 least = (u64)part31(min_p) << 9;
     const bool by_k = top_k >= 1 && top_k < V;
-    if (by_k || top_p < 1.0f) {
+    if (kLimited && (by_k || top_p < 1.0f)) {
         r.limited(by_k ? top_k : 0, top_p, least, g);
         return;
     }
@@ -1194,12 +1236,19 @@ __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__
     });
 }
 
+template <int kType, bool kLimited>
+cudaError_t launch_limited(const SampleArgs &a, cudaStream_t s) {
+    const size_t smem = kLimited ? sizeof(SampleShared) : sizeof(SampleSmall);
+    const cudaError_t e = func_attr(reinterpret_cast<const void *>(k_sample<kType, kLimited>),
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch_cluster(k_sample<kType, kLimited>, dim3((unsigned)(a.j.T * a.ctas)), a.ctas, kSThreads, smem, s, a);
+}
 template <int kType>
 cudaError_t launch_type(const SampleArgs &a, cudaStream_t s) {
-    const cudaError_t e = func_attr(reinterpret_cast<const void *>(k_sample<kType>), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)sizeof(SampleShared));
-    if (e != cudaSuccess) return e;
-    return launch_cluster(k_sample<kType>, dim3((unsigned)(a.j.T * a.ctas)), a.ctas, kSThreads, sizeof(SampleShared), s, a);
+    const pvmvmd_sampling &how = a.j.how;
+    const bool by_k = how.top_k_dev || (how.top_k >= 1 && how.top_k < a.j.V), by_p = how.top_p_dev || how.top_p < 1.0f;
+    return by_k || by_p ? launch_limited<kType, true>(a, s) : launch_limited<kType, false>(a, s);
 }
 
 }  // namespace
