@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kSThreads = 512, kSWarps = kSThreads / 32;
 constexpr int kBins = 2048;
+
 constexpr int kList = 4096;      // tokens of the list
 constexpr int kMostK = 1024;     // a larger k (twice of it with several CTAs) is not looked for in a list
 constexpr int kMembers = 1024;   // of a bin at most that are compared with one another
@@ -158,9 +159,11 @@ struct Row : RowData {
         else
             __syncthreads();
     }
-    // This warp's tiles that lie in the row whole: from .. to - 1 (from <= to).
-    __device__ __forceinline__ int whole_from() const { return min(last, max(begin, (off + kTile - 1) / kTile)); }
-    __device__ __forceinline__ int whole_to() const { return max(whole_from(), min(last, end / kTile)); }
+    // Of tiles begin .. last - 1 those that lie in the row whole: from .. to - 1 (from <= to).
+    __device__ __forceinline__ int whole_from(int begin, int last) const { return min(last, max(begin, (off + kTile - 1) / kTile)); }
+    __device__ __forceinline__ int whole_to(int begin, int last) const {
+        return max(whole_from(begin, last), min(last, end / kTile));
+    }
     __device__ __forceinline__ Raw load_inside(int tile) const {
         Raw r;
         const char *p = base + (int64_t)(tile * kTile + lane * kWide) * (two_bytes(type) ? 2 : 4);
@@ -236,11 +239,11 @@ struct Row : RowData {
     }
     __device__ __forceinline__ int index_of(int tile) const { return tile * kTile + lane * kWide - off; }
 
-    // f(x, index) for every token of this warp's tiles that may be chosen
+    // f(x, index) for every token of tiles from .. to - 1 that may be chosen
     template <typename F>
-    __device__ __forceinline__ void each(F f) const {
+    __device__ __forceinline__ void each(int from, int to, F f) const {
 #pragma unroll 1
-        for (int k = begin; k < last; ++k) {
+        for (int k = from; k < to; ++k) {
             float x[kWide];
             const int i0 = tokens(k, x);
 #pragma unroll
@@ -290,7 +293,7 @@ struct Row : RowData {
 #pragma unroll
             for (int e = 0; e < kWide; ++e) g[e % kGroups] = fmaxf(g[e % kGroups], x[e]);
         };
-        const int from = whole_from(), to = whole_to();
+        const int from = whole_from(begin, last), to = whole_to(begin, last);
         for (; k < from; ++k) edge(k);
         if (m > 0.0f && !allowed && !a.j.logits.channel_scale_dev) {
             // rounding keeps the order, so that the largest logit has the largest x
@@ -350,15 +353,16 @@ struct Row : RowData {
         for (; k < last; ++k) edge(k);
     }
 
-    // One pass over the warp's tiles: the sum, where asked for, of the weights that are at least `least` (and with kCut of
+    // One pass over tiles begin .. last - 1: the sum, where asked for, of the weights that are at least `least` (and with kCut of
     // tokens up to a cut); collect(x, index) for the tokens whose distance is below `near`; hist(d, w) for all of some weight.
     struct Cut {
         float x;
         uint32_t index;
         __device__ __forceinline__ bool keeps(float v, int i) const { return v > x || (v == x && (uint32_t)i <= index); }
     };
-    template <bool kSum, bool kCollect, bool kHist, bool kCut, typename C, typename H>
-    __device__ __forceinline__ u64 pass(u64 least, float near, Cut cut, C collect, H hist) const {
+    // kLeast: `least` may be above 0.
+    template <bool kSum, bool kCollect, bool kHist, bool kCut, bool kLeast, typename C, typename H>
+    __device__ __forceinline__ u64 pass(int begin, int last, u64 least, float near, Cut cut, C collect, H hist) const {
         u64 sum = 0;
         int k;
         auto edge = [&](int tile) {
@@ -377,7 +381,7 @@ struct Row : RowData {
                 }
             }
         };
-        const int from = whole_from(), to = big < kFltMax ? whole_to() : from;  // (else x may be cut)
+        const int from = whole_from(begin, last), to = big < kFltMax ? whole_to(begin, last) : from;  // (else x may be cut)
 #pragma unroll 1
         for (k = last - 1; k >= to; --k) edge(k);
         // Backwards: the cache still has what was read last.  The next two tiles are on their way meanwhile.
@@ -408,12 +412,14 @@ struct Row : RowData {
                         uint32_t p = (uint32_t)(h ? r.v >> 32 : r.v) & 0x7fffffu;
                         const uint32_t q = (uint32_t)(h ? n.v >> 32 : n.v);
                         if (kCut && !cut.keeps(h ? second(x[i]) : first(x[i]), i0 + 2 * i + h)) p = 0;
-                        if (kHist) {
-                            hist(h ? second(d) : first(d), ((u64)p << 18) >> (q - 0x4b400000u));
-                        } else if (least) {
+                        if (kHist || kLeast) {
                             const u64 w = ((u64)p << 18) >> (q - 0x4b400000u);
-                            sum += w >= least ? w : 0ull;
-                        } else {  // p 2^(18 - n) for n < 18; the others are below 2^23
+                            if (kHist)
+                                hist(h ? second(d) : first(d), w);
+                            else
+                                sum += w >= least ? w : 0ull;
+                        } else {
+                            // p 2^(18 - n) for n < 18, a product that is added in one instruction; the others are below 2^23
                             sum += (u64)p * shift_left(2u, 0x4b400000u + 17u - q);
                             low += shift_right(p, q - (0x4b400000u + 18u));
                         }
@@ -473,7 +479,7 @@ struct Row : RowData {
             if (threadIdx.x == 0) sh.found = ~0u;
             __syncthreads();
             const uint32_t high = v;
-            each([&](float x, int i) {
+            each(begin, last, [&](float x, int i) {
                 uint32_t value;
                 u64 w;
                 if (f(x, i, value, w) && ((u64)value >> left) == ((u64)high >> left) && w)
@@ -545,14 +551,20 @@ struct Row : RowData {
         }
     }
 
-    // The choice among the tokens that kept(x, index) gives a weight to, `sum` being that of this warp's.
-    template <typename F>
-    __device__ __forceinline__ void choose_in_order(u64 sum, F kept) {
+    // The choice among the tokens that kept(x, index) gives a weight to; sum_of_tiles(begin, last): what those of a warp's
+    // tiles weigh.
+    template <typename F, typename G>
+    __device__ __forceinline__ void choose_in_order(F kept, G sum_of_tiles) {
+        auto warp_sum = [&](int from, int to) {
+            u64 sum = sum_of_tiles(from, to);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-        __syncthreads();
-        if (lane == 0) sh.warp[warp] = sum;
-        __syncthreads();
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+            __syncthreads();  // (earlier ones have been read)
+            if (lane == 0) sh.warp[warp] = sum;
+            __syncthreads();
+            return sum;
+        };
+        warp_sum(begin, last);
         u64 mine = 0, front = 0, Z = 0;  // of this CTA; of the CTAs in front; of all
 #pragma unroll
         for (int k = 0; k < kSWarps; ++k) mine += sh.warp[k];
@@ -575,34 +587,16 @@ struct Row : RowData {
         }
         const int per = (last_of(owner) - begin_of(owner) + kSWarps - 1) / kSWarps;
         const int from = min(last_of(owner), begin_of(owner) + warp * per), to = min(last_of(owner), from + per);
-        auto weights = [&](int k, u64 (&w)[kWide]) {
-            float x[kWide];
-            const int i0 = tokens(k, x);
-#pragma unroll
-            for (int e = 0; e < kWide; ++e) w[e] = x[e] > -INFINITY ? kept(x[e], i0 + e) : 0ull;
-            return i0;
-        };
-        u64 part = 0;
-#pragma unroll 1
-        for (int k = from; k < to; ++k) {
-            u64 w[kWide];
-            weights(k, w);
-#pragma unroll
-            for (int e = 0; e < kWide; ++e) part += w[e];
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(kFull, part, o);
-        __syncthreads();
-        if (lane == 0) sh.warp[warp] = part;
-        __syncthreads();
+        const u64 part = warp_sum(from, to);
         for (int k = 0; k < warp; ++k) front += sh.warp[k];
         if (at < front || at >= front + part) return;
 #pragma unroll 1
         for (int k = from; k < to; ++k) {
+            float x[kWide];
             u64 w[kWide], all = 0;
-            const int i0 = weights(k, w);
+            const int i0 = tokens(k, x);
 #pragma unroll
-            for (int e = 0; e < kWide; ++e) all += w[e];
+            for (int e = 0; e < kWide; ++e) all += w[e] = x[e] > -INFINITY ? kept(x[e], i0 + e) : 0ull;
             u64 pre = all;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -676,9 +670,11 @@ struct Row : RowData {
             const u64 w = weight(big, x);
             return (v < cut || (v == cut && (uint32_t)i <= cut_index)) && w >= least ? w : 0ull;
         };
-        u64 sum = 0;
-        each([&](float x, int i) { sum += kept(x, i); });
-        choose_in_order(sum, kept);
+        choose_in_order(kept, [&](int from, int to) {
+            u64 sum = 0;
+            each(from, to, [&](float x, int i) { sum += kept(x, i); });
+            return sum;
+        });
     }
 
     // ------------------------------------------------------------ the list
@@ -859,7 +855,7 @@ struct Row : RowData {
                 sh.index[p] = i;
             }
         };
-        total = pass<kSum, true, false, false>(0, __uint_as_float(range.to), no_cut(), collect, [](float, u64) {});
+        total = pass<kSum, true, false, false, false>(begin, last, 0, __uint_as_float(range.to), no_cut(), collect, [](float, u64) {});
         if (kSum) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
@@ -969,7 +965,7 @@ struct Row : RowData {
                                               uint32_t (&count)[kMine], uint32_t &pre_count, uint32_t &number) {
         for (int i = threadIdx.x; i < kBins; i += kSThreads) sh.low[i] = sh.high[i] = sh.counts[i] = 0;
         __syncthreads();
-        pass<false, false, true, false>(0, 0.0f, no_cut(), [](float, int) {}, [&](float d, u64 w) {
+        pass<false, false, true, false, false>(begin, last, 0, 0.0f, no_cut(), [](float, int) {}, [&](float d, u64 w) {
             const uint32_t bits = __float_as_uint(d);
             if (w && bits >= range.from && bits < range.to) {
                 const int b = bin(d, bits);
@@ -1087,11 +1083,14 @@ struct Row : RowData {
         }
         exchanges = 0;
         meet();
-        const u64 sum = pass<true, false, false, true>(least, 0.0f, cut, [](float, int) {}, [](float, u64) {});
-        choose_in_order(sum, [&](float x, int i) {
-            const u64 w = cut.keeps(x, i) ? weight(big, x) : 0ull;
-            return w >= least ? w : 0ull;
-        });
+        choose_in_order(
+            [&](float x, int i) {
+                const u64 w = cut.keeps(x, i) ? weight(big, x) : 0ull;
+                return w >= least ? w : 0ull;
+            },
+            [&](int from, int to) {
+                return pass<true, false, false, true, true>(from, to, least, 0.0f, cut, [](float, int) {}, [](float, u64) {});
+            });
         return true;
     }
 
@@ -1163,7 +1162,7 @@ __device__ void limits_in_all(RowData d, int top_k, float top_p, u64 least) {
 
 // kLimited: rows may have top-k or top-p.  Without them there is room for a third CTA an SM.
 template <int kType, bool kLimited>
-__global__ void __launch_bounds__(kSThreads, kLimited ? 2 : 3) k_sample(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__ SampleArgs a) {
     follow();
     extern __shared__ __align__(16) unsigned char s_mem[];
     SampleShared &sh = *reinterpret_cast<SampleShared *>(s_mem);
@@ -1229,10 +1228,15 @@ __global__ void __launch_bounds__(kSThreads, kLimited ? 2 : 3) k_sample(const __
         r.limited(by_k ? top_k : 0, top_p, least, g);
         return;
     }
-    const u64 sum = r.template pass<true, false, false, false>(least, 0.0f, r.no_cut(), [](float, int) {}, [](float, u64) {});
-    r.choose_in_order(sum, [&](float x, int) {
+    auto none = [](float, int) {};
+    auto no_bin = [](float, u64) {};
+    auto kept = [&](float x, int) {
         const u64 w = weight(r.big, x);
         return w >= least ? w : 0ull;
+    };
+    r.choose_in_order(kept, [&](int from, int to) {
+        return least ? r.template pass<true, false, false, false, true>(from, to, least, 0.0f, r.no_cut(), none, no_bin)
+                     : r.template pass<true, false, false, false, false>(from, to, 0, 0.0f, r.no_cut(), none, no_bin);
     });
 }
 
