@@ -209,16 +209,16 @@ def test_block_norm_of_nothing_and_of_what_is_not_finite(pv):
 
 
 @pytest.mark.gpu
-def test_large_values_keep_their_norm(pv):
-    """Squares far above and below what 16 bits hold."""
+def test_norm_of_large_and_small_values(pv):
+    """Squares far above and below what 16 bits hold: the definition's values.  (An eps of 2^-126 is 2^-26 of the mean of
+    squares of 2^-100, and moves the inverse root by 2^-27 of itself: norms of a row and of the row times 2^-50 need not
+    be the same.)"""
     import torch
-    for gain in (2.0**50, 2.0**-50):
-        x = torch.randn(3, 3000, device="cuda")
-        z, big = torch.empty_like(x), torch.empty_like(x)
-        n = pv.Norm("rms", eps=1e-38)
-        pv.pvmvmd_block_norm(None, x, residual_out=False, pre=n, out=z)
-        pv.pvmvmd_block_norm(None, x * gain, residual_out=False, pre=n, out=big)
-        assert torch.equal(z, big)
+    x = np.random.default_rng(12).standard_normal((3, 3000)).astype(np.float32)
+    for gain in (1, 2.0**50, 2.0**-50):
+        z = torch.empty(3, 3000, device="cuda")
+        pv.pvmvmd_block_norm(None, _dev(x * np.float32(gain)), residual_out=False, pre=pv.Norm("rms", eps=1e-38), out=z)
+        assert np.array_equal(_host(z), plain.norm(x * np.float32(gain), "rms", eps=1e-38))
 
 
 # ---------------------------------------------------------------- gated activation
