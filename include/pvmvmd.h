@@ -527,8 +527,8 @@ int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, in
  * Conventions, besides those at the top of this file and of the client's attention
  * (types, structs read during the call):
  *  - Tensors are T rows (tokens) of D values, contiguous in a row; `token` is the
- *    stride between rows in elements.  Rows have any alignment; those on 16-byte
- *    boundaries are read and written 16 bytes at a time.
+ *    stride between rows in elements.  Addresses are those of whole values (PVMVMD_E_ARG
+ *    otherwise); rows on 16-byte boundaries are read and written 16 bytes at a time.
  *  - An output may be one of the call's inputs of the same address, row stride and
  *    type size, and must not overlap them otherwise.
  *  - T = 0 does nothing.  The calls use no scratch, so that any number of them may run at

@@ -21,15 +21,18 @@ bool float_type(int t) { return t == PVMVMD_BF16 || t == PVMVMD_F16 || t == PVMV
 bool any_type(int t) { return float_type(t) || t == PVMVMD_FIELD; }
 int size_of(int t) { return t == PVMVMD_BF16 || t == PVMVMD_F16 ? 2 : 4; }
 
+bool misaligned(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % size != 0; }
+
 // T rows of D values: addresses of whole values
 int check(const pvmvmd_rows &r, bool field = true) {
     if (!r.data_dev || !(field ? any_type(r.type) : float_type(r.type))) return PVMVMD_E_ARG;
-    if (reinterpret_cast<uintptr_t>(r.data_dev) % size_of(r.type)) return PVMVMD_E_ARG;
+    if (misaligned(r.data_dev, size_of(r.type)) || misaligned(r.token_scale_dev, 4) || misaligned(r.channel_scale_dev, 4))
+        return PVMVMD_E_ARG;
     return std::isfinite(r.scale) ? PVMVMD_OK : PVMVMD_E_PARAM;
 }
 int check(const pvmvmd_rows_out &o, bool field = true) {
     if (!o.data_dev || !(field ? any_type(o.type) : float_type(o.type))) return PVMVMD_E_ARG;
-    if (reinterpret_cast<uintptr_t>(o.data_dev) % size_of(o.type)) return PVMVMD_E_ARG;
+    if (misaligned(o.data_dev, size_of(o.type)) || misaligned(o.token_scale_dev, 4)) return PVMVMD_E_ARG;
     if (o.type != PVMVMD_FIELD) return o.token_scale_dev ? PVMVMD_E_ARG : PVMVMD_OK;
     if (o.limit < 1 || o.limit > 1 << 22) return PVMVMD_E_PARAM;
     return o.token_scale_dev || std::isfinite(o.scale) ? PVMVMD_OK : PVMVMD_E_PARAM;
@@ -37,6 +40,7 @@ int check(const pvmvmd_rows_out &o, bool field = true) {
 int check(const pvmvmd_norm &n) {
     if (n.kind != PVMVMD_NORM_RMS && n.kind != PVMVMD_NORM_LAYER) return PVMVMD_E_ARG;
     if ((n.weight_dev || n.bias_dev) && !float_type(n.type)) return PVMVMD_E_ARG;
+    if (misaligned(n.weight_dev, size_of(n.type)) || misaligned(n.bias_dev, size_of(n.type))) return PVMVMD_E_ARG;
     if (!(n.eps > 0) || !std::isfinite(n.eps) || !std::isfinite(n.weight_add)) return PVMVMD_E_PARAM;
     return PVMVMD_OK;
 }
@@ -107,6 +111,11 @@ int pvmvmd_sample(int T, int V, const pvmvmd_rows *logits, const pvmvmd_sampling
     const int st = check(*logits);
     if (st) return st;
     if (!random_dev || !token_dev) return PVMVMD_E_ARG;
+    for (const void *p : {static_cast<const void *>(random_dev), static_cast<const void *>(token_dev),
+                          static_cast<const void *>(logprob_dev), static_cast<const void *>(allowed_dev),
+                          static_cast<const void *>(sampling->temperature_dev), static_cast<const void *>(sampling->top_k_dev),
+                          static_cast<const void *>(sampling->top_p_dev), static_cast<const void *>(sampling->min_p_dev)})
+        if (misaligned(p, 4)) return PVMVMD_E_ARG;
     SampleJob j{};
     j.T = T;
     j.V = V;

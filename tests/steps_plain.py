@@ -155,6 +155,28 @@ def sample(x, temperature, top_k, top_p, min_p, word):
     raise AssertionError("the whole is more than a part of it")
 
 
+def sample_long(x, temperature, top_k, top_p, min_p, word):
+    """The same for many tokens, whose sums fit 62 bits: numpy's sorts and sums of whole numbers of 64 bits."""
+    with np.errstate(all="ignore"):
+        d = np.fmin(x.max() - x, F(63))
+    n = np.rint(d)
+    w = (np.rint(poly((d - n).astype(F)) * F(4194304)).astype(np.int64) << 18) >> n.astype(np.int64)
+    keep = w >= (int(float(F(min(max(min_p, 0), 1))) * 2**31) << 9)
+    if 0 < top_k < len(x) or top_p < 1:
+        order = np.lexsort((np.arange(len(x)), -x.astype(np.float64)))
+        last = top_k if 0 < top_k < len(x) else len(x)
+        run = np.cumsum(w[order[:last]])
+        if top_p < 1:
+            part = int(run[-1]) * int(float(F(top_p)) * 2**31) >> 31
+            last = max(1, int(np.searchsorted(run, part, side="left")) + 1)
+        limits = np.zeros(len(x), bool)
+        limits[order[:last]] = True
+        keep &= limits
+    run = np.cumsum(np.where(keep, w, 0))
+    i = int(np.searchsorted(run, int(run[-1]) * (int(word) & 0xFFFFFFFF) >> 32, side="right"))
+    return i, float(np.log(int(w[i]) / int(run[-1])))
+
+
 def multiplier(scale, token_scale, temperature):
     with np.errstate(all="ignore"):
         m = F(scale) if token_scale is None else F(scale) * F(token_scale)

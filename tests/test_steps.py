@@ -125,6 +125,8 @@ NORMS = [
     dict(T=160, D=8192, post="rms", scale=1e6, limit=1 << 22),
     dict(T=1, D=16384, post="rms", pre="layer", w=None, add=0.5),
     dict(T=153, D=16392, dynamic=True, limit=1),
+    dict(T=2, D=2048, dynamic=True, limit=1 << 22),
+    dict(T=160, D=2560, y="bf16", out="bf16", gate="tokens", post="rms"),
     dict(T=2, D=40000, y="bf16", out="f16", gate="row", dynamic=False),
     dict(T=153, D=40008, res="f16", dynamic=True, post="layer"),
     dict(T=1, D=131071, dynamic=True, post="rms"),
@@ -290,6 +292,53 @@ def test_glu_at_the_ends_of_its_range(pv, act):
     assert (np.abs(got - true) <= np.abs(true) * E * (15 + 8 * 90) + 2.0**-115).all()
 
 
+def _silu_or_gelu(x, act):
+    """The definition on the device: each operation is a kernel of its own, and rounds by itself."""
+    import math
+    import torch
+    l = 1.4426950408889634
+    c = 2 * math.sqrt(2 / math.pi) * l
+    d = (x * x * (0.044715 * c) + c) * x if act == "gelu" else x * l
+    d = torch.clamp(d, -128.0, 125.0)
+    n = torch.round(d)
+    f = d - n
+    p = f * float(plain.COEF[0]) + float(plain.COEF[1])
+    for k in plain.COEF[2:]:
+        p = p * f + float(k)
+    p = p * f + 1.0
+    return x / (1.0 + (p.view(torch.int32) - (n.nan_to_num().to(torch.int32) << 23)).view(torch.float32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_quotients_of_all_numbers(pv, act):
+    """Every number of 32 bits: the quotient by the inverse is the quotient of two numbers, rounded once."""
+    import torch
+    T, D = 1024, 32768
+    out = torch.empty(T, D, device="cuda")
+    for k in range(2**32 // (T * D)):
+        bits = torch.arange(k * T * D, (k + 1) * T * D, device="cuda", dtype=torch.int64)
+        x = torch.where(bits >= 2**31, bits - 2**32, bits).to(torch.int32).view(torch.float32).view(T, D)
+        pv.pvmvmd_glu(x, act=act, out=out)
+        want = _silu_or_gelu(x, act)
+        assert bool(((out == want) | (out.isnan() & want.isnan())).all()), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,D", [(3, 700), (2, 12000), (160, 12000), (200, 512)])
+def test_glu_in_place(pv, T, D):
+    """out is gate, or up, and the step a token's scale that is replaced."""
+    import torch
+    g, u = (torch.randint(-30000, 30000, (T, D), device="cuda").remainder(plain.Q).to(torch.int32) for _ in range(2))
+    ts = torch.rand(T, device="cuda") + 0.5
+    for which in (0, 1):
+        a, b, s = g.clone(), u.clone(), ts.clone()
+        step = torch.empty(T, device="cuda")
+        want = pv.pvmvmd_glu(pv.Rows(a, 1e-4, s), pv.Rows(b, 1e-4, s), out_token_scale=step)
+        pv.pvmvmd_glu(pv.Rows(a, 1e-4, s), pv.Rows(b, 1e-4, s), out=(a, b)[which], out_token_scale=s)
+        assert torch.equal((a, b)[which], want) and torch.equal(s, step) and torch.equal((b, a)[which], (u, g)[which])
+
+
 def test_power_of_two_within_its_bound():
     """E of the header against 64 bits: 2^-22.3, at a million places and next to the halves where n changes."""
     d = np.concatenate([np.linspace(-127, 125, 1 << 20), np.arange(-126.5, 125, 1)]).astype(np.float32)
@@ -430,6 +479,51 @@ def test_sample_allowed_tokens_and_values_that_are_not_finite(pv):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [131073, 1 << 22])
+def test_sample_of_large_vocabularies(pv, V, kind):
+    """Up to the largest one, and rows of all equal logits, whose weights come to 2^62."""
+    import torch
+    rng = np.random.default_rng(V % 1000)
+    l = (rng.standard_normal((3, V)) * 1.5).astype(np.float32)
+    l[1] = 0.25
+    l[2, rng.integers(0, V, 60)] += 12
+    x = _dev(l, kind)
+    h = _host(x)
+    words = np.array([2**32 - 1, 2**31 + 12345, 77777777], np.uint32)
+    for t, k, p, m in ((0.8, 0, 1.0, 0.0), (0.8, 40, 0.9, 0.0), (1.0, 0, 0.7, 0.0), (0.7, 100000, 0.95, 0.0), (0.9, 0, 1.0, 0.3),
+                       (3.0, 70001, 1.0, 0.001)):
+        lp = torch.empty(3, device="cuda")
+        tok = pv.pvmvmd_sample(x, torch.from_numpy(words.view(np.int32)).cuda().view(torch.uint32), pv.Sampling(t, k, p, m),
+                               logprob=lp)
+        for r in range(3):
+            want, wlp = plain.sample_long(plain.distances(h[r], plain.multiplier(1.0, None, t)), t, k, p, m, words[r])
+            assert int(tok[r]) == want, (r, t, k, p, m)
+            assert abs(float(lp[r]) - wlp) <= 4 * E * (1 + abs(wlp))
+
+
+@pytest.mark.gpu
+def test_rows_far_apart(pv):
+    """Rows further apart than 2^31 elements."""
+    import torch
+    V, far = 5000, 2**31 + 64
+    flat = torch.empty(far + V, dtype=torch.bfloat16, device="cuda")
+    x = flat.as_strided((2, V), (far, 1))
+    x.copy_(torch.randn(2, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)))
+    near = x.clone()
+    word, how = torch.tensor([123456789, -5], dtype=torch.int32, device="cuda"), pv.Sampling(0.9, 200, 0.9)
+    assert torch.equal(pv.pvmvmd_sample(x, word, how), pv.pvmvmd_sample(near, word, how))
+    n = pv.Norm("layer", eps=1e-5)
+    a = pv.pvmvmd_block_norm(near, near, pre=n, out=torch.empty_like(near))
+    b = pv.pvmvmd_block_norm(x, x, residual_out=x, pre=n, out=torch.empty_like(near))
+    assert torch.equal(a[0], x) and torch.equal(a[1], b[1])
+    z = pv.pvmvmd_glu(near, near, out=torch.empty_like(near))
+    x.copy_(near)
+    pv.pvmvmd_glu(x, x, out=x)
+    assert torch.equal(z, x)
+
+
+@pytest.mark.gpu
 def test_sample_frequencies(pv):
     """Random words in even steps draw each token as often as its probability says, to one draw of 4096 and what the
     weights' 22 bits are off."""
@@ -542,6 +636,8 @@ def test_steps_refuse_bad_arguments_before_device_use(pv):
     assert norm(out=O(token_scale_dev=64, **F32)) == ARG
     assert norm(out=O(limit=0)) == norm(out=O(limit=(1 << 22) + 1)) == norm(out=O(scale=inf)) == PARAM
     assert norm(pre=N(kind=3)) == norm(post=N(kind=0)) == norm(pre=N(weight_dev=64, type=4)) == ARG
+    assert norm(y=R(token_scale_dev=66)) == norm(y=R(channel_scale_dev=65)) == norm(pre=N(weight_dev=66)) == ARG
+    assert norm(out=O(token_scale_dev=70)) == ARG
     assert norm(pre=N(eps=0.0)) == norm(pre=N(eps=float("nan"))) == norm(post=N(weight_add=inf)) == PARAM
     assert norm(branch=inf) == norm(keep=float("nan")) == norm(y=R(scale=inf)) == PARAM
 
@@ -559,6 +655,7 @@ def test_steps_refuse_bad_arguments_before_device_use(pv):
     assert sample(T=0) == pv.PVMVMD_OK
     assert sample(T=-1) == sample(V=0) == sample(V=pv.PVMVMD_MAX_V + 1) == SHAPE
     assert sample(l=None) == sample(how=None) == sample(random=None) == sample(token=None) == ARG
+    assert sample(random=66) == sample(token=65) == sample(how=pv.pvmvmd_sampling(top_k_dev=2)) == ARG
     assert sample(l=R(type=7)) == sample(l=R(data_dev=None)) == ARG and sample(l=R(scale=inf)) == PARAM
 
 
