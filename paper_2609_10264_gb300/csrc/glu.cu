@@ -124,27 +124,30 @@ __global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 ? 1 : 2) k_glu(c
 }
 
 // One CTA a row, for rows that are too long for the registers of one: the values wait in shared memory
-// for the largest of them.  (4096 x 28672 field elements to integers 308 us, 343 with the row in the
-// registers of a cluster of 8; 14336 values a row 157 and 171.)
-constexpr int kLongThreads = 512, kLongMost = 57344;
+// for the largest of them.  (4096 x 28672 field elements to integers 296 us, 343 with the row in the
+// registers of a cluster of 8; 14336 values a row 144 and 171.)  Raw values of 32 bits take so many registers
+// that 512 threads, of 64 each, spill: 308 us and 157.  Those of 16 bits do not: 241 us with 512 threads, 265 with 448.
+constexpr int kLongMost = 57344;
 template <int kX>
-__global__ void __launch_bounds__(kLongThreads, 2) k_glu_long(const __grid_constant__ GluArgs a) {
+constexpr int kLongThreads = kX == kField ? 448 : 512;
+template <int kX>
+__global__ void __launch_bounds__(kLongThreads<kX>, 2) k_glu_long(const __grid_constant__ GluArgs a) {
     follow();
     const GluJob &j = a.j;
-    extern __shared__ __align__(16) float4 s_z[];  // of chunk c and half h at (2 c + h) kLongThreads + thread
+    extern __shared__ __align__(16) float4 s_z[];  // of chunk c and half h at (2 c + h) kThreads + thread
     __shared__ RowShared sh;
     RowThreads r = row_threads(&sh, a.d);
     const int64_t t = r.t;
     const int gt = known<kX>(j.gate.type), ut = known<kX>(j.up.type);
     const void *g_row = row_of(j.gate, gt, t), *u_row = row_of(j.up, ut, t);
     const float gc = row_scale(j.gate, t), uc = j.has_up ? row_scale(j.up, t) : 0.0f;
-    constexpr int kStride = kLongThreads * kWide;
+    constexpr int kThreads = kLongThreads<kX>, kStride = kThreads * kWide;
     Place<true> p{(int)threadIdx.x * kWide, j.D};
     Raw g = load_raw<true>(g_row, gt, p), u = g;
     if (j.has_up) u = load_raw<true>(u_row, ut, p);
     float big = 0.0f;
     float4 *z = s_z + threadIdx.x;
-    for (; p.any(); p.at += kStride, z += 2 * kLongThreads) {
+    for (; p.any(); p.at += kStride, z += 2 * kThreads) {
         const Raw g0 = g, u0 = u;
         const Place<true> next{p.at + kStride, p.D};
         g = load_raw<true>(g_row, gt, next);
@@ -161,27 +164,27 @@ __global__ void __launch_bounds__(kLongThreads, 2) k_glu_long(const __grid_const
 #pragma unroll
         for (int i = 0; i < kTwos; ++i) big = larger(larger(big, first(x[i])), second(x[i]));
         z[0] = make_float4(first(x[0]), second(x[0]), first(x[1]), second(x[1]));
-        z[kLongThreads] = make_float4(first(x[2]), second(x[2]), first(x[3]), second(x[3]));
+        z[kThreads] = make_float4(first(x[2]), second(x[2]), first(x[3]), second(x[3]));
     }
     big = row_max(r, big);
     const Step m = step_of(j.out, big);
     if (threadIdx.x == 0) write_step(j.out, t, big);
     z = s_z + threadIdx.x;
-    for (p.at = (int)threadIdx.x * kWide; p.any(); p.at += kStride, z += 2 * kLongThreads) {
-        const float4 lo = z[0], hi = z[kLongThreads];
+    for (p.at = (int)threadIdx.x * kWide; p.any(); p.at += kStride, z += 2 * kThreads) {
+        const float4 lo = z[0], hi = z[kThreads];
         const Two x[kTwos] = {two(lo.x, lo.y), two(lo.z, lo.w), two(hi.x, hi.y), two(hi.z, hi.w)};
         write<true>(j.out, PVMVMD_FIELD, t, p, x, m);
     }
 }
 template <int kX>
 cudaError_t launch_long(GluArgs a, cudaStream_t s) {
-    a.d = RowDeal{kLongThreads, 1, 0, 1, true};
-    const int chunks = (a.j.D + kLongThreads * kWide - 1) / (kLongThreads * kWide);
-    const size_t smem = (size_t)chunks * kLongThreads * kWide * sizeof(float);
+    constexpr int kStride = kLongThreads<kX> * kWide;
+    a.d = RowDeal{kLongThreads<kX>, 1, 0, 1, true};
+    const size_t smem = (size_t)((a.j.D + kStride - 1) / kStride) * kStride * sizeof(float);
     const cudaError_t e = func_attr(reinterpret_cast<const void *>(k_glu_long<kX>), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     kLongMost * (int)sizeof(float));
     if (e != cudaSuccess) return e;
-    return launch_dependent(k_glu_long<kX>, grid_of(a.d, a.j.T), kLongThreads, smem, s, a);
+    return launch_dependent(k_glu_long<kX>, grid_of(a.d, a.j.T), kLongThreads<kX>, smem, s, a);
 }
 
 template <bool kVec, int kX, int kO>
