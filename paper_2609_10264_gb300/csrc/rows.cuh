@@ -461,7 +461,11 @@ inline RowDeal deal_rows(int T, int D, bool joint) {
         d.threads = 32 * d.rows;
         return d;
     }
-    d.chunks = T >= sms ? 2 : 1;
+    d.chunks = T > 100 ? 2 : 1;
+    // Few rows: CTAs of about four warps, as many as two an SM, since each waits for its own loads alone (one row of 8192
+    // between two norms 5.2 us with a cluster of 2, 4.1 with one of 8; 64 rows 5.5 and, with 4, 5.1).
+    if (d.chunks == 1)
+        while (tiles > 4 << d.log_ctas && d.log_ctas < 3 && (T << (d.log_ctas + 1)) <= 2 * sms) ++d.log_ctas;
     // CTAs of 8 warps where they need not wait for one another, else as few as there can be
     while (tiles > (joint ? most : 8) * d.chunks << d.log_ctas && (d.log_ctas < 3 || !joint)) ++d.log_ctas;
     while (tiles > most * d.chunks << d.log_ctas) d.chunks *= 2;
