@@ -271,68 +271,71 @@ typedef struct {
     int64_t T;
 } SamplingView;
 
-/* T x D values with contiguous rows, of which `one` says whether a single row (or D values) may stand for all. */
-static int matrix(PyObject *t, const char *name, int64_t T, int64_t D, int one, void **p, int64_t *token) {
-    int64_t d[2], s[2];
+/* T x D values with contiguous rows, of which `one` says whether a single row (or D values) may stand for all.  Where *T is
+ * negative, T and D are the tensor's. */
+static int matrix(PyObject *t, const char *name, int64_t *T, int64_t *D, int one, void **p, int64_t *token) {
+    int64_t d[2] = {1, 0}, s[2] = {0, 0};
     if (!on_device(t, name)) return 0;
     PyObject *shape = PyObject_GetAttr(t, s_shape);
-    const int flat = one && shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 1;
-    Py_XDECREF(shape);
     if (!shape) return 0;
-    if (flat) {
-        if (!dims(t, name, 1, d + 1) || !numbers(PyObject_CallMethodNoArgs(t, s_stride), 1, s + 1)) return 0;
-        d[0] = 1;
-        s[0] = 0;
-    } else if (!dims(t, name, 2, d) || !numbers(PyObject_CallMethodNoArgs(t, s_stride), 2, s)) {
+    const Py_ssize_t n = PyTuple_Check(shape) ? PyTuple_GET_SIZE(shape) : 0;
+    if (n != 2 && !(one && n == 1)) {
+        Py_DECREF(shape);
+        PyErr_Format(PyExc_ValueError, "%s must have 2 dimensions", name);
         return 0;
     }
-    if (d[1] != D || (d[0] != T && !(one && d[0] == 1))) {
-        PyErr_Format(PyExc_ValueError, "%s must be %lld x %lld, got %lld x %lld", name, (long long)T, (long long)D,
+    if (!numbers(shape, (int)n, d + 2 - n) || !numbers(PyObject_CallMethodNoArgs(t, s_stride), (int)n, s + 2 - n)) return 0;
+    if (*T < 0) {
+        *T = d[0];
+        *D = d[1];
+    }
+    if (d[1] != *D || (d[0] != *T && !(one && d[0] == 1))) {
+        PyErr_Format(PyExc_ValueError, "%s must be %lld x %lld, got %lld x %lld", name, (long long)*T, (long long)*D,
                      (long long)d[0], (long long)d[1]);
         return 0;
     }
-    if (s[1] != 1 && D > 1) {
+    if (s[1] != 1 && *D > 1) {
         PyErr_Format(PyExc_ValueError, "the last dimension of %s must be contiguous", name);
         return 0;
     }
-    *token = d[0] == 1 && T != 1 ? 0 : s[0];
+    *token = d[0] == 1 && *T != 1 ? 0 : s[0];
     return to_ptr(t, p);
 }
 /* The tensor of a Rows (a tuple: data, scale, token_scale, channel_scale), or the tensor itself. */
 static PyObject *data_of(PyObject *o) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4 ? PyTuple_GET_ITEM(o, 0) : o; }
-static int rows_in(PyObject *o, const char *name, int64_t T, int64_t D, int one, pvmvmd_rows *r) {
+static int rows_in(PyObject *o, const char *name, int64_t *d, int one, pvmvmd_rows *r) {
     PyObject *data = data_of(o), *type;
     void *p;
     memset(r, 0, sizeof(*r));
     r->scale = 1.0f;
-    if (!matrix(data, name, T, D, one, &p, &r->token) || !type_code(data, name, 1, &r->type, &type)) return 0;
+    if (!matrix(data, name, d, d + 1, one, &p, &r->token) || !type_code(data, name, 1, &r->type, &type)) return 0;
     r->data_dev = p;
     if (data == o) return 1;
     PyObject *scale = PyTuple_GET_ITEM(o, 1), *token = PyTuple_GET_ITEM(o, 2), *channel = PyTuple_GET_ITEM(o, 3);
     r->scale = (float)PyFloat_AsDouble(scale);
     if (PyErr_Occurred()) return 0;
     if (token != Py_None) {
-        if (!vector(token, "token_scale", T, t_float[2], &p)) return 0;
+        if (!vector(token, "token_scale", d[0], t_float[2], &p)) return 0;
         r->token_scale_dev = p;
     }
     if (channel != Py_None) {
-        if (!vector(channel, "channel_scale", D, t_float[2], &p)) return 0;
+        if (!vector(channel, "channel_scale", d[1], t_float[2], &p)) return 0;
         r->channel_scale_dev = p;
     }
     return 1;
 }
 /* out, its scale, limit and token_scale (three arguments from a on) */
-static int rows_out(PyObject *o, const char *name, int64_t T, int64_t D, PyObject *const *a, pvmvmd_rows_out *r) {
+static int rows_out(PyObject *o, const char *name, int64_t *d, PyObject *const *a, pvmvmd_rows_out *r) {
     PyObject *type;
     memset(r, 0, sizeof(*r));
     r->scale = 1.0f;
     r->limit = 1;
-    if (!matrix(o, name, T, D, 0, &r->data_dev, &r->token) || !type_code(o, name, a != NULL, &r->type, &type)) return 0;
+    if (!matrix(o, name, d, d + 1, 0, &r->data_dev, &r->token) || !type_code(o, name, a != NULL, &r->type, &type)) return 0;
     if (!a) return 1;
     r->scale = (float)PyFloat_AsDouble(a[0]);
     if (PyErr_Occurred() || !to_int(a[1], "limit", &r->limit)) return 0;
     void *p = NULL;
-    if (a[2] != Py_None && !vector(a[2], "out_token_scale", T, t_float[2], &p)) return 0;
+    if (a[2] != Py_None && !vector(a[2], "out_token_scale", d[0], t_float[2], &p)) return 0;
     r->token_scale_dev = p;
     return 1;
 }
@@ -354,7 +357,7 @@ static int has(void *f) {
 /* norm(y or None, residual or None, post or 0, gate or None, branch_scale, residual_scale, residual_out or None, pre or 0,
  *      out or None, out_scale, limit, out_token_scale or None, stream) */
 static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    int64_t d[2];
+    int64_t d[2] = {-1, 0};
     pvmvmd_rows y, gate, residual;
     pvmvmd_rows_out residual_out, out;
     const NormView *post, *pre;
@@ -365,12 +368,10 @@ static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
         PyErr_SetString(PyExc_ValueError, "y or residual must be there");
         return NULL;
     }
-    if (!dims(a[0] != Py_None ? data_of(a[0]) : a[1], a[0] != Py_None ? "y" : "residual", 2, d) ||
-        (a[0] != Py_None && !rows_in(a[0], "y", d[0], d[1], 0, &y)) ||
-        (a[1] != Py_None && !rows_in(a[1], "residual", d[0], d[1], 0, &residual)) ||
-        !norm_view(a[2], "post", d[1], &post) || (a[3] != Py_None && !rows_in(a[3], "gate", d[0], d[1], 1, &gate)) ||
-        (a[6] != Py_None && !rows_out(a[6], "residual_out", d[0], d[1], NULL, &residual_out)) ||
-        !norm_view(a[7], "pre", d[1], &pre) || (a[8] != Py_None && !rows_out(a[8], "out", d[0], d[1], a + 9, &out)))
+    if ((a[0] != Py_None && !rows_in(a[0], "y", d, 0, &y)) || (a[1] != Py_None && !rows_in(a[1], "residual", d, 0, &residual)) ||
+        !norm_view(a[2], "post", d[1], &post) || (a[3] != Py_None && !rows_in(a[3], "gate", d, 1, &gate)) ||
+        (a[6] != Py_None && !rows_out(a[6], "residual_out", d, NULL, &residual_out)) || !norm_view(a[7], "pre", d[1], &pre) ||
+        (a[8] != Py_None && !rows_out(a[8], "out", d, a + 9, &out)))
         return NULL;
     const double branch = PyFloat_AsDouble(a[4]), keep = PyErr_Occurred() ? 0 : PyFloat_AsDouble(a[5]);
     if (PyErr_Occurred() || !stream_of(a[12], &stream)) return NULL;
@@ -384,15 +385,13 @@ static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 
 /* glu(gate, act, up or None, out, out_scale, limit, out_token_scale or None, stream) */
 static PyObject *glu(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    int64_t d[2];
+    int64_t d[2] = {-1, 0};
     pvmvmd_rows gate, up;
     pvmvmd_rows_out out;
     void *stream;
     int act, status;
-    if (!has((void *)f_glu) || !arity(n, 8) || !dims(data_of(a[0]), "gate", 2, d) ||
-        !rows_in(a[0], "gate", d[0], d[1], 0, &gate) || !to_int(a[1], "act", &act) ||
-        (a[2] != Py_None && !rows_in(a[2], "up", d[0], d[1], 0, &up)) ||
-        !rows_out(a[3], "out", d[0], d[1], a + 4, &out) || !stream_of(a[7], &stream))
+    if (!has((void *)f_glu) || !arity(n, 8) || !rows_in(a[0], "gate", d, 0, &gate) || !to_int(a[1], "act", &act) ||
+        (a[2] != Py_None && !rows_in(a[2], "up", d, 0, &up)) || !rows_out(a[3], "out", d, a + 4, &out) || !stream_of(a[7], &stream))
         return NULL;
     if (d[0] > INT_MAX || d[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
     CALL(status, f_glu((int)d[0], (int)d[1], &gate, act, a[2] != Py_None ? &up : NULL, &out, stream))
@@ -412,13 +411,12 @@ static int words(PyObject *t, const char *name, int64_t n, void **p) {
 }
 /* sample(logits, random, sampling, allowed or None, token, logprob or None, stream) */
 static PyObject *sample(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    int64_t d[2], row = 0;
+    int64_t d[2] = {-1, 0}, row = 0;
     pvmvmd_rows logits;
     void *v, *random, *allowed = NULL, *token, *logprob = NULL, *stream;
     PyObject *type;
     int code, status;
-    if (!has((void *)f_sample) || !arity(n, 7) || !dims(data_of(a[0]), "logits", 2, d) ||
-        !rows_in(a[0], "logits", d[0], d[1], 0, &logits) || !words(a[1], "random", d[0], &random) || !address(a[2], &v))
+    if (!has((void *)f_sample) || !arity(n, 7) || !rows_in(a[0], "logits", d, 0, &logits) || !words(a[1], "random", d[0], &random) || !address(a[2], &v))
         return NULL;
     const SamplingView *how = v;
     if (how->T && how->T != d[0]) {
@@ -427,7 +425,8 @@ static PyObject *sample(PyObject *self, PyObject *const *a, Py_ssize_t n) {
         return NULL;
     }
     if (a[3] != Py_None) {
-        if (!matrix(a[3], "allowed", d[0], (d[1] + 31) / 32, 1, &allowed, &row) ||
+        int64_t bits = (d[1] + 31) / 32;
+        if (!matrix(a[3], "allowed", d, &bits, 1, &allowed, &row) ||
             !type_code(a[3], "allowed", 1, &code, &type))
             return NULL;
         if (code != PVMVMD_FIELD) {
