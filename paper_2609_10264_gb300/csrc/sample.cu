@@ -362,7 +362,8 @@ struct Row : RowData {
         __device__ __forceinline__ bool keeps(float v, int i) const { return v > x || (v == x && (uint32_t)i <= index); }
     };
     // kLeast: `least` may be above 0.
-    template <bool kSum, bool kCollect, bool kHist, bool kCut, bool kLeast, typename C, typename H>
+    // kSparse: few tokens are collected.
+    template <bool kSum, bool kCollect, bool kHist, bool kCut, bool kLeast, bool kSparse = false, typename C, typename H>
     __device__ __forceinline__ u64 pass(int begin, int last, u64 least, float near, Cut cut, C collect, H hist) const {
         u64 sum = 0;
         int k;
@@ -428,6 +429,15 @@ struct Row : RowData {
                 }
             }
             if (kSum) sum += low;
+            if (kSparse) {  // (most tiles have none)
+#pragma unroll 1
+                while (hits) {
+                    const int e = __ffs(hits) - 1;
+                    const Two v = e & 4 ? (e & 2 ? x[3] : x[2]) : (e & 2 ? x[1] : x[0]);
+                    collect(e & 1 ? second(v) : first(v), i0 + e);
+                    hits &= hits - 1;
+                }
+            }
             if (kCollect && hits) {
 #pragma unroll
                 for (int e = 0; e < kWide; ++e)
@@ -895,7 +905,7 @@ struct Row : RowData {
 
     // The tokens whose distance's bits are in a range, to this CTA's part of the list; then, in the first CTA, all of them.  Their number, in every CTA; what is above kList is not in the list.
     // total (of the weights, where asked for).
-    template <bool kSum>
+    template <bool kSum, bool kSparse = false>
     __device__ __forceinline__ uint32_t collect_list(Range range, u64 &total) {
         if (threadIdx.x == 0) sh.count = 0;
         __syncthreads();
@@ -907,7 +917,7 @@ struct Row : RowData {
                 sh.index[p] = i;
             }
         };
-        total = pass<kSum, true, false, false, false>(begin, last, 0, __uint_as_float(range.to), no_cut(), collect, [](float, u64) {});
+        total = pass<kSum, true, false, false, false, kSparse>(begin, last, 0, __uint_as_float(range.to), no_cut(), collect, [](float, u64) {});
         if (kSum) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
@@ -988,6 +998,25 @@ struct Row : RowData {
     // Of the listed tokens that `within` keeps, in order: those up to which `target` of weight lies (one each where
     // ones).  The cut after them.
     __device__ __forceinline__ Cut cut_listed(int n, u64 target, bool ones, Cut within) const {
+        if (n <= kFew) {  // a thread each, which compares its token with all others
+            const int i = threadIdx.x;
+            const bool mine = i < n && within.keeps(sh.x[i], sh.index[i]);
+            const float x = i < n ? sh.x[i] : 0.0f;
+            const int at = i < n ? sh.index[i] : 0;
+            const u64 w = !mine ? 0ull : ones ? 1ull : weight(big, x);
+            if (i < n) sh.few[i] = w;
+            __syncthreads();
+            u64 before = 0;
+            if (i < (n + 31) / 32 * 32)
+#pragma unroll 4
+                for (int k = 0; k < n; ++k) before += ahead(sh.x[k], sh.index[k], x, at) ? sh.few[k] : 0ull;
+            if (mine && before < target && before + w >= target) {
+                sh.cut_x = x;
+                sh.cut_index = (uint32_t)at;
+            }
+            __syncthreads();
+            return Cut{sh.cut_x, sh.cut_index};
+        }
         uint32_t v;
         u64 before, at;
         reach_listed(n, 32, target, [&](float x, int i, uint32_t &value, u64 &w) {
@@ -1179,7 +1208,7 @@ struct Row : RowData {
             __syncthreads();
             const Range near{0, range_of<5>((int)sh.found).to};
             u64 total = 0;
-            const uint32_t n = top_k ? collect_list<false>(near, total) : collect_list<true>(near, total);
+            const uint32_t n = top_k ? collect_list<false, true>(near, total) : collect_list<true>(near, total);
             again = n > (uint32_t)kList;
             if (!again) {
                 if (rank == 0) {
@@ -1311,7 +1340,7 @@ cudaError_t launch_type(const SampleArgs &a, cudaStream_t s) {
 
 cudaError_t launch_sample(const SampleJob &j, cudaStream_t s) {
     SampleArgs a{j, 1};
-    while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 304 && j.V / a.ctas >= 8192) a.ctas *= 2;
+    while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 304 && j.V / a.ctas >= 6000) a.ctas *= 2;
     switch (j.logits.type) {
         case kBf16: return launch_type<kBf16>(a, s);
         case kF16: return launch_type<kF16>(a, s);
