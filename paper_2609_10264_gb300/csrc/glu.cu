@@ -1,4 +1,8 @@
 // The gated activation of a feed-forward block (pvmvmd_glu).
+//
+// Bound by its instructions, about 50 a field element with its scales, power and quotient, of which an SM issues two
+// in a cycle: 4096 rows of 28672 to integers by a scale known ahead 239 us (5.9 TB/s), with a step a row 296, bf16 to
+// bf16 164 (4.3 TB/s).  One row of 14336 3.3 us.
 #include "rows.cuh"
 
 namespace pv {

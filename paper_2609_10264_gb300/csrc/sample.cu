@@ -12,6 +12,9 @@
 // Where the list does not hold what the limits leave (flat rows, a large k), a histogram of all tokens says in
 // which bin a limit falls; that bin's tokens become the list, in which the limit is looked for digit by digit.
 // Where they are too many for it (equal logits), the digits are those of all tokens, each another reading.
+//
+// 128000 logits a row: greedily 512 rows in 44 us (32 bits; 6.0 TB/s), whole distributions 113, top-k 50 74, top-p
+// 0.5 139, flat rows with top-p 0.9 720; one row 3.9, 9.8, 10.9 and 16.8 us.
 #include "rows.cuh"
 
 namespace pv {
@@ -1339,6 +1342,8 @@ cudaError_t launch_type(const SampleArgs &a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_sample(const SampleJob &j, cudaStream_t s) {
+    // A row over as many CTAs as leave two an SM, of 6000 tokens at least (one row of 128000 with top-k and top-p 35 us by
+    // one CTA, 23, 16 and 13 by 2, 4 and 8; 512 rows 119 by one each, 121 by two, 135 by four).
     SampleArgs a{j, 1};
     while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 304 && j.V / a.ctas >= 6000) a.ctas *= 2;
     switch (j.logits.type) {
