@@ -7,6 +7,7 @@
 #pragma once
 
 #include <algorithm>
+#include <climits>
 
 #include "attention.cuh"
 #include "steps.h"
@@ -472,7 +473,11 @@ inline RowDeal deal_rows(int T, int D, bool joint) {
     d.threads = 32 * ((tiles + (d.chunks << d.log_ctas) - 1) / (d.chunks << d.log_ctas));
     return d;
 }
-inline dim3 grid_of(const RowDeal &d, int T) { return dim3((unsigned)((T + d.rows - 1) / d.rows) << d.log_ctas); }
+// (No CTAs, which no launch takes, where there are more than a grid has.)
+inline dim3 grid_of(const RowDeal &d, int T) {
+    const int64_t n = (((int64_t)T + d.rows - 1) / d.rows) << d.log_ctas;
+    return dim3(n > INT_MAX ? 0u : (unsigned)n);
+}
 inline int cluster_of(const RowDeal &d) { return d.joint ? 1 << d.log_ctas : 1; }
 
 __device__ __forceinline__ RowThreads row_threads(RowShared *sh, const RowDeal &d) {
@@ -484,7 +489,7 @@ __device__ __forceinline__ RowThreads row_threads(RowShared *sh, const RowDeal &
     r.ctas = d.joint ? 1u << d.log_ctas : 1u;
     r.rank = blockIdx.x & ((1u << d.log_ctas) - 1);  // in a cluster, too
     r.place = 0;
-    r.t = d.rows > 1 ? (int)blockIdx.x * d.rows + r.warp : (int)(blockIdx.x >> d.log_ctas);
+    r.t = d.rows > 1 ? (int64_t)blockIdx.x * d.rows + r.warp : blockIdx.x >> d.log_ctas;
     cluster_begin(r.ctas);
     return r;
 }

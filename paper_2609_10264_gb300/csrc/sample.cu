@@ -441,7 +441,7 @@ struct Row : RowData {
                     hits &= hits - 1;
                 }
             }
-            if (kCollect && hits) {
+            if (kCollect && !kSparse && hits) {
 #pragma unroll
                 for (int e = 0; e < kWide; ++e)
                     if (hits >> e & 1) collect(e & 1 ? second(x[e / 2]) : first(x[e / 2]), i0 + e);
@@ -906,8 +906,9 @@ struct Row : RowData {
         return true;
     }
 
-    // The tokens whose distance's bits are in a range, to this CTA's part of the list; then, in the first CTA, all of them.  Their number, in every CTA; what is above kList is not in the list.
-    // total (of the weights, where asked for).
+    // The tokens whose distance's bits are in a range, to this CTA's part of the list; then, in the first CTA, all of
+    // them.  Their number, in every CTA; what is above kList is not in the list.  total: of the row's weights, where
+    // asked for.
     template <bool kSum, bool kSparse = false>
     __device__ __forceinline__ uint32_t collect_list(Range range, u64 &total) {
         if (threadIdx.x == 0) sh.count = 0;
@@ -920,7 +921,8 @@ struct Row : RowData {
                 sh.index[p] = i;
             }
         };
-        total = pass<kSum, true, false, false, false, kSparse>(begin, last, 0, __uint_as_float(range.to), no_cut(), collect, [](float, u64) {});
+        total = pass<kSum, true, false, false, false, kSparse>(begin, last, 0, __uint_as_float(range.to), no_cut(), collect,
+                                                               [](float, u64) {});
         if (kSum) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
@@ -933,7 +935,6 @@ struct Row : RowData {
             for (int k = 0; k < kSWarps; ++k) total += sh.warp[k];
         uint32_t n = sh.count;
         if (ctas == 1) return n;
-        // (weights' sums are below 2^64 / 2^5; numbers go beside them, up to kList + 1)
         const uint32_t mine = min(n, (uint32_t)kList + 1);
         const u64 *all = exchange(mine);
         n = 0;
@@ -1244,7 +1245,8 @@ __device__ void limits_in_all(RowData d, int top_k, float top_p, u64 least) {
     }
 }
 
-// kLimited: rows may have top-k or top-p.  Without them there is room for a third CTA an SM.
+// kLimited: rows may have top-k or top-p.  (Without them a third CTA an SM would find room, of 40 registers a thread; 512
+// rows of 128000 take 122 us so, 113 with two.)
 template <int kType, bool kLimited>
 __global__ void __launch_bounds__(kSThreads, 2) k_sample(const __grid_constant__ SampleArgs a) {
     follow();
