@@ -54,7 +54,7 @@ __device__ __forceinline__ void over_one_plus_all(Two (&x)[kTwos], float most) {
     for (int i = 0; i < kTwos; ++i) big = larger(larger(big, first(x[i])), second(x[i]));
     if (big <= most) {
 #pragma unroll
-        for (int i = 0; i < kTwos; ++i) x[i] = over_one_plus(x[i], power(distance<kAct>(x[i])));
+        for (int i = 0; i < kTwos; ++i) x[i] = over_one_plus(x[i], power_near(distance<kAct>(x[i])));  // (at 126 or 125, 1 + 2^-d is 1)
     } else {
 #pragma unroll
         for (int i = 0; i < kTwos; ++i) x[i].v = activate_any<kAct>(x[i].v);

@@ -295,12 +295,15 @@ __device__ __forceinline__ Two split(Two d, Two &sum) {
     sum = add2(d, both(12582912.0f));
     return sub2(d, sub2(sum, both(12582912.0f)));
 }
-// 2^-d for d cut to [-128, 125], infinity at -128.  (23 bits up, nothing is left of 0x4b400000.)
-__device__ __forceinline__ Two power(Two d) {
+// 2^-d for |d| < 127.  (23 bits up, nothing is left of 0x4b400000.)
+__device__ __forceinline__ Two power_near(Two d) {
     Two n;
-    d = two(fminf(fmaxf(first(d), -128.0f), 125.0f), fminf(fmaxf(second(d), -128.0f), 125.0f));
     const Two p = exp_poly(split(d, n));
     return two((uint32_t)p.v - ((uint32_t)n.v << 23), (uint32_t)(p.v >> 32) - ((uint32_t)(n.v >> 32) << 23));
+}
+// 2^-d for d cut to [-128, 125], infinity at -128.
+__device__ __forceinline__ Two power(Two d) {
+    return power_near(two(fminf(fmaxf(first(d), -128.0f), 125.0f), fminf(fmaxf(second(d), -128.0f), 125.0f)));
 }
 
 // ---------------------------------------------------------------- sums in pairs
