@@ -72,11 +72,11 @@ __device__ __forceinline__ void norm(RowThreads &r, const pvmvmd_norm &n, Pair i
 }
 
 // kY, kR, kO, kG: the types of y, of the residual and its output, of out, and of the gate (kNone: there is
-// none).  With a gate of a known type two CTAs of the most threads would spill registers (4096 rows of 2560 37 us
-// instead of 32).
-constexpr int kNone = -1;
-template <bool kVec, int kChunks, int kY, int kR, int kO, int kG>
-__global__ void __launch_bounds__(kRowThreadsMost, kChunks == 4 || kG > kAny ? 1 : 2)
+// none).  kMost: threads at most.  With a gate 64 registers a thread, which let two CTAs of 512 run, spill a few; CTAs of up to
+// 224 have 72 (4096 gated rows of 8192 94 us with 64 and 116 with 72, where one CTA runs; of 2560 31.4 and 28.9).
+constexpr int kNone = -1, kFewThreads = 224;
+template <bool kVec, int kChunks, int kY, int kR, int kO, int kG, int kMost = kRowThreadsMost>
+__global__ void __launch_bounds__(kMost, kMost == kFewThreads ? 4 : kChunks == 4 ? 1 : 2)
     k_block_norm(const __grid_constant__ NormArgs a) {
     follow();
     const NormJob &j = a.j;
@@ -153,7 +153,11 @@ cudaError_t launch_types(const NormArgs &a, cudaStream_t s) {
     const int ctas = cluster_of(a.d);
     switch (a.d.chunks) {
         case 1: return launch_cluster(k_block_norm<kVec, 1, kY, kR, kO, kG>, grid, ctas, a.d.threads, 0, s, a);
-        case 2: return launch_cluster(k_block_norm<kVec, 2, kY, kR, kO, kG>, grid, ctas, a.d.threads, 0, s, a);
+        case 2:
+            if constexpr (kG > kAny)
+                if (a.d.threads <= kFewThreads)
+                    return launch_cluster(k_block_norm<kVec, 2, kY, kR, kO, kG, kFewThreads>, grid, ctas, a.d.threads, 0, s, a);
+            return launch_cluster(k_block_norm<kVec, 2, kY, kR, kO, kG>, grid, ctas, a.d.threads, 0, s, a);
         default: return launch_cluster(k_block_norm<kVec, 4, kAny, kAny, kAny, kAny>, grid, ctas, a.d.threads, 0, s, a);
     }
 }
