@@ -554,7 +554,8 @@ typedef struct {
  *     m = min(limit / a, FLT_MAX) with a = max_i |z_i| of the row, whose step
  *     token_scale_dev[t] = a / limit is written (a row with a value that is not finite
  *     gives zeros, and NaN for its step).
- * 1 <= limit <= 2^22. */
+ * 1 <= limit <= 2^22.  Rows must not lie on one another: of several, `token` is D at least
+ * (or -D at most; PVMVMD_E_ARG). */
 typedef struct {
     void *data_dev;
     float *token_scale_dev; /* [T] or null; null for floating types */
@@ -586,7 +587,7 @@ typedef struct {
  * residual_out, pre, out; y or residual, and residual_out or out, must be there.
  * residual and residual_out have floating types, no scales, and may be one tensor.
  * D <= PVMVMD_MAX_K.  Errors: PVMVMD_E_ARG (null pointer, unknown type or norm, a step for a
- * floating output), PVMVMD_E_SHAPE (T < 0, D outside [1, PVMVMD_MAX_K]), PVMVMD_E_PARAM (eps
+ * floating output, rows to write that lie on one another), PVMVMD_E_SHAPE (T < 0, D outside [1, PVMVMD_MAX_K]), PVMVMD_E_PARAM (eps
  * not above 0, a limit outside [1, 2^22], a scale that is not finite). */
 int pvmvmd_block_norm(int T, int D, const pvmvmd_rows *y, const pvmvmd_norm *post, const pvmvmd_rows *gate,
                       float branch_scale, const pvmvmd_rows *residual, float residual_scale,

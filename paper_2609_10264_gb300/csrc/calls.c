@@ -331,6 +331,10 @@ static int rows_out(PyObject *o, const char *name, int64_t *d, PyObject *const *
     r->scale = 1.0f;
     r->limit = 1;
     if (!matrix(o, name, d, d + 1, 0, &r->data_dev, &r->token) || !type_code(o, name, a != NULL, &r->type, &type)) return 0;
+    if (d[0] > 1 && r->token < d[1]) {
+        PyErr_Format(PyExc_ValueError, "the rows of %s must not lie on one another", name);
+        return 0;
+    }
     if (!a) return 1;
     r->scale = (float)PyFloat_AsDouble(a[0]);
     if (PyErr_Occurred() || !to_int(a[1], "limit", &r->limit)) return 0;

@@ -30,9 +30,11 @@ int check(const pvmvmd_rows &r, bool field = true) {
         return PVMVMD_E_ARG;
     return std::isfinite(r.scale) ? PVMVMD_OK : PVMVMD_E_PARAM;
 }
-int check(const pvmvmd_rows_out &o, bool field = true) {
+// (rows closer than they are long would be written by several threads at once)
+int check(const pvmvmd_rows_out &o, int T, int D, bool field = true) {
     if (!o.data_dev || !(field ? any_type(o.type) : float_type(o.type))) return PVMVMD_E_ARG;
     if (misaligned(o.data_dev, size_of(o.type)) || misaligned(o.token_scale_dev, 4)) return PVMVMD_E_ARG;
+    if (T > 1 && o.token < D && o.token > -(int64_t)D) return PVMVMD_E_ARG;
     if (o.type != PVMVMD_FIELD) return o.token_scale_dev ? PVMVMD_E_ARG : PVMVMD_OK;
     if (o.limit < 1 || o.limit > 1 << 22) return PVMVMD_E_PARAM;
     return o.token_scale_dev || std::isfinite(o.scale) ? PVMVMD_OK : PVMVMD_E_PARAM;
@@ -65,8 +67,8 @@ int pvmvmd_block_norm(int T, int D, const pvmvmd_rows *y, const pvmvmd_norm *pos
     if (y && (st = check(*y))) return st;
     if (gate && (st = check(*gate))) return st;
     if (residual && (st = check(*residual, false))) return st;
-    if (residual_out && (st = check(*residual_out, false))) return st;
-    if (out && (st = check(*out))) return st;
+    if (residual_out && (st = check(*residual_out, T, D, false))) return st;
+    if (out && (st = check(*out, T, D))) return st;
     NormJob j{};
     j.T = T;
     j.D = D;
@@ -90,7 +92,7 @@ int pvmvmd_glu(int T, int D, const pvmvmd_rows *gate, int act, const pvmvmd_rows
     if (st) return st;
     if (!gate || !out || act < PVMVMD_ACT_NONE || act > PVMVMD_ACT_GELU) return PVMVMD_E_ARG;
     if (T == 0) return PVMVMD_OK;
-    if ((st = check(*gate)) || (up && (st = check(*up))) || (st = check(*out))) return st;
+    if ((st = check(*gate)) || (up && (st = check(*up))) || (st = check(*out, T, D))) return st;
     GluJob j{};
     j.T = T;
     j.D = D;
