@@ -341,13 +341,22 @@ __device__ __forceinline__ Pair mean_of(Pair s, Pair inverse) {
     return Pair{p, __fmaf_rn(l, inverse.h, __fmaf_rn(h, inverse.l, __fmaf_rn(h, inverse.h, -p)))};
 }
 // 1 / sqrt(a + eps), rounded once: the approximation y of a's upper part, corrected by
-// what 1 - a y^2 is in twice the bits.
+// what 1 - a y^2 is in twice the bits.  Of sums far from 1, whose y^2 or its lower 24 bits 32-bit numbers do not
+// hold, it is taken of the sum times a power of four, which comes off the root exactly.  (Of all sums: 8192 x 8192 155.8 us,
+// 154.3 so.)
 __device__ __forceinline__ float inverse_root(Pair a, float eps) {
     const Pair s = join(a, Pair{eps, 0.0f});
-    const float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l);
-    const float y = rsqrtf(h), t = __fmul_rn(y, y), te = __fmaf_rn(y, y, -t);
+    float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l), back = 1.0f;
+    if (!(h >= 0x1p-100f && h <= 0x1p100f)) {
+        const bool below1 = h < 1.0f;
+        const float gain = below1 ? 0x1p64f : 0x1p-64f;
+        h = __fmul_rn(h, gain);
+        l = __fmul_rn(l, gain);
+        back = below1 ? 0x1p32f : 0x1p-32f;
+    }
+    const float y = rsqrtf(h), t = __fmul_rn(y, y), te = __fmaf_rn(y, y, -t), root = __fmul_rn(y, back);
     const float r = -__fmaf_rn(l, t, __fmaf_rn(h, te, __fmaf_rn(h, t, -1.0f)));
-    return __fmaf_rn(y, __fmul_rn(r, __fmaf_rn(0.375f, r, 0.5f)), y);
+    return __fmaf_rn(root, __fmul_rn(r, __fmaf_rn(0.375f, r, 0.5f)), root);
 }
 
 // ---------------------------------------------------------------- across a row's threads

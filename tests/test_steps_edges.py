@@ -46,3 +46,46 @@ def test_one_row_to_write_of_any_stride(pv):
         out = torch.empty(40, device="cuda").as_strided((1, 40), (stride, 1))
         pv.pvmvmd_glu(x, act="relu", out=out)
         assert torch.equal(out, x.clamp(min=0))
+
+
+# ---------------------------------------------------------------- the ends of a norm's range
+
+def _inverse_bounds(x, eps):
+    """1 / sqrt of a row's mean of squares and eps, which is formed within 2^-40 of itself and 2^-146, rounded once: the
+    smallest and the largest value that has."""
+    M = np.square(x.astype(np.float64)).mean(-1, keepdims=True) + np.float64(np.float32(eps))
+    off = M * 2.0**-40 + 2.0**-146
+    return (1 / np.sqrt(M + off)).astype(np.float32), (1 / np.sqrt(np.maximum(M - off, 2.0**-149))).astype(np.float32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [1, 8, 40, 1100])
+@pytest.mark.parametrize("lo,hi,eps", [(96, 126, 1e-6), (-30, 30, 1e-6), (-104, -40, 1e-38), (-150, -90, 1e-30), (-150, -90, 1e-38)],
+                         ids=["large", "usual", "small", "small-eps", "smallest"])
+def test_norm_over_its_range(pv, D, lo, hi, eps):
+    """Rows whose squares' sums are 2^lo to just below 2^hi."""
+    rng = np.random.default_rng(D)
+    T = 20000 if D < 100 else 3000
+    x = rng.standard_normal((T, D))
+    x *= np.sqrt(np.exp2(rng.uniform(lo, hi - 0.001, (T, 1))) / np.square(x).sum(-1, keepdims=True))
+    x = x.astype(np.float32)
+    z = _dev(np.zeros((T, D), np.float32))
+    pv.pvmvmd_block_norm(None, _dev(x), residual_out=False, pre=pv.Norm("rms", eps=eps), out=z)
+    got = np.abs(_host(z))
+    low, high = (np.abs(x * v) for v in _inverse_bounds(x, eps))
+    bad = ~((got >= low) & (got <= high))
+    assert not bad.any(), f"{bad.any(-1).sum()} of {T} rows, of squares' sums from " \
+                          f"2^{np.log2(np.square(x.astype(np.float64)).sum(-1)[bad.any(-1)].min()):.1f} on"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("D", [5, 1500, 9000])
+def test_norm_of_zeros_with_any_eps(pv, kind, D):
+    """Zeros, also with the smallest number above 0."""
+    import torch
+    x = torch.zeros(3, D, device="cuda")
+    for eps in (1e-45, 1e-42, 1e-40, 1e-38, 1e-30, 1e-6, 1.0, 3e38):
+        z = torch.full((3, D), 7.0, device="cuda")
+        pv.pvmvmd_block_norm(None, x, residual_out=False, pre=pv.Norm(kind, eps=eps), out=z)
+        assert (z == 0).all(), eps
