@@ -521,8 +521,11 @@ int pvmvmd_kv_evict(const pvmvmd_kv_pool *pool, const pvmvmd_kv_batch *batch, in
  * elements.  Those are whole numbers, which the next check compares as they are, so the
  * steps are defined in IEEE numbers of 32 bits: every product, sum, quotient and
  * conversion written below is rounded to nearest by itself, in the order written.
- * Means and mean squares are formed in more bits (of 2^-40 and better) and rounded
- * once.  Rows' squares must stay below 2^126 in sum; beyond, a norm gives NaN or 0.
+ * A norm's mean is formed within 2^-39 of mean_i |x_i| and its mean of squares within 2^-39 of itself,
+ * and both within 2^-146 besides; mu and inv are rounded from them once.  Where they lie closer than that to the middle
+ * of two 32-bit numbers they may be either, and not the same one for every T and alignment; all else that is
+ * written below has one value, but for the logarithm of pvmvmd_sample.  Rows' squares must stay below 2^126 in sum;
+ * beyond, a norm's values may be NaN or 0.
  *
  * Conventions, besides those at the top of this file and of the client's attention
  * (types, structs read during the call):
@@ -638,7 +641,8 @@ typedef struct {
  *   Choice.  Z the kept tokens' weight: the first kept token, in the order of the vocabulary, up to
  *     which they weigh more than floor(Z random_dev[t] / 2^32).
  * token_dev[t] is its index, and logprob_dev[t] (or null) = log(W / Z), the log of the
- * probability that it was drawn with; the token of lowest index among the largest and 0 for a greedy row;
+ * probability that it was drawn with, within 2^-22 (1 + |log(W / Z)|); the token of lowest
+ * index among the largest and 0 for a greedy row;
  * -1 and -infinity where no token can be chosen.  logits->token as for other rows, not
  * below V unless it is 0 (equal rows).  1 <= V <= 2^22 (whose
  * weights' sums are below 2^62).  Errors: PVMVMD_E_ARG (null pointer,

@@ -308,7 +308,10 @@ __device__ __forceinline__ Two power(Two d) {
 
 // ---------------------------------------------------------------- sums in pairs
 // h + l, |l| about 2^-24 |h|: sums and squares to about 2^-45 of the sum of their terms'
-// sizes (Dekker, Numer. Math. 1971; Knuth, TAOCP vol. 2, 4.2.2).
+// sizes (Dekker, Numer. Math. 1971; Knuth, TAOCP vol. 2, 4.2.2).  At worst, of 16 terms in a row l takes an error of
+// 2^-24 of the sum with each, and as many of its own of 2^-24 of what it has, in all (1 + 2 + .. + 16 + 48) 2^-48; a
+// warp's sum below adds 32 of 2^-25 in 2^21 or more, that of 16 warps half of it and that of 8 CTAs a quarter: below 2^-39.
+// What falls below 2^-149 is lost: 2^-150 and 2^-149 of each term, and 2^-149 of each lane's sum.
 struct Pair {
     float h, l;
 };

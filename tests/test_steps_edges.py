@@ -51,10 +51,10 @@ def test_one_row_to_write_of_any_stride(pv):
 # ---------------------------------------------------------------- the ends of a norm's range
 
 def _inverse_bounds(x, eps):
-    """1 / sqrt of a row's mean of squares and eps, which is formed within 2^-40 of itself and 2^-146, rounded once: the
+    """1 / sqrt of a row's mean of squares and eps, which is formed within 2^-39 of itself and 2^-146, rounded once: the
     smallest and the largest value that has."""
     M = np.square(x.astype(np.float64)).mean(-1, keepdims=True) + np.float64(np.float32(eps))
-    off = M * 2.0**-40 + 2.0**-146
+    off = M * 2.0**-39 + 2.0**-146
     return (1 / np.sqrt(M + off)).astype(np.float32), (1 / np.sqrt(np.maximum(M - off, 2.0**-149))).astype(np.float32)
 
 
