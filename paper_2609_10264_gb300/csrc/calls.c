@@ -379,6 +379,10 @@ static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
         return NULL;
     const double branch = PyFloat_AsDouble(a[4]), keep = PyErr_Occurred() ? 0 : PyFloat_AsDouble(a[5]);
     if (PyErr_Occurred() || !stream_of(a[12], &stream)) return NULL;
+    if (a[8] == Py_None && a[11] != Py_None) {
+        PyErr_SetString(PyExc_ValueError, "out_token_scale is of the rows of out, which is not there");
+        return NULL;
+    }
     if (d[0] > INT_MAX || d[1] > INT_MAX) return PyLong_FromLong(PVMVMD_E_SHAPE);
     CALL(status, f_norm((int)d[0], (int)d[1], a[0] != Py_None ? &y : NULL, post ? &post->norm : NULL,
                         a[3] != Py_None ? &gate : NULL, (float)branch, a[1] != Py_None ? &residual : NULL, (float)keep,

@@ -89,3 +89,12 @@ def test_norm_of_zeros_with_any_eps(pv, kind, D):
         z = torch.full((3, D), 7.0, device="cuda")
         pv.pvmvmd_block_norm(None, x, residual_out=False, pre=pv.Norm(kind, eps=eps), out=z)
         assert (z == 0).all(), eps
+
+
+# ---------------------------------------------------------------- what the binding takes
+
+def test_steps_to_no_output_are_refused(pv):
+    import torch
+    x, s = Fake((3, 16), torch.float32, address=64), Fake((3,), torch.float32, address=64)
+    with pytest.raises(ValueError, match="out_token_scale"):
+        pv.pvmvmd_block_norm(x, x, residual_out=x, out_token_scale=s, stream=0)
