@@ -902,6 +902,8 @@ class Norm:
         for t in given:
             if t.dim() != 1 or t.dtype != given[0].dtype or t.shape != given[0].shape:
                 raise ValueError("weight and bias must be vectors of one length and type")
+            if t.numel() == 0:
+                raise ValueError("weight and bias must have one value a column")
             code, D = _type_code(t, "weight"), t.numel()
         ptrs = [None if t is None else _dev_ptr(t, n, (t.dtype,)) for t, n in ((weight, "weight"), (bias, "bias"))]
         self.weight, self.bias = weight, bias

@@ -98,3 +98,13 @@ def test_steps_to_no_output_are_refused(pv):
     x, s = Fake((3, 16), torch.float32, address=64), Fake((3,), torch.float32, address=64)
     with pytest.raises(ValueError, match="out_token_scale"):
         pv.pvmvmd_block_norm(x, x, residual_out=x, out_token_scale=s, stream=0)
+
+
+
+@pytest.mark.gpu
+def test_norm_of_no_weights_is_refused(pv):
+    """A vector of no values is not the absence of weights, which holds for rows of any length."""
+    import torch
+    for name in ("weight", "bias"):
+        with pytest.raises(ValueError, match="one value"):
+            pv.Norm("rms", **{name: torch.empty(0, device="cuda")})
