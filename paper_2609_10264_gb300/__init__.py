@@ -918,11 +918,11 @@ class Sampling:
 
     def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         torch = _torch or _lazy_torch()
-        self.T, ptrs, numbers = 0, [], []
+        self.T, ptrs, numbers = None, [], []  # T: None for any
         for v, name in ((temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p")):
             if isinstance(v, torch.Tensor):
-                ptrs.append(_dev_ptr(v, name, (torch.int32 if name == "top_k" else torch.float32,), self.T or None))
-                if v.dim() != 1 or v.numel() == 0:
+                ptrs.append(_dev_ptr(v, name, (torch.int32 if name == "top_k" else torch.float32,), self.T))
+                if v.dim() != 1:
                     raise ValueError(f"{name} must be a vector of one value a row")
                 self.T = v.numel()
                 numbers.append(0)
@@ -932,7 +932,7 @@ class Sampling:
         if not -2**31 <= numbers[1] < 2**31:
             raise OverflowError("top_k does not fit 32 bits")
         self.kept = (temperature, top_k, top_p, min_p)
-        self.view = _SamplingView(pvmvmd_sampling(*ptrs, *numbers), self.T)
+        self.view = _SamplingView(pvmvmd_sampling(*ptrs, *numbers), -1 if self.T is None else self.T)
         self.address = ctypes.addressof(self.view)
 
 

@@ -261,7 +261,8 @@ static PyObject *evict(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 
 /* ---- the client's other steps */
 
-/* What a Norm and a Sampling of the binding hold: the library's struct and the length it is for (0: any). */
+/* What a Norm and a Sampling of the binding hold: the library's struct and the length it is for (any: 0 of
+ * D, -1 of T). */
 typedef struct {
     pvmvmd_norm norm;
     int64_t D;
@@ -427,7 +428,7 @@ static PyObject *sample(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (!has((void *)f_sample) || !arity(n, 7) || !rows_in(a[0], "logits", d, 0, &logits) || !words(a[1], "random", d[0], &random) || !address(a[2], &v))
         return NULL;
     const SamplingView *how = v;
-    if (how->T && how->T != d[0]) {
+    if (how->T >= 0 && how->T != d[0]) {
         PyErr_Format(PyExc_ValueError, "the sampling is of %lld rows, the logits of %lld", (long long)how->T,
                      (long long)d[0]);
         return NULL;

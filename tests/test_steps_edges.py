@@ -108,3 +108,18 @@ def test_norm_of_no_weights_is_refused(pv):
     for name in ("weight", "bias"):
         with pytest.raises(ValueError, match="one value"):
             pv.Norm("rms", **{name: torch.empty(0, device="cuda")})
+
+
+
+@pytest.mark.gpu
+def test_sampling_of_an_empty_batch(pv):
+    """Parameters of no rows are for calls of no rows, and those alone."""
+    import torch
+    d = dict(device="cuda")
+    how = pv.Sampling(torch.empty(0, **d), torch.empty(0, dtype=torch.int32, **d), 0.9)
+    word = torch.empty(0, dtype=torch.int32, **d)
+    assert pv.pvmvmd_sample(torch.empty(0, 50, **d), word, how).shape == (0,)
+    with pytest.raises(ValueError, match="of 0 rows"):
+        pv.pvmvmd_sample(torch.zeros(1, 50, **d), torch.zeros(1, dtype=torch.int32, **d), how)
+    with pytest.raises(ValueError):
+        pv.Sampling(torch.empty(0, **d), torch.ones(2, dtype=torch.int32, **d))
