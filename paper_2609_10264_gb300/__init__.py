@@ -941,15 +941,17 @@ def pvmvmd_block_norm(y, residual=None, post: Norm | None = None, gate=None, bra
                       out_scale: float = 1.0, limit: int = 127, out_token_scale=None, stream=None):
     """r' = residual_scale residual + branch_scale gate post(y), out = pre(r') -> (residual_out, out).
 
-    y (T x D): a Rows or tensor, or None (r' = residual_scale residual); gate: the same, or one row of D values for all.
+    y (T x D): a Rows or tensor, or None (r' = residual_scale residual); gate: the same, or one row of D values for all;
+    residual: floating, without scales.
     residual_out: a floating tensor to take r' (may be residual itself); default: a new one of residual's type, bf16 without
     one; False: r' is not kept.  out: a floating tensor, or an int32 one for field elements of the integers round(z out_scale) within +-limit; with
     out_token_scale (float32, T) each row has a step of its own, max |z| / limit, which is written there.  Without out,
     only r' is formed."""
-    like = residual if y is None else y[0] if type(y) is Rows else y
     if residual_out is None:
         torch = _torch or _lazy_torch()
-        residual_out = like.new_empty(like.shape, dtype=torch.bfloat16 if residual is None else residual.dtype)
+        kept = residual[0] if type(residual) is Rows else residual
+        like = kept if y is None else y[0] if type(y) is Rows else y
+        residual_out = like.new_empty(like.shape, dtype=torch.bfloat16 if kept is None else kept.dtype)
     elif residual_out is False:
         residual_out = None
     _check((_native or _open_calls()).norm(y, residual, 0 if post is None else post.address, gate, branch_scale,

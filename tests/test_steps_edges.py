@@ -123,3 +123,16 @@ def test_sampling_of_an_empty_batch(pv):
         pv.pvmvmd_sample(torch.zeros(1, 50, **d), torch.zeros(1, dtype=torch.int32, **d), how)
     with pytest.raises(ValueError):
         pv.Sampling(torch.empty(0, **d), torch.ones(2, dtype=torch.int32, **d))
+
+
+
+@pytest.mark.gpu
+def test_residual_as_rows(pv):
+    """Rows without scales, as a tensor alone."""
+    import torch
+    y, r = (torch.randn(3, 40, device="cuda") for _ in range(2))
+    want = pv.pvmvmd_block_norm(y, r)[0]
+    assert want.dtype == torch.float32 and torch.equal(pv.pvmvmd_block_norm(y, pv.Rows(r))[0], want)
+    assert torch.equal(pv.pvmvmd_block_norm(None, pv.Rows(r))[0], r)
+    with pytest.raises(pv.PvmvmdError):
+        pv.pvmvmd_block_norm(y, pv.Rows(r, 2.0))
