@@ -136,3 +136,80 @@ def test_residual_as_rows(pv):
     assert torch.equal(pv.pvmvmd_block_norm(None, pv.Rows(r))[0], r)
     with pytest.raises(pv.PvmvmdError):
         pv.pvmvmd_block_norm(y, pv.Rows(r, 2.0))
+
+
+# ---------------------------------------------------------------- the next token of many rows: one CTA each
+
+def _many(pv, l, kind, scale=1.0, t=1.0, k=0, p=1.0, m=0.0, seed=0):
+    import torch
+    T, V = l.shape
+    x = _dev(l, kind)
+    per = lambda v, d: _dev(np.asarray(v, np.float32)[None])[0].to(d) if not np.isscalar(v) else v  # noqa: E731
+    words = np.random.default_rng(seed).integers(0, 2**32, T, dtype=np.uint32)
+    words[:2] = 0, 2**32 - 1
+    lp = torch.empty(T, device="cuda")
+    how = pv.Sampling(per(t, torch.float32), per(k, torch.int32), per(p, torch.float32), per(m, torch.float32))
+    tok = pv.pvmvmd_sample(pv.Rows(x, scale), torch.from_numpy(words.view(np.int32)).cuda(), how, logprob=lp).cpu().numpy()
+    lp = lp.cpu().numpy()
+    h = plain.centred(_host(x)).astype(np.float32) if kind == "field" else _host(x)
+    row = lambda v, r: v if np.isscalar(v) else v[r]  # noqa: E731
+    for r in range(T):
+        tr = row(t, r)
+        xs = plain.distances(h[r], plain.multiplier(scale, None, tr))
+        if tr > 0:
+            want, wlp = plain.sample_long(xs, tr, int(row(k, r)), float(np.float32(row(p, r))), float(np.float32(row(m, r))), words[r])
+        else:
+            want, wlp = int(np.argmax(xs)), 0.0
+        assert tok[r] == want, (r, tok[r], want)
+        # the quotient of two whole numbers, each rounded, and log1p of a unit: 2^-23 of 1 and of the value
+        assert abs(lp[r] - wlp) <= 2.0**-22 * (1 + abs(wlp)), (r, lp[r], wlp)
+
+
+MANY = [
+    dict(t=20.0, p=0.9), dict(t=20.0, k=1025), dict(t=1.0, k=1024), dict(t=5.0, k=1024, p=0.99), dict(t=8.0, k=7000, p=0.6),
+    dict(t=3000.0, p=0.5), dict(t=3000.0, k=6001), dict(t=3000.0, k=6500, p=0.3), dict(t=1.0, p=0.95, m=0.05), dict(t=30.0, m=0.5),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V,kind", [(6000, "f16"), (9001, "field"), (30000, "bf16"), (30011, "f32")])
+@pytest.mark.parametrize("k", range(len(MANY)), ids=lambda k: "-".join(f"{a}={b}" for a, b in MANY[k].items()))
+def test_tokens_of_many_rows(pv, V, kind, k):
+    """More rows than SMs: lists, the histograms of flat rows (whose distances come down to one bin of them), several of
+    each limit's ways."""
+    rng = np.random.default_rng(V + k)
+    l = (rng.standard_normal((160, V)) * 1.5).astype(np.float32)
+    l[:40] *= 4
+    scale = 1.0
+    if kind == "field":
+        l, scale = plain.field(np.rint(l * 5000)), 1 / 5000
+    _many(pv, l, kind, scale, seed=k, **MANY[k])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V,kind", [(6500, "f32"), (9001, "bf16"), (30000, "field")])
+def test_tokens_of_many_rows_of_equal_values(pv, V, kind):
+    """More equal logits than a list takes, and limits among them."""
+    rng = np.random.default_rng(V)
+    l = np.rint(rng.standard_normal((160, V)) * 0.8).astype(np.float32)
+    l[:3] = 2.5 if kind != "field" else 2
+    scale = 1.0
+    if kind == "field":
+        l, scale = plain.field(l.astype(np.int64)), 1.0
+    for how in (dict(k=V // 3), dict(p=0.5), dict(t=2.0, k=V - 1, p=0.7), dict(t=0.5, k=1500, p=0.999, m=0.01), dict(k=1), dict(p=1e-7)):
+        _many(pv, l, kind, scale, seed=len(how), **how)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+def test_tokens_of_many_rows_of_all_kinds(pv, kind):
+    """Rows that take every way in one call."""
+    rng = np.random.default_rng(11)
+    T, V = 200, 12011
+    l = (rng.standard_normal((T, V)) * np.exp2(rng.uniform(-12, 3, (T, 1)))).astype(np.float32)
+    off = rng.random((4, T))
+    t = np.where(off[0] < 0.15, 0.0, np.exp2(rng.uniform(-2, 4, T)))
+    k = np.where(off[1] < 0.3, 0, np.exp2(rng.uniform(0, 13.6, T)).astype(int))
+    p = np.where(off[2] < 0.3, 1.0, rng.random(T))
+    m = np.where(off[3] < 0.5, 0.0, rng.random(T) * 0.3)
+    _many(pv, l, kind, t=t.astype(np.float32), k=k, p=p.astype(np.float32), m=m.astype(np.float32))
