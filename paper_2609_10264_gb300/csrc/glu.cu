@@ -220,7 +220,7 @@ cudaError_t launch_glu(const GluJob &j, cudaStream_t s) {
     const bool vec = j.D % kWide == 0 && whole16(j.gate) && (!j.has_up || whole16(j.up)) && whole16(j.out);
     if (!vec) return launch_types<false, kAny, kAny>(a, s);
     if (j.has_up && j.up.type != j.gate.type) return launch_types<true, kAny, kAny>(a, s);
-    const bool is_long = j.T >= 152 && j.D > 8192 && j.D <= kLongMost && j.out.token_scale_dev;
+    const bool is_long = j.T >= kSms && j.D > 8192 && j.D <= kLongMost && j.out.token_scale_dev;
     switch (j.gate.type) {
         case kField: return is_long ? launch_long<kField>(a, s) : launch_out<kField>(a, s);
         case kBf16: return is_long ? launch_long<kBf16>(a, s) : launch_out<kBf16>(a, s);

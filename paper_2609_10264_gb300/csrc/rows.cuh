@@ -17,6 +17,7 @@ namespace pv {
 constexpr float kFltMax = 3.402823466e+38f;
 constexpr int kWide = 8;  // values that a thread takes at a time
 constexpr int kTwos = kWide / 2;
+constexpr int kSms = 152;  // of the GPU that the library is compiled for; the rules that use it were measured there
 
 __host__ __device__ inline bool two_bytes(int type) { return type == PVMVMD_BF16 || type == PVMVMD_F16; }
 
@@ -179,14 +180,13 @@ __device__ __forceinline__ void outside_zero(const Place<kVec> &p, Two (&x)[kTwo
 }
 
 // ---------------------------------------------------------------- writing
-// A number of up to 2^22 rounded to a whole one, halves to even, as a field element: adding
+// A number of up to kMostLimit rounded to a whole one, halves to even, as a field element: adding
 // 1.5 2^23 leaves the whole number in the sum's lower bits; of n and n + q, read without signs, the
 // smaller one is canonical.
 __device__ __forceinline__ uint32_t field_of(float v) {
     const uint32_t b = __float_as_uint(__fadd_rn(v, 12582912.0f));
     return min(b - 0x4b400000u, b + (kQ - 0x4b400000u));
 }
-constexpr int kMostLimit = 1 << 22;
 
 // What becomes of a row's values: by_row: m is the row's own, so that every |z m| is below limit + 1/2,
 // or 0 where the row is not finite.
@@ -469,19 +469,23 @@ __device__ __forceinline__ float row_max(RowThreads &r, float value) {
 
 // joint: the row's CTAs have something to tell one another.
 inline RowDeal deal_rows(int T, int D, bool joint) {
-    const int tiles = (D + kTile - 1) / kTile, sms = 152, most = kRowThreadsMost / 32;
+    const int tiles = (D + kTile - 1) / kTile, most = kRowThreadsMost / 32;
     RowDeal d{32, 1, 0, 1, joint};
     if (tiles <= 2) {
         d.chunks = tiles;
-        d.rows = std::max(1, std::min(kWarpRows, T / sms));
+        d.rows = std::max(1, std::min(kWarpRows, T / kSms));
         d.threads = 32 * d.rows;
         return d;
     }
+    // Few rows: as many threads as can be, each waiting for little.  Of many, two chunks a thread let two rows' CTAs run
+    // on an SM.  (Norms to integers with a step a row, one chunk and two.  8 rows: of 4096 3.7 and 3.2 us, of 8192 3.8 and 4.4,
+    // of 16384 4.0 and 5.5; 64: 4.0 and 3.4, 4.4 and 4.5, 6.1 and 5.7; 128: 4.4 and 3.4, 5.9 and 4.7, 12.1 and 9.5; 2048: 31
+    // and 20, 79 and 40, 158 and 100.)
     d.chunks = T > 100 ? 2 : 1;
     // Few rows: CTAs of about four warps, as many as two an SM, since each waits for its own loads alone (one row of 8192
     // between two norms 5.2 us with a cluster of 2, 4.1 with one of 8; 64 rows 5.5 and, with 4, 5.1).
     if (d.chunks == 1)
-        while (tiles > 4 << d.log_ctas && d.log_ctas < 3 && (T << (d.log_ctas + 1)) <= 2 * sms) ++d.log_ctas;
+        while (tiles > 4 << d.log_ctas && d.log_ctas < 3 && (T << (d.log_ctas + 1)) <= 2 * kSms) ++d.log_ctas;
     // CTAs of 8 warps where they need not wait for one another, else as few as there can be
     while (tiles > (joint ? most : 8) * d.chunks << d.log_ctas && (d.log_ctas < 3 || !joint)) ++d.log_ctas;
     while (tiles > most * d.chunks << d.log_ctas) d.chunks *= 2;

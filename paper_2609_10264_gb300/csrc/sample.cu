@@ -24,9 +24,13 @@ constexpr int kSThreads = 512, kSWarps = kSThreads / 32;
 constexpr int kBins = 2048;
 
 constexpr int kList = 4096;      // tokens of the list
-constexpr int kMostK = 1024;     // a larger k (twice of it with several CTAs) is not looked for in a list
+// A larger k (twice of it with several CTAs) is not looked for in a list.  (512 rows of 128000 with k 1000: 99 us from the
+// list, 313 by histograms.  Up to 2000, k 1500 takes 124 in place of 321, but with 2000 the list overflows: 427 for 325.)
+constexpr int kMostK = 1024;
 constexpr int kMembers = 1024;   // of a bin at most that are compared with one another
-constexpr int kTopPList = 768;   // tokens that are put in a list for top-p alone, about
+// Tokens that are put in a list for top-p alone, about.  (With 384, 768 and 1536: 512 rows of 128000 with top-p 0.5 114, 127 and
+// 193 us, 64 rows with 0.9 79, 74 and 70, 64 flat ones with 0.1 103, 105 and 44.)
+constexpr int kTopPList = 768;
 constexpr int kFew = 128;        // tokens of a list that are compared with one another at once
 constexpr int kGroups = 4;       // largest values that a thread keeps
 constexpr int kExchanges = 4;    // between the CTAs of a row, at most
@@ -1344,10 +1348,12 @@ cudaError_t launch_type(const SampleArgs &a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_sample(const SampleJob &j, cudaStream_t s) {
-    // A row over as many CTAs as leave two an SM, of 6000 tokens at least (one row of 128000 with top-k and top-p 35 us by
-    // one CTA, 23, 16 and 13 by 2, 4 and 8; 512 rows 119 by one each, 121 by two, 135 by four).
+    // A row over as many CTAs as leave two an SM, of which each halving leaves 3000 tokens at least (one row of 128000 with
+    // top-k and top-p 35 us by one CTA, 23, 16 and 13 by 2, 4 and 8; of 12000 8.9, 8.8 and 9.1 by 2, 4 and 8; of 6000 6.9
+    // by one and 8.5 by two; 512 rows of 128000 119 by one each, 121 by two, 135 by four).  Clusters of 8 do not fill all
+    // places: 33 to 38 rows take two turns (37 of 32001 19 us, 10.2 by clusters of 4).
     SampleArgs a{j, 1};
-    while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 304 && j.V / a.ctas >= 6000) a.ctas *= 2;
+    while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 2 * kSms && j.V / a.ctas >= 6000) a.ctas *= 2;
     switch (j.logits.type) {
         case kBf16: return launch_type<kBf16>(a, s);
         case kF16: return launch_type<kF16>(a, s);

@@ -5,6 +5,8 @@
 
 namespace pv {
 
+constexpr int kMostLimit = 1 << 22;  // of integers to write
+
 struct NormJob {
     int T, D;
     bool has_y, has_gate, has_residual;

@@ -36,7 +36,7 @@ int check(const pvmvmd_rows_out &o, int T, int D, bool field = true) {
     if (misaligned(o.data_dev, size_of(o.type)) || misaligned(o.token_scale_dev, 4)) return PVMVMD_E_ARG;
     if (T > 1 && o.token < D && o.token > -(int64_t)D) return PVMVMD_E_ARG;
     if (o.type != PVMVMD_FIELD) return o.token_scale_dev ? PVMVMD_E_ARG : PVMVMD_OK;
-    if (o.limit < 1 || o.limit > 1 << 22) return PVMVMD_E_PARAM;
+    if (o.limit < 1 || o.limit > kMostLimit) return PVMVMD_E_PARAM;
     return o.token_scale_dev || std::isfinite(o.scale) ? PVMVMD_OK : PVMVMD_E_PARAM;
 }
 int check(const pvmvmd_norm &n) {
