@@ -737,8 +737,8 @@ def _open_calls():
     try:
         from . import _calls
     except ImportError as e:
-        raise ImportError("the client's attention goes through the native module _calls, which the build makes where "
-                          "Python's headers are installed") from e
+        raise ImportError("the client's attention and other steps go through the native module _calls, which the build "
+                          "makes where Python's headers are installed") from e
     get, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
     if not (get and dev):
         get, dev = _current_stream, None
@@ -944,9 +944,9 @@ def pvmvmd_block_norm(y, residual=None, post: Norm | None = None, gate=None, bra
     y (T x D): a Rows or tensor, or None (r' = residual_scale residual); gate: the same, or one row of D values for all;
     residual: floating, without scales.
     residual_out: a floating tensor to take r' (may be residual itself); default: a new one of residual's type, bf16 without
-    one; False: r' is not kept.  out: a floating tensor, or an int32 one for field elements of the integers round(z out_scale) within +-limit; with
-    out_token_scale (float32, T) each row has a step of its own, max |z| / limit, which is written there.  Without out,
-    only r' is formed."""
+    one; False: r' is not kept.  out: a floating tensor, or an int32 one for field elements of the integers
+    round(z out_scale) within +-limit; with out_token_scale (float32, T) each row has a step of its own, max |z| / limit,
+    which is written there.  Without out, only r' is formed."""
     if residual_out is None:
         torch = _torch or _lazy_torch()
         kept = residual[0] if type(residual) is Rows else residual

@@ -2,8 +2,8 @@
 
 Each translation unit under csrc/ is compiled in parallel into _build/, then
 linked into paper_2609_10264_gb300/libpvmvmd.so; csrc/calls.c becomes the Python
-module _calls beside it, which the client's attention goes through, where Python's
-headers are installed.  Rebuilds only when a source or header is newer.
+module _calls beside it, which the client's attention and other steps go through, where
+Python's headers are installed.  Rebuilds only when a source or header is newer.
 """
 from __future__ import annotations
 

@@ -4,7 +4,8 @@
 // order, and no result depends on the order of atomic operations or of a list.
 //
 // Without top-k and top-p a row is read twice: for the largest x, and for the weights' sum; then the warp's
-// share where the choice falls is read once more.  Bound by the arithmetic of the weights.
+// share where the choice falls is read once more.  The first reading waits for memory and the second for the pipe of products
+// and sums, in turn in each CTA: over both, half of an SM's issue slots are used.
 // With them, the threads' largest values, four a thread, say where about the k-th largest lies (there are at least k
 // values above the k-th largest of them); the second reading puts the tokens up to there into a list, of a few
 // times k, and the first CTA finds limits and choice in it: by histograms, whose one bin
@@ -1350,8 +1351,8 @@ cudaError_t launch_type(const SampleArgs &a, cudaStream_t s) {
 cudaError_t launch_sample(const SampleJob &j, cudaStream_t s) {
     // A row over as many CTAs as leave two an SM, of which each halving leaves 3000 tokens at least (one row of 128000 with
     // top-k and top-p 35 us by one CTA, 23, 16 and 13 by 2, 4 and 8; of 12000 8.9, 8.8 and 9.1 by 2, 4 and 8; of 6000 6.9
-    // by one and 8.5 by two; 512 rows of 128000 119 by one each, 121 by two, 135 by four).  Clusters of 8 do not fill all
-    // places: 33 to 38 rows take two turns (37 of 32001 19 us, 10.2 by clusters of 4).
+    // by one and 8.5 by two; 512 rows of 128000 119 by one each, 121 by two, 135 by four).  Clusters of 8 do not find
+    // that many places: with 35 to 38 rows some wait for others (37 of 32001 19 us, 10.2 by clusters of 4; 32 11.2).
     SampleArgs a{j, 1};
     while (a.ctas < kMostCluster && (int64_t)j.T * a.ctas * 2 <= 2 * kSms && j.V / a.ctas >= 6000) a.ctas *= 2;
     switch (j.logits.type) {
