@@ -644,9 +644,9 @@ typedef struct {
  * probability that it was drawn with, within 2^-22 (1 + |log(W / Z)|); the token of lowest
  * index among the largest and 0 for a greedy row;
  * -1 and -infinity where no token can be chosen.  logits->token as for other rows, not
- * below V unless it is 0 (equal rows).  1 <= V <= 2^22 (whose
+ * below V unless it is 0 (equal rows).  Neither result may lie in random_dev.  1 <= V <= 2^22 (whose
  * weights' sums are below 2^62).  Errors: PVMVMD_E_ARG (null pointer,
- * unknown type), PVMVMD_E_SHAPE (T < 0, V outside its range), PVMVMD_E_PARAM (a logits' scale that
+ * unknown type, a result in random_dev), PVMVMD_E_SHAPE (T < 0, V outside its range), PVMVMD_E_PARAM (a logits' scale that
  * is not finite). */
 #define PVMVMD_MAX_V (1 << 22)
 int pvmvmd_sample(int T, int V, const pvmvmd_rows *logits, const pvmvmd_sampling *sampling, const uint32_t *allowed_dev,

@@ -21,6 +21,11 @@ bool float_type(int t) { return t == PVMVMD_BF16 || t == PVMVMD_F16 || t == PVMV
 bool any_type(int t) { return float_type(t) || t == PVMVMD_FIELD; }
 int size_of(int t) { return t == PVMVMD_BF16 || t == PVMVMD_F16 ? 2 : 4; }
 
+// whether two vectors of n 32-bit values share some
+bool overlap(const void *a, const void *b, int n) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && (x < y ? y - x : x - y) < (uintptr_t)n * 4;
+}
 bool misaligned(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % size != 0; }
 
 // T rows of D values: addresses of whole values
@@ -118,6 +123,8 @@ int pvmvmd_sample(int T, int V, const pvmvmd_rows *logits, const pvmvmd_sampling
                           static_cast<const void *>(sampling->temperature_dev), static_cast<const void *>(sampling->top_k_dev),
                           static_cast<const void *>(sampling->top_p_dev), static_cast<const void *>(sampling->min_p_dev)})
         if (misaligned(p, 4)) return PVMVMD_E_ARG;
+    // (a row's CTAs read its word one after the other, some when its token is written)
+    if (overlap(random_dev, token_dev, T) || overlap(random_dev, logprob_dev, T)) return PVMVMD_E_ARG;
     SampleJob j{};
     j.T = T;
     j.V = V;

@@ -213,3 +213,11 @@ def test_tokens_of_many_rows_of_all_kinds(pv, kind):
     p = np.where(off[2] < 0.3, 1.0, rng.random(T))
     m = np.where(off[3] < 0.5, 0.0, rng.random(T) * 0.3)
     _many(pv, l, kind, t=t.astype(np.float32), k=k, p=p.astype(np.float32), m=m.astype(np.float32))
+
+
+def test_results_in_the_random_words_are_refused(pv):
+    """Every CTA of a row reads its word, some after another has chosen the row's token."""
+    R = ctypes.byref(pv.pvmvmd_rows(data_dev=64, token=8, scale=1.0, type=pv.PVMVMD_F32))
+    how = ctypes.byref(pv.pvmvmd_sampling(temperature=1.0, top_p=1.0))
+    for token, logprob in ((1024, None), (1028, 4096), (1012, None), (4096, 1024), (4096, 1036), (4096, 1012)):
+        assert pv._lib.pvmvmd_sample(4, 8, R, how, None, 0, 1024, token, logprob, None) == pv.PVMVMD_E_ARG, (token, logprob)
