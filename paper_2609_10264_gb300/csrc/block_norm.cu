@@ -29,8 +29,7 @@ __device__ __forceinline__ void norm(RowThreads &r, const pvmvmd_norm &n, Pair i
         for (int c = 0; c < kChunks; ++c)
 #pragma unroll
             for (int i = 0; i < kTwos; ++i) add_terms(s, x[c][i]);
-        const Pair m = mean_of(row_sum(r, join(s)), inverse);
-        const Two mu = both(__fadd_rn(m.h, m.l));
+        const Two mu = both(rounded_mean(row_sum(r, join(s)), (float)at.D, inverse.h));
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
 #pragma unroll

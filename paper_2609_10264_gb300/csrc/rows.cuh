@@ -338,6 +338,14 @@ __device__ __forceinline__ Pair join(Pair a, Pair b) {  // the same for (b, a)
     return Pair{t, __fadd_rn(__fadd_rn(a.l, b.l), e)};
 }
 __device__ __forceinline__ Pair join(const Pairs &s) { return join(Pair{first(s.h), first(s.l)}, Pair{second(s.h), second(s.l)}); }
+// s / n rounded once, by the rounded inverse of n.  The quotient's rest is exact (18 bits), and so is its n-th part
+// (Markstein, IBM J. Res. Dev. 34, 1990) where s / n is the middle of two numbers, as rows of few different values often
+// have it: the even one is taken.
+__device__ __forceinline__ float rounded_mean(Pair s, float n, float inverse) {
+    const float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l), q = __fmul_rn(h, inverse);
+    const float rest = __fadd_rn(__fmaf_rn(-q, n, h), l), part = __fmul_rn(rest, inverse);
+    return __fadd_rn(q, __fmaf_rn(__fmaf_rn(-part, n, rest), inverse, part));
+}
 // s (1 / n), the latter a pair of the host's
 __device__ __forceinline__ Pair mean_of(Pair s, Pair inverse) {
     const float h = __fadd_rn(s.h, s.l), l = __fadd_rn(__fsub_rn(s.h, h), s.l), p = __fmul_rn(h, inverse.h);

@@ -221,3 +221,20 @@ def test_results_in_the_random_words_are_refused(pv):
     how = ctypes.byref(pv.pvmvmd_sampling(temperature=1.0, top_p=1.0))
     for token, logprob in ((1024, None), (1028, 4096), (1012, None), (4096, 1024), (4096, 1036), (4096, 1012)):
         assert pv._lib.pvmvmd_sample(4, 8, R, how, None, 0, 1024, token, logprob, None) == pv.PVMVMD_E_ARG, (token, logprob)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [6, 28, 100, 1022, 5004, 12000, 40000])
+def test_mean_in_the_middle_of_two_numbers(pv, D):
+    """Rows of two neighbouring numbers, as many of each: the mean is the even one of them.  (Sums of D of them and their
+    D-th part are exact in 64 bits.)"""
+    rng = np.random.default_rng(D)
+    T = 400 if D < 5000 else 60
+    low = np.exp2(rng.uniform(-3, 3, (T, 1))).astype(np.float32) * rng.choice([-1, 1], (T, 1)).astype(np.float32)
+    x = np.repeat(low, D, axis=1)
+    for row in x:
+        up = rng.permutation(D)[:D // 2]
+        row[up] = np.nextafter(row[up], np.float32(np.inf))
+    z = _dev(np.zeros((T, D), np.float32))
+    pv.pvmvmd_block_norm(None, _dev(x), residual_out=False, pre=pv.Norm("layer", eps=1e-5), out=z)
+    assert np.array_equal(_host(z), plain.norm(x, "layer", eps=1e-5))
