@@ -7,7 +7,7 @@ import pytest
 
 import steps_plain as plain
 from test_attention import Fake
-from test_steps import _dev, _host, pv  # noqa: F401
+from test_steps import _dev, _host, _sample, pv  # noqa: F401
 
 
 # ---------------------------------------------------------------- rows to write that lie on one another
@@ -238,3 +238,54 @@ def test_mean_in_the_middle_of_two_numbers(pv, D):
     z = _dev(np.zeros((T, D), np.float32))
     pv.pvmvmd_block_norm(None, _dev(x), residual_out=False, pre=pv.Norm("layer", eps=1e-5), out=z)
     assert np.array_equal(_host(z), plain.norm(x, "layer", eps=1e-5))
+
+
+# ---------------------------------------------------------------- numbers and addresses of any kind
+
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 160])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_sample_with_any_parameters(pv, kind, T):
+    """Scales, temperatures and limits that are zero, negative, tiny, huge or no numbers."""
+    rng = np.random.default_rng(T)
+    V = 1201
+    l = (rng.standard_normal((T, V)) * 2).astype(np.float32)
+    l[:, rng.integers(0, V, 20)] = np.array([INF, -INF, NAN, 3e38, -3e38] * 4, np.float32)
+    l[0] = rng.standard_normal(V)
+    ts, cs = np.ones(T, np.float32), np.ones(V, np.float32)
+    ts[:5] = 1, 0, INF, NAN, -1
+    cs[[3, 50, 700, 1199]] = 0, INF, NAN, -2
+    for scale in (1.0, -1.0, 0.0, 1e-40, 1e30):
+        _sample(pv, l, kind, scale, p=0.9, k=100)
+    per = lambda *v: np.array([v[(i * 7) % len(v)] for i in range(T)])  # noqa: E731
+    t, k = per(1.0, 0.7, 0.0, INF, NAN, 1e-40, -2.0, 1e30), per(0, 1, V, -3, 50, V - 1, 2**31 - 1)
+    p, m = per(1.0, 0.9, 0.0, -1.0, NAN, 1e-12, 2.0), per(0.0, 1.0, NAN, 3.0, -1.0, 1e-9)
+    for a in ((None, None), (ts, None), (None, cs), (ts, cs)):
+        _sample(pv, l, kind, 1.0, *a, t=t, k=k, p=p, m=m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("at", [1, 2, 3])
+def test_scales_and_weights_off_the_16_byte_boundaries(pv, at):
+    """Vectors that begin at any value: the same results as from the boundaries, with rows on these."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(at)
+    T, D = 30, 4096
+    x, y = (torch.randn(T, D, device="cuda", generator=g) for _ in range(2))
+    v = [torch.rand(D, device="cuda", generator=g) + 0.5 for _ in range(3)]
+    off = []
+    for a in v:
+        wide = torch.empty(D + at, device="cuda")
+        wide[at:] = a
+        off.append(wide[at:])
+    word = torch.randint(-2**31, 2**31, (T,), device="cuda", generator=g).to(torch.int32)
+    got = []
+    for c, w, b in (v, off):
+        n = pv.Norm("layer", w, b)
+        r, o = pv.pvmvmd_block_norm(pv.Rows(x, 0.5, None, c), y, pre=n, out=torch.empty(T, D, dtype=torch.int32, device="cuda"), out_scale=30.0)
+        z = pv.pvmvmd_glu(pv.Rows(x, 1.0, None, c), pv.Rows(y, 1.0, None, w), out=torch.empty_like(x))
+        got.append((r, o, z, pv.pvmvmd_sample(pv.Rows(x, 1.0, None, c), word, pv.Sampling(0.9, 100, 0.9))))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
